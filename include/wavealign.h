@@ -351,6 +351,71 @@ wa_status wa_sparse_attn_vt_noalloc(const void* q, const void* k, const void* vt
                                     const wa_shape* shape, const wa_attn_options* options, void* o, float* lse,
                                     int32_t* status, void* stream);
 
+/* ---- rotary positions ---- */
+
+enum { WA_BF16 = 0, WA_F16 = 1, WA_F32 = 2 };
+
+/* Pair i of the rotated columns: HALF columns i and i + pairs, INTERLEAVED columns 2i and 2i + 1. */
+enum { WA_ROTARY_HALF = 0, WA_ROTARY_INTERLEAVED = 1 };
+
+typedef struct wa_rotary_params {
+  int32_t batch;
+  int32_t tokens;
+  int32_t head_dim;       /* any, 2 * pairs at least */
+  int32_t dtype;          /* WA_BF16, WA_F16 or WA_F32, of every tensor */
+  int32_t layout;         /* WA_ROTARY_HALF or WA_ROTARY_INTERLEAVED */
+  int32_t pairs;          /* rotated pairs; columns from 2 * pairs on are copied */
+  int32_t axes;           /* position axes, 1..3 (a video's frame, row and column: 3) */
+  int32_t axis_pairs[3];  /* pairs of each axis, in pair order; they sum to `pairs` */
+  int32_t position_batch; /* sequences `positions` holds: batch, or 1 for all alike */
+  int32_t backward;       /* nonzero: the gradient, the transposed rotation */
+  double scale;           /* factor of the rotated values (1; with YaRN wa_rotary_frequencies gives it) */
+} wa_rotary_params;
+
+/* One tensor [batch][heads][tokens][head_dim]; element (b, h, n, c) lies at
+ * b stride[0] + h stride[1] + n stride[2] + c elements, so the input may be the
+ * [batch][tokens][heads][head_dim] of a projection, or a part of a fused one, and the
+ * output the layout of the attention calls. */
+typedef struct wa_rotary_tensor {
+  const void* in;
+  void* out;              /* in place (out == in, with equal strides) or apart from every input */
+  int32_t heads;
+  int64_t in_stride[3];   /* 0 repeats the input along that index */
+  int64_t out_stride[3];  /* elements of the output may not coincide */
+} wa_rotary_tensor;
+
+/* Rotary position embedding: pair i of a token at position p of the pair's axis is turned
+ * by the angle t = p * inv_freq[i], (x, y) -> scale (x cos t - y sin t, x sin t + y cos t),
+ * computed in float32 and rounded once (the angle in float64, so far positions
+ * lose nothing). With `backward` the map is its transpose, which takes the gradient of the
+ * output to that of the input; where the input repeats (stride 0) the caller sums.
+ *   tensors    host array of 1 or 2 tensors (q; q and k) that share one launch
+ *   inv_freq   double [pairs], device, 8-byte aligned: radians a position
+ *   positions  int32 [axes][position_batch][tokens], device; NULL: token n is at n (axes = 1)
+ * Rows of aligned 16-byte pieces are the fast form; any stride and alignment of whole elements is valid. */
+wa_status wa_rotary(const wa_rotary_params* params, const wa_rotary_tensor* tensors, int32_t n_tensors,
+                    const double* inv_freq, const int32_t* positions, void* stream);
+
+enum { WA_ROTARY_PLAIN = 0, WA_ROTARY_LINEAR = 1, WA_ROTARY_NTK = 2, WA_ROTARY_YARN = 3 };
+
+typedef struct wa_rotary_scaling {
+  int32_t kind;           /* WA_ROTARY_* */
+  double factor;          /* context length over the trained one, >= 1 */
+  double original_len;    /* YARN: the trained length, in positions */
+  double beta_fast;       /* YARN: turns over the trained length from which a pair keeps its frequency (32) */
+  double beta_slow;       /* YARN: turns up to which it is divided by factor (1) */
+} wa_rotary_scaling;
+
+/* Frequencies of one axis, on the HOST: inv_freq[i] = base^(-i / pairs), changed for contexts
+ * longer than the trained one:
+ *   LINEAR  divided by factor
+ *   NTK     with base * factor^(pairs / (pairs - 1)): the first pair unchanged, the last divided by factor
+ *   YARN    f (w + (1 - w) / factor) with w rising from 0 at beta_slow to 1 at beta_fast turns
+ *           original_len f / 2 pi; *scale = 0.1 ln(factor) + 1
+ * *scale (nullable) is 1 otherwise. scaling NULL: PLAIN. */
+wa_status wa_rotary_frequencies(int32_t pairs, double base, const wa_rotary_scaling* scaling, double* inv_freq,
+                                double* scale);
+
 /* ---- diagnostics (used by the test suite; not needed by callers) ---- */
 
 /* Evaluates on the GPU the fp64 operations the exact permutation relies on, for

@@ -3,7 +3,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_size_t, c_uint64, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libwavealign.so")
 
@@ -21,6 +21,9 @@ WA_ATTN_BAD_PERM, WA_ATTN_BAD_KV_INDEX = 1, 2
 WA_PRODUCE_WAIT_EXPIRED = 1
 WA_HEADS_IN_ORDER, WA_HEADS_INTERLEAVED = 0, 1
 WA_NOALLOC_SCRATCH_BYTES = 4 * 1024 * 1024
+WA_BF16, WA_F16, WA_F32 = 0, 1, 2
+WA_ROTARY_HALF, WA_ROTARY_INTERLEAVED = 0, 1
+WA_ROTARY_PLAIN, WA_ROTARY_LINEAR, WA_ROTARY_NTK, WA_ROTARY_YARN = 0, 1, 2, 3
 
 
 class WaShape(ctypes.Structure):
@@ -42,6 +45,22 @@ class WaPermParams(ctypes.Structure):
 
 class WaAttnOptions(ctypes.Structure):
     _fields_ = [("softmax_scale", c_float), ("n_xcd", c_int32), ("head_order", c_int32)]
+
+
+class WaRotaryParams(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("tokens", c_int32), ("head_dim", c_int32), ("dtype", c_int32), ("layout", c_int32),
+                ("pairs", c_int32), ("axes", c_int32), ("axis_pairs", c_int32 * 3), ("position_batch", c_int32),
+                ("backward", c_int32), ("scale", c_double)]
+
+
+class WaRotaryTensor(ctypes.Structure):
+    _fields_ = [("inp", c_void_p), ("out", c_void_p), ("heads", c_int32), ("in_stride", c_int64 * 3),
+                ("out_stride", c_int64 * 3)]
+
+
+class WaRotaryScaling(ctypes.Structure):
+    _fields_ = [("kind", c_int32), ("factor", c_double), ("original_len", c_double), ("beta_fast", c_double),
+                ("beta_slow", c_double)]
 
 
 class WaError(RuntimeError):
@@ -82,6 +101,8 @@ _SIGNATURES = {
     "wa_sparse_attn_vt": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                     POINTER(WaShape), POINTER(WaAttnOptions), c_void_p, c_void_p, c_void_p, c_void_p,
                                     c_size_t, c_void_p]),
+    "wa_rotary": (c_int32, [POINTER(WaRotaryParams), POINTER(WaRotaryTensor), c_int32, c_void_p, c_void_p, c_void_p]),
+    "wa_rotary_frequencies": (c_int32, [c_int32, c_double, POINTER(WaRotaryScaling), c_void_p, c_void_p]),
     "wa_fp64_probe": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p]),
     "wa_xcc_probe": (c_int32, [c_void_p, c_int32, c_void_p]),
 }

@@ -14,6 +14,10 @@ import torch
 from . import _lib as L
 
 _SKIP = {"auto": L.WA_SKIP_AUTO, "never": L.WA_SKIP_NEVER, "always": L.WA_SKIP_ALWAYS}
+_DTYPE = {torch.bfloat16: L.WA_BF16, torch.float16: L.WA_F16, torch.float32: L.WA_F32}
+_ROTARY_LAYOUT = {"half": L.WA_ROTARY_HALF, "interleaved": L.WA_ROTARY_INTERLEAVED}
+_ROTARY_SCALING = {"none": L.WA_ROTARY_PLAIN, "linear": L.WA_ROTARY_LINEAR, "ntk": L.WA_ROTARY_NTK,
+                   "yarn": L.WA_ROTARY_YARN}
 _HEAD_ORDER = {"in-order": L.WA_HEADS_IN_ORDER, "interleaved": L.WA_HEADS_INTERLEAVED}
 
 
@@ -407,6 +411,100 @@ def sparse_attn_vt_noalloc(q, k, vt, row_ptr, col_idx, perm=None, seg=None, *, b
                                           _ptr(seg), ctypes.byref(shape), ctypes.byref(opts), _ptr(out), _ptr(lse),
                                           _ptr(status), _stream()))
     return out
+
+
+def _one_device(**tensors) -> torch.device:
+    """The device that all given tensors share; work is enqueued on that device's current stream."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {dev}")
+        dev = t.device
+    return dev
+
+
+def _call_on(device: torch.device, call, *args) -> None:
+    """The library call with ``device`` current and its current stream as the last argument."""
+    if device.index in (None, torch.cuda.current_device()):
+        L.check(call(*args, _stream()))
+        return
+    with torch.cuda.device(device):
+        L.check(call(*args, _stream()))
+
+
+def rotary_frequencies(pairs: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                       original_len: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda"):
+    """(inv_freq float64 [pairs] on ``device``, scale) of one position axis for ``rotary``: base^(-i / pairs), for
+    contexts ``factor`` times the trained length divided by it ("linear"), with a larger base ("ntk") or by the pair's
+    turns over ``original_len`` ("yarn", which also grows the values by scale). Axes are concatenated by the caller."""
+    if scaling not in _ROTARY_SCALING:
+        raise ValueError(f"scaling must be one of {sorted(_ROTARY_SCALING)}")
+    freq, scale = (ctypes.c_double * max(int(pairs), 1))(), ctypes.c_double(1.0)
+    how = L.WaRotaryScaling(_ROTARY_SCALING[scaling], float(factor), float(original_len), float(beta_fast),
+                            float(beta_slow))
+    L.check(L.load().wa_rotary_frequencies(int(pairs), float(base), ctypes.byref(how), freq, ctypes.byref(scale)))
+    return torch.tensor(list(freq), dtype=torch.float64, device=device), scale.value
+
+
+def rotary(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, inv_freq: torch.Tensor,
+           positions: Optional[torch.Tensor] = None, layout: str = "half", axis_pairs=None, scale: float = 1.0,
+           backward: bool = False, out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None):
+    """q (and k) [B][H][N][d] with the first 2 P columns of every head rotated by their tokens' positions; (q, k) in
+    one launch. bfloat16, float16 or float32 of any strides with whole rows (a projection's [B][N][H][d] comes as
+    ``x.transpose(1, 2)``); the result is contiguous, or written to out_q and out_k: any strides, the input itself for in place.
+
+    inv_freq   float64 [P]: radians a position, from rotary_frequencies
+    positions  int32 [N], [B][N] or [axes][1 or B][N]; None: token n is at n
+    layout     "half" (pair i: columns i and i + P) or "interleaved" (2i and 2i + 1)
+    axis_pairs pairs of each position axis (None: one axis)
+    scale      factor of the rotated values
+    backward   the transposed map: gradients of the outputs in, gradients of q and k out"""
+    lib = L.load()
+    if layout not in _ROTARY_LAYOUT:
+        raise ValueError(f"layout must be one of {sorted(_ROTARY_LAYOUT)}")
+    if k is None and out_k is not None:
+        raise ValueError("out_k without k")
+    if q.dim() != 4 or q.dtype not in _DTYPE:
+        raise ValueError("q must be a bfloat16, float16 or float32 [B][H][N][d] tensor")
+    b, _, n, d = q.shape
+    if k is not None and (k.dim() != 4 or k.dtype != q.dtype or (k.shape[0], k.shape[2], k.shape[3]) != (b, n, d)):
+        raise ValueError(f"k must be a {q.dtype} tensor [{b}][H][{n}][{d}], got {k.dtype} {tuple(k.shape)}")
+    if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous float64 vector")
+    axis = [inv_freq.numel()] if axis_pairs is None else [int(x) for x in axis_pairs]
+    if not 1 <= len(axis) <= 3:
+        raise ValueError("axis_pairs must name 1 to 3 axes")
+    pos_batch = 1
+    if positions is not None:
+        want = [(len(axis), 1, n), (len(axis), b, n)] + ([(n,), (b, n)] if len(axis) == 1 else [])
+        if positions.dtype != torch.int32 or tuple(positions.shape) not in want or not positions.is_contiguous():
+            raise ValueError(f"positions must be contiguous int32 of a shape in {want}, got {positions.dtype} "
+                             f"{tuple(positions.shape)}")
+        pos_batch = positions.numel() // (len(axis) * n) if n else 1
+    pairs = [(q, out_q, "q"), (k, out_k, "k")][:1 if k is None else 2]
+    for x, o, name in pairs:
+        if o is not None and (o.dtype != x.dtype or o.shape != x.shape):
+            raise ValueError(f"out_{name} must be {x.dtype} of shape {tuple(x.shape)}, got {o.dtype} {tuple(o.shape)}")
+        for y in (x, o):
+            if y is not None and d > 1 and y.stride(3) != 1:
+                raise ValueError(f"{name} and its output must have contiguous rows (last stride 1)")
+    dev = _one_device(q=q, k=k, inv_freq=inv_freq, positions=positions, out_q=out_q, out_k=out_k)
+    outs, tensors = [], (L.WaRotaryTensor * 2)()
+    for t, (x, o, _) in zip(tensors, pairs):
+        if o is None:
+            o = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        outs.append(o)
+        t.inp, t.out, t.heads = x.data_ptr(), o.data_ptr(), x.shape[1]
+        t.in_stride[:] = x.stride()[:3]
+        t.out_stride[:] = o.stride()[:3]
+    params = L.WaRotaryParams(b, n, d, _DTYPE[q.dtype], _ROTARY_LAYOUT[layout], inv_freq.numel(), len(axis),
+                              (ctypes.c_int32 * 3)(*axis), pos_batch, 1 if backward else 0, float(scale))
+    _call_on(dev, lib.wa_rotary, ctypes.byref(params), tensors, len(pairs), _ptr(inv_freq), _ptr(positions))
+    return outs[0] if k is None else tuple(outs)
 
 
 def fp64_probe(a: torch.Tensor, b: torch.Tensor, c: torch.Tensor) -> torch.Tensor:

@@ -27,6 +27,7 @@ SOURCES = {
     "perm_kernel.hip": ["-ffp-contract=off"],
     # the mask producer's float32 folds, divisions and products must round as specified
     "mask_producer.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"],
+    "rotary.hip": [],
     "abi.cpp": [],
 }
 

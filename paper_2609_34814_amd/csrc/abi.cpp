@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -11,6 +12,7 @@
 #include "common.h"
 #include "perm_launch.h"
 #include "producer_launch.h"
+#include "rotary_launch.h"
 #include "wavealign.h"
 
 namespace {
@@ -229,6 +231,73 @@ wa_status perm_launch_common(const uint8_t* mask, const Dims& d, const PermWs& L
   hipError_t e = wa_launch_pack(mask, (int)d.bh, d.mb, d.mb, (uint64_t*)(base + L.rowbits), (uint64_t*)(base + L.colbits),
                                 row_nnz, (int2*)(base + L.adj), st);
   if (e != hipSuccess) return hip_fail(e, "pack launch");
+  return WA_OK;
+}
+
+// Whether two elements of an output [batch][heads][tokens][head_dim] lie at one place: each index, from the
+// smallest stride up, has to step past all that the smaller ones span.
+bool rotary_overlaps(const int64_t size[3], const int64_t stride[3], int64_t head_dim) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+  int64_t span = head_dim;
+  for (int i : order) {
+    if (size[i] == 1) continue;
+    if (stride[i] < span) return true;
+    span += (size[i] - 1) * stride[i];
+  }
+  return false;
+}
+
+wa_status check_rotary(const wa_rotary_params* p, const wa_rotary_tensor* t, int32_t n, const double* freq,
+                       const int32_t* pos) {
+  if (!p || !t || !freq) return fail(WA_ERR_INVALID_ARG, "params, tensors and inv_freq must be non-null");
+  if (n < 1 || n > 2) return fail(WA_ERR_INVALID_ARG, "n_tensors %d outside 1..2", n);
+  if (p->batch < 1 || p->tokens < 1) return fail(WA_ERR_INVALID_ARG, "batch and tokens must be >= 1 (got %d, %d)", p->batch, p->tokens);
+  if (p->dtype < WA_BF16 || p->dtype > WA_F32) return fail(WA_ERR_INVALID_ARG, "dtype %d invalid", p->dtype);
+  if (p->layout != WA_ROTARY_HALF && p->layout != WA_ROTARY_INTERLEAVED)
+    return fail(WA_ERR_INVALID_ARG, "layout %d invalid", p->layout);
+  if (p->pairs < 1 || p->head_dim < 1 || p->pairs > p->head_dim / 2)
+    return fail(WA_ERR_INVALID_ARG, "%d pairs do not fit %d columns", p->pairs, p->head_dim);
+  if (p->head_dim > 65536) return fail(WA_ERR_UNSUPPORTED, "head_dim %d exceeds 65536", p->head_dim);
+  if (p->axes < 1 || p->axes > 3) return fail(WA_ERR_INVALID_ARG, "axes %d outside 1..3", p->axes);
+  int64_t sum = 0;
+  for (int i = 0; i < p->axes; ++i) {
+    if (p->axis_pairs[i] < 0) return fail(WA_ERR_INVALID_ARG, "axis_pairs[%d] is negative", i);
+    sum += p->axis_pairs[i];
+  }
+  if (sum != p->pairs) return fail(WA_ERR_INVALID_ARG, "axis_pairs sum to %lld, not %d", (long long)sum, p->pairs);
+  if (!pos && p->axes != 1) return fail(WA_ERR_INVALID_ARG, "positions are required for %d axes", p->axes);
+  if (pos && p->position_batch != 1 && p->position_batch != p->batch)
+    return fail(WA_ERR_INVALID_ARG, "position_batch must be 1 or %d (got %d)", p->batch, p->position_batch);
+  if (!std::isfinite(p->scale) || !std::isfinite((float)p->scale)) return fail(WA_ERR_INVALID_ARG, "scale must be finite");
+  if (!aligned(freq, 8)) return fail(WA_ERR_ALIGNMENT, "inv_freq must be 8-byte aligned");
+  if (!aligned(pos, 4)) return fail(WA_ERR_ALIGNMENT, "positions must be 4-byte aligned");
+  const size_t elem = p->dtype == WA_F32 ? 4 : 2;
+  int64_t heads = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!t[i].in || !t[i].out) return fail(WA_ERR_INVALID_ARG, "tensor %d: in and out must be non-null", i);
+    if (t[i].heads < 1) return fail(WA_ERR_INVALID_ARG, "tensor %d: heads must be >= 1 (got %d)", i, t[i].heads);
+    if (!aligned(t[i].in, elem) || !aligned(t[i].out, elem))
+      return fail(WA_ERR_ALIGNMENT, "tensor %d is not aligned to its elements", i);
+    const int64_t size[3] = {p->batch, t[i].heads, p->tokens};
+    heads += t[i].heads;
+    for (int x = 0; x < 3; ++x) {
+      if (t[i].in_stride[x] < 0 || t[i].out_stride[x] < 0) return fail(WA_ERR_INVALID_ARG, "tensor %d: negative stride", i);
+      if (t[i].in_stride[x] >= (int64_t(1) << 40) || t[i].out_stride[x] >= (int64_t(1) << 40))
+        return fail(WA_ERR_UNSUPPORTED, "tensor %d: stride too large", i);
+      if (t[i].in == t[i].out && size[x] > 1 && t[i].in_stride[x] != t[i].out_stride[x])
+        return fail(WA_ERR_INVALID_ARG, "tensor %d: in place, the strides must be equal", i);
+    }
+    if (rotary_overlaps(size, t[i].out_stride, p->head_dim))
+      return fail(WA_ERR_INVALID_ARG, "tensor %d: elements of the output coincide", i);
+  }
+  if (n == 2 && (t[0].out == t[1].out || t[0].out == t[1].in || t[1].out == t[0].in))
+    return fail(WA_ERR_INVALID_ARG, "an output is the other tensor's input or output");
+  // each factor is below 2^31 and head_dim at most 2^16: the products are taken so that none passes 2^63
+  const int64_t rows = (int64_t)p->batch * p->tokens;
+  if (heads > INT32_MAX || rows >= (int64_t(1) << 40) || heads * p->head_dim >= (int64_t(1) << 40) ||
+      (double)rows * (double)heads * p->head_dim >= 1099511627776.0)
+    return fail(WA_ERR_UNSUPPORTED, "tensor too large");
   return WA_OK;
 }
 
@@ -570,6 +639,67 @@ wa_status wa_sparse_attn_vt(const void* q, const void* k, const void* vt, const 
                   split_part(workspace, workspace_bytes, attn_sched_bytes(d), d), row_ptr, nullptr, col_idx, perm, seg_start, d, options->softmax_scale, options->n_xcd, options->head_order, o, lse, status,
                   (hipStream_t)stream);
   if (s != WA_OK) return s;
+  return ok();
+}
+
+wa_status wa_rotary(const wa_rotary_params* params, const wa_rotary_tensor* tensors, int32_t n_tensors,
+                    const double* inv_freq, const int32_t* positions, void* stream) {
+  wa_status s = check_rotary(params, tensors, n_tensors, inv_freq, positions);
+  if (s != WA_OK) return s;
+  WaRotaryLaunch a{};
+  for (int i = 0; i < n_tensors; ++i) {
+    a.in[i] = tensors[i].in;
+    a.out[i] = tensors[i].out;
+    a.heads[i] = tensors[i].heads;
+    a.copy[i] = tensors[i].in != tensors[i].out && params->head_dim > 2 * params->pairs;
+    std::copy(tensors[i].in_stride, tensors[i].in_stride + 3, a.in_stride[i]);
+    std::copy(tensors[i].out_stride, tensors[i].out_stride + 3, a.out_stride[i]);
+  }
+  a.freq = inv_freq;
+  a.pos = positions;
+  a.pos_batch = params->position_batch;
+  a.axes = params->axes;
+  for (int i = 0, end = 0; i < 3; ++i) a.axis_end[i] = end += i < params->axes ? params->axis_pairs[i] : 0;
+  a.batch = params->batch; a.tokens = params->tokens; a.head_dim = params->head_dim; a.pairs = params->pairs;
+  a.interleaved = params->layout == WA_ROTARY_INTERLEAVED;
+  a.dtype = params->dtype;
+  a.cos_scale = (float)params->scale;
+  a.sin_scale = params->backward ? -a.cos_scale : a.cos_scale;
+  const hipError_t e = wa_launch_rotary(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "rotary launch");
+  return ok();
+}
+
+wa_status wa_rotary_frequencies(int32_t pairs, double base, const wa_rotary_scaling* scaling, double* inv_freq,
+                                double* scale) {
+  if (!inv_freq) return fail(WA_ERR_INVALID_ARG, "inv_freq is null");
+  if (pairs < 1 || pairs > 32768) return fail(WA_ERR_INVALID_ARG, "pairs %d outside 1..32768", pairs);
+  if (!(base > 0) || !std::isfinite(base)) return fail(WA_ERR_INVALID_ARG, "base must be positive and finite");
+  const int32_t kind = scaling ? scaling->kind : WA_ROTARY_PLAIN;
+  if (kind < WA_ROTARY_PLAIN || kind > WA_ROTARY_YARN) return fail(WA_ERR_INVALID_ARG, "scaling kind %d invalid", kind);
+  const double factor = kind == WA_ROTARY_PLAIN ? 1.0 : scaling->factor;
+  if (!(factor >= 1) || !std::isfinite(factor)) return fail(WA_ERR_INVALID_ARG, "factor must be >= 1 and finite");
+  if (kind == WA_ROTARY_NTK) {
+    if (pairs < 2) return fail(WA_ERR_INVALID_ARG, "NTK scaling needs two pairs");
+    base *= std::pow(factor, (double)pairs / (pairs - 1));
+  }
+  if (kind == WA_ROTARY_YARN) {
+    if (!(scaling->original_len > 0) || !std::isfinite(scaling->original_len))
+      return fail(WA_ERR_INVALID_ARG, "original_len must be positive and finite");
+    if (!(scaling->beta_slow >= 0) || !(scaling->beta_fast > scaling->beta_slow) || !std::isfinite(scaling->beta_fast))
+      return fail(WA_ERR_INVALID_ARG, "beta_fast must exceed beta_slow, both finite and not negative");
+  }
+  for (int i = 0; i < pairs; ++i) {
+    double f = std::pow(base, -(double)i / pairs);
+    if (kind == WA_ROTARY_LINEAR) f /= factor;
+    if (kind == WA_ROTARY_YARN) {
+      const double turns = scaling->original_len * f / 6.283185307179586;
+      const double w = std::min(1.0, std::max(0.0, (turns - scaling->beta_slow) / (scaling->beta_fast - scaling->beta_slow)));
+      f = f * w + f / factor * (1 - w);
+    }
+    inv_freq[i] = f;
+  }
+  if (scale) *scale = kind == WA_ROTARY_YARN ? 0.1 * std::log(factor) + 1 : 1.0;
   return ok();
 }
 
