@@ -416,6 +416,54 @@ typedef struct wa_rotary_scaling {
 wa_status wa_rotary_frequencies(int32_t pairs, double base, const wa_rotary_scaling* scaling, double* inv_freq,
                                 double* scale);
 
+/* ---- differential attention ---- */
+
+typedef struct wa_diff_shape {
+  int32_t batch;
+  int32_t heads;      /* differential heads H, a multiple of kv_heads */
+  int32_t kv_heads;   /* key heads Hk: heads h with equal h / (H / Hk) share keys and values */
+  int32_t q_len;
+  int32_t kv_len;     /* keys a sequence has room for */
+  int32_t head_dim;   /* d of a map's queries and keys: 64 or 128 */
+  int32_t value_dim;  /* d or 2 d */
+  int32_t block;      /* tokens of a mask block: 64 or 128 */
+} wa_diff_shape;
+
+typedef struct wa_diff_options {
+  float softmax_scale;  /* <= 0 selects 1/sqrt(head_dim) */
+  int32_t causal;       /* nonzero: query i of sequence b sees the keys j <= q_start[b] + i */
+} wa_diff_options;
+
+/* Workspace bytes needed by wa_diff_attn (partial results of calls with few rows, whose keys are split over
+ * workgroups; 0 for others) and by wa_diff_attn_backward. Calls that share a workspace must
+ * not overlap, captured ones included. */
+wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes);
+
+/* Differential attention forward: head h has two softmax maps over the same kept keys,
+ *   P_m = softmax(scale Q_m K_m^T), m = 1, 2,   O = P_1 V - lam[h] P_2 V.
+ * A key j of sequence b is kept for query i if j < kv_lens[b], the mask keeps its block, and, with
+ * `causal`, j <= q_start[b] + i. A query with no kept key gets O = 0 and LSE = -inf. bf16 inputs, float32
+ * scores, sums and O, probabilities rounded to bf16 for the product with V, bf16 output.
+ * Values must be finite in the keys below kv_lens[b]; memory past them is not used, whatever it holds.
+ *   q        bf16 [B][2H][q_len][d], 16-byte aligned: the maps of head h are 2h and 2h + 1
+ *   k        bf16 [B][2Hk][kv_len][d], likewise
+ *   v        bf16 [B][Hk][kv_len][value_dim]
+ *   lam      float [H], device
+ *   mask     uint8 [B][H][ceil(q_len/block)][ceil(kv_len/block)], NULL keeps every block;
+ *            both maps of a head share it (wa_produce_block_mask makes square ones)
+ *   q_start  int32 [B], device: position of each sequence's first query; only with causal; NULL: kv_len - q_len
+ *   kv_lens  int32 [B], device: keys each sequence holds, taken into 0..kv_len; NULL: kv_len
+ *   o        out bf16 [B][H][q_len][value_dim]
+ *   o2       out bf16, as o, nullable: P_2 V, which the gradient needs
+ *   lse      out float [B][2H][q_len], nullable: natural-log sum-exp of each map's scaled scores
+ *   workspace  >= wa_diff_attn_workspace_size(shape), 256-byte aligned; NULL if that is 0
+ * How a call is cut into workgroups follows from its shape alone, so equal calls give equal bits. At most
+ * 4096 blocks of queries and of keys. */
+wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
+                       const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
+                       const wa_diff_options* options, void* o, void* o2, float* lse, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
 /* ---- diagnostics (used by the test suite; not needed by callers) ---- */
 
 /* Evaluates on the GPU the fp64 operations the exact permutation relies on, for

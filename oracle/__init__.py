@@ -18,5 +18,6 @@ Modules
   objective    the intra-wave distance objective of Eq. 1 (diagnostic)
   mask_producer  pooled-score top-k block mask from Q and K (a content-dependent producer of the
                mask the path consumes, Sec. II-B; float32 where the method rounds, fixed order)
+  diff_attention  differential attention and its gradient (fp64)
   rotary       rotary positions and their frequencies (fp64)
 """

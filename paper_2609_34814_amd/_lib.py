@@ -63,6 +63,15 @@ class WaRotaryScaling(ctypes.Structure):
                 ("beta_slow", c_double)]
 
 
+class WaDiffShape(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("heads", c_int32), ("kv_heads", c_int32), ("q_len", c_int32), ("kv_len", c_int32),
+                ("head_dim", c_int32), ("value_dim", c_int32), ("block", c_int32)]
+
+
+class WaDiffOptions(ctypes.Structure):
+    _fields_ = [("softmax_scale", c_float), ("causal", c_int32)]
+
+
 class WaError(RuntimeError):
     def __init__(self, status: int, detail: str):
         super().__init__(f"wavealign error {status}: {detail}")
@@ -103,6 +112,10 @@ _SIGNATURES = {
                                     c_size_t, c_void_p]),
     "wa_rotary": (c_int32, [POINTER(WaRotaryParams), POINTER(WaRotaryTensor), c_int32, c_void_p, c_void_p, c_void_p]),
     "wa_rotary_frequencies": (c_int32, [c_int32, c_double, POINTER(WaRotaryScaling), c_void_p, c_void_p]),
+    "wa_diff_attn_workspace_size": (c_int32, [POINTER(WaDiffShape), POINTER(c_size_t)]),
+    "wa_diff_attn": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                               POINTER(WaDiffShape), POINTER(WaDiffOptions), c_void_p, c_void_p, c_void_p, c_void_p,
+                               c_size_t, c_void_p]),
     "wa_fp64_probe": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p]),
     "wa_xcc_probe": (c_int32, [c_void_p, c_int32, c_void_p]),
 }

@@ -507,6 +507,77 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, inv_freq: torch
     return outs[0] if k is None else tuple(outs)
 
 
+def diff_shape_of(batch: int, heads: int, kv_heads: int, q_len: int, kv_len: int, head_dim: int, value_dim: int,
+                  block: int = 128) -> L.WaDiffShape:
+    return L.WaDiffShape(batch, heads, kv_heads, q_len, kv_len, head_dim, value_dim, block)
+
+
+def diff_attn_workspace_size(shape: L.WaDiffShape) -> int:
+    """Bytes for diff_attn (0 for calls of many rows)."""
+    return _size("wa_diff_attn_workspace_size", shape)
+
+
+def _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens):
+    """(shape, mask as uint8) of a differential-attention call; q [B][2H][M][d], k [B][2Hk][N][d], v [B][Hk][N][dv]."""
+    for t, nm in ((q, "q"), (k, "k"), (v, "v")):
+        if t.dtype != torch.bfloat16 or t.dim() != 4:
+            raise ValueError(f"{nm} must be a bfloat16 tensor of four dimensions")
+    b, h2, m, d = q.shape
+    hk, n, dv = v.shape[1:]
+    if h2 % 2 or hk == 0 or (h2 // 2) % hk:
+        raise ValueError(f"q must have two maps for each of a multiple of v's {hk} heads, got {h2}")
+    if tuple(k.shape) != (b, 2 * hk, n, d) or v.shape[0] != b:
+        raise ValueError(f"k must have shape {(b, 2 * hk, n, d)} and v {(b, hk, n, dv)}, got {tuple(k.shape)} and "
+                         f"{tuple(v.shape)}")
+    h = h2 // 2
+    _check(lam, "lam", torch.float32, (h,))
+    _check(q_start, "q_start", torch.int32, (b,))
+    _check(kv_lens, "kv_lens", torch.int32, (b,))
+    if q_start is not None and not causal:
+        raise ValueError("q_start without causal")
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("mask must be uint8 or bool")
+        want = (b, h, -(-m // block), -(-n // block))
+        if tuple(mask.shape) != want:
+            raise ValueError(f"mask must have shape {want}, got {tuple(mask.shape)}")
+        mask = mask.view(torch.uint8) if mask.dtype == torch.bool else mask
+    return diff_shape_of(b, h, hk, m, n, d, dv, block), mask
+
+
+def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor, mask: Optional[torch.Tensor] = None,
+              *, block: int = 128, scale: Optional[float] = None, causal: bool = False,
+              q_start: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None, return_stats: bool = False,
+              out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Differential attention: O = P_1 V - lam_h P_2 V bf16 [B][H][M][dv], P_m = softmax(scale Q_m K_m^T) over the kept keys.
+
+    q, k, v   bfloat16 [B][2H][M][d], [B][2Hk][N][d], [B][Hk][N][dv] with dv = d or 2 d; the maps of head h are
+              2h and 2h + 1, and H / Hk heads in a row share keys and values
+    lam       float32 [H]
+    mask      uint8 or bool [B][H][ceil(M/block)][ceil(N/block)] of kept blocks; None keeps all
+    causal    query i of sequence b sees the keys up to q_start[b] + i (q_start int32 [B]; None: N - M)
+    kv_lens   int32 [B]: keys each sequence holds; what lies behind them is not used
+    return_stats  also P_2 V (as O) and the float32 log-sum-exps [B][2H][M], which diff_attn_backward takes"""
+    lib = L.load()
+    shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)
+    want = (shape.batch, shape.heads, shape.q_len, shape.value_dim)
+    _check(out, "out", torch.bfloat16, want)
+    _check(workspace, "workspace", torch.uint8)
+    _on_device(q=q, k=k, v=v, lam=lam, mask=mask, q_start=q_start, kv_lens=kv_lens, out=out, workspace=workspace)
+    dev = _one_device(q=q, k=k, v=v, lam=lam, mask=mask, q_start=q_start, kv_lens=kv_lens, out=out, workspace=workspace)
+    need = diff_attn_workspace_size(shape)
+    if need and (workspace is None or workspace.numel() < need):
+        workspace = _workspace(need, dev)
+    o = torch.empty(want, dtype=torch.bfloat16, device=dev) if out is None else out
+    o2 = torch.empty_like(o) if return_stats else None
+    lse = torch.empty((want[0], 2 * want[1], want[2]), dtype=torch.float32, device=dev) if return_stats else None
+    opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
+    _call_on(dev, lib.wa_diff_attn, _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(mask), _ptr(q_start), _ptr(kv_lens),
+             ctypes.byref(shape), ctypes.byref(opts), _ptr(o), _ptr(o2), _ptr(lse), _ptr(workspace),
+             0 if workspace is None else workspace.numel())
+    return (o, o2, lse) if return_stats else o
+
+
 def fp64_probe(a: torch.Tensor, b: torch.Tensor, c: torch.Tensor) -> torch.Tensor:
     lib = L.load()
     out = torch.empty((a.numel(), 6), dtype=torch.float64, device=a.device)

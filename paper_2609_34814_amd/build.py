@@ -28,6 +28,7 @@ SOURCES = {
     # the mask producer's float32 folds, divisions and products must round as specified
     "mask_producer.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"],
     "rotary.hip": [],
+    "diff_attn.hip": [],
     "abi.cpp": [],
 }
 

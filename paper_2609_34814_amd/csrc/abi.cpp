@@ -10,6 +10,7 @@
 #include <cstring>
 
 #include "common.h"
+#include "diff_launch.h"
 #include "perm_launch.h"
 #include "producer_launch.h"
 #include "rotary_launch.h"
@@ -298,6 +299,54 @@ wa_status check_rotary(const wa_rotary_params* p, const wa_rotary_tensor* t, int
   if (heads > INT32_MAX || rows >= (int64_t(1) << 40) || heads * p->head_dim >= (int64_t(1) << 40) ||
       (double)rows * (double)heads * p->head_dim >= 1099511627776.0)
     return fail(WA_ERR_UNSUPPORTED, "tensor too large");
+  return WA_OK;
+}
+
+// Shape of a differential-attention call, as a launch without pointers.
+wa_status check_diff_shape(const wa_diff_shape* s, WaDiffLaunch* out) {
+  if (!s) return fail(WA_ERR_INVALID_ARG, "shape is null");
+  if (s->batch < 1 || s->heads < 1 || s->kv_heads < 1 || s->q_len < 1 || s->kv_len < 1)
+    return fail(WA_ERR_INVALID_ARG, "batch, heads, kv_heads, q_len and kv_len must be >= 1 (got %d, %d, %d, %d, %d)",
+                s->batch, s->heads, s->kv_heads, s->q_len, s->kv_len);
+  if (s->heads % s->kv_heads) return fail(WA_ERR_INVALID_ARG, "%d heads are not a multiple of %d key heads", s->heads, s->kv_heads);
+  if (s->head_dim != 64 && s->head_dim != 128)
+    return fail(WA_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", s->head_dim);
+  if (s->value_dim != s->head_dim && s->value_dim != 2 * s->head_dim)
+    return fail(WA_ERR_UNSUPPORTED, "value_dim %d not supported (head_dim or twice that)", s->value_dim);
+  if (s->block != 64 && s->block != 128) return fail(WA_ERR_UNSUPPORTED, "block %d not supported (64 or 128)", s->block);
+  const int64_t mb = ((int64_t)s->q_len + s->block - 1) / s->block, nb = ((int64_t)s->kv_len + s->block - 1) / s->block;
+  if (mb > WA_MAX_BLOCKS || nb > WA_MAX_BLOCKS)
+    return fail(WA_ERR_UNSUPPORTED, "%lld x %lld blocks exceed %d", (long long)mb, (long long)nb, WA_MAX_BLOCKS);
+  const int64_t bh = (int64_t)s->batch * s->heads;
+  if (bh >= (int64_t(1) << 31) || bh * mb * nb >= (int64_t(1) << 31))
+    return fail(WA_ERR_UNSUPPORTED, "batch*heads*M_B*N_B must be < 2^31");
+  const int64_t tokens = std::max((int64_t)s->q_len, (int64_t)s->kv_len);
+  if (2 * bh * tokens >= (int64_t(1) << 40) / s->head_dim) return fail(WA_ERR_UNSUPPORTED, "tensor too large");
+  out->batch = s->batch; out->heads = s->heads; out->kv_heads = s->kv_heads;
+  out->q_len = s->q_len; out->kv_len = s->kv_len; out->head_dim = s->head_dim; out->value_dim = s->value_dim;
+  out->block = s->block; out->mb = (int32_t)mb; out->nb = (int32_t)nb;
+  return WA_OK;
+}
+
+size_t diff_ws_bytes(const WaDiffLaunch& a) {
+  return align_up(4 * std::max(wa_diff_part_floats(wa_diff_plan(a, false), a.value_dim),
+                               wa_diff_part_floats(wa_diff_plan(a, true), a.value_dim)));
+}
+
+// Arguments that both directions share, checked and put into the launch.
+wa_status check_diff_args(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
+                          const int32_t* q_start, const int32_t* kv_lens, const wa_diff_options* options, WaDiffLaunch* a) {
+  if (!options) return fail(WA_ERR_INVALID_ARG, "options is null");
+  if (!q || !k || !v || !lam) return fail(WA_ERR_INVALID_ARG, "q, k, v and lam must be non-null");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16))
+    return fail(WA_ERR_ALIGNMENT, "q, k and v must be 16-byte aligned");
+  if (!aligned(lam, 4) || !aligned(q_start, 4) || !aligned(kv_lens, 4))
+    return fail(WA_ERR_ALIGNMENT, "lam, q_start and kv_lens must be 4-byte aligned");
+  if (q_start && !options->causal) return fail(WA_ERR_INVALID_ARG, "q_start without causal");
+  a->q = q; a->k = k; a->v = v; a->lam = lam; a->mask = mask; a->q_start = q_start; a->kv_lens = kv_lens;
+  a->causal = options->causal ? 1 : 0;
+  const float scale = options->softmax_scale;
+  a->scale = scale > 0.f && std::isfinite(scale) ? scale : (float)(1.0 / std::sqrt((double)a->head_dim));
   return WA_OK;
 }
 
@@ -700,6 +749,36 @@ wa_status wa_rotary_frequencies(int32_t pairs, double base, const wa_rotary_scal
     inv_freq[i] = f;
   }
   if (scale) *scale = kind == WA_ROTARY_YARN ? 0.1 * std::log(factor) + 1 : 1.0;
+  return ok();
+}
+
+wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes) {
+  WaDiffLaunch a{};
+  wa_status s = check_diff_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
+  *bytes = diff_ws_bytes(a);
+  return ok();
+}
+
+wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
+                       const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
+                       const wa_diff_options* options, void* o, void* o2, float* lse, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  WaDiffLaunch a{};
+  wa_status s = check_diff_shape(shape, &a);
+  if (s != WA_OK) return s;
+  s = check_diff_args(q, k, v, lam, mask, q_start, kv_lens, options, &a);
+  if (s != WA_OK) return s;
+  if (!o) return fail(WA_ERR_INVALID_ARG, "o must be non-null");
+  if (!aligned(o, 16) || !aligned(o2, 16)) return fail(WA_ERR_ALIGNMENT, "o and o2 must be 16-byte aligned");
+  if (!aligned(lse, 4)) return fail(WA_ERR_ALIGNMENT, "lse must be 4-byte aligned");
+  s = check_ws(workspace, workspace_bytes, diff_ws_bytes(a));
+  if (s != WA_OK) return s;
+  a.o = o; a.o2 = o2; a.lse = lse;
+  a.part = (float*)workspace;
+  const hipError_t e = wa_launch_diff_attn(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "differential attention launch");
   return ok();
 }
 

@@ -1,0 +1,361 @@
+// Differential attention forward for gfx950 (MI355X): per head two softmax maps over the same kept keys,
+//   O = P_1 V - lam_h P_2 V,   P_m = softmax(scale Q_m K_m^T).
+//
+// One workgroup computes one tile of 32 W query rows (W = 1, 2, 4) of both maps: W wavefronts a map, 32 rows each, so the V
+// tile is read from memory once for both and the maps meet in LDS when the keys are done. In one pass over the keys, a
+// tile of KB at a time (copied into LDS while the one before is worked on), a wavefront computes
+//   S^T = K_m Q_m^T (v_mfma_f32_32x32x16_bf16: keys in registers, one query a lane), the running maximum and sum of its
+//   queries, P^T rounded to bf16, and O_m^T += V^T P^T, whose operand P^T is in the registers that S^T came out in.
+// Scores, maxima, sums and O are float32; P is rounded to bf16 because the matrix cores multiply that (half a step, 2^-9 of each
+// probability, averages out over the keys of a row).
+//
+// Running maximum: O and l are rescaled only when a row's maximum grows by more than 2^8: probabilities up to 2^8 keep
+// their bf16 and float32 precision, and after a row's first tiles it hardly ever happens.
+//
+// Few rows (tokens of a decoding step): the rows of all heads that share a key head fill one tile, and the keys are
+// split over workgroups whose partial results a second kernel joins in key order, so a result does not depend on
+// the order in which workgroups run.
+
+#include "diff_tiles.h"
+#include "wavealign.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+using namespace wa;
+
+constexpr float kGrow = 8.f;  // log2 units
+
+template <int D, int DV, int W>
+struct Fwd {
+  // 64 keys a tile with four wavefronts a map (two tiles of 64 KiB for D 128, DV 256); with fewer, 32, so that two
+  // workgroups fit a compute unit.
+  static constexpr int KB = W == 4 ? 64 : 32;
+  static constexpr int NWV = 2 * W;
+  static constexpr int KRB = D * 2, VRB = DV * 2;
+  static constexpr int KBYTES = KB * KRB, VBYTES = KB * VRB, STAGE = 2 * KBYTES + VBYTES;
+  static constexpr int KT = KB / 32, DT = DV / 32, KS = D / 16;
+  static_assert(W * 32 * DV * 4 <= 2 * STAGE, "the maps are joined in the tiles' memory");
+};
+
+template <int D, int DV, int W>
+__global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch a, const WaDiffPlan p) {
+  using C = Fwd<D, DV, W>;
+  constexpr int KB = C::KB;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE];
+
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int map = w / W, slice = w % W;
+
+  // Work item: the key range fastest, then the units of a group in turn, tile after tile; longest tiles first where
+  // later queries see more keys.
+  int id = blockIdx.x;
+  const int chunk = id % p.splits;
+  id /= p.splits;
+  const int item = id;
+  const int first = id / (p.tiles * p.group) * p.group;  // unit
+  id -= first * p.tiles;
+  const int count = min(p.group, p.units - first);
+  const int unit = first + id % count;
+  int tile = id / count;
+  if (a.causal) tile = p.tiles - 1 - tile;
+  const int per_key_head = a.heads / a.kv_heads;
+  const int heads = p.packed ? a.kv_heads : a.heads;
+  const int b = unit / heads;
+  const int hk = p.packed ? unit % heads : unit % heads / per_key_head;
+
+  const int row = tile * 32 * W + slice * 32 + l32;
+  const int sub = p.packed ? row / a.q_len : 0;
+  const int h = p.packed ? hk * per_key_head + sub : unit % heads;
+  const int i = row - sub * a.q_len;
+  const bool valid = p.packed ? sub < per_key_head : i < a.q_len;
+
+  // limits: of this lane's query, of the wavefront's (all below `some`, all at or past `all`), of the workgroup's
+  const int keys = keys_of(a, b), start = start_of(a, b);
+  const int limit = valid ? key_limit(a, keys, start, i) : 0;
+  const int i0 = tile * 32 * W + slice * 32;  // not packed: the wavefront's first query
+  const int i_last = a.q_len - 1;
+  const int some = p.packed ? key_limit(a, keys, start, i_last) : i0 > i_last ? 0 : key_limit(a, keys, start, min(i0 + 31, i_last));
+  const int all = key_limit(a, keys, start, p.packed ? 0 : min(i0, i_last));
+  const int most = key_limit(a, keys, start, p.packed ? i_last : min(tile * 32 * W + 32 * W - 1, i_last));
+  // this workgroup's keys: a range of whole blocks and tiles
+  const int unit_keys = a.mask ? max(a.block, KB) : KB;
+  const int per = ((most + unit_keys - 1) / unit_keys + p.splits - 1) / p.splits;
+  const int lo = min((int64_t)chunk * per * unit_keys, (int64_t)most);
+  const int hi = min((int64_t)lo + per * unit_keys, (int64_t)most);
+
+  const unsigned char* kg[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+    kg[m] = (const unsigned char*)a.k + (((int64_t)b * 2 * a.kv_heads + 2 * hk + m) * a.kv_len) * C::KRB;
+  const unsigned char* vg = (const unsigned char*)a.v + (((int64_t)b * a.kv_heads + hk) * a.kv_len) * C::VRB;
+
+  MaskWalk walk;
+  const int shift = a.block == 128 ? 7 : 6;
+  if (a.mask) {
+    walk.at = a.mask + (((int64_t)b * a.heads + h) * a.mb + (tile * 32 * W >> shift)) * a.nb;
+    walk.at = uniform_ptr(walk.at);
+    walk.entries = (hi + a.block - 1) >> shift;
+  }
+  // first kept tile at or past `key`, a multiple of KB
+  auto next_tile = [&](int key) {
+    if (!a.mask || (key & (a.block - 1))) return key;
+    return walk.next(key >> shift, lane) << shift;
+  };
+  auto copy = [&](int key, int buf) {
+    const unsigned char* t = lds + buf * C::STAGE;
+    copy_tile<C::KRB, KB, C::NWV>(t, kg[0], key, keys - 1, w, lane);
+    copy_tile<C::KRB, KB, C::NWV>(t + C::KBYTES, kg[1], key, keys - 1, w, lane);
+    copy_tile<C::VRB, KB, C::NWV>(t + 2 * C::KBYTES, vg, key, keys - 1, w, lane);
+  };
+
+  bf16x8 qf[C::KS];
+  const uint16_t* qg = (const uint16_t*)a.q + (((int64_t)b * 2 * a.heads + 2 * h + map) * a.q_len + i) * D;
+#pragma unroll
+  for (int s = 0; s < C::KS; ++s) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (valid) u = *(const uint4*)(qg + 16 * s + 8 * hf);
+    qf[s] = as_bf16x8(u);
+  }
+  uint32_t kofs[C::KS], vofs[2][4];
+#pragma unroll
+  for (int s = 0; s < C::KS; ++s) kofs[s] = map * C::KBYTES + row_operand<C::KRB>(lane, s);
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) vofs[j][c] = 2 * C::KBYTES + col_operand<C::VRB>(lane, c & (C::DT - 1), j);
+
+  const float c2 = a.scale * kLog2e;
+  f32x16 acc[C::DT];
+#pragma unroll
+  for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[t][v] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  auto work = [&](int key, const unsigned char* t) {
+    f32x16 s[C::KT];
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[kt][v] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+      for (int kt = 0; kt < C::KT; ++kt)
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row(t + kofs[ks] + kt * 32 * C::KRB), qf[ks], s[kt], 0, 0, 0);
+    if (key + KB > all) {
+      const int rest = limit - key - 4 * hf;
+#pragma unroll
+      for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (kt * 32 + 8 * (v >> 2) + (v & 3) >= rest) s[kt][v] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, s[kt][v]);
+    top = max_halves(top) * c2;
+    const bool grow = top > m_run + kGrow;  // also from -inf; a row that has seen no key keeps -inf
+    if (__ballot(grow)) {
+      const float m_new = grow ? top : m_run;
+      const float f = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+      m_run = m_new;
+      l_run *= f;
+#pragma unroll
+      for (int t2 = 0; t2 < C::DT; ++t2)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[t2][v] *= f;
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    uint32_t pk[C::KT][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][v], c2, -ref));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][v + 1], c2, -ref));
+        sum += p0 + p1;
+        pk[kt][v >> 1] = pack_bf16x2(p0, p1);
+      }
+    l_run += sum;
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const bf16x8 pb = as_bf16x8(make_uint4(pk[kt][4 * s2], pk[kt][4 * s2 + 1], pk[kt][4 * s2 + 2], pk[kt][4 * s2 + 3]));
+        const unsigned char* tv = t + (kt * 32 + 16 * s2) * C::VRB;
+#pragma unroll
+        for (int dt = 0; dt < C::DT; ++dt)
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              read_cols(tv + vofs[0][dt & 3] + (dt >> 2) * 256, tv + vofs[1][dt & 3] + (dt >> 2) * 256), pb, acc[dt], 0, 0, 0);
+      }
+  };
+
+  int key = lo < hi ? next_tile(lo) : hi, buf = 0;
+  if (key < hi) copy(key, 0);
+  while (key < hi) {
+    const int next = next_tile(key + KB);
+    WA_WAIT_VM(0);  // this wavefront's part of the tile has arrived
+    WA_BARRIER();   // everyone's has, and everyone is done with the other buffer
+    if (next < hi) copy(next, buf ^ 1);
+    if (key < some) work(key, lds + buf * C::STAGE);
+    key = next;
+    buf ^= 1;
+  }
+
+  const float l = add_halves(l_run);
+  if (p.splits > 1) {
+    if (!valid) return;
+    const int64_t n = (int64_t)item * p.splits + chunk, rows = 32 * W;
+    const int64_t at = (n * 2 + map) * rows + slice * 32 + l32;
+    float* out = a.part + at * DV;
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4)
+        *(float4*)(out + dt * 32 + 2 * v + 4 * hf) = make_float4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3]);
+    if (hf == 0) {
+      float2* stat = (float2*)(a.part + (int64_t)p.units * p.tiles * p.splits * 2 * rows * DV);
+      stat[at] = make_float2(m_run, l);
+    }
+    return;
+  }
+
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+  if (a.lse && valid && hf == 0)
+    a.lse[((int64_t)b * 2 * a.heads + 2 * h + map) * a.q_len + i] = l == 0.f ? -INFINITY : (m_run + __log2f(l)) * kLn2;
+  // the second map's wavefronts hand their rows to the first's
+  float* meet = (float*)lds + slice * 32 * DV;
+  __syncthreads();
+  const int64_t at = (((int64_t)b * a.heads + h) * a.q_len + i) * DV;
+  if (map == 1) {
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        acc[dt][v] *= inv;
+        meet[(dt * 16 + v) * 64 + lane] = acc[dt][v];
+      }
+  }
+  __syncthreads();
+  uint16_t* out = (uint16_t*)(map == 1 ? a.o2 : a.o);
+  if (map == 0) {
+    const float lam = valid ? a.lam[h] : 0.f;
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[dt][v] = acc[dt][v] * inv - lam * meet[(dt * 16 + v) * 64 + lane];
+  }
+  if (valid && out) {
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4)
+        *(uint2*)(out + at + dt * 32 + 2 * v + 4 * hf) =
+            make_uint2(pack_bf16x2(acc[dt][v], acc[dt][v + 1]), pack_bf16x2(acc[dt][v + 2], acc[dt][v + 3]));
+  }
+}
+
+// Joins the key ranges of split tiles, in order: one wavefront a query row, DV / 64 columns a lane.
+template <int DV>
+__global__ __launch_bounds__(256) void diff_join_kernel(const WaDiffLaunch a, const WaDiffPlan p) {
+  constexpr int E = DV / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= (int64_t)a.batch * a.heads * a.q_len) return;
+  const int i = r % a.q_len;
+  const int bh = r / a.q_len, b = bh / a.heads, h = bh % a.heads;
+  const int per_key_head = a.heads / a.kv_heads;
+  const int unit = p.packed ? b * a.kv_heads + h / per_key_head : bh;
+  const int row = p.packed ? h % per_key_head * a.q_len + i : i;
+  const int rows = 32 * p.waves, tile = row / rows;
+  // the tile's place in the order of the work items
+  const int first = unit / p.group * p.group, count = min(p.group, p.units - first);
+  const int64_t item = (int64_t)first * p.tiles + (int64_t)(a.causal ? p.tiles - 1 - tile : tile) * count + unit - first;
+  const float2* stat = (const float2*)(a.part + (int64_t)p.units * p.tiles * p.splits * 2 * rows * DV);
+  float o[2][E];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    auto at = [&](int c) { return ((item * p.splits + c) * 2 + m) * rows + row % rows; };
+    float top = -INFINITY, l = 0.f;
+    for (int c = lane; c < p.splits; c += 64) top = fmaxf(top, stat[at(c)].x);
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[m][e] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < p.splits; ++c) {
+      const float2 s = stat[at(c)];
+      const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
+      l += f * s.y;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[m][e] += f * a.part[at(c) * DV + lane * E + e];
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[m][e] *= inv;
+    if (a.lse && lane == 0)
+      a.lse[((int64_t)b * 2 * a.heads + 2 * h + m) * a.q_len + i] = l == 0.f ? -INFINITY : (top + __log2f(l)) * kLn2;
+  }
+  const float lam = a.lam[h];
+  __bf16* out = (__bf16*)a.o + r * DV + lane * E;
+  __bf16* out2 = (__bf16*)a.o2 + r * DV + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    out[e] = (__bf16)(o[0][e] - lam * o[1][e]);
+    if (a.o2) out2[e] = (__bf16)o[1][e];
+  }
+}
+
+template <int D, int DV>
+hipError_t launch_dims(const WaDiffLaunch& a, const WaDiffPlan& p, hipStream_t stream) {
+  const int64_t grid = (int64_t)p.units * p.tiles * p.splits;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 g((unsigned)grid), t(128 * p.waves);
+  if (p.waves == 1) hipLaunchKernelGGL((diff_fwd_kernel<D, DV, 1>), g, t, 0, stream, a, p);
+  if (p.waves == 2) hipLaunchKernelGGL((diff_fwd_kernel<D, DV, 2>), g, t, 0, stream, a, p);
+  if (p.waves == 4) hipLaunchKernelGGL((diff_fwd_kernel<D, DV, 4>), g, t, 0, stream, a, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const int64_t rows = (int64_t)a.batch * a.heads * a.q_len;
+  hipLaunchKernelGGL((diff_join_kernel<DV>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked) {
+  WaDiffPlan p{};
+  const int per_key_head = a.heads / a.kv_heads;
+  // Heads that share keys share a tile while one head's queries would leave most of it empty; a mask is a head's own.
+  p.packed = !masked && per_key_head > 1 && a.q_len <= 32;
+  const int64_t rows = p.packed ? (int64_t)per_key_head * a.q_len : a.q_len;
+  p.waves = rows <= 32 ? 1 : rows <= 64 || (masked && a.block == 64) ? 2 : 4;
+  p.units = a.batch * (p.packed ? a.kv_heads : a.heads);
+  p.tiles = (int32_t)((rows + 32 * p.waves - 1) / (32 * p.waves));
+  // Key ranges: as many as keep 256 compute units busy (two workgroups each of less than four wavefronts a map), of
+  // 256 keys at least.
+  const int64_t slots = p.waves == 4 ? 256 : 512, items = (int64_t)p.units * p.tiles;
+  p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(slots / items, a.kv_len / 256));
+  p.group = 8;
+  return p;
+}
+
+size_t wa_diff_part_floats(const WaDiffPlan& p, int value_dim) {
+  return p.splits == 1 ? 0 : (size_t)p.units * p.tiles * p.splits * 2 * 32 * p.waves * (value_dim + 2);
+}
+
+hipError_t wa_launch_diff_attn(const WaDiffLaunch& a, hipStream_t stream) {
+  const WaDiffPlan p = wa_diff_plan(a, a.mask != nullptr);
+  if (a.head_dim == 64 && a.value_dim == 64) return launch_dims<64, 64>(a, p, stream);
+  if (a.head_dim == 64 && a.value_dim == 128) return launch_dims<64, 128>(a, p, stream);
+  if (a.head_dim == 128 && a.value_dim == 128) return launch_dims<128, 128>(a, p, stream);
+  if (a.head_dim == 128 && a.value_dim == 256) return launch_dims<128, 256>(a, p, stream);
+  return hipErrorInvalidValue;
+}

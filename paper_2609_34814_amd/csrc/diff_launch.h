@@ -1,0 +1,45 @@
+// Internal launch interface of the differential-attention kernels (not part of the ABI).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+struct WaDiffLaunch {
+  const void* q;      // bf16 [batch][2 heads][q_len][head_dim]: maps 2h and 2h + 1 of head h
+  const void* k;      // bf16 [batch][2 kv_heads][kv_len][head_dim]
+  const void* v;      // bf16 [batch][kv_heads][kv_len][value_dim]
+  const float* lam;   // [heads]
+  const uint8_t* mask;     // [batch][heads][mb][nb], null: every block
+  const int32_t* q_start;  // [batch], null: kv_len - q_len
+  const int32_t* kv_lens;  // [batch], null: kv_len
+  void* o;            // bf16 [batch][heads][q_len][value_dim]
+  void* o2;           // the second map's output, nullable
+  float* lse;         // [batch][2 heads][q_len], nullable
+  float* part;        // split calls: partial tiles, then their statistics
+  int32_t batch, heads, kv_heads, q_len, kv_len, head_dim, value_dim, block, mb, nb, causal;
+  float scale;
+  // backward
+  const void* dout;   // bf16 [batch][heads][q_len][value_dim]
+  void* dq;
+  void* dk;
+  void* dv;
+  float* dlam;        // [heads]
+  float* rows;        // workspace: [batch][2 heads][q_len] dO . O_m
+  float* lam_part;    // workspace: [batch][heads][tiles of q_len] partial sums for dlam
+};
+
+// How a forward call is cut into workgroups (see diff_plan in diff_attn.hip).
+struct WaDiffPlan {
+  int32_t waves;   // wavefronts a map of a workgroup, 32 query rows each: 1, 2 or 4
+  int32_t packed;  // 1: the rows of a tile run over the queries of all heads of a key head
+  int32_t units;   // (sequence, head) or, packed, (sequence, key head) pairs
+  int32_t tiles;   // row tiles of a unit
+  int32_t splits;  // key ranges a tile is computed in
+  int32_t group;   // units whose tiles are dealt out in turn
+};
+WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked);
+size_t wa_diff_part_floats(const WaDiffPlan& p, int value_dim);
+
+hipError_t wa_launch_diff_attn(const WaDiffLaunch& a, hipStream_t stream);
+hipError_t wa_launch_diff_backward(const WaDiffLaunch& a, hipStream_t stream);
+int32_t wa_diff_bwd_tiles(const WaDiffLaunch& a);

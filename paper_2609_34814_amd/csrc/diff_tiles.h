@@ -1,0 +1,147 @@
+// Tiles, masks and row limits shared by the differential-attention kernels.
+//
+// Every operand tile lies in LDS as it lies in memory, one token a row, and serves two kinds of matrix operand:
+// rows (16 consecutive bytes of one token, ds_read_b128) for products over the head's columns, and columns (4
+// tokens of one column, ds_read_b64_tr_b16) for products over the tokens. So no tensor is transposed beforehand and no tile
+// is held twice.
+#pragma once
+
+#include "diff_launch.h"
+#include "tile_ops.h"
+
+namespace wa {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Physical 16-byte chunk of (row, chunk) in a tile with rows of RB bytes. 64 banks of 4 bytes are 256 bytes: of
+// 256-byte (or longer) rows, 16 rows read at one chunk fall on 16 different places, and 4 consecutive rows, of which a transposed read
+// takes 64 bytes each, on 4 different quarters; of 128-byte rows, two make such a line and the same holds
+// for pairs.
+template <int RB>
+__device__ __forceinline__ int tile_chunk(int row, int chunk) {
+  return RB >= 256 ? chunk ^ ((row & 3) << 2 | (row >> 2 & 3)) : chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
+}
+
+// Byte offset of the row operand: 8 columns from 16 s + 8 (lane / 32) of row lane % 32 (a multiple of 32 rows further
+// is that many RB further).
+template <int RB>
+__device__ __forceinline__ uint32_t row_operand(int lane, int s) {
+  const int row = lane & 31;
+  return row * RB + tile_chunk<RB>(row, 2 * s + (lane >> 5)) * 16;
+}
+
+// Byte offset of half j of the column operand of column tile c (32 columns): the lane receives rows
+// 4 (lane / 32) + 8 j + 0..3 of column 32 c + lane % 32 (a multiple of 16 rows further is that many RB further).
+// Sixteen lanes read 4 rows of 16 columns, lane i row i / 4 and columns 4 (i % 4) on, and exchange them.
+template <int RB>
+__device__ __forceinline__ uint32_t col_operand(int lane, int c, int j) {
+  const int g = lane >> 4, i = lane & 15;
+  const int row = 8 * j + 4 * (g >> 1) + (i >> 2);
+  return row * RB + tile_chunk<RB>(row, 4 * c + 2 * (g & 1) + (i >> 1 & 1)) * 16 + (i & 1) * 8;
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// The column operand from its two halves: rows (lane / 32) 4 + {0..3, 8..11} of 16, the order in which a product's
+// output registers hold them, so a product over those rows takes them as they are.
+__device__ __forceinline__ bf16x8 read_cols(const unsigned char* h0, const unsigned char* h1) {
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)h0);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)h1);
+  const s16x8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+__device__ __forceinline__ bf16x8 read_row(const unsigned char* p) { return as_bf16x8(*(const uint4*)p); }
+
+// Copies rows [row0, row0 + ROWS) of g (rows of RB bytes) into a tile, by NWV wavefronts; rows past `last` are row
+// `last` again (what they add is masked, and they hold no memory that the caller did not write).
+template <int RB, int ROWS, int NWV>
+__device__ __forceinline__ void copy_tile(const unsigned char* tile, const unsigned char* g, int row0, int last, int w,
+                                          int lane) {
+  constexpr int RPI = 1024 / RB, LPR = RB / 16, N = ROWS * RB / 1024 / NWV;
+  static_assert(N >= 1 && N * NWV * 1024 == ROWS * RB, "a tile is whole copies of every wavefront");
+  constexpr bool kSame = NWV * RPI % 16 == 0;  // the swizzle repeats from copy to copy
+  const int r0 = w * RPI + lane / LPR;
+  if (row0 + ROWS <= last + 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = r0 + i * NWV * RPI;
+      dma16(g + (int64_t)(row0 + i * NWV * RPI) * RB,
+            (uint32_t)(r0 * RB + tile_chunk<RB>(kSame ? r0 : r, lane % LPR) * 16), tile + (i * NWV + w) * 1024);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = r0 + i * NWV * RPI;
+      dma16(g, (uint32_t)(min(row0 + r, last) * RB + tile_chunk<RB>(r, lane % LPR) * 16), tile + (i * NWV + w) * 1024);
+    }
+  }
+}
+
+// Keys that exist for sequence b, and the first query's position; both clamped, so that no value of the device
+// arrays leads out of a tensor.
+__device__ __forceinline__ int keys_of(const WaDiffLaunch& a, int b) {
+  return a.kv_lens ? min(max(a.kv_lens[b], 0), a.kv_len) : a.kv_len;
+}
+__device__ __forceinline__ int start_of(const WaDiffLaunch& a, int b) {
+  return a.q_start ? min(max(a.q_start[b], -a.q_len), a.kv_len) : a.kv_len - a.q_len;
+}
+// Query i sees the keys below this.
+__device__ __forceinline__ int key_limit(const WaDiffLaunch& a, int keys, int start, int i) {
+  return a.causal ? min(keys, max(start + i + 1, 0)) : keys;
+}
+
+// A pointer that is the same in every lane, as scalar registers (the builtin returns signed words).
+template <typename T>
+__device__ __forceinline__ T* uniform_ptr(T* p) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+  return (T*)((uint64_t)hi << 32 | lo);
+}
+
+// Walks the kept blocks of one row (step 1) or column (step nb) of a head's mask: 64 entries at a time, one a lane, as
+// a word of bits.
+struct MaskWalk {
+  const uint8_t* at = nullptr;  // entry 0; null: every block is kept
+  int64_t step = 1;
+  int entries = 0, word_i = -1;
+  uint64_t word = 0;
+
+  // First kept entry at or past j, or a value >= entries.
+  __device__ __forceinline__ int next(int j, int lane) {
+    while (j < entries) {
+      if (j >> 6 != word_i) {
+        word_i = j >> 6;
+        const int e = word_i * 64 + lane;
+        word = __ballot(e < entries && at[e * step] != 0);
+      }
+      const uint64_t rest = word >> (j & 63);
+      if (rest) return j + __builtin_ctzll(rest);
+      j = (word_i + 1) * 64;
+    }
+    return j;
+  }
+};
+
+// The value of lane % 32 and that of lane % 32 + 32. In assembly: the compiler reads both results of its builtin from
+// one register. The exchange needs two wait states after a write of its operands.
+__device__ __forceinline__ f32x2 both_halves(float x) {
+  float lo = x, hi = x;
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(lo), "+v"(hi));
+  const f32x2 v = {lo, hi};
+  return v;
+}
+__device__ __forceinline__ float max_halves(float x) {
+  const f32x2 v = both_halves(x);
+  return fmaxf(v[0], v[1]);
+}
+__device__ __forceinline__ float add_halves(float x) {
+  const f32x2 v = both_halves(x);
+  return v[0] + v[1];
+}
+
+}  // namespace wa

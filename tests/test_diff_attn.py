@@ -1,0 +1,279 @@
+"""Differential attention: refusals on the CPU, the forward kernels against the fp64 oracle on the GPU."""
+import ctypes
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2609_34814_amd as W                     # noqa: E402
+from oracle import diff_attention as D               # noqa: E402
+from paper_2609_34814_amd import _lib as L           # noqa: E402
+from tests.test_abi import FAKE, _lib                # noqa: E402
+
+INVALID, ALIGN, UNSUP, WORK = L.WA_ERR_INVALID_ARG, L.WA_ERR_ALIGNMENT, L.WA_ERR_UNSUPPORTED, L.WA_ERR_WORKSPACE
+
+
+# ---- CPU ---------------------------------------------------------------------------------------------------
+
+def _shape(**kw):
+    d = dict(batch=2, heads=4, kv_heads=2, q_len=300, kv_len=300, head_dim=64, value_dim=128, block=64)
+    d.update(kw)
+    return L.WaDiffShape(*[d[n] for n, _ in L.WaDiffShape._fields_])
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(q_len=0), INVALID),
+    (dict(kv_len=0), INVALID), (dict(kv_heads=3), INVALID), (dict(head_dim=96), UNSUP), (dict(value_dim=192), UNSUP),
+    (dict(value_dim=32), UNSUP), (dict(block=32), UNSUP), (dict(kv_len=64 * 4097), UNSUP), (dict(q_len=64 * 4097), UNSUP),
+    (dict(batch=1 << 16, heads=1 << 16, kv_heads=1), UNSUP),
+])
+def test_shape_refusals(kw, code):
+    lib, n = _lib(), ctypes.c_size_t(0)
+    assert lib.wa_diff_attn_workspace_size(ctypes.byref(_shape(**kw)), ctypes.byref(n)) == code
+    assert lib.wa_last_error()
+    assert lib.wa_diff_attn_workspace_size(None, ctypes.byref(n)) == INVALID
+    assert lib.wa_diff_attn_workspace_size(ctypes.byref(_shape()), None) == INVALID
+
+
+def test_argument_refusals():
+    lib = _lib()
+    odd = ctypes.c_void_p((1 << 20) + 2)
+    few = _shape(batch=1, heads=1, kv_heads=1, q_len=1, kv_len=8192)
+    n = ctypes.c_size_t(0)
+    assert lib.wa_diff_attn_workspace_size(ctypes.byref(few), ctypes.byref(n)) == 0 and n.value > 0
+
+    def call(q=FAKE, k=FAKE, v=FAKE, lam=FAKE, mask=None, start=None, lens=None, shape=few, opts=L.WaDiffOptions(0.0, 1),
+             o=FAKE, o2=None, lse=None, ws=FAKE, size=n.value):
+        return lib.wa_diff_attn(q, k, v, lam, mask, start, lens, ctypes.byref(shape),
+                                None if opts is None else ctypes.byref(opts), o, o2, lse, ws, size, None)
+
+    for name in ("q", "k", "v", "lam", "o"):
+        assert call(**{name: None}) == INVALID, name
+    for name in ("q", "k", "v", "lam", "o", "o2", "lse", "start", "lens"):
+        assert call(**{name: odd}) == ALIGN, name
+    assert call(opts=None) == INVALID
+    assert call(start=FAKE, opts=L.WaDiffOptions(0.0, 0)) == INVALID
+    assert call(ws=None) == INVALID and call(size=n.value - 1) == WORK
+    assert call(ws=ctypes.c_void_p((1 << 20) + 64)) == ALIGN
+    assert call(shape=_shape(block=16)) == UNSUP
+
+
+def _host(b=1, h=2, hk=1, m=70, n=70, d=64, dv=64):
+    bf = torch.bfloat16
+    return dict(q=torch.zeros(b, 2 * h, m, d, dtype=bf), k=torch.zeros(b, 2 * hk, n, d, dtype=bf),
+                v=torch.zeros(b, hk, n, dv, dtype=bf), lam=torch.zeros(h))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=torch.zeros(1, 4, 70, 64)), dict(q=torch.zeros(1, 3, 70, 64, dtype=torch.bfloat16)),
+    dict(k=torch.zeros(1, 4, 70, 64, dtype=torch.bfloat16)), dict(v=torch.zeros(2, 1, 70, 64, dtype=torch.bfloat16)),
+    dict(lam=torch.zeros(3)), dict(lam=torch.zeros(2, dtype=torch.bfloat16)), dict(mask=torch.zeros(1, 2, 1, 2, dtype=torch.uint8)),
+    dict(mask=torch.zeros(1, 2, 1, 1)), dict(q_start=torch.zeros(1, dtype=torch.int32)),
+    dict(kv_lens=torch.zeros(1, dtype=torch.int64)), dict(kv_lens=torch.zeros(2, dtype=torch.int32)),
+    dict(out=torch.zeros(1, 2, 70, 64)), dict(workspace=torch.zeros(4)), dict(),   # the last: host tensors
+])
+def test_binding_refusals(kw):
+    args = _host()
+    args.update(kw)
+    with pytest.raises(ValueError):
+        W.diff_attn(args.pop("q"), args.pop("k"), args.pop("v"), args.pop("lam"), args.pop("mask", None), **args)
+
+
+def test_oracle_gradient_by_differences():
+    """The oracle's own gradients against central differences of its forward (step 1e-5: the error is about 1e-10
+    of third derivatives and 1e-11 of rounding)."""
+    rng = np.random.default_rng(5)
+    q, k, v = rng.standard_normal((1, 4, 5, 3)), rng.standard_normal((1, 2, 6, 3)), rng.standard_normal((1, 1, 6, 2))
+    lam, g = rng.standard_normal(2), rng.standard_normal((1, 2, 5, 2))
+    kw = dict(causal=True, kv_lens=[5], mask=None)
+    got = D.forward_backward(q, k, v, lam, dout=g, **kw)
+    for x, name in ((q, "dq"), (k, "dk"), (v, "dv"), (lam, "dlam")):
+        num = np.zeros_like(x)
+        for idx in np.ndindex(x.shape):
+            old = x[idx]
+            x[idx] = old + 1e-5
+            up = (D.forward_backward(q, k, v, lam, **kw)["o"] * g).sum()
+            x[idx] = old - 1e-5
+            num[idx] = (up - (D.forward_backward(q, k, v, lam, **kw)["o"] * g).sum()) / 2e-5
+            x[idx] = old
+        assert np.abs(num - got[name]).max() < 1e-8, name
+
+
+# ---- GPU ---------------------------------------------------------------------------------------------------
+
+def make(b, h, hk, m, n, d, dv, seed=0, gain=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def r(*s):
+        return torch.randn(s, generator=g, device="cuda")
+    bf = torch.bfloat16
+    return [(r(b, 2 * h, m, d) * gain).to(bf), r(b, 2 * hk, n, d).to(bf), r(b, hk, n, dv).to(bf), r(h) * 0.3 + 0.5]
+
+
+def block_mask(b, h, m, n, block, rho, seed=1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    mask = (torch.rand((b, h, -(-m // block), -(-n // block)), generator=g, device="cuda") < rho).to(torch.uint8)
+    mask[:, :, -1] = 0          # rows that see nothing
+    mask[:, :, 0, -1] = 1
+    return mask
+
+
+def reference(args, mask, block, kw, dout=None):
+    host = [x.double().cpu().numpy() for x in args]
+    okw = {x: y.cpu().numpy() if torch.is_tensor(y) else y for x, y in kw.items()}
+    return D.forward_backward(*host, block=block, mask=None if mask is None else mask.cpu().numpy(),
+                              dout=None if dout is None else dout.double().cpu().numpy(), **okw)
+
+
+def check_forward(args, mask=None, block=128, **kw):
+    """Probabilities are rounded once, at most 2^-8 of each; float32 scores: 130 operations of 2^-24 on at most
+    scale sum |q k| < 30 in these tests, 2^-12 in the exponent, so 2^-11 of a probability; the result is rounded
+    once, 2^-8 of it."""
+    o, o2, lse = W.diff_attn(*args, mask, block=block, return_stats=True, **kw)
+    plain = W.diff_attn(*args, mask, block=block, **kw)
+    assert torch.equal(plain, o)                       # the statistics change nothing
+    ref = reference(args, mask, block, kw)
+    for name, y in (("o", o), ("o2", o2)):
+        err = np.abs(y.double().cpu().numpy() - ref[name])
+        tol = (2.0 ** -8 + 2.0 ** -11) * ref["bound"][name] * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref[name])
+        assert np.all(err <= tol), (name, float((err - tol).max()))
+    got = lse.double().cpu().numpy()
+    assert np.array_equal(np.isneginf(got), np.isneginf(ref["lse"]))
+    some = np.isfinite(ref["lse"])
+    assert np.all(np.abs(got[some] - ref["lse"][some]) <= 2.0 ** -11 + 2.0 ** -22 * np.abs(ref["lse"][some]))
+
+
+DIMS = [(64, 64), (64, 128), (128, 128), (128, 256)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dv", DIMS)
+@pytest.mark.parametrize("b,h,hk,m,n", [(1, 1, 1, 1, 1), (2, 4, 2, 1, 777), (1, 2, 1, 200, 200), (1, 3, 3, 33, 500),
+                                        (2, 2, 1, 65, 31), (1, 8, 1, 5, 1030)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_dense(b, h, hk, m, n, d, dv, causal):
+    check_forward(make(b, h, hk, m, n, d, dv), causal=causal)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dv", DIMS)
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("b,h,hk,m,n,causal", [(1, 2, 2, 300, 300, False), (2, 2, 1, 321, 321, True), (1, 2, 1, 20, 900, False),
+                                               (1, 1, 1, 200, 9000, False)])
+def test_block_masks(b, h, hk, m, n, d, dv, block, causal):
+    """The last shape's rows are longer than one word of 64 blocks; the last query block of each sees nothing."""
+    args = make(b, h, hk, m, n, d, dv)
+    check_forward(args, block_mask(b, h, m, n, block, 0.4), block, causal=causal)
+    empty = torch.zeros((b, h, -(-m // block), -(-n // block)), dtype=torch.bool, device="cuda")
+    o, _, lse = W.diff_attn(*args, empty, block=block, return_stats=True)
+    assert not o.any() and torch.all(lse == -float("inf"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dv", DIMS)
+@pytest.mark.parametrize("m,hk", [(1, 1), (3, 2), (70, 4), (260, 1)])
+def test_ragged_batches(d, dv, m, hk):
+    """Lengths from nothing to everything; what lies behind them is not a number and does not matter."""
+    n, lens = 600, [0, 1, 63, 64, 65, 599, 600]
+    args = make(len(lens), 4, hk, m, n, d, dv)
+    for b, x in enumerate(lens):
+        args[1][b, :, x:] = float("nan")
+        args[2][b, :, x:] = float("nan")
+    kv = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    check_forward(args, kv_lens=kv)
+    check_forward(args, kv_lens=kv, causal=True, q_start=kv - m)
+    # lengths outside 0..n are taken into it
+    assert torch.equal(W.diff_attn(*args[:1], *(torch.nan_to_num(x) for x in args[1:3]), args[3],
+                                   kv_lens=torch.tensor([-5, 2 ** 31 - 1] + [n] * 5, dtype=torch.int32, device="cuda")),
+                       W.diff_attn(*args[:1], *(torch.nan_to_num(x) for x in args[1:3]), args[3],
+                                   kv_lens=torch.tensor([0, n] + [n] * 5, dtype=torch.int32, device="cuda")))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(40, 300), (300, 300), (130, 40)])
+def test_query_positions(m, n):
+    args = make(5, 2, 1, m, n, 64, 128)
+    start = torch.tensor([-2 ** 31, -7, 0, n // 2, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    seen = start.clamp(-m, n)
+    ref = dict(causal=True, q_start=seen)
+    o, o2, lse = W.diff_attn(*args, causal=True, q_start=start, return_stats=True)
+    assert torch.equal(o, W.diff_attn(*args, **ref))
+    check_forward(args, **ref)
+
+
+@pytest.mark.gpu
+def test_blocks_that_are_dropped_are_not_read():
+    args = make(1, 1, 1, 256, 512, 128, 128)
+    mask = torch.tensor([[1, 0, 1, 0], [0, 0, 1, 0]], dtype=torch.uint8, device="cuda").view(1, 1, 2, 4)
+    for x in (1, 2):
+        args[x][:, :, 128:256] = args[x][:, :, 384:] = float("nan")
+    check_forward(args, mask)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [1, 200])
+def test_growing_and_large_scores(m):
+    """The running maximum grows along the keys, in one map only; and scores of hundreds, where one key takes all."""
+    args = make(1, 2, 1, m, 700, 64, 64)
+    ramp = torch.linspace(0, 6, 700, device="cuda")
+    args[1][:, 1] = (args[1][:, 1].float() * ramp[:, None]).to(torch.bfloat16)
+    o = W.diff_attn(*args, return_stats=True)
+    ref = reference(args, None, 128, {})
+    # scores up to about 40 here: 2^-24 (64 + 2) 40 sqrt(64) in the exponent, below 2^-9
+    for name, y in zip(("o", "o2"), o):
+        err = np.abs(y.double().cpu().numpy() - ref[name])
+        assert np.all(err <= (2.0 ** -8 + 2.0 ** -8) * ref["bound"][name] + 2.0 ** -8 * np.abs(ref[name])), name
+    args = make(1, 2, 1, m, 700, 64, 64, gain=100.0)
+    o = W.diff_attn(*args)
+    assert torch.isfinite(o).all() and o.float().abs().max() <= 2 * args[2].float().abs().max() * 1.01
+
+
+@pytest.mark.gpu
+def test_scale_and_given_outputs():
+    args = make(1, 2, 2, 100, 100, 64, 64)
+    check_forward(args, scale=0.3)
+    out = torch.empty((1, 2, 100, 64), dtype=torch.bfloat16, device="cuda")
+    assert W.diff_attn(*args, out=out) is out and torch.equal(out, W.diff_attn(*args))
+
+
+@pytest.mark.gpu
+def test_one_map_less_is_attention():
+    """lam 0 leaves the first map's attention, which sparse_attn computes too: two roundings of probabilities and
+    of results, and P V of magnitude below 5."""
+    q, k, v, lam = make(1, 2, 2, 512, 512, 128, 128)
+    mask = block_mask(1, 2, 512, 512, 128, 0.6)
+    o = W.diff_attn(q, k, v, torch.zeros_like(lam), mask)
+    first = W.sparse_attn(q[:, ::2].contiguous(), k[:, ::2].contiguous(), v, mask, block=128)
+    assert (o.float() - first.float()).abs().max() <= 5 * 4 * 2.0 ** -8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(1, 3000), (200, 300)])
+def test_streams_and_replays(m, n):
+    """Two calls at once with workspaces of their own, and a captured call replayed on new inputs."""
+    args = make(2, 4, 2, m, n, 64, 128)
+    want = W.diff_attn(*args)
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = []
+    for s in sides:
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            outs.append(W.diff_attn(*args))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in outs)
+    shape = W.diff_shape_of(2, 4, 2, m, n, 64, 128)
+    ws = torch.empty(max(1, W.diff_attn_workspace_size(shape)), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        W.diff_attn(*args, out=out, workspace=ws)
+    for seed in (7, 8, 9):
+        for x, y in zip(args, make(2, 4, 2, m, n, 64, 128, seed=seed)):
+            x.copy_(y)
+        out.zero_()
+        ws.fill_(255)
+        want = W.diff_attn(*args)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
