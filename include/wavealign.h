@@ -434,9 +434,8 @@ typedef struct wa_diff_options {
   int32_t causal;       /* nonzero: query i of sequence b sees the keys j <= q_start[b] + i */
 } wa_diff_options;
 
-/* Workspace bytes needed by wa_diff_attn (partial results of calls with few rows, whose keys are split over
- * workgroups; 0 for others) and by wa_diff_attn_backward. Calls that share a workspace must
- * not overlap, captured ones included. */
+/* Workspace bytes needed by wa_diff_attn: partial results of calls with few rows, whose keys are split over
+ * workgroups; 0 for others. Calls that share a workspace must not overlap, captured ones included. */
 wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes);
 
 /* Differential attention forward: head h has two softmax maps over the same kept keys,
@@ -463,6 +462,28 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
                        const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
                        const wa_diff_options* options, void* o, void* o2, float* lse, void* workspace,
                        size_t workspace_bytes, void* stream);
+
+/* Workspace bytes needed by wa_diff_attn_backward: 2 B H q_len float32 row sums and a float32 per tile of queries. */
+wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_t* bytes);
+
+/* Gradient of wa_diff_attn: with dO of O it writes
+ *   dV = sum over the heads of a key head of (P_1 - lam P_2)^T dO,
+ *   dQ_m = scale dS_m K_m, dK_m = sum of scale dS_m^T Q_m, dlam[h] = -sum over b, i of dO_i . (P_2 V)_i,
+ *   dS_1 = P_1 (dP - dO . O_1), dS_2 = -lam P_2 (dP - dO . O_2), dP = dO V^T,
+ * probabilities recomputed in float32 from lse, sums in float32 (dlam in float64 over tiles), P and dS rounded to
+ * bf16 for the matrix products. Every output is overwritten; keys at or past kv_lens[b] get 0, and so do queries
+ * with no kept key. Nothing is added with atomics: equal calls give equal bits.
+ *   dout     bf16 [B][H][q_len][value_dim], 16-byte aligned
+ *   q, k, v, lam, mask, q_start, kv_lens, shape, options   as given to wa_diff_attn
+ *   o, o2, lse   what that call wrote
+ *   dq, dk, dv   out bf16, shaped as q, k and v, 16-byte aligned
+ *   dlam         out float [H]
+ *   workspace    >= wa_diff_attn_backward_workspace_size(shape), 256-byte aligned */
+wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, const void* v, const float* lam,
+                                const void* o, const void* o2, const float* lse, const uint8_t* mask,
+                                const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
+                                const wa_diff_options* options, void* dq, void* dk, void* dv, float* dlam,
+                                void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- diagnostics (used by the test suite; not needed by callers) ---- */
 

@@ -578,6 +578,39 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
     return (o, o2, lse) if return_stats else o
 
 
+def diff_attn_backward_workspace_size(shape: L.WaDiffShape) -> int:
+    return _size("wa_diff_attn_backward_workspace_size", shape)
+
+
+def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor,
+                       mask: Optional[torch.Tensor], o: torch.Tensor, o2: torch.Tensor, lse: torch.Tensor, *,
+                       block: int = 128, scale: Optional[float] = None, causal: bool = False,
+                       q_start: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None):
+    """(dq, dk, dv bf16, dlam float32) from dout, the gradient of diff_attn's O: the other arguments as that call had
+    them, o, o2 and lse as it returned them with return_stats. Keys past kv_lens get 0. Equal calls give equal bits."""
+    lib = L.load()
+    shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)
+    want = (shape.batch, shape.heads, shape.q_len, shape.value_dim)
+    for t, nm in ((dout, "dout"), (o, "o"), (o2, "o2")):
+        _check(t, nm, torch.bfloat16, want)
+    _check(lse, "lse", torch.float32, (want[0], 2 * want[1], want[2]))
+    _check(workspace, "workspace", torch.uint8)
+    given = dict(dout=dout, q=q, k=k, v=v, lam=lam, mask=mask, o=o, o2=o2, lse=lse, q_start=q_start, kv_lens=kv_lens,
+                 workspace=workspace)
+    _on_device(**given)
+    dev = _one_device(**given)
+    need = diff_attn_backward_workspace_size(shape)
+    if workspace is None or workspace.numel() < need:
+        workspace = _workspace(need, dev)
+    dq, dk, dv, dlam = (torch.empty_like(t) for t in (q, k, v, lam))
+    opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
+    _call_on(dev, lib.wa_diff_attn_backward, _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(o), _ptr(o2),
+             _ptr(lse), _ptr(mask), _ptr(q_start), _ptr(kv_lens), ctypes.byref(shape), ctypes.byref(opts), _ptr(dq),
+             _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), workspace.numel())
+    return dq, dk, dv, dlam
+
+
 def fp64_probe(a: torch.Tensor, b: torch.Tensor, c: torch.Tensor) -> torch.Tensor:
     lib = L.load()
     out = torch.empty((a.numel(), 6), dtype=torch.float64, device=a.device)

@@ -29,6 +29,7 @@ SOURCES = {
     "mask_producer.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"],
     "rotary.hip": [],
     "diff_attn.hip": [],
+    "diff_bwd.hip": [],
     "abi.cpp": [],
 }
 

@@ -333,6 +333,12 @@ size_t diff_ws_bytes(const WaDiffLaunch& a) {
                                wa_diff_part_floats(wa_diff_plan(a, true), a.value_dim)));
 }
 
+// Workspace of the gradient: the row sums, then the parts of dlam (tiles of 64 queries at the least).
+size_t diff_rows_bytes(const WaDiffLaunch& a) { return align_up((size_t)2 * a.batch * a.heads * a.q_len * 4); }
+size_t diff_backward_ws_bytes(const WaDiffLaunch& a) {
+  return diff_rows_bytes(a) + align_up((size_t)a.batch * a.heads * ((a.q_len + 63) / 64) * 4);
+}
+
 // Arguments that both directions share, checked and put into the launch.
 wa_status check_diff_args(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
                           const int32_t* q_start, const int32_t* kv_lens, const wa_diff_options* options, WaDiffLaunch* a) {
@@ -779,6 +785,41 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
   a.part = (float*)workspace;
   const hipError_t e = wa_launch_diff_attn(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention launch");
+  return ok();
+}
+
+wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_t* bytes) {
+  WaDiffLaunch a{};
+  wa_status s = check_diff_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
+  *bytes = diff_backward_ws_bytes(a);
+  return ok();
+}
+
+wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, const void* v, const float* lam,
+                                const void* o, const void* o2, const float* lse, const uint8_t* mask,
+                                const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
+                                const wa_diff_options* options, void* dq, void* dk, void* dv, float* dlam,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  WaDiffLaunch a{};
+  wa_status s = check_diff_shape(shape, &a);
+  if (s != WA_OK) return s;
+  s = check_diff_args(q, k, v, lam, mask, q_start, kv_lens, options, &a);
+  if (s != WA_OK) return s;
+  if (!dout || !o || !o2 || !lse || !dq || !dk || !dv || !dlam)
+    return fail(WA_ERR_INVALID_ARG, "dout, o, o2, lse, dq, dk, dv and dlam must be non-null");
+  if (!aligned(dout, 16) || !aligned(o, 16) || !aligned(o2, 16) || !aligned(dq, 16) || !aligned(dk, 16) || !aligned(dv, 16))
+    return fail(WA_ERR_ALIGNMENT, "dout, o, o2, dq, dk and dv must be 16-byte aligned");
+  if (!aligned(lse, 4) || !aligned(dlam, 4)) return fail(WA_ERR_ALIGNMENT, "lse and dlam must be 4-byte aligned");
+  s = check_ws(workspace, workspace_bytes, diff_backward_ws_bytes(a));
+  if (s != WA_OK) return s;
+  a.dout = dout; a.o = const_cast<void*>(o); a.o2 = const_cast<void*>(o2); a.lse = const_cast<float*>(lse);
+  a.dq = dq; a.dk = dk; a.dv = dv; a.dlam = dlam;
+  a.rows = (float*)workspace;
+  a.lam_part = (float*)((char*)workspace + diff_rows_bytes(a));
+  const hipError_t e = wa_launch_diff_backward(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "differential attention gradient launch");
   return ok();
 }
 

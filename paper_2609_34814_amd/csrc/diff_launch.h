@@ -42,4 +42,3 @@ size_t wa_diff_part_floats(const WaDiffPlan& p, int value_dim);
 
 hipError_t wa_launch_diff_attn(const WaDiffLaunch& a, hipStream_t stream);
 hipError_t wa_launch_diff_backward(const WaDiffLaunch& a, hipStream_t stream);
-int32_t wa_diff_bwd_tiles(const WaDiffLaunch& a);
