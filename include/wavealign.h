@@ -441,7 +441,7 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
 /* Differential attention forward: head h has two softmax maps over the same kept keys,
  *   P_m = softmax(scale Q_m K_m^T), m = 1, 2,   O = P_1 V - lam[h] P_2 V.
  * A key j of sequence b is kept for query i if j < kv_lens[b], the mask keeps its block, and, with
- * `causal`, j <= q_start[b] + i. A query with no kept key gets O = 0 and LSE = -inf. bf16 inputs, float32
+ * `causal`, j <= q_start[b] + i. A query with no kept key gets O = 0 and a sum-exp of -inf. bf16 inputs, float32
  * scores, sums and O, probabilities rounded to bf16 for the product with V, bf16 output.
  * Values must be finite in the keys below kv_lens[b]; memory past them is not used, whatever it holds.
  *   q        bf16 [B][2H][q_len][d], 16-byte aligned: the maps of head h are 2h and 2h + 1
@@ -453,35 +453,37 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
  *   q_start  int32 [B], device: position of each sequence's first query; only with causal; NULL: kv_len - q_len
  *   kv_lens  int32 [B], device: keys each sequence holds, taken into 0..kv_len; NULL: kv_len
  *   o        out bf16 [B][H][q_len][value_dim]
- *   o2       out bf16, as o, nullable: P_2 V, which the gradient needs
- *   lse      out float [B][2H][q_len], nullable: natural-log sum-exp of each map's scaled scores
+ *   maps     out int16 [B][2H][q_len][value_dim], 16-byte aligned, nullable: each P_m V, a row in steps of 1/32767 of its
+ *            largest magnitude; for the gradient
+ *   stats    out float [B][2H][q_len][3], with maps: natural-log sum-exp of the map's scaled scores, the step, and the factor
+ *            (1 but for roundings) from probabilities recomputed with that sum-exp to the exact ones
  *   workspace  >= wa_diff_attn_workspace_size(shape), 256-byte aligned; NULL if that is 0
  * How a call is cut into workgroups follows from its shape alone, so equal calls give equal bits. At most
  * 4096 blocks of queries and of keys. */
 wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
                        const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
-                       const wa_diff_options* options, void* o, void* o2, float* lse, void* workspace,
+                       const wa_diff_options* options, void* o, int16_t* maps, float* stats, void* workspace,
                        size_t workspace_bytes, void* stream);
 
-/* Workspace bytes needed by wa_diff_attn_backward: 2 B H q_len float32 row sums and a float32 per tile of queries. */
+/* Workspace bytes needed by wa_diff_attn_backward: 4 B H q_len float32 of row values and a float64 per 64 queries of a head. */
 wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_t* bytes);
 
 /* Gradient of wa_diff_attn: with dO of O it writes
  *   dV = sum over the heads of a key head of (P_1 - lam P_2)^T dO,
  *   dQ_m = scale dS_m K_m, dK_m = sum of scale dS_m^T Q_m, dlam[h] = -sum over b, i of dO_i . (P_2 V)_i,
  *   dS_1 = P_1 (dP - dO . O_1), dS_2 = -lam P_2 (dP - dO . O_2), dP = dO V^T,
- * probabilities recomputed in float32 from lse, sums in float32 (dlam in float64 over tiles), P and dS rounded to
+ * probabilities recomputed in float32 from stats, sums in float32 (dlam over queries in float64), P and dS rounded to
  * bf16 for the matrix products. Every output is overwritten; keys at or past kv_lens[b] get 0, and so do queries
  * with no kept key. Nothing is added with atomics: equal calls give equal bits.
  *   dout     bf16 [B][H][q_len][value_dim], 16-byte aligned
  *   q, k, v, lam, mask, q_start, kv_lens, shape, options   as given to wa_diff_attn
- *   o, o2, lse   what that call wrote
+ *   maps, stats  what that call wrote
  *   dq, dk, dv   out bf16, shaped as q, k and v, 16-byte aligned
  *   dlam         out float [H]
  *   workspace    >= wa_diff_attn_backward_workspace_size(shape), 256-byte aligned */
 wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, const void* v, const float* lam,
-                                const void* o, const void* o2, const float* lse, const uint8_t* mask,
-                                const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
+                                const int16_t* maps, const float* stats, const uint8_t* mask, const int32_t* q_start,
+                                const int32_t* kv_lens, const wa_diff_shape* shape,
                                 const wa_diff_options* options, void* dq, void* dk, void* dv, float* dlam,
                                 void* workspace, size_t workspace_bytes, void* stream);
 

@@ -29,13 +29,13 @@ def softmax_map(q, k, keep, scale):
 
 
 def forward_backward(q, k, v, lam, block=128, scale=None, dout=None, **kw):
-    """q [B][2H][M][d], k [B][2Hk][N][d], v [B][Hk][N][dv], lam [H], fp64. A dict: o, o2, lse and, given dout, dq, dk, dv,
+    """q [B][2H][M][d], k [B][2Hk][N][d], v [B][Hk][N][dv], lam [H], fp64. A dict: o, maps (each P_m V), lse and, given dout, dq, dk, dv,
     dlam; "bound" holds the same outputs with every product and sum taken of magnitudes (for error bounds)."""
     b_, h2, m, d = q.shape
     hk, n, dv = v.shape[1:]
     h_ = h2 // 2
     scale = 1 / np.sqrt(d) if scale is None else scale
-    out = dict(o=np.zeros((b_, h_, m, dv)), o2=np.zeros((b_, h_, m, dv)), lse=np.zeros((b_, h2, m)))
+    out = dict(o=np.zeros((b_, h_, m, dv)), maps=np.zeros((b_, h2, m, dv)), lse=np.zeros((b_, h2, m)))
     names = ("dq", "dk", "dv") if dout is not None else ()
     out.update({x: np.zeros_like(y) for x, y in zip(names, (q, k, v))})
     bound = {x: np.zeros_like(y) for x, y in out.items()}
@@ -50,11 +50,11 @@ def forward_backward(q, k, v, lam, block=128, scale=None, dout=None, **kw):
             maps = [softmax_map(q[b, 2 * h + t], ks[t], keep, scale) for t in range(2)]
             p = [y[0] for y in maps]
             out["lse"][b, 2 * h], out["lse"][b, 2 * h + 1] = maps[0][1], maps[1][1]
-            out["o2"][b, h] = p[1] @ vx
-            out["o"][b, h] = p[0] @ vx - lam[h] * out["o2"][b, h]
             av = np.abs(vx)
-            bound["o2"][b, h] = p[1] @ av
-            bound["o"][b, h] = p[0] @ av + abs(lam[h]) * bound["o2"][b, h]
+            for t in range(2):
+                out["maps"][b, 2 * h + t], bound["maps"][b, 2 * h + t] = p[t] @ vx, p[t] @ av
+            out["o"][b, h] = out["maps"][b, 2 * h] - lam[h] * out["maps"][b, 2 * h + 1]
+            bound["o"][b, h] = bound["maps"][b, 2 * h] + abs(lam[h]) * bound["maps"][b, 2 * h + 1]
             if not names:
                 continue
             do = dout[b, h]

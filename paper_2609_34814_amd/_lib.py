@@ -117,7 +117,7 @@ _SIGNATURES = {
                                POINTER(WaDiffShape), POINTER(WaDiffOptions), c_void_p, c_void_p, c_void_p, c_void_p,
                                c_size_t, c_void_p]),
     "wa_diff_attn_backward_workspace_size": (c_int32, [POINTER(WaDiffShape), POINTER(c_size_t)]),
-    "wa_diff_attn_backward": (c_int32, [c_void_p] * 11 + [POINTER(WaDiffShape), POINTER(WaDiffOptions)] + [c_void_p] * 5
+    "wa_diff_attn_backward": (c_int32, [c_void_p] * 10 + [POINTER(WaDiffShape), POINTER(WaDiffOptions)] + [c_void_p] * 5
                               + [c_size_t, c_void_p]),
     "wa_fp64_probe": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p]),
     "wa_xcc_probe": (c_int32, [c_void_p, c_int32, c_void_p]),

@@ -557,7 +557,9 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
     mask      uint8 or bool [B][H][ceil(M/block)][ceil(N/block)] of kept blocks; None keeps all
     causal    query i of sequence b sees the keys up to q_start[b] + i (q_start int32 [B]; None: N - M)
     kv_lens   int32 [B]: keys each sequence holds; what lies behind them is not used
-    return_stats  also P_2 V (as O) and the float32 log-sum-exps [B][2H][M], which diff_attn_backward takes"""
+    return_stats  also (maps, stats), which diff_attn_backward takes: each P_m V int16 [B][2H][M][dv] in steps of 1/32767 of
+              its row's largest magnitude, and float32 [B][2H][M][3]: the log-sum-exp of the scaled scores, the step, and a
+              factor of roundings"""
     lib = L.load()
     shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)
     want = (shape.batch, shape.heads, shape.q_len, shape.value_dim)
@@ -569,13 +571,14 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
     if need and (workspace is None or workspace.numel() < need):
         workspace = _workspace(need, dev)
     o = torch.empty(want, dtype=torch.bfloat16, device=dev) if out is None else out
-    o2 = torch.empty_like(o) if return_stats else None
-    lse = torch.empty((want[0], 2 * want[1], want[2]), dtype=torch.float32, device=dev) if return_stats else None
+    rows = (want[0], 2 * want[1], want[2])
+    maps = torch.empty((*rows, want[3]), dtype=torch.int16, device=dev) if return_stats else None
+    stats = torch.empty((*rows, 3), dtype=torch.float32, device=dev) if return_stats else None
     opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
     _call_on(dev, lib.wa_diff_attn, _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(mask), _ptr(q_start), _ptr(kv_lens),
-             ctypes.byref(shape), ctypes.byref(opts), _ptr(o), _ptr(o2), _ptr(lse), _ptr(workspace),
+             ctypes.byref(shape), ctypes.byref(opts), _ptr(o), _ptr(maps), _ptr(stats), _ptr(workspace),
              0 if workspace is None else workspace.numel())
-    return (o, o2, lse) if return_stats else o
+    return (o, maps, stats) if return_stats else o
 
 
 def diff_attn_backward_workspace_size(shape: L.WaDiffShape) -> int:
@@ -583,21 +586,22 @@ def diff_attn_backward_workspace_size(shape: L.WaDiffShape) -> int:
 
 
 def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor,
-                       mask: Optional[torch.Tensor], o: torch.Tensor, o2: torch.Tensor, lse: torch.Tensor, *,
-                       block: int = 128, scale: Optional[float] = None, causal: bool = False,
+                       mask: Optional[torch.Tensor], maps: torch.Tensor, stats: torch.Tensor, *, block: int = 128,
+                       scale: Optional[float] = None, causal: bool = False,
                        q_start: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None,
                        workspace: Optional[torch.Tensor] = None):
     """(dq, dk, dv bf16, dlam float32) from dout, the gradient of diff_attn's O: the other arguments as that call had
-    them, o, o2 and lse as it returned them with return_stats. Keys past kv_lens get 0. Equal calls give equal bits."""
+    them, maps and stats as it returned them with return_stats. Keys past kv_lens get 0. Equal calls give equal bits."""
     lib = L.load()
     shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)
     want = (shape.batch, shape.heads, shape.q_len, shape.value_dim)
-    for t, nm in ((dout, "dout"), (o, "o"), (o2, "o2")):
-        _check(t, nm, torch.bfloat16, want)
-    _check(lse, "lse", torch.float32, (want[0], 2 * want[1], want[2]))
+    rows = (want[0], 2 * want[1], want[2])
+    _check(dout, "dout", torch.bfloat16, want)
+    _check(maps, "maps", torch.int16, (*rows, want[3]))
+    _check(stats, "stats", torch.float32, (*rows, 3))
     _check(workspace, "workspace", torch.uint8)
-    given = dict(dout=dout, q=q, k=k, v=v, lam=lam, mask=mask, o=o, o2=o2, lse=lse, q_start=q_start, kv_lens=kv_lens,
-                 workspace=workspace)
+    given = dict(dout=dout, q=q, k=k, v=v, lam=lam, mask=mask, maps=maps, stats=stats, q_start=q_start,
+                 kv_lens=kv_lens, workspace=workspace)
     _on_device(**given)
     dev = _one_device(**given)
     need = diff_attn_backward_workspace_size(shape)
@@ -605,8 +609,8 @@ def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
         workspace = _workspace(need, dev)
     dq, dk, dv, dlam = (torch.empty_like(t) for t in (q, k, v, lam))
     opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
-    _call_on(dev, lib.wa_diff_attn_backward, _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(o), _ptr(o2),
-             _ptr(lse), _ptr(mask), _ptr(q_start), _ptr(kv_lens), ctypes.byref(shape), ctypes.byref(opts), _ptr(dq),
+    _call_on(dev, lib.wa_diff_attn_backward, _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(maps),
+             _ptr(stats), _ptr(mask), _ptr(q_start), _ptr(kv_lens), ctypes.byref(shape), ctypes.byref(opts), _ptr(dq),
              _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), workspace.numel())
     return dq, dk, dv, dlam
 

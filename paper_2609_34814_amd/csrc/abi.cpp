@@ -333,10 +333,10 @@ size_t diff_ws_bytes(const WaDiffLaunch& a) {
                                wa_diff_part_floats(wa_diff_plan(a, true), a.value_dim)));
 }
 
-// Workspace of the gradient: the row sums, then the parts of dlam (tiles of 64 queries at the least).
-size_t diff_rows_bytes(const WaDiffLaunch& a) { return align_up((size_t)2 * a.batch * a.heads * a.q_len * 4); }
+// Workspace of the gradient: two floats a row and map, then the parts of dlam (tiles of 64 queries at the least).
+size_t diff_rows_bytes(const WaDiffLaunch& a) { return align_up((size_t)4 * a.batch * a.heads * a.q_len * 4); }
 size_t diff_backward_ws_bytes(const WaDiffLaunch& a) {
-  return diff_rows_bytes(a) + align_up((size_t)a.batch * a.heads * ((a.q_len + 63) / 64) * 4);
+  return diff_rows_bytes(a) + align_up((size_t)a.batch * a.heads * ((a.q_len + 63) / 64) * 8);
 }
 
 // Arguments that both directions share, checked and put into the launch.
@@ -769,7 +769,7 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
 
 wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
                        const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
-                       const wa_diff_options* options, void* o, void* o2, float* lse, void* workspace,
+                       const wa_diff_options* options, void* o, int16_t* maps, float* stats, void* workspace,
                        size_t workspace_bytes, void* stream) {
   WaDiffLaunch a{};
   wa_status s = check_diff_shape(shape, &a);
@@ -777,11 +777,12 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
   s = check_diff_args(q, k, v, lam, mask, q_start, kv_lens, options, &a);
   if (s != WA_OK) return s;
   if (!o) return fail(WA_ERR_INVALID_ARG, "o must be non-null");
-  if (!aligned(o, 16) || !aligned(o2, 16)) return fail(WA_ERR_ALIGNMENT, "o and o2 must be 16-byte aligned");
-  if (!aligned(lse, 4)) return fail(WA_ERR_ALIGNMENT, "lse must be 4-byte aligned");
+  if (!maps != !stats) return fail(WA_ERR_INVALID_ARG, "maps and stats go together");
+  if (!aligned(o, 16) || !aligned(maps, 16)) return fail(WA_ERR_ALIGNMENT, "o and maps must be 16-byte aligned");
+  if (!aligned(stats, 4)) return fail(WA_ERR_ALIGNMENT, "stats must be 4-byte aligned");
   s = check_ws(workspace, workspace_bytes, diff_ws_bytes(a));
   if (s != WA_OK) return s;
-  a.o = o; a.o2 = o2; a.lse = lse;
+  a.o = o; a.maps = maps; a.stats = stats;
   a.part = (float*)workspace;
   const hipError_t e = wa_launch_diff_attn(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention launch");
@@ -798,8 +799,8 @@ wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_
 }
 
 wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, const void* v, const float* lam,
-                                const void* o, const void* o2, const float* lse, const uint8_t* mask,
-                                const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
+                                const int16_t* maps, const float* stats, const uint8_t* mask, const int32_t* q_start,
+                                const int32_t* kv_lens, const wa_diff_shape* shape,
                                 const wa_diff_options* options, void* dq, void* dk, void* dv, float* dlam,
                                 void* workspace, size_t workspace_bytes, void* stream) {
   WaDiffLaunch a{};
@@ -807,17 +808,17 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
   if (s != WA_OK) return s;
   s = check_diff_args(q, k, v, lam, mask, q_start, kv_lens, options, &a);
   if (s != WA_OK) return s;
-  if (!dout || !o || !o2 || !lse || !dq || !dk || !dv || !dlam)
-    return fail(WA_ERR_INVALID_ARG, "dout, o, o2, lse, dq, dk, dv and dlam must be non-null");
-  if (!aligned(dout, 16) || !aligned(o, 16) || !aligned(o2, 16) || !aligned(dq, 16) || !aligned(dk, 16) || !aligned(dv, 16))
-    return fail(WA_ERR_ALIGNMENT, "dout, o, o2, dq, dk and dv must be 16-byte aligned");
-  if (!aligned(lse, 4) || !aligned(dlam, 4)) return fail(WA_ERR_ALIGNMENT, "lse and dlam must be 4-byte aligned");
+  if (!dout || !maps || !stats || !dq || !dk || !dv || !dlam)
+    return fail(WA_ERR_INVALID_ARG, "dout, maps, stats, dq, dk, dv and dlam must be non-null");
+  if (!aligned(dout, 16) || !aligned(maps, 16) || !aligned(dq, 16) || !aligned(dk, 16) || !aligned(dv, 16))
+    return fail(WA_ERR_ALIGNMENT, "dout, maps, dq, dk and dv must be 16-byte aligned");
+  if (!aligned(stats, 4) || !aligned(dlam, 4)) return fail(WA_ERR_ALIGNMENT, "stats and dlam must be 4-byte aligned");
   s = check_ws(workspace, workspace_bytes, diff_backward_ws_bytes(a));
   if (s != WA_OK) return s;
-  a.dout = dout; a.o = const_cast<void*>(o); a.o2 = const_cast<void*>(o2); a.lse = const_cast<float*>(lse);
+  a.dout = dout; a.maps = const_cast<int16_t*>(maps); a.stats = const_cast<float*>(stats);
   a.dq = dq; a.dk = dk; a.dv = dv; a.dlam = dlam;
   a.rows = (float*)workspace;
-  a.lam_part = (float*)((char*)workspace + diff_rows_bytes(a));
+  a.lam_part = (double*)((char*)workspace + diff_rows_bytes(a));
   const hipError_t e = wa_launch_diff_backward(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention gradient launch");
   return ok();

@@ -229,38 +229,55 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   }
 
   const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-  if (a.lse && valid && hf == 0)
-    a.lse[((int64_t)b * 2 * a.heads + 2 * h + map) * a.q_len + i] = l == 0.f ? -INFINITY : (m_run + __log2f(l)) * kLn2;
+#pragma unroll
+  for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[dt][v] *= inv;
+  if (a.maps) {
+    float big = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) big = fmaxf(big, fabsf(acc[dt][v]));
+    const RowStats r = row_stats(m_run, l, max_halves(big));
+    const float per_step = r.step > 0.f ? 1.f / r.step : 0.f;
+    const int64_t at = ((int64_t)b * 2 * a.heads + 2 * h + map) * a.q_len + i;
+    if (valid) {
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *(uint2*)(a.maps + at * DV + dt * 32 + 2 * v + 4 * hf) =
+              make_uint2(pack_steps(acc[dt][v], acc[dt][v + 1], per_step), pack_steps(acc[dt][v + 2], acc[dt][v + 3], per_step));
+      if (hf == 0) {
+        a.stats[3 * at] = r.lse;
+        a.stats[3 * at + 1] = r.step;
+        a.stats[3 * at + 2] = r.factor;
+      }
+    }
+  }
   // the second map's wavefronts hand their rows to the first's
   float* meet = (float*)lds + slice * 32 * DV;
   __syncthreads();
-  const int64_t at = (((int64_t)b * a.heads + h) * a.q_len + i) * DV;
   if (map == 1) {
 #pragma unroll
     for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        acc[dt][v] *= inv;
-        meet[(dt * 16 + v) * 64 + lane] = acc[dt][v];
-      }
+      for (int v = 0; v < 16; ++v) meet[(dt * 16 + v) * 64 + lane] = acc[dt][v];
   }
   __syncthreads();
-  uint16_t* out = (uint16_t*)(map == 1 ? a.o2 : a.o);
-  if (map == 0) {
-    const float lam = valid ? a.lam[h] : 0.f;
+  if (map == 1 || !valid) return;
+  const float lam = a.lam[h];
+  uint16_t* out = (uint16_t*)a.o + (((int64_t)b * a.heads + h) * a.q_len + i) * DV + 4 * hf;
 #pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt)
+  for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[dt][v] = acc[dt][v] * inv - lam * meet[(dt * 16 + v) * 64 + lane];
-  }
-  if (valid && out) {
+    for (int v = 0; v < 16; v += 4) {
+      float x[4];
 #pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-      for (int v = 0; v < 16; v += 4)
-        *(uint2*)(out + at + dt * 32 + 2 * v + 4 * hf) =
-            make_uint2(pack_bf16x2(acc[dt][v], acc[dt][v + 1]), pack_bf16x2(acc[dt][v + 2], acc[dt][v + 3]));
-  }
+      for (int e = 0; e < 4; ++e) x[e] = acc[dt][v + e] - lam * meet[(dt * 16 + v + e) * 64 + lane];
+      *(uint2*)(out + dt * 32 + 2 * v) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+    }
 }
 
 // Joins the key ranges of split tiles, in order: one wavefront a query row, DV / 64 columns a lane.
@@ -300,17 +317,27 @@ __global__ __launch_bounds__(256) void diff_join_kernel(const WaDiffLaunch a, co
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[m][e] *= inv;
-    if (a.lse && lane == 0)
-      a.lse[((int64_t)b * 2 * a.heads + 2 * h + m) * a.q_len + i] = l == 0.f ? -INFINITY : (top + __log2f(l)) * kLn2;
+    if (a.maps) {
+      float big = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) big = fmaxf(big, fabsf(o[m][e]));
+      for (int x = 32; x > 0; x >>= 1) big = fmaxf(big, __shfl_xor(big, x));
+      const RowStats s = row_stats(top, l, big);
+      const float per_step = s.step > 0.f ? 1.f / s.step : 0.f;
+      const int64_t to = ((int64_t)b * 2 * a.heads + 2 * h + m) * a.q_len + i;
+#pragma unroll
+      for (int e = 0; e < E; ++e) a.maps[to * DV + lane * E + e] = (int16_t)rintf(o[m][e] * per_step);
+      if (lane == 0) {
+        a.stats[3 * to] = s.lse;
+        a.stats[3 * to + 1] = s.step;
+        a.stats[3 * to + 2] = s.factor;
+      }
+    }
   }
   const float lam = a.lam[h];
   __bf16* out = (__bf16*)a.o + r * DV + lane * E;
-  __bf16* out2 = (__bf16*)a.o2 + r * DV + lane * E;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    out[e] = (__bf16)(o[0][e] - lam * o[1][e]);
-    if (a.o2) out2[e] = (__bf16)o[1][e];
-  }
+  for (int e = 0; e < E; ++e) out[e] = (__bf16)(o[0][e] - lam * o[1][e]);
 }
 
 template <int D, int DV>

@@ -1,7 +1,6 @@
 // Gradient of differential attention for gfx950 (MI355X). With P_m recomputed from the forward's log-sum-exps,
 //   dP = dO V^T,   D_m = sum_j P_m dP = dO . O_m,   dS_1 = P_1 (dP - D_1),   dS_2 = -lam P_2 (dP - D_2),
 //   dQ_m = scale dS_m K_m,   dK_m = scale dS_m^T Q_m,   dV = (P_1 - lam P_2)^T dO,   dlam_h = -sum D_2.
-// O_1 = O + lam O_2 with the forward's two outputs, so D_1 = dO . O + lam dO . O_2.
 //
 // Two kernels, each owning what it writes, so nothing is added with atomics and equal calls give equal bits:
 //   diff_dq_kernel: a tile of queries, over its keys; also writes D_m and the tile's part of dlam.
@@ -10,7 +9,8 @@
 // maps with their accumulators in registers (for d 128 one wavefront a SIMD, which may use 512), and the other side's tiles pass
 // through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are.
-// dlam is summed from the float32 P_2 dP, not from the rounded outputs, and over tiles in float64.
+// dlam is summed from the float32 P_2 dP, not from the stored maps: over a lane's keys with the roundings carried along, over
+// queries in float64.
 
 #include "diff_tiles.h"
 #include "wavealign.h"
@@ -29,8 +29,11 @@ struct Bwd {
   static constexpr int KBYTES = TB * KRB, VBYTES = TB * VRB, STAGE = 2 * KBYTES + VBYTES;
   static constexpr int DT = D / 32, VT = DV / 32, KS = D / 16, VS = DV / 16;
 };
+// Wavefronts a SIMD: two share its 512 registers a lane where both hold their accumulators without spilling.
 template <int D>
-constexpr int kWavesPerSimd = D == 64 ? 2 : 1;
+constexpr int kDqWaves = D == 64 ? 2 : 1;
+template <int DV>
+constexpr int kDkvWaves = DV == 64 ? 2 : 1;
 
 __device__ __forceinline__ void clear(f32x16& x) {
 #pragma unroll
@@ -43,9 +46,11 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
 __device__ __forceinline__ bf16x8 pack8(const float* p) {
   return as_bf16x8(make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
 }
-__device__ __forceinline__ float dot8(bf16x8 a, bf16x8 b, float sum) {
+__device__ __forceinline__ float dot8(bf16x8 a, uint4 b, float sum) {
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  const s16x8 n = __builtin_bit_cast(s16x8, b);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)a[i], (float)b[i], sum);
+  for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)a[i], (float)n[i], sum);
   return sum;
 }
 __device__ __forceinline__ bf16x8 load8(const uint16_t* p, bool ok) {
@@ -65,11 +70,11 @@ __device__ __forceinline__ void store_row(uint16_t* out, const f32x16 (&acc)[T],
 }
 
 template <int D, int DV, int W>
-__global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dq_kernel(const WaDiffLaunch a, int tiles) {
+__global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDiffLaunch a, int tiles) {
   using C = Bwd<D, DV, W>;
   constexpr int KB = C::TB;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE];
-  __shared__ float lam_sum[W];
+  __shared__ double lam_sum[W];
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -113,26 +118,33 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dq_kernel(const
 #pragma unroll
     for (int m = 0; m < 2; ++m)
       qf[m][s] = load8((const uint16_t*)a.q + (row0 + (int64_t)m * a.q_len) * D + 16 * s + 8 * hf, valid);
-  float d_both = 0.f, d_2 = 0.f;
+  float d[2] = {0.f, 0.f}, ref[2] = {0.f, 0.f}, factor = 1.f;  // ref: log-sum-exp in log2 units
 #pragma unroll
   for (int s = 0; s < C::VS; ++s) {
-    const int64_t at = row + 16 * s + 8 * hf;
-    dof[s] = load8((const uint16_t*)a.dout + at, valid);
-    d_both = dot8(dof[s], load8((const uint16_t*)a.o + at, valid), d_both);
-    d_2 = dot8(dof[s], load8((const uint16_t*)a.o2 + at, valid), d_2);
-  }
-  const float lam = a.lam[h];
-  d_2 = add_halves(d_2);
-  const float d_1 = add_halves(d_both) + lam * d_2;
-  float ref[2] = {0.f, 0.f};  // log-sum-exp in log2 units
-  if (valid) {
+    dof[s] = load8((const uint16_t*)a.dout + row + 16 * s + 8 * hf, valid);
 #pragma unroll
-    for (int m = 0; m < 2; ++m) ref[m] = a.lse[row0 + (int64_t)m * a.q_len] * kLog2e;
-    if (hf == 0) {
-      a.rows[row0] = d_1;
-      a.rows[row0 + a.q_len] = d_2;
+    for (int m = 0; m < 2; ++m) {
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (valid) u = *(const uint4*)(a.maps + (row0 + (int64_t)m * a.q_len) * DV + 16 * s + 8 * hf);
+      d[m] = dot8(dof[s], u, d[m]);
     }
   }
+  const int64_t all_rows = (int64_t)a.batch * 2 * a.heads * a.q_len;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    d[m] = add_halves(d[m]);
+    if (valid) {
+      const int64_t at = row0 + (int64_t)m * a.q_len;
+      ref[m] = a.stats[3 * at] * kLog2e;
+      d[m] *= a.stats[3 * at + 1];
+      factor = a.stats[3 * at + 2];  // of the second map, in the end
+      if (hf == 0) {
+        a.rows[at] = ref[m];
+        a.rows[all_rows + at] = d[m];
+      }
+    }
+  }
+  const float lam = a.lam[h];
 
   uint32_t kofs[C::KS], vofs[C::VS < 16 ? C::VS : 8], kcol[2][C::DT];
 #pragma unroll
@@ -150,7 +162,7 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dq_kernel(const
   for (int m = 0; m < 2; ++m)
 #pragma unroll
     for (int c = 0; c < C::DT; ++c) clear(dq[m][c]);
-  float lam_dot = 0.f;
+  float lam_dot = 0.f, lam_lost = 0.f;
 
   while (key < hi) {
     const int next = next_tile(key + KB);
@@ -183,12 +195,16 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dq_kernel(const
         for (int v = 0; v < 16; ++v)
           if (8 * (v >> 2) + (v & 3) >= rest) p[0][v] = p[1][v] = 0.f;
       }
+      float dot = 0.f;
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        lam_dot = __builtin_fmaf(p[1][v], dp[v], lam_dot);
-        p[0][v] *= dp[v] - d_1;
-        p[1][v] *= dp[v] - d_2;
+        dot = __builtin_fmaf(p[1][v], dp[v], dot);
+        p[0][v] *= dp[v] - d[0];
+        p[1][v] *= dp[v] - d[1];
       }
+      const float add = dot - lam_lost, grown = lam_dot + add;
+      lam_lost = (grown - lam_dot) - add;
+      lam_dot = grown;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -206,12 +222,13 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dq_kernel(const
     store_row(((uint16_t*)a.dq) + row0 * D, dq[0], a.scale, hf);
     store_row(((uint16_t*)a.dq) + (row0 + a.q_len) * D, dq[1], -lam * a.scale, hf);
   }
+  double lam_row = (double)lam_dot * factor;
 #pragma unroll
-  for (int x = 32; x > 0; x >>= 1) lam_dot += __shfl_xor(lam_dot, x);
-  if (lane == 0) lam_sum[w] = lam_dot;
+  for (int x = 32; x > 0; x >>= 1) lam_row += __shfl_xor(lam_row, x);
+  if (lane == 0) lam_sum[w] = lam_row;
   __syncthreads();
   if (tid == 0) {
-    float sum = 0.f;
+    double sum = 0.0;
     for (int x = 0; x < W; ++x) sum += lam_sum[x];
     a.lam_part[(int64_t)bh * tiles + tile] = sum;
   }
@@ -232,11 +249,11 @@ __device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, const uns
 }
 
 template <int D, int DV, int W>
-__global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dkv_kernel(const WaDiffLaunch a, int tiles, int q_tiles) {
+__global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const WaDiffLaunch a, int tiles, int q_tiles) {
   using C = Bwd<D, DV, W>;
   constexpr int QB = C::TB;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE];
-  __shared__ __attribute__((aligned(1024))) float stat[2][4 * QB];  // log-sum-exps of both maps, then D_1, D_2
+  __shared__ __attribute__((aligned(1024))) float stat[2][4 * QB];  // of both maps: log-sum-exps (log2 units), then D_m
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -245,7 +262,7 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dkv_kernel(cons
     if (tid < 64) {
       double sum = 0.0;
       for (int b = 0; b < a.batch; ++b)
-        for (int t = lane; t < q_tiles; t += 64) sum += (double)a.lam_part[((int64_t)b * a.heads + h) * q_tiles + t];
+        for (int t = lane; t < q_tiles; t += 64) sum += a.lam_part[((int64_t)b * a.heads + h) * q_tiles + t];
       for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
       if (lane == 0) a.dlam[h] = (float)-sum;
     }
@@ -304,8 +321,8 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dkv_kernel(cons
     const int64_t qh = (int64_t)b * 2 * a.heads + 2 * h;
     const unsigned char* qg = (const unsigned char*)a.q + qh * a.q_len * C::KRB;
     const unsigned char* og = (const unsigned char*)a.dout + ((int64_t)b * a.heads + h) * a.q_len * C::VRB;
-    const float* lse = a.lse + qh * a.q_len;
-    const float* rows = a.rows + qh * a.q_len;
+    const float* ref = a.rows + qh * a.q_len;
+    const float* dots = ref + (int64_t)a.batch * 2 * a.heads * a.q_len;
     MaskWalk walk;
     if (a.mask) {
       walk.at = uniform_ptr(a.mask + ((int64_t)b * a.heads + h) * a.mb * a.nb + (tile * 32 * W >> shift));
@@ -326,7 +343,7 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dkv_kernel(cons
       for (int c = w; c < QB / 16; c += W) {
         const int at = c * 64 + lane;  // statistic at / QB of query i + at % QB
         const int x = min(i + at % QB, a.q_len - 1) + (at / QB & 1) * a.q_len;
-        dma4(c * 64 < 2 * QB ? lse : rows, (uint32_t)x * 4, (const unsigned char*)(stat[buf] + c * 64));
+        dma4(c * 64 < 2 * QB ? ref : dots, (uint32_t)x * 4, (const unsigned char*)(stat[buf] + c * 64));
       }
     };
     // The first tile may begin inside a mask block that the walk has not looked at.
@@ -363,8 +380,8 @@ __global__ __launch_bounds__(64 * W, kWavesPerSimd<D>) void diff_dkv_kernel(cons
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int v = 4 * q4 + e;
-            p[0][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][v], c2, -(&l0.x)[e] * kLog2e));
-            p[1][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][v], c2, -(&l1.x)[e] * kLog2e));
+            p[0][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][v], c2, -(&l0.x)[e]));
+            p[1][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][v], c2, -(&l1.x)[e]));
           }
         }
         if (!whole || i1 < all || i1 + 32 > hi) {

@@ -13,8 +13,8 @@ struct WaDiffLaunch {
   const int32_t* q_start;  // [batch], null: kv_len - q_len
   const int32_t* kv_lens;  // [batch], null: kv_len
   void* o;            // bf16 [batch][heads][q_len][value_dim]
-  void* o2;           // the second map's output, nullable
-  float* lse;         // [batch][2 heads][q_len], nullable
+  int16_t* maps;      // [batch][2 heads][q_len][value_dim]: P_m V in steps of its row's, nullable
+  float* stats;       // [batch][2 heads][q_len][3]: log-sum-exp, step, correction (diff_tiles.h), with maps
   float* part;        // split calls: partial tiles, then their statistics
   int32_t batch, heads, kv_heads, q_len, kv_len, head_dim, value_dim, block, mb, nb, causal;
   float scale;
@@ -24,8 +24,8 @@ struct WaDiffLaunch {
   void* dk;
   void* dv;
   float* dlam;        // [heads]
-  float* rows;        // workspace: [batch][2 heads][q_len] dO . O_m
-  float* lam_part;    // workspace: [batch][heads][tiles of q_len] partial sums for dlam
+  float* rows;        // workspace: [2][batch][2 heads][q_len]: log-sum-exps in log2 units, then dO . O_m
+  double* lam_part;   // workspace: [batch][heads][tiles of q_len] partial sums for dlam
 };
 
 // How a forward call is cut into workgroups (see diff_plan in diff_attn.hip).

@@ -127,6 +127,26 @@ struct MaskWalk {
   }
 };
 
+// What the gradient takes from the forward, per row and map: the log-sum-exp of the scaled scores; the step in which the row of
+// P_m V is held as 16-bit integers (its largest magnitude is 32767 steps, so dO . O_m is within 2^-16 of that times
+// sum |dO|, where bfloat16 values gave dQ and dK a fifth more error in all); and the factor that takes probabilities recomputed
+// from the float32 log-sum-exp (rounded by up to 2^-21) to the forward's, for the sum dlam.
+struct RowStats {
+  float lse, step, factor;
+};
+// top: the maximum the sum l was taken against, in log2 units; big: the row's largest |P_m V|
+__device__ __forceinline__ RowStats row_stats(float top, float l, float big) {
+  RowStats r = {-INFINITY, big * (1.f / 32767.f), 1.f};
+  if (l != 0.f) {
+    r.lse = (top + __log2f(l)) * kLn2;
+    r.factor = __builtin_amdgcn_exp2f(r.lse * kLog2e - top) / l;
+  }
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_steps(float x, float y, float per_step) {
+  return (uint32_t)(uint16_t)(int16_t)rintf(x * per_step) | (uint32_t)(uint16_t)(int16_t)rintf(y * per_step) << 16;
+}
+
 // The value of lane % 32 and that of lane % 32 + 32. In assembly: the compiler reads both results of its builtin from
 // one register. The exchange needs two wait states after a write of its operands.
 __device__ __forceinline__ f32x2 both_halves(float x) {

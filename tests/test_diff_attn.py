@@ -44,14 +44,16 @@ def test_argument_refusals():
     assert lib.wa_diff_attn_workspace_size(ctypes.byref(few), ctypes.byref(n)) == 0 and n.value > 0
 
     def call(q=FAKE, k=FAKE, v=FAKE, lam=FAKE, mask=None, start=None, lens=None, shape=few, opts=L.WaDiffOptions(0.0, 1),
-             o=FAKE, o2=None, lse=None, ws=FAKE, size=n.value):
+             o=FAKE, maps=None, stats=None, ws=FAKE, size=n.value):
         return lib.wa_diff_attn(q, k, v, lam, mask, start, lens, ctypes.byref(shape),
-                                None if opts is None else ctypes.byref(opts), o, o2, lse, ws, size, None)
+                                None if opts is None else ctypes.byref(opts), o, maps, stats, ws, size, None)
 
     for name in ("q", "k", "v", "lam", "o"):
         assert call(**{name: None}) == INVALID, name
-    for name in ("q", "k", "v", "lam", "o", "o2", "lse", "start", "lens"):
+    for name in ("q", "k", "v", "lam", "o", "start", "lens"):
         assert call(**{name: odd}) == ALIGN, name
+    assert call(maps=odd, stats=FAKE) == ALIGN and call(maps=FAKE, stats=odd) == ALIGN
+    assert call(maps=FAKE) == INVALID and call(stats=FAKE) == INVALID
     assert call(opts=None) == INVALID
     assert call(start=FAKE, opts=L.WaDiffOptions(0.0, 0)) == INVALID
     assert call(ws=None) == INVALID and call(size=n.value - 1) == WORK
@@ -130,18 +132,26 @@ def check_forward(args, mask=None, block=128, **kw):
     """Probabilities are rounded once, at most 2^-8 of each; float32 scores: 130 operations of 2^-24 on at most
     scale sum |q k| < 30 in these tests, 2^-12 in the exponent, so 2^-11 of a probability; the result is rounded
     once, 2^-8 of it."""
-    o, o2, lse = W.diff_attn(*args, mask, block=block, return_stats=True, **kw)
+    o, maps, stats = W.diff_attn(*args, mask, block=block, return_stats=True, **kw)
     plain = W.diff_attn(*args, mask, block=block, **kw)
     assert torch.equal(plain, o)                       # the statistics change nothing
     ref = reference(args, mask, block, kw)
-    for name, y in (("o", o), ("o2", o2)):
-        err = np.abs(y.double().cpu().numpy() - ref[name])
-        tol = (2.0 ** -8 + 2.0 ** -11) * ref["bound"][name] * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref[name])
-        assert np.all(err <= tol), (name, float((err - tol).max()))
-    got = lse.double().cpu().numpy()
-    assert np.array_equal(np.isneginf(got), np.isneginf(ref["lse"]))
+    arith = (2.0 ** -8 + 2.0 ** -11) * (1 + 2.0 ** -8)
+    err = np.abs(o.double().cpu().numpy() - ref["o"])
+    tol = arith * ref["bound"]["o"] + 2.0 ** -8 * np.abs(ref["o"])
+    assert np.all(err <= tol), float((err - tol).max())
+    # each map's output in steps of its row's largest / 32767, half a step off at most; float32 adds 2^-16 of it
+    lse, step, factor = (x.double().cpu().numpy() for x in stats.unbind(-1))
+    big = np.abs(ref["maps"]).max(-1, keepdims=True)
+    held = maps.double().cpu().numpy() * step[..., None]
+    tol = arith * ref["bound"]["maps"] + (0.5 / 32767 + 2.0 ** -16) * big * (1 + 2.0 ** -6)
+    assert np.all(np.abs(held - ref["maps"]) <= tol)
+    assert np.array_equal(np.isneginf(lse), np.isneginf(ref["lse"]))
     some = np.isfinite(ref["lse"])
-    assert np.all(np.abs(got[some] - ref["lse"][some]) <= 2.0 ** -11 + 2.0 ** -22 * np.abs(ref["lse"][some]))
+    assert np.all(np.abs(lse[some] - ref["lse"][some]) <= 2.0 ** -11 + 2.0 ** -22 * np.abs(ref["lse"][some]))
+    # the factor undoes the rounding of the float32 sum-exp, of its product with log2 e, and of their functions: 2^-24
+    # of the larger of it and the maximum, a few times
+    assert np.all(np.abs(factor - 1) <= 2.0 ** -20 + 2.0 ** -22 * np.where(some, np.abs(ref["lse"]), 0))
 
 
 DIMS = [(64, 64), (64, 128), (128, 128), (128, 256)]
@@ -166,8 +176,8 @@ def test_block_masks(b, h, hk, m, n, d, dv, block, causal):
     args = make(b, h, hk, m, n, d, dv)
     check_forward(args, block_mask(b, h, m, n, block, 0.4), block, causal=causal)
     empty = torch.zeros((b, h, -(-m // block), -(-n // block)), dtype=torch.bool, device="cuda")
-    o, _, lse = W.diff_attn(*args, empty, block=block, return_stats=True)
-    assert not o.any() and torch.all(lse == -float("inf"))
+    o, maps, stats = W.diff_attn(*args, empty, block=block, return_stats=True)
+    assert not o.any() and not maps.any() and torch.all(stats[..., 0] == -float("inf"))
 
 
 @pytest.mark.gpu
@@ -197,8 +207,7 @@ def test_query_positions(m, n):
     start = torch.tensor([-2 ** 31, -7, 0, n // 2, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
     seen = start.clamp(-m, n)
     ref = dict(causal=True, q_start=seen)
-    o, o2, lse = W.diff_attn(*args, causal=True, q_start=start, return_stats=True)
-    assert torch.equal(o, W.diff_attn(*args, **ref))
+    assert torch.equal(W.diff_attn(*args, causal=True, q_start=start), W.diff_attn(*args, **ref))
     check_forward(args, **ref)
 
 
@@ -218,12 +227,11 @@ def test_growing_and_large_scores(m):
     args = make(1, 2, 1, m, 700, 64, 64)
     ramp = torch.linspace(0, 6, 700, device="cuda")
     args[1][:, 1] = (args[1][:, 1].float() * ramp[:, None]).to(torch.bfloat16)
-    o = W.diff_attn(*args, return_stats=True)
+    o = W.diff_attn(*args)
     ref = reference(args, None, 128, {})
     # scores up to about 40 here: 2^-24 (64 + 2) 40 sqrt(64) in the exponent, below 2^-9
-    for name, y in zip(("o", "o2"), o):
-        err = np.abs(y.double().cpu().numpy() - ref[name])
-        assert np.all(err <= (2.0 ** -8 + 2.0 ** -8) * ref["bound"][name] + 2.0 ** -8 * np.abs(ref[name])), name
+    err = np.abs(o.double().cpu().numpy() - ref["o"])
+    assert np.all(err <= (2.0 ** -8 + 2.0 ** -8) * ref["bound"]["o"] + 2.0 ** -8 * np.abs(ref["o"]))
     args = make(1, 2, 1, m, 700, 64, 64, gain=100.0)
     o = W.diff_attn(*args)
     assert torch.isfinite(o).all() and o.float().abs().max() <= 2 * args[2].float().abs().max() * 1.01
