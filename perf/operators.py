@@ -233,8 +233,8 @@ def run(state):
         args = [state[x] for x in ("q", "k", "v", "lam", "mask")]
         if case["op"] == "diff":
             return W.diff_attn(*args, **how)
-        o, o2, lse = W.diff_attn(*args, return_stats=True, **how)
-        return (o, *W.diff_attn_backward(state["dout"], *args, o, o2, lse, **how))
+        o, maps, stats = W.diff_attn(*args, return_stats=True, **how)
+        return (o, *W.diff_attn_backward(state["dout"], *args, maps, stats, **how))
     if case["op"] == "rotary":
         return tuple(_plain_rotary(state, state[x]) for x in ("q", "k"))
     return _plain_diff(state)
