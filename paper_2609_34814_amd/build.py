@@ -30,6 +30,7 @@ SOURCES = {
     "rotary.hip": [],
     "diff_attn.hip": [],
     "diff_bwd.hip": [],
+    "diff_order.hip": [],
     "abi.cpp": [],
 }
 

@@ -328,15 +328,34 @@ wa_status check_diff_shape(const wa_diff_shape* s, WaDiffLaunch* out) {
   return WA_OK;
 }
 
+// Forward: split results, or the order of a masked call that is not split.
 size_t diff_ws_bytes(const WaDiffLaunch& a) {
-  return align_up(4 * std::max(wa_diff_part_floats(wa_diff_plan(a, false), a.value_dim),
-                               wa_diff_part_floats(wa_diff_plan(a, true), a.value_dim)));
+  const WaDiffPlan dense = wa_diff_plan(a, false), masked = wa_diff_plan(a, true);
+  return align_up(4 * std::max({wa_diff_part_floats(dense, a.value_dim), wa_diff_part_floats(masked, a.value_dim),
+                                wa_diff_order_ints((int64_t)masked.units * masked.tiles)}));
 }
 
-// Workspace of the gradient: two floats a row and map, then the parts of dlam (tiles of 64 queries at the least).
-size_t diff_rows_bytes(const WaDiffLaunch& a) { return align_up((size_t)4 * a.batch * a.heads * a.q_len * 4); }
-size_t diff_backward_ws_bytes(const WaDiffLaunch& a) {
-  return diff_rows_bytes(a) + align_up((size_t)a.batch * a.heads * ((a.q_len + 63) / 64) * 8);
+// Gradient: two floats a row and map; the parts of dlam; the order of a masked call; the results of parts of tiles, those of the
+// queries and then those of the keys. Sized for either value of causal and with or without a mask.
+struct DiffBackwardWs {
+  size_t lam, order, part, total;
+};
+DiffBackwardWs diff_backward_ws(WaDiffLaunch a) {
+  size_t lam = 0, order = 0, part = 0;
+  for (int x = 0; x < 4; ++x) {
+    const bool masked = x & 1;
+    a.causal = x >> 1;
+    const WaDiffSide q = wa_diff_dq_side(a, masked), k = wa_diff_dkv_side(a, masked);
+    lam = std::max(lam, (size_t)q.items * q.parts);
+    if (masked) order = std::max({order, wa_diff_order_ints(q.items), wa_diff_order_ints(k.items)});
+    part = std::max({part, wa_diff_dq_floats(a, q), wa_diff_dkv_floats(a, k)});
+  }
+  DiffBackwardWs w;
+  w.lam = align_up((size_t)4 * a.batch * a.heads * a.q_len * 4);
+  w.order = w.lam + align_up(lam * 8);
+  w.part = w.order + align_up(order * 4);
+  w.total = w.part + align_up(part * 4);
+  return w;
 }
 
 // Arguments that both directions share, checked and put into the launch.
@@ -784,6 +803,7 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
   if (s != WA_OK) return s;
   a.o = o; a.maps = maps; a.stats = stats;
   a.part = (float*)workspace;
+  a.order = (int32_t*)workspace;
   const hipError_t e = wa_launch_diff_attn(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention launch");
   return ok();
@@ -794,7 +814,7 @@ wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_
   wa_status s = check_diff_shape(shape, &a);
   if (s != WA_OK) return s;
   if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
-  *bytes = diff_backward_ws_bytes(a);
+  *bytes = diff_backward_ws(a).total;
   return ok();
 }
 
@@ -813,12 +833,15 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
   if (!aligned(dout, 16) || !aligned(maps, 16) || !aligned(dq, 16) || !aligned(dk, 16) || !aligned(dv, 16))
     return fail(WA_ERR_ALIGNMENT, "dout, maps, dq, dk and dv must be 16-byte aligned");
   if (!aligned(stats, 4) || !aligned(dlam, 4)) return fail(WA_ERR_ALIGNMENT, "stats and dlam must be 4-byte aligned");
-  s = check_ws(workspace, workspace_bytes, diff_backward_ws_bytes(a));
+  const DiffBackwardWs L = diff_backward_ws(a);
+  s = check_ws(workspace, workspace_bytes, L.total);
   if (s != WA_OK) return s;
   a.dout = dout; a.maps = const_cast<int16_t*>(maps); a.stats = const_cast<float*>(stats);
   a.dq = dq; a.dk = dk; a.dv = dv; a.dlam = dlam;
   a.rows = (float*)workspace;
-  a.lam_part = (double*)((char*)workspace + diff_rows_bytes(a));
+  a.lam_part = (double*)((char*)workspace + L.lam);
+  a.order = (int32_t*)((char*)workspace + L.order);
+  a.part = (float*)((char*)workspace + L.part);
   const hipError_t e = wa_launch_diff_backward(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention gradient launch");
   return ok();

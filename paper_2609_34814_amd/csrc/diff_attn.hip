@@ -27,6 +27,8 @@ namespace {
 using namespace wa;
 
 constexpr float kGrow = 8.f;  // log2 units
+constexpr int kAheadRows = 4, kAheadCols = 4;  // operands read ahead
+constexpr int kMaxSplits = 128;
 
 template <int D, int DV, int W>
 struct Fwd {
@@ -37,6 +39,8 @@ struct Fwd {
   static constexpr int KRB = D * 2, VRB = DV * 2;
   static constexpr int KBYTES = KB * KRB, VBYTES = KB * VRB, STAGE = 2 * KBYTES + VBYTES;
   static constexpr int KT = KB / 32, DT = DV / 32, KS = D / 16;
+  // Two tiles are held. More on their way (3 or 4 where they fit) took as long or longer, since they displace workgroups: one
+  // token of 16 sequences 37, 38 and 41 us, 2 x 16 heads of 4,096 tokens (d 64, values 64) 353, 360 and 431 us.
   static_assert(W * 32 * DV * 4 <= 2 * STAGE, "the maps are joined in the tiles' memory");
 };
 
@@ -52,7 +56,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
 
   // Work item: the key range fastest, then the units of a group in turn, tile after tile; longest tiles first where
   // later queries see more keys.
-  int id = blockIdx.x;
+  int id = a.order ? a.order[blockIdx.x] : blockIdx.x;
   const int chunk = id % p.splits;
   id /= p.splits;
   const int item = id;
@@ -61,7 +65,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   const int count = min(p.group, p.units - first);
   const int unit = first + id % count;
   int tile = id / count;
-  if (a.causal) tile = p.tiles - 1 - tile;
+  if (a.causal && !a.order) tile = p.tiles - 1 - tile;
   const int per_key_head = a.heads / a.kv_heads;
   const int heads = p.packed ? a.kv_heads : a.heads;
   const int b = unit / heads;
@@ -112,21 +116,8 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
     copy_tile<C::VRB, KB, C::NWV>(t + 2 * C::KBYTES, vg, key, keys - 1, w, lane);
   };
 
-  bf16x8 qf[C::KS];
-  const uint16_t* qg = (const uint16_t*)a.q + (((int64_t)b * 2 * a.heads + 2 * h + map) * a.q_len + i) * D;
-#pragma unroll
-  for (int s = 0; s < C::KS; ++s) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (valid) u = *(const uint4*)(qg + 16 * s + 8 * hf);
-    qf[s] = as_bf16x8(u);
-  }
-  uint32_t kofs[C::KS], vofs[2][4];
-#pragma unroll
-  for (int s = 0; s < C::KS; ++s) kofs[s] = map * C::KBYTES + row_operand<C::KRB>(lane, s);
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) vofs[j][c] = 2 * C::KBYTES + col_operand<C::VRB>(lane, c & (C::DT - 1), j);
+  const uint32_t kbase = map * C::KBYTES + row_operand<C::KRB>(lane, 0);
+  const uint32_t vbase0 = 2 * C::KBYTES + col_operand<C::VRB>(lane, 0, 0), vbase1 = 2 * C::KBYTES + col_operand<C::VRB>(lane, 0, 1);
 
   const float c2 = a.scale * kLog2e;
   f32x16 acc[C::DT];
@@ -136,17 +127,37 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
     for (int v = 0; v < 16; ++v) acc[t][v] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
 
+  bf16x8 qf[C::KS];
   auto work = [&](int key, const unsigned char* t) {
+    // The operands' offsets are taken from their first in every tile (opaque, so that all of them are not held all along).
+    uint32_t kb = kbase, vb0 = vbase0, vb1 = vbase1;
+    asm volatile("" : "+v"(kb), "+v"(vb0), "+v"(vb1));
+    auto row = [&](int x) { return read_row(t + row_step(kb, x / C::KT) + x % C::KT * 32 * C::KRB); };
+    auto col = [&](int x) {  // column tile x mod DT of 16 keys
+      const unsigned char* at = t + x / C::DT * 16 * C::VRB + (x % C::DT >> 2) * 256;
+      return read_cols(at + col_step(vb0, x % C::DT & 3), at + col_step(vb1, x % C::DT & 3));
+    };
+    // Operands are read ahead of the products; fences keep the order written here (the scheduler sinks each read to its product).
     f32x16 s[C::KT];
 #pragma unroll
     for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[kt][v] = 0.f;
+    constexpr int ROWS = C::KS * C::KT, COLS = 2 * C::KT * C::DT;
+    bf16x8 ring[kAheadRows];
 #pragma unroll
-    for (int ks = 0; ks < C::KS; ++ks)
+    for (int x = 0; x < kAheadRows; ++x) ring[x] = row(x);
 #pragma unroll
-      for (int kt = 0; kt < C::KT; ++kt)
-        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row(t + kofs[ks] + kt * 32 * C::KRB), qf[ks], s[kt], 0, 0, 0);
+    for (int x = 0; x < ROWS; ++x) {
+      WA_SCHED_FENCE();
+      s[x % C::KT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[x % kAheadRows], qf[x / C::KT], s[x % C::KT], 0, 0, 0);
+      if (x + kAheadRows < ROWS) ring[x % kAheadRows] = row(x + kAheadRows);
+    }
+    WA_SCHED_FENCE();
+    bf16x8 cring[kAheadCols];
+#pragma unroll
+    for (int x = 0; x < kAheadCols; ++x) cring[x] = col(x);
+    WA_SCHED_FENCE();
     if (key + KB > all) {
       const int rest = limit - key - 4 * hf;
 #pragma unroll
@@ -173,36 +184,44 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
         for (int v = 0; v < 16; ++v) acc[t2][v] *= f;
     }
     const float ref = m_run == -INFINITY ? 0.f : m_run;
-    uint32_t pk[C::KT][8];
-    float sum = 0.f;
+    uint32_t pk[2 * C::KT][4];
+    auto pair = [&](int k16, int j) {  // probabilities 2 j and 2 j + 1 of the lane's 8 of 16 keys
+      const f32x16& x = s[k16 >> 1];
+      const int v = 8 * (k16 & 1) + 2 * j;
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], c2, -ref));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v + 1], c2, -ref));
+      l_run += p0 + p1;
+      pk[k16][j] = pack_bf16x2(p0, p1);
+    };
 #pragma unroll
-    for (int kt = 0; kt < C::KT; ++kt)
+    for (int j = 0; j < 4; ++j) pair(0, j);
 #pragma unroll
-      for (int v = 0; v < 16; v += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][v], c2, -ref));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][v + 1], c2, -ref));
-        sum += p0 + p1;
-        pk[kt][v >> 1] = pack_bf16x2(p0, p1);
-      }
-    l_run += sum;
+    for (int x = 0; x < COLS; ++x) {
+      WA_SCHED_FENCE();
+      const int k16 = x / C::DT, dt = x % C::DT;
+      acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          cring[x % kAheadCols], as_bf16x8(make_uint4(pk[k16][0], pk[k16][1], pk[k16][2], pk[k16][3])), acc[dt], 0, 0, 0);
+      if (x + kAheadCols < COLS) cring[x % kAheadCols] = col(x + kAheadCols);
 #pragma unroll
-    for (int kt = 0; kt < C::KT; ++kt)
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        const bf16x8 pb = as_bf16x8(make_uint4(pk[kt][4 * s2], pk[kt][4 * s2 + 1], pk[kt][4 * s2 + 2], pk[kt][4 * s2 + 3]));
-        const unsigned char* tv = t + (kt * 32 + 16 * s2) * C::VRB;
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              read_cols(tv + vofs[0][dt & 3] + (dt >> 2) * 256, tv + vofs[1][dt & 3] + (dt >> 2) * 256), pb, acc[dt], 0, 0, 0);
-      }
+      for (int j = 0; j < 4; ++j)  // the next 16 keys' probabilities beside this product
+        if (k16 + 1 < 2 * C::KT && dt == j * C::DT / 4) pair(k16 + 1, j);
+    }
+    WA_SCHED_FENCE();
   };
+
+  const uint16_t* qg = (const uint16_t*)a.q + (((int64_t)b * 2 * a.heads + 2 * h + map) * a.q_len + i) * D;
+#pragma unroll
+  for (int s = 0; s < C::KS; ++s) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (valid) u = *(const uint4*)(qg + 16 * s + 8 * hf);
+    qf[s] = as_bf16x8(u);
+  }
 
   int key = lo < hi ? next_tile(lo) : hi, buf = 0;
   if (key < hi) copy(key, 0);
   while (key < hi) {
     const int next = next_tile(key + KB);
-    WA_WAIT_VM(0);  // this wavefront's part of the tile has arrived
+    WA_WAIT_VM(0);  // this wavefront's part of the tile has arrived (and the queries, so that nothing waits for them below)
     WA_BARRIER();   // everyone's has, and everyone is done with the other buffer
     if (next < hi) copy(next, buf ^ 1);
     if (key < some) work(key, lds + buf * C::STAGE);
@@ -280,15 +299,20 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
     }
 }
 
-// Joins the key ranges of split tiles, in order: one wavefront a query row, DV / 64 columns a lane.
-template <int DV>
+// Joins the key ranges of split tiles, in a fixed order: R wavefronts a query row, each the ranges of its number modulo R,
+// DV / 64 columns a lane. R is 4 where a row has eight ranges and more, else 1 (16 x 16 rows of 8 ranges of 128 columns: 6.1 us
+// with 1, 4.7 with 4).
+template <int DV, int R>
 __global__ __launch_bounds__(256) void diff_join_kernel(const WaDiffLaunch a, const WaDiffPlan p) {
   constexpr int E = DV / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= (int64_t)a.batch * a.heads * a.q_len) return;
+  typedef float cols __attribute__((ext_vector_type(E)));
+  __shared__ float weight[4][2][kMaxSplits];
+  __shared__ cols sums[4][2][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t r = (int64_t)blockIdx.x * (4 / R) + w / R;
+  const bool valid = r < (int64_t)a.batch * a.heads * a.q_len;
   const int i = r % a.q_len;
-  const int bh = r / a.q_len, b = bh / a.heads, h = bh % a.heads;
+  const int bh = valid ? r / a.q_len : 0, b = bh / a.heads, h = bh % a.heads;
   const int per_key_head = a.heads / a.kv_heads;
   const int unit = p.packed ? b * a.kv_heads + h / per_key_head : bh;
   const int row = p.packed ? h % per_key_head * a.q_len + i : i;
@@ -297,32 +321,58 @@ __global__ __launch_bounds__(256) void diff_join_kernel(const WaDiffLaunch a, co
   const int first = unit / p.group * p.group, count = min(p.group, p.units - first);
   const int64_t item = (int64_t)first * p.tiles + (int64_t)(a.causal ? p.tiles - 1 - tile : tile) * count + unit - first;
   const float2* stat = (const float2*)(a.part + (int64_t)p.units * p.tiles * p.splits * 2 * rows * DV);
-  float o[2][E];
+  auto at = [&](int c, int m) { return ((item * p.splits + c) * 2 + m) * rows + row % rows; };
+  float top[2], l[2];
+  cols o[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    auto at = [&](int c) { return ((item * p.splits + c) * 2 + m) * rows + row % rows; };
-    float top = -INFINITY, l = 0.f;
-    for (int c = lane; c < p.splits; c += 64) top = fmaxf(top, stat[at(c)].x);
-    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    // a range a lane (kMaxSplits is at most twice 64)
+    float2 s[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int c = lane + 64 * x;
+      s[x] = valid && c < p.splits ? stat[at(c, m)] : make_float2(-INFINITY, 0.f);
+    }
+    top[m] = fmaxf(s[0].x, s[1].x);
+    for (int x = 32; x > 0; x >>= 1) top[m] = fmaxf(top[m], __shfl_xor(top[m], x));
+    l[m] = 0.f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float f = s[x].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[x].x - top[m]);
+      if (lane + 64 * x < p.splits) weight[w][m][lane + 64 * x] = f;
+      l[m] += f * s[x].y;
+    }
+    for (int x = 32; x > 0; x >>= 1) l[m] += __shfl_xor(l[m], x);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[m][e] = 0.f;
+  }
+  __syncthreads();
+  if (valid) {
 #pragma unroll 4
-    for (int c = 0; c < p.splits; ++c) {
-      const float2 s = stat[at(c)];
-      const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
-      l += f * s.y;
+    for (int c = w % R; c < p.splits; c += R)
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[m][e] += f * a.part[at(c) * DV + lane * E + e];
-    }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+      for (int m = 0; m < 2; ++m) o[m] += *(const cols*)(a.part + at(c, m) * DV + lane * E) * weight[w][m][c];
+  }
+  if constexpr (R > 1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[m][e] *= inv;
+    for (int m = 0; m < 2; ++m) sums[w][m][lane] = o[m];
+    __syncthreads();
+    if (w % R) return;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int x = 1; x < R; ++x) o[m] += sums[w + x][m][lane];
+  }
+  if (!valid) return;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    o[m] *= l[m] > 0.f ? 1.f / l[m] : l[m] == 0.f ? 0.f : NAN;
     if (a.maps) {
       float big = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) big = fmaxf(big, fabsf(o[m][e]));
       for (int x = 32; x > 0; x >>= 1) big = fmaxf(big, __shfl_xor(big, x));
-      const RowStats s = row_stats(top, l, big);
+      const RowStats s = row_stats(top[m], l[m], big);
       const float per_step = s.step > 0.f ? 1.f / s.step : 0.f;
       const int64_t to = ((int64_t)b * 2 * a.heads + 2 * h + m) * a.q_len + i;
 #pragma unroll
@@ -341,7 +391,13 @@ __global__ __launch_bounds__(256) void diff_join_kernel(const WaDiffLaunch a, co
 }
 
 template <int D, int DV>
-hipError_t launch_dims(const WaDiffLaunch& a, const WaDiffPlan& p, hipStream_t stream) {
+hipError_t launch_dims(WaDiffLaunch a, const WaDiffPlan& p, hipStream_t stream) {
+  if (a.mask && p.splits == 1 && wa_diff_ordered((int64_t)p.units * p.tiles)) {
+    const hipError_t e = wa_launch_diff_order(a, false, stream);
+    if (e != hipSuccess) return e;
+  } else {
+    a.order = nullptr;
+  }
   const int64_t grid = (int64_t)p.units * p.tiles * p.splits;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   const dim3 g((unsigned)grid), t(128 * p.waves);
@@ -351,7 +407,10 @@ hipError_t launch_dims(const WaDiffLaunch& a, const WaDiffPlan& p, hipStream_t s
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t rows = (int64_t)a.batch * a.heads * a.q_len;
-  hipLaunchKernelGGL((diff_join_kernel<DV>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, p);
+  if (p.splits >= 8)
+    hipLaunchKernelGGL((diff_join_kernel<DV, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a, p);
+  else
+    hipLaunchKernelGGL((diff_join_kernel<DV, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, p);
   return hipGetLastError();
 }
 
@@ -369,8 +428,9 @@ WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked) {
   // Key ranges: as many as keep 256 compute units busy (two workgroups each of less than four wavefronts a map), of
   // 256 keys at least.
   const int64_t slots = p.waves == 4 ? 256 : 512, items = (int64_t)p.units * p.tiles;
-  p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(slots / items, a.kv_len / 256));
-  p.group = 8;
+  p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / items, kMaxSplits), a.kv_len / 256));
+  // Heads of a mask one after another, so that one head's keys are in the caches; dense ones eight together, one an XCD.
+  p.group = masked ? 1 : 8;
   return p;
 }
 

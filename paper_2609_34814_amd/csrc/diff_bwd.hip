@@ -9,8 +9,8 @@
 // maps with their accumulators in registers (for d 128 one wavefront a SIMD, which may use 512), and the other side's tiles pass
 // through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are.
-// dlam is summed from the float32 P_2 dP, not from the stored maps: over a lane's keys with the roundings carried along, over
-// queries in float64.
+// dlam is the sum of D_2 from the stored maps and of the float32 P_2 (dP - D_2), which takes their steps' error back: over a
+// lane's keys with the roundings carried along, over queries in float64.
 
 #include "diff_tiles.h"
 #include "wavealign.h"
@@ -21,23 +21,25 @@ namespace {
 
 using namespace wa;
 
-template <int D, int DV, int W>
+template <int D, int DV, int W, bool SMALL = false>
 struct Bwd {
-  // Tokens of a passing tile: 64 with four wavefronts, 32 with two (two workgroups share a compute unit's LDS).
-  static constexpr int TB = W == 4 ? 64 : 32;
+  // Tokens of a passing tile: 64 with four wavefronts, 32 with two (two workgroups share a compute unit's LDS) or where the
+  // own side takes LDS too.
+  static constexpr int TB = W == 4 && !SMALL ? 64 : 32;
   static constexpr int KRB = D * 2, VRB = DV * 2;
   static constexpr int KBYTES = TB * KRB, VBYTES = TB * VRB, STAGE = 2 * KBYTES + VBYTES;
   static constexpr int DT = D / 32, VT = DV / 32, KS = D / 16, VS = DV / 16;
 };
-// Wavefronts a SIMD: two share its 512 registers a lane where both hold their accumulators without spilling.
+constexpr int kAhead = 6, kAheadCols = 4;  // operands read ahead: rows, columns
+// Wavefronts a SIMD: two share its 512 registers a lane where both hold their accumulators.
 template <int D>
 constexpr int kDqWaves = D == 64 ? 2 : 1;
 template <int DV>
 constexpr int kDkvWaves = DV == 64 ? 2 : 1;
 
-__device__ __forceinline__ void clear(f32x16& x) {
+__device__ __forceinline__ void fill(f32x16& x, float f) {
 #pragma unroll
-  for (int v = 0; v < 16; ++v) x[v] = 0.f;
+  for (int v = 0; v < 16; ++v) x[v] = f;
 }
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -69,8 +71,18 @@ __device__ __forceinline__ void store_row(uint16_t* out, const f32x16 (&acc)[T],
           make_uint2(pack_bf16x2(acc[t][v] * f, acc[t][v + 1] * f), pack_bf16x2(acc[t][v + 2] * f, acc[t][v + 3] * f));
 }
 
+// the same unrounded, as a row of a part's result
+template <int T>
+__device__ __forceinline__ void store_part(float* out, const f32x16 (&acc)[T], float f, int hf) {
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4)
+      *(float4*)(out + t * 32 + 2 * v + 4 * hf) = make_float4(acc[t][v] * f, acc[t][v + 1] * f, acc[t][v + 2] * f, acc[t][v + 3] * f);
+}
+
 template <int D, int DV, int W>
-__global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDiffLaunch a, int tiles) {
+__global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDiffLaunch a, const WaDiffSide n) {
   using C = Bwd<D, DV, W>;
   constexpr int KB = C::TB;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE];
@@ -78,16 +90,22 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // heads one after another, the longest tiles of each first where later queries see more keys
-  const int bh = blockIdx.x / tiles, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
-  const int tile = a.causal ? tiles - 1 - blockIdx.x % tiles : blockIdx.x % tiles;
+  // The parts of a tile together; the longest tiles of all heads first where later queries see more keys, else head
+  // after head, or as the order says.
+  const int part = blockIdx.x % n.parts, turn = blockIdx.x / n.parts;
+  const int item = a.order ? a.order[turn] : a.causal ? turn % (a.batch * a.heads) * n.tiles + n.tiles - 1 - turn / (a.batch * a.heads) : turn;
+  const int bh = item / n.tiles, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
+  const int tile = item % n.tiles;
   const int i0 = tile * 32 * W + w * 32, i = i0 + l32, i_last = a.q_len - 1;
   const bool valid = i <= i_last;
   const int keys = keys_of(a, b), start = start_of(a, b);
   const int limit = valid ? key_limit(a, keys, start, i) : 0;
   const int some = i0 > i_last ? 0 : key_limit(a, keys, start, min(i0 + 31, i_last));
   const int all = key_limit(a, keys, start, min(i0, i_last));
-  const int hi = key_limit(a, keys, start, min(tile * 32 * W + 32 * W - 1, i_last));
+  // this part's keys: whole blocks and tiles
+  const int most = key_limit(a, keys, start, min(tile * 32 * W + 32 * W - 1, i_last));
+  const int unit = a.mask ? max(a.block, KB) : KB, per = ((most + unit - 1) / unit + n.parts - 1) / n.parts;
+  const int lo = min((int64_t)part * per * unit, (int64_t)most), hi = min((int64_t)lo + per * unit, (int64_t)most);
 
   const unsigned char* kg = (const unsigned char*)a.k + (((int64_t)b * 2 * a.kv_heads + 2 * hk) * a.kv_len) * C::KRB;
   const unsigned char* vg = (const unsigned char*)a.v + (((int64_t)b * a.kv_heads + hk) * a.kv_len) * C::VRB;
@@ -102,12 +120,14 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     return walk.next(key >> shift, lane) << shift;
   };
   auto copy = [&](int key, int buf) {
+    int lane_o = lane;
+    asm volatile("" : "+v"(lane_o));  // nor those of the copies
     const unsigned char* t = lds + buf * C::STAGE;
-    copy_tile<C::KRB, KB, W>(t, kg, key, keys - 1, w, lane);
-    copy_tile<C::KRB, KB, W>(t + C::KBYTES, kg + (int64_t)a.kv_len * C::KRB, key, keys - 1, w, lane);
-    copy_tile<C::VRB, KB, W>(t + 2 * C::KBYTES, vg, key, keys - 1, w, lane);
+    copy_tile<C::KRB, KB, W>(t, kg, key, keys - 1, w, lane_o);
+    copy_tile<C::KRB, KB, W>(t + C::KBYTES, kg + (int64_t)a.kv_len * C::KRB, key, keys - 1, w, lane_o);
+    copy_tile<C::VRB, KB, W>(t + 2 * C::KBYTES, vg, key, keys - 1, w, lane_o);
   };
-  int key = hi > 0 ? next_tile(0) : 0, buf = 0;
+  int key = lo < hi ? next_tile(lo) : hi, buf = 0;
   if (key < hi) copy(key, 0);
 
   // the wavefront's queries, their dO, and D_m
@@ -118,7 +138,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
 #pragma unroll
     for (int m = 0; m < 2; ++m)
       qf[m][s] = load8((const uint16_t*)a.q + (row0 + (int64_t)m * a.q_len) * D + 16 * s + 8 * hf, valid);
-  float d[2] = {0.f, 0.f}, ref[2] = {0.f, 0.f}, factor = 1.f;  // ref: log-sum-exp in log2 units
+  float d[2] = {0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < C::VS; ++s) {
     dof[s] = load8((const uint16_t*)a.dout + row + 16 * s + 8 * hf, valid);
@@ -129,100 +149,148 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
       d[m] = dot8(dof[s], u, d[m]);
     }
   }
-  const int64_t all_rows = (int64_t)a.batch * 2 * a.heads * a.q_len;
+  // The products start from what is subtracted from them: scores from the log-sum-exp, so P_m = exp2(c2 s), and dP from D_1;
+  // with D_1 - D_2 they are all that diff_dkv_kernel needs of a row.
+  const float c2 = a.scale * kLog2e;
+  float from[2] = {0.f, 0.f}, factor = 1.f;
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     d[m] = add_halves(d[m]);
     if (valid) {
-      const int64_t at = row0 + (int64_t)m * a.q_len;
-      ref[m] = a.stats[3 * at] * kLog2e;
-      d[m] *= a.stats[3 * at + 1];
-      factor = a.stats[3 * at + 2];  // of the second map, in the end
-      if (hf == 0) {
-        a.rows[at] = ref[m];
-        a.rows[all_rows + at] = d[m];
-      }
+      const float* st = a.stats + 3 * (row0 + (int64_t)m * a.q_len);
+      from[m] = -st[0] * kLog2e / c2;
+      d[m] *= st[1];
+      factor = st[2];  // of the second map, in the end
     }
+  }
+  const float step = d[0] - d[1];
+  if (valid && hf == 0 && part == 0) {
+    float* to = a.rows + (int64_t)bh * 4 * a.q_len + i;
+    to[0] = from[0];
+    to[a.q_len] = from[1];
+    to[2 * (int64_t)a.q_len] = -d[0];
+    to[3 * (int64_t)a.q_len] = step;
   }
   const float lam = a.lam[h];
 
-  uint32_t kofs[C::KS], vofs[C::VS < 16 ? C::VS : 8], kcol[2][C::DT];
-#pragma unroll
-  for (int s = 0; s < C::KS; ++s) kofs[s] = row_operand<C::KRB>(lane, s);
-#pragma unroll
-  for (int s = 0; s < (C::VS < 16 ? C::VS : 8); ++s) vofs[s] = 2 * C::KBYTES + row_operand<C::VRB>(lane, s);
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int c = 0; c < C::DT; ++c) kcol[j][c] = col_operand<C::KRB>(lane, c, j);
+  const uint32_t k_row = row_operand<C::KRB>(lane, 0), v_row = 2 * C::KBYTES + row_operand<C::VRB>(lane, 0);
+  const uint32_t k_col0 = col_operand<C::KRB>(lane, 0, 0), k_col1 = col_operand<C::KRB>(lane, 0, 1);
 
-  const float c2 = a.scale * kLog2e;
   f32x16 dq[2][C::DT];
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int c = 0; c < C::DT; ++c) clear(dq[m][c]);
+    for (int c = 0; c < C::DT; ++c) fill(dq[m][c], 0.f);
   float lam_dot = 0.f, lam_lost = 0.f;
 
+  // 32 keys; masked: this lane's query sees only `rest` of them, counted from its first register's.
+  auto work = [&](const unsigned char* t, const unsigned char* tv, bool masked, int rest) {
+    // opaque, so that the offsets of all operands are not held across the loop
+    uint32_t kr = k_row, vr = v_row, kc0 = k_col0, kc1 = k_col1;
+    asm volatile("" : "+v"(kr), "+v"(vr), "+v"(kc0), "+v"(kc1));
+    auto row = [&](int x) {  // operand of product x of the scores, then of dP
+      const int y = x - 2 * C::KS;
+      return x < 2 * C::KS ? read_row(t + (x & 1) * C::KBYTES + row_step(kr, x >> 1)) : read_row(tv + row_step(vr, y & 7) + (y >> 3) * 256);
+    };
+    auto col = [&](int x) {  // operand of product x of dQ: 16 keys, map, 32 columns
+      const unsigned char* at = t + (x / C::DT & 1) * C::KBYTES + 16 * (x / (2 * C::DT)) * C::KRB;
+      return read_cols(at + col_step(kc0, x % C::DT), at + col_step(kc1, x % C::DT));
+    };
+    constexpr int ROWS = 2 * C::KS + C::VS, COLS = 4 * C::DT;
+    f32x16 s[2], dp;
+    fill(s[0], from[0]);
+    fill(s[1], from[1]);
+    fill(dp, -d[0]);
+    float p[2][16];
+    bf16x8 ring[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) ring[x] = row(x);
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x) {
+      WA_SCHED_FENCE();
+      if (x < 2 * C::KS)
+        s[x & 1] = mfma(ring[x % kAhead], qf[x & 1][x >> 1], s[x & 1]);
+      else
+        dp = mfma(ring[x % kAhead], dof[x - 2 * C::KS], dp);
+      if (x + kAhead < ROWS) ring[x % kAhead] = row(x + kAhead);
+      if (x >= 2 * C::KS) {  // the exponentials run beside the products of dP
+        constexpr int PER = 32 / C::VS;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          const int v = (x - 2 * C::KS) * PER + e;
+          p[v >> 4][v & 15] = __builtin_amdgcn_exp2f(s[v >> 4][v & 15] * c2);
+        }
+      }
+    }
+    bf16x8 cring[kAheadCols];
+#pragma unroll
+    for (int x = 0; x < kAheadCols; ++x) cring[x] = col(x);
+    if (masked) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (8 * (v >> 2) + (v & 3) >= rest) p[0][v] = p[1][v] = 0.f;
+    }
+    float dot = 0.f;
+    auto dscore = [&](int m, int v) {
+      p[m][v] *= m ? dp[v] + step : dp[v];
+      if (m) dot += p[m][v];
+    };
+    bf16x8 ds[2];
+#pragma unroll
+    for (int v = 0; v < 8; ++v) dscore(0, v);
+    ds[0] = pack8(p[0]);
+#pragma unroll
+    for (int v = 0; v < 8; ++v) dscore(1, v);
+    ds[1] = pack8(p[1]);
+#pragma unroll
+    for (int x = 0; x < COLS; ++x) {
+      WA_SCHED_FENCE();
+      const int m = x / C::DT & 1;
+      if (x == 2 * C::DT) ds[0] = pack8(p[0] + 8);
+      if (x == 3 * C::DT) ds[1] = pack8(p[1] + 8);
+      dq[m][x % C::DT] = mfma(cring[x % kAheadCols], ds[m], dq[m][x % C::DT]);
+      if (x + kAheadCols < COLS) cring[x % kAheadCols] = col(x + kAheadCols);
+      if (x < 2 * C::DT) {  // dS of the second 16 keys beside the products of the first
+        constexpr int PER = 16 / (2 * C::DT);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          const int v = x * PER + e;
+          dscore(v >> 3, 8 + (v & 7));
+        }
+      }
+    }
+    WA_SCHED_FENCE();
+    const float add = dot - lam_lost, grown = lam_dot + add;
+    lam_lost = (grown - lam_dot) - add;
+    lam_dot = grown;
+  };
   while (key < hi) {
     const int next = next_tile(key + KB);
     WA_WAIT_VM(0);
     WA_BARRIER();
     if (next < hi) copy(next, buf ^ 1);
+    int end = KB;
+    asm volatile("" : "+s"(end));
 #pragma unroll 1
-    for (int half = 0; half < KB; half += 32) {
+    for (int half = 0; half < end; half += 32) {
       if (key + half >= some) break;
       const unsigned char* t = lds + buf * C::STAGE + half * C::KRB;
       const unsigned char* tv = lds + buf * C::STAGE + half * C::VRB;
-      f32x16 s[2], dp;
-      clear(s[0]);
-      clear(s[1]);
-      clear(dp);
-#pragma unroll
-      for (int x = 0; x < C::KS; ++x)
-#pragma unroll
-        for (int m = 0; m < 2; ++m) s[m] = mfma(read_row(t + m * C::KBYTES + kofs[x]), qf[m][x], s[m]);
-#pragma unroll
-      for (int x = 0; x < C::VS; ++x) dp = mfma(read_row(tv + vofs[x & 7] + (x >> 3) * 256), dof[x], dp);
-      float p[2][16];
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) p[m][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][v], c2, -ref[m]));
-      if (key + half + 32 > all) {
-        const int rest = limit - key - half - 4 * hf;
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (8 * (v >> 2) + (v & 3) >= rest) p[0][v] = p[1][v] = 0.f;
-      }
-      float dot = 0.f;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        dot = __builtin_fmaf(p[1][v], dp[v], dot);
-        p[0][v] *= dp[v] - d[0];
-        p[1][v] *= dp[v] - d[1];
-      }
-      const float add = dot - lam_lost, grown = lam_dot + add;
-      lam_lost = (grown - lam_dot) - add;
-      lam_dot = grown;
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const bf16x8 ds = pack8(p[m] + 8 * x);
-          const unsigned char* tk = t + m * C::KBYTES + 16 * x * C::KRB;
-#pragma unroll
-          for (int c = 0; c < C::DT; ++c) dq[m][c] = mfma(read_cols(tk + kcol[0][c], tk + kcol[1][c]), ds, dq[m][c]);
-        }
+      work(t, tv, key + half + 32 > all, limit - key - half - 4 * hf);
     }
     key = next;
     buf ^= 1;
   }
-  if (valid) {
+  if (n.parts > 1) {
+    float* to = a.part + (((int64_t)item * n.parts + part) * 32 * W + w * 32 + l32) * 2 * D;
+    store_part(to, dq[0], a.scale, hf);
+    store_part(to + D, dq[1], -lam * a.scale, hf);
+  } else if (valid) {
     store_row(((uint16_t*)a.dq) + row0 * D, dq[0], a.scale, hf);
     store_row(((uint16_t*)a.dq) + (row0 + a.q_len) * D, dq[1], -lam * a.scale, hf);
   }
-  double lam_row = (double)lam_dot * factor;
+  // sum_j P_2 (dP - D_2), which the stored maps' steps leave of their D_2 (the sum of P_2 is 1), and that D_2
+  double lam_row = (double)lam_dot * factor + (valid && hf == 0 && part == 0 ? (double)d[1] : 0.0);
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) lam_row += __shfl_xor(lam_row, x);
   if (lane == 0) lam_sum[w] = lam_row;
@@ -230,7 +298,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
   if (tid == 0) {
     double sum = 0.0;
     for (int x = 0; x < W; ++x) sum += lam_sum[x];
-    a.lam_part[(int64_t)bh * tiles + tile] = sum;
+    a.lam_part[(int64_t)item * n.parts + part] = sum;
   }
 }
 
@@ -249,11 +317,14 @@ __device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, const uns
 }
 
 template <int D, int DV, int W>
-__global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const WaDiffLaunch a, int tiles, int q_tiles) {
-  using C = Bwd<D, DV, W>;
-  constexpr int QB = C::TB;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE];
-  __shared__ __attribute__((aligned(1024))) float stat[2][4 * QB];  // of both maps: log-sum-exps (log2 units), then D_m
+__global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const WaDiffLaunch a, const WaDiffSide n, int lam_parts) {
+  // Values of 256 columns lie in LDS, where four wavefronts leave the room: with the keys and the sums of dK and dV, they
+  // do not fit 512 registers.
+  constexpr bool kValuesInLds = DV == 256 && W == 4;
+  using C = Bwd<D, DV, W, kValuesInLds>;
+  constexpr int QB = C::TB, VALUES = kValuesInLds ? 32 * W * C::VRB : 0;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE + VALUES];
+  __shared__ __attribute__((aligned(1024))) float stat[2][4 * QB];  // the rows of a.rows
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -262,15 +333,17 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const W
     if (tid < 64) {
       double sum = 0.0;
       for (int b = 0; b < a.batch; ++b)
-        for (int t = lane; t < q_tiles; t += 64) sum += a.lam_part[((int64_t)b * a.heads + h) * q_tiles + t];
+        for (int t = lane; t < lam_parts; t += 64) sum += a.lam_part[((int64_t)b * a.heads + h) * lam_parts + t];
       for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
       if (lane == 0) a.dlam[h] = (float)-sum;
     }
   }
 
-  // the first tiles of keys, which the most queries see, come first
-  const int bh = blockIdx.x / tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
-  const int tile = blockIdx.x % tiles;
+  // The parts of a tile together; the first tiles of all heads, which the most queries see, first where that differs.
+  const int part = blockIdx.x % n.parts, turn = blockIdx.x / n.parts;
+  const int item = a.order ? a.order[turn] : a.causal ? turn % (a.batch * a.kv_heads) * n.tiles + turn / (a.batch * a.kv_heads) : turn;
+  const int bh = item / n.tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
+  const int tile = item % n.tiles;
   const int keys = keys_of(a, b), start = start_of(a, b);
   const int k0 = tile * 32 * W + w * 32, kj = k0 + l32;
   const bool valid = kj < keys;
@@ -279,181 +352,300 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const W
   const int from = first_query(kj);
   const int some = first_query(k0), all = first_query(min(k0 + 31, max(keys - 1, k0)));
   const bool whole = k0 + 31 < keys;
-  const int lo = first_query(tile * 32 * W) / QB * QB, hi = a.q_len;
+  // this part's tiles of queries, counted through the heads one after another
+  const int from0 = first_query(tile * 32 * W), first = from0 / QB * QB;
+  const int q_tiles = from0 < a.q_len ? (a.q_len - first + QB - 1) / QB : 0;
+  const int64_t all_tiles = (int64_t)per_key_head * q_tiles;
+  const int64_t t0 = all_tiles * part / n.parts, t1 = all_tiles * (part + 1) / n.parts;
 
   const int64_t krow0 = ((int64_t)b * 2 * a.kv_heads + 2 * hk) * a.kv_len + kj, vrow = (int64_t)bh * a.kv_len + kj;
-  bf16x8 kf[2][C::KS], vf[C::VS];
+  bf16x8 kf[2][C::KS], vf[kValuesInLds ? 1 : C::VS];
 #pragma unroll
   for (int s = 0; s < C::KS; ++s)
 #pragma unroll
     for (int m = 0; m < 2; ++m)
       kf[m][s] = load8((const uint16_t*)a.k + (krow0 + (int64_t)m * a.kv_len) * D + 16 * s + 8 * hf, valid);
+  unsigned char* const values = lds + 2 * C::STAGE;
+  if constexpr (kValuesInLds) {
+    if (q_tiles > 0)  // so there are keys; those past the last are the last again
+      copy_tile<C::VRB, 32 * W, W>(values, (const unsigned char*)a.v + (int64_t)bh * a.kv_len * C::VRB, tile * 32 * W, keys - 1, w, lane);
+  } else {
 #pragma unroll
-  for (int s = 0; s < C::VS; ++s) vf[s] = load8((const uint16_t*)a.v + vrow * DV + 16 * s + 8 * hf, valid);
-
-  uint32_t qofs[C::KS], oofs[C::VS < 16 ? C::VS : 8], qcol[2][C::DT], ocol[2][C::VT < 8 ? C::VT : 4];
-#pragma unroll
-  for (int s = 0; s < C::KS; ++s) qofs[s] = row_operand<C::KRB>(lane, s);
-#pragma unroll
-  for (int s = 0; s < (C::VS < 16 ? C::VS : 8); ++s) oofs[s] = 2 * C::KBYTES + row_operand<C::VRB>(lane, s);
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-#pragma unroll
-    for (int c = 0; c < C::DT; ++c) qcol[j][c] = col_operand<C::KRB>(lane, c, j);
-#pragma unroll
-    for (int c = 0; c < (C::VT < 8 ? C::VT : 4); ++c) ocol[j][c] = 2 * C::KBYTES + col_operand<C::VRB>(lane, c, j);
+    for (int s = 0; s < C::VS; ++s) vf[s] = load8((const uint16_t*)a.v + vrow * DV + 16 * s + 8 * hf, valid);
   }
+
+  const uint32_t q_row = row_operand<C::KRB>(lane, 0), o_row = 2 * C::KBYTES + row_operand<C::VRB>(lane, 0);
+  const uint32_t q_col0 = col_operand<C::KRB>(lane, 0, 0), q_col1 = col_operand<C::KRB>(lane, 0, 1);
+  const uint32_t o_col0 = 2 * C::KBYTES + col_operand<C::VRB>(lane, 0, 0), o_col1 = 2 * C::KBYTES + col_operand<C::VRB>(lane, 0, 1);
+  const uint32_t v_row = w * 32 * C::VRB + row_operand<C::VRB>(lane, 0);
 
   const float c2 = a.scale * kLog2e;
   f32x16 dk[2][C::DT], dv[C::VT];
 #pragma unroll
   for (int c = 0; c < C::DT; ++c) {
-    clear(dk[0][c]);
-    clear(dk[1][c]);
+    fill(dk[0][c], 0.f);
+    fill(dk[1][c], 0.f);
   }
 #pragma unroll
-  for (int c = 0; c < C::VT; ++c) clear(dv[c]);
+  for (int c = 0; c < C::VT; ++c) fill(dv[c], 0.f);
 
+  // One loop over the tiles of all heads: head g's run from lo to hi; i is the next one's first query.
   const int shift = a.block == 128 ? 7 : 6;
-  for (int g = 0; g < per_key_head; ++g) {
-    const int h = hk * per_key_head + g;
-    const float lam = a.lam[h];
-    const int64_t qh = (int64_t)b * 2 * a.heads + 2 * h;
-    const unsigned char* qg = (const unsigned char*)a.q + qh * a.q_len * C::KRB;
-    const unsigned char* og = (const unsigned char*)a.dout + ((int64_t)b * a.heads + h) * a.q_len * C::VRB;
-    const float* ref = a.rows + qh * a.q_len;
-    const float* dots = ref + (int64_t)a.batch * 2 * a.heads * a.q_len;
-    MaskWalk walk;
-    if (a.mask) {
-      walk.at = uniform_ptr(a.mask + ((int64_t)b * a.heads + h) * a.mb * a.nb + (tile * 32 * W >> shift));
-      walk.step = a.nb;
-      walk.entries = a.mb;
-    }
-    auto next_tile = [&](int i) {
-      if (!a.mask || (i & (a.block - 1))) return i;
-      return walk.next(i >> shift, lane) << shift;
-    };
-    auto copy = [&](int i, int buf) {
-      const unsigned char* t = lds + buf * C::STAGE;
-      copy_tile<C::KRB, QB, W>(t, qg, i, a.q_len - 1, w, lane);
-      copy_tile<C::KRB, QB, W>(t + C::KBYTES, qg + (int64_t)a.q_len * C::KRB, i, a.q_len - 1, w, lane);
-      copy_tile<C::VRB, QB, W>(t + 2 * C::KBYTES, og, i, a.q_len - 1, w, lane);
-      // 4 QB statistics: QB / 16 copies of 64, wavefront w takes copies w, w + W, ...
-#pragma unroll
-      for (int c = w; c < QB / 16; c += W) {
-        const int at = c * 64 + lane;  // statistic at / QB of query i + at % QB
-        const int x = min(i + at % QB, a.q_len - 1) + (at / QB & 1) * a.q_len;
-        dma4(c * 64 < 2 * QB ? ref : dots, (uint32_t)x * 4, (const unsigned char*)(stat[buf] + c * 64));
+  MaskWalk walk;
+  int g = q_tiles > 0 ? (int)(t0 / q_tiles) - 1 : per_key_head, i = 0, hi = 0;
+  auto kept = [&](int x) { return a.mask && !(x & (a.block - 1)) ? walk.next(x >> shift, lane) << shift : x; };
+  auto advance = [&](int from) {
+    i = kept(from);
+    while (i >= hi && (g + 1) * (int64_t)q_tiles < t1) {
+      ++g;
+      const int lo = first + (int)max(t0 - g * (int64_t)q_tiles, (int64_t)0) * QB;
+      hi = min((int64_t)first + (t1 - g * (int64_t)q_tiles) * QB, (int64_t)a.q_len);
+      if (a.mask) {
+        walk.at = uniform_ptr(a.mask + ((int64_t)b * a.heads + hk * per_key_head + g) * a.mb * a.nb + (tile * 32 * W >> shift));
+        walk.step = a.nb;
+        walk.entries = a.mb;
+        walk.word_i = -1;
       }
+      // the first tile may begin inside a mask block that the walk has not looked at
+      i = a.mask ? max(kept(lo & ~(a.block - 1)), lo) : lo;
+    }
+    return i < hi;
+  };
+  auto copy = [&](int buf) {
+    int lane_o = lane;
+    asm volatile("" : "+v"(lane_o));
+    const int64_t bh2 = (int64_t)b * a.heads + hk * per_key_head + g;
+    const unsigned char* t = lds + buf * C::STAGE;
+    const unsigned char* qg = (const unsigned char*)a.q + 2 * bh2 * a.q_len * C::KRB;
+    copy_tile<C::KRB, QB, W>(t, qg, i, a.q_len - 1, w, lane_o);
+    copy_tile<C::KRB, QB, W>(t + C::KBYTES, qg + (int64_t)a.q_len * C::KRB, i, a.q_len - 1, w, lane_o);
+    copy_tile<C::VRB, QB, W>(t + 2 * C::KBYTES, (const unsigned char*)a.dout + bh2 * a.q_len * C::VRB, i, a.q_len - 1, w, lane_o);
+    // 4 QB statistics: QB / 16 copies of 64, wavefront w takes copies w, w + W, ...
+#pragma unroll
+    for (int c = w; c < QB / 16; c += W) {
+      const int at = c * 64 + lane_o;  // row at / QB of query i + at % QB
+      dma4(a.rows + bh2 * 4 * a.q_len, (uint32_t)(min(i + at % QB, a.q_len - 1) + at / QB * a.q_len) * 4,
+           (const unsigned char*)(stat[buf] + c * 64));
+    }
+  };
+  // 32 queries; q0: the query of this lane's first register
+  auto work = [&](const unsigned char* t, const unsigned char* to, const float* st, float lam, bool masked, int q0) {
+    uint32_t qr = q_row, orow = o_row, qc0 = q_col0, qc1 = q_col1, oc0 = o_col0, oc1 = o_col1, vr = v_row;
+    asm volatile("" : "+v"(qr), "+v"(orow), "+v"(qc0), "+v"(qc1), "+v"(oc0), "+v"(oc1), "+v"(vr));
+    auto row = [&](int x) {
+      const int y = x - 2 * C::KS;
+      return x < 2 * C::KS ? read_row(t + (x & 1) * C::KBYTES + row_step(qr, x >> 1)) : read_row(to + row_step(orow, y & 7) + (y >> 3) * 256);
     };
-    // The first tile may begin inside a mask block that the walk has not looked at.
-    int i = lo < hi ? (a.mask ? max(next_tile(lo & ~(a.block - 1)), lo) : lo) : hi, buf = 0;
-    WA_BARRIER();  // everyone is done with the tiles of the head before
-    if (i < hi) copy(i, 0);
-    while (i < hi) {
-      const int next = next_tile(i + QB);
-      WA_WAIT_VM(0);
-      WA_BARRIER();
-      if (next < hi) copy(next, buf ^ 1);
+    auto value = [&](int y) { return read_row(values + row_step(vr, y & 7) + (y >> 3) * 256); };
+    auto col = [&](int x) {  // of the products of 16 queries: dV's column tiles, then dK's of both maps
+      const int x16 = x / (C::VT + 2 * C::DT), y = x % (C::VT + 2 * C::DT);
+      if (y < C::VT) {
+        const unsigned char* at = to + 16 * x16 * C::VRB + (y >> 2) * 256;
+        return read_cols(at + col_step(oc0, y & 3), at + col_step(oc1, y & 3));
+      }
+      const int c = (y - C::VT) % C::DT;
+      const unsigned char* at = t + (y - C::VT) / C::DT * C::KBYTES + 16 * x16 * C::KRB;
+      return read_cols(at + col_step(qc0, c), at + col_step(qc1, c));
+    };
+    constexpr int ROWS = 2 * C::KS + C::VS, HALF = C::VT + 2 * C::DT;
+    f32x16 s[2], dp;
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[0][4 * q4 + e] = st[8 * q4 + e];
+        s[1][4 * q4 + e] = st[QB + 8 * q4 + e];
+        dp[4 * q4 + e] = st[2 * QB + 8 * q4 + e];
+      }
+    float p[2][16], pc[16];
+    bf16x8 ring[kAhead], vring[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) ring[x] = row(x);
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x) {
+      WA_SCHED_FENCE();
+      if (x < 2 * C::KS)
+        s[x & 1] = mfma(ring[x % kAhead], kf[x & 1][x >> 1], s[x & 1]);
+      else
+        dp = mfma(ring[x % kAhead], kValuesInLds ? vring[x % kAhead] : vf[kValuesInLds ? 0 : x - 2 * C::KS], dp);
+      if (x + kAhead < ROWS) {
+        ring[x % kAhead] = row(x + kAhead);
+        if (kValuesInLds && x + kAhead >= 2 * C::KS) vring[x % kAhead] = value(x + kAhead - 2 * C::KS);
+      }
+      if (x >= 2 * C::KS) {
+        constexpr int PER = 32 / C::VS;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          const int v = (x - 2 * C::KS) * PER + e;
+          p[v >> 4][v & 15] = __builtin_amdgcn_exp2f(s[v >> 4][v & 15] * c2);
+        }
+      }
+    }
+    float step[16];
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) step[4 * q4 + e] = st[3 * QB + 8 * q4 + e];
+    bf16x8 cring[kAheadCols];
+#pragma unroll
+    for (int x = 0; x < kAheadCols; ++x) cring[x] = col(x);
+    if (masked) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int q = q0 + 8 * (v >> 2) + (v & 3);
+        if (q < from || q >= a.q_len) p[0][v] = p[1][v] = 0.f;
+      }
+    }
+    auto weigh = [&](int v) {
+      const float p2 = -lam * p[1][v];
+      pc[v] = p[0][v] + p2;
+      p[0][v] *= dp[v];
+      p[1][v] = p2 * (dp[v] + step[v]);
+    };
+    bf16x8 w8[3];  // of 16 queries: P_1 - lam P_2, dS_1, dS_2
+#pragma unroll
+    for (int v = 0; v < 8; ++v) weigh(v);
+    w8[0] = pack8(pc);
+    w8[1] = pack8(p[0]);
+    w8[2] = pack8(p[1]);
+#pragma unroll
+    for (int x = 0; x < 2 * HALF; ++x) {
+      WA_SCHED_FENCE();
+      const int y = x % HALF;
+      if (x == HALF) w8[0] = pack8(pc + 8);
+      if (x == HALF + C::VT) w8[1] = pack8(p[0] + 8);
+      if (x == HALF + C::VT + C::DT) w8[2] = pack8(p[1] + 8);
+      if (y < C::VT)
+        dv[y] = mfma(cring[x % kAheadCols], w8[0], dv[y]);
+      else
+        dk[(y - C::VT) / C::DT][(y - C::VT) % C::DT] =
+            mfma(cring[x % kAheadCols], w8[1 + (y - C::VT) / C::DT], dk[(y - C::VT) / C::DT][(y - C::VT) % C::DT]);
+      if (x + kAheadCols < 2 * HALF) cring[x % kAheadCols] = col(x + kAheadCols);
+#pragma unroll
+      for (int v = 8; v < 16; ++v)  // the second 16 queries' beside the products of the first
+        if (x == (v - 8) * HALF / 8) weigh(v);
+    }
+    WA_SCHED_FENCE();
+  };
+  bool more = advance(0);
+  if (more) copy(0);
+  int buf = 0;
+  while (more) {
+    const int i0 = i;
+    const float lam = a.lam[hk * per_key_head + g];
+    more = advance(i0 + QB);
+    WA_WAIT_VM(0);
+    WA_BARRIER();
+    if (more) copy(buf ^ 1);
+    int end = QB;  // opaque: without a loop of its own, the work shares its registers with the next tile's addresses and spills
+    asm volatile("" : "+s"(end));
 #pragma unroll 1
-      for (int half = 0; half < QB; half += 32) {
-        const int i1 = i + half;
-        if (i1 + 32 <= some || i1 >= hi) continue;
-        const unsigned char* t = lds + buf * C::STAGE + half * C::KRB;
-        const unsigned char* to = lds + buf * C::STAGE + half * C::VRB;
-        f32x16 s[2], dp;
-        clear(s[0]);
-        clear(s[1]);
-        clear(dp);
-#pragma unroll
-        for (int x = 0; x < C::KS; ++x)
-#pragma unroll
-          for (int m = 0; m < 2; ++m) s[m] = mfma(read_row(t + m * C::KBYTES + qofs[x]), kf[m][x], s[m]);
-#pragma unroll
-        for (int x = 0; x < C::VS; ++x) dp = mfma(read_row(to + oofs[x & 7] + (x >> 3) * 256), vf[x], dp);
-        // register v holds query 8 (v / 4) + 4 hf + v % 4
-        const float* st = stat[buf] + half + 4 * hf;
-        float p[2][16], pc[16];
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const float4 l0 = *(const float4*)(st + 8 * q4), l1 = *(const float4*)(st + QB + 8 * q4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = 4 * q4 + e;
-            p[0][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][v], c2, -(&l0.x)[e]));
-            p[1][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][v], c2, -(&l1.x)[e]));
-          }
-        }
-        if (!whole || i1 < all || i1 + 32 > hi) {
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int q = i1 + 8 * (v >> 2) + 4 * hf + (v & 3);
-            if (q < from || q >= hi) p[0][v] = p[1][v] = 0.f;
-          }
-        }
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const float4 d0 = *(const float4*)(st + 2 * QB + 8 * q4), d1 = *(const float4*)(st + 3 * QB + 8 * q4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = 4 * q4 + e;
-            const float p2 = -lam * p[1][v];
-            pc[v] = p[0][v] + p2;
-            p[0][v] *= dp[v] - (&d0.x)[e];
-            p[1][v] = p2 * (dp[v] - (&d1.x)[e]);
-          }
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const bf16x8 pb = pack8(pc + 8 * x);
-          const unsigned char* tc = to + 16 * x * C::VRB;
-#pragma unroll
-          for (int c = 0; c < C::VT; ++c)
-            dv[c] = mfma(read_cols(tc + ocol[0][c & 3] + (c >> 2) * 256, tc + ocol[1][c & 3] + (c >> 2) * 256), pb, dv[c]);
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const bf16x8 ds = pack8(p[m] + 8 * x);
-            const unsigned char* tq = t + m * C::KBYTES + 16 * x * C::KRB;
-#pragma unroll
-            for (int c = 0; c < C::DT; ++c) dk[m][c] = mfma(read_cols(tq + qcol[0][c], tq + qcol[1][c]), ds, dk[m][c]);
-          }
-        }
-      }
-      i = next;
-      buf ^= 1;
+    for (int half = 0; half < end; half += 32) {
+      const int i1 = i0 + half;
+      if (i1 + 32 <= some || i1 >= a.q_len) continue;
+      const unsigned char* t = lds + buf * C::STAGE + half * C::KRB;
+      const unsigned char* to = lds + buf * C::STAGE + half * C::VRB;
+      const float* st = stat[buf] + half + 4 * hf;
+      work(t, to, st, lam, !whole || i1 < all || i1 + 32 > a.q_len, i1 + 4 * hf);
     }
+    buf ^= 1;
   }
-  if (kj < a.kv_len) {  // keys that the sequence does not hold get 0
+  if (n.parts > 1) {
+    float* to = a.part + (((int64_t)item * n.parts + part) * 32 * W + w * 32 + l32) * (2 * D + DV);
+    store_part(to, dk[0], a.scale, hf);
+    store_part(to + D, dk[1], a.scale, hf);
+    store_part(to + 2 * D, dv, 1.f, hf);
+  } else if (kj < a.kv_len) {  // keys that the sequence does not hold get 0
     store_row((uint16_t*)a.dk + krow0 * D, dk[0], a.scale, hf);
     store_row((uint16_t*)a.dk + (krow0 + a.kv_len) * D, dk[1], a.scale, hf);
     store_row((uint16_t*)a.dv + vrow * DV, dv, 1.f, hf);
   }
 }
 
-int waves_of(const WaDiffLaunch& a, int len) { return len <= 64 || (a.mask && a.block == 64) ? 2 : 4; }
+// Adds the parts' results in order and rounds: a thread four columns of a row (2 D of both maps, then DV).
+__global__ __launch_bounds__(256) void diff_parts_kernel(const float* part, uint16_t* maps, uint16_t* values, int64_t rows, int len,
+                                                         int tile_rows, int tiles, int parts, int d, int dv) {
+  const int width = 2 * d + dv, quads = width / 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / quads;
+  if (row >= rows) return;
+  const int c = (int)(id % quads) * 4;
+  const int64_t unit = row / len;
+  const int i = row % len;
+  const float* at = part + ((unit * tiles + i / tile_rows) * parts * tile_rows + i % tile_rows) * width + c;
+  float4 sum = *(const float4*)at;
+#pragma unroll 4
+  for (int x = 1; x < parts; ++x) {
+    const float4 y = *(const float4*)(at + (int64_t)x * tile_rows * width);
+    sum.x += y.x;
+    sum.y += y.y;
+    sum.z += y.z;
+    sum.w += y.w;
+  }
+  uint16_t* out = c < 2 * d ? maps + ((unit * 2 + c / d) * len + i) * d + c % d : values + row * dv + c - 2 * d;
+  *(uint2*)out = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
+}
 
-template <int D, int DV, int W>
-hipError_t launch_dq(const WaDiffLaunch& a, hipStream_t stream) {
-  const int tiles = (a.q_len + 32 * W - 1) / (32 * W);
-  hipLaunchKernelGGL((diff_dq_kernel<D, DV, W>), dim3((unsigned)(a.batch * a.heads * tiles)), dim3(64 * W), 0, stream, a, tiles);
+hipError_t launch_parts(const WaDiffLaunch& a, const WaDiffSide& n, void* maps, void* values, int64_t rows, int len, int dv,
+                        hipStream_t stream) {
+  const int64_t threads = rows * ((2 * a.head_dim + dv) / 4);
+  hipLaunchKernelGGL(diff_parts_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a.part, (uint16_t*)maps,
+                     (uint16_t*)values, rows, len, 32 * n.waves, n.tiles, n.parts, a.head_dim, dv);
   return hipGetLastError();
 }
-template <int D, int DV, int W>
-hipError_t launch_dkv(const WaDiffLaunch& a, int q_tiles, hipStream_t stream) {
-  const int tiles = (a.kv_len + 32 * W - 1) / (32 * W);
-  hipLaunchKernelGGL((diff_dkv_kernel<D, DV, W>), dim3((unsigned)(a.batch * a.kv_heads * tiles)), dim3(64 * W), 0, stream, a, tiles,
-                     q_tiles);
-  return hipGetLastError();
-}
+
 template <int D, int DV>
-hipError_t launch_dims(const WaDiffLaunch& a, hipStream_t stream) {
-  const int wq = waves_of(a, a.q_len), wk = waves_of(a, a.kv_len), q_tiles = (a.q_len + 32 * wq - 1) / (32 * wq);
-  const hipError_t e = wq == 2 ? launch_dq<D, DV, 2>(a, stream) : launch_dq<D, DV, 4>(a, stream);
-  if (e != hipSuccess) return e;
-  return wk == 2 ? launch_dkv<D, DV, 2>(a, q_tiles, stream) : launch_dkv<D, DV, 4>(a, q_tiles, stream);
+hipError_t launch_dims(WaDiffLaunch a, hipStream_t stream) {
+  const WaDiffSide q = wa_diff_dq_side(a, a.mask), k = wa_diff_dkv_side(a, a.mask);
+  int32_t* const order = a.order;
+  hipError_t e = hipSuccess;
+  a.order = a.mask && wa_diff_ordered(q.items) ? order : nullptr;
+  if (a.order && (e = wa_launch_diff_order(a, false, stream)) != hipSuccess) return e;
+  const dim3 gq((unsigned)(q.items * q.parts)), tq(64 * q.waves);
+  if (q.waves == 2)
+    hipLaunchKernelGGL((diff_dq_kernel<D, DV, 2>), gq, tq, 0, stream, a, q);
+  else
+    hipLaunchKernelGGL((diff_dq_kernel<D, DV, 4>), gq, tq, 0, stream, a, q);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (q.parts > 1 && (e = launch_parts(a, q, a.dq, nullptr, (int64_t)a.batch * a.heads * a.q_len, a.q_len, 0, stream)) != hipSuccess)
+    return e;
+
+  a.order = a.mask && wa_diff_ordered(k.items) ? order : nullptr;
+  if (a.order && (e = wa_launch_diff_order(a, true, stream)) != hipSuccess) return e;
+  const dim3 gk((unsigned)(k.items * k.parts)), tk(64 * k.waves);
+  if (k.waves == 2)
+    hipLaunchKernelGGL((diff_dkv_kernel<D, DV, 2>), gk, tk, 0, stream, a, k, q.tiles * q.parts);
+  else
+    hipLaunchKernelGGL((diff_dkv_kernel<D, DV, 4>), gk, tk, 0, stream, a, k, q.tiles * q.parts);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (k.parts > 1) e = launch_parts(a, k, a.dk, a.dv, (int64_t)a.batch * a.kv_heads * a.kv_len, a.kv_len, DV, stream);
+  return e;
+}
+
+// Tiles of 128 tokens, or 64 where a mask block or the sequence is no longer. A call of few tiles does each in parts, so many
+// as fill the chip's workgroups (those of one wavefront a SIMD: 256 of four, 512 of two) once; twice where the tiles are of
+// different lengths. A part is 4 tiles of 64 of the other side at least, and its float32 result is written and read once more.
+WaDiffSide side_of(const WaDiffLaunch& a, bool masked, int len, int units, int64_t other) {
+  WaDiffSide s;
+  s.waves = len <= 64 || (masked && a.block == 64) ? 2 : 4;
+  s.tiles = (len + 32 * s.waves - 1) / (32 * s.waves);
+  s.items = (int64_t)units * s.tiles;
+  const int64_t slots = (s.waves == 2 ? 512 : 256) * (a.causal || masked ? 2 : 1);
+  s.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(slots / s.items, other / 256));
+  return s;
 }
 
 }  // namespace
+
+WaDiffSide wa_diff_dq_side(const WaDiffLaunch& a, bool masked) { return side_of(a, masked, a.q_len, a.batch * a.heads, a.kv_len); }
+WaDiffSide wa_diff_dkv_side(const WaDiffLaunch& a, bool masked) {
+  return side_of(a, masked, a.kv_len, a.batch * a.kv_heads, (int64_t)(a.heads / a.kv_heads) * a.q_len);
+}
+size_t wa_diff_dq_floats(const WaDiffLaunch& a, const WaDiffSide& s) {
+  return s.parts == 1 ? 0 : (size_t)s.items * s.parts * 32 * s.waves * 2 * a.head_dim;
+}
+size_t wa_diff_dkv_floats(const WaDiffLaunch& a, const WaDiffSide& s) {
+  return s.parts == 1 ? 0 : (size_t)s.items * s.parts * 32 * s.waves * (2 * a.head_dim + a.value_dim);
+}
 
 hipError_t wa_launch_diff_backward(const WaDiffLaunch& a, hipStream_t stream) {
   if (a.head_dim == 64 && a.value_dim == 64) return launch_dims<64, 64>(a, stream);

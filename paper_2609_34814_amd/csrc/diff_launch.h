@@ -15,7 +15,8 @@ struct WaDiffLaunch {
   void* o;            // bf16 [batch][heads][q_len][value_dim]
   int16_t* maps;      // [batch][2 heads][q_len][value_dim]: P_m V in steps of its row's, nullable
   float* stats;       // [batch][2 heads][q_len][3]: log-sum-exp, step, correction (diff_tiles.h), with maps
-  float* part;        // split calls: partial tiles, then their statistics
+  int32_t* order;     // workspace of masked calls: work items by falling length, then their lengths
+  float* part;        // workspace of split calls: partial tiles, then (forward) their statistics
   int32_t batch, heads, kv_heads, q_len, kv_len, head_dim, value_dim, block, mb, nb, causal;
   float scale;
   // backward
@@ -24,8 +25,8 @@ struct WaDiffLaunch {
   void* dk;
   void* dv;
   float* dlam;        // [heads]
-  float* rows;        // workspace: [2][batch][2 heads][q_len]: log-sum-exps in log2 units, then dO . O_m
-  double* lam_part;   // workspace: [batch][heads][tiles of q_len] partial sums for dlam
+  float* rows;        // workspace: [batch][heads][4][q_len]: what the products of a query start from (diff_bwd.hip)
+  double* lam_part;   // workspace: [batch][heads][tiles of q_len][parts] partial sums for dlam
 };
 
 // How a forward call is cut into workgroups (see diff_plan in diff_attn.hip).
@@ -39,6 +40,26 @@ struct WaDiffPlan {
 };
 WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked);
 size_t wa_diff_part_floats(const WaDiffPlan& p, int value_dim);
+
+// Tiles of masked calls run longest first where there are this many of them: fewer all run at once; with more, a long one
+// that starts late is short next to the call, and running heads one after another keeps their keys in the caches.
+constexpr int kDiffOrderMin = 257, kDiffOrderMax = 8192;
+inline bool wa_diff_ordered(int64_t items) { return items >= kDiffOrderMin && items <= kDiffOrderMax; }
+inline size_t wa_diff_order_ints(int64_t items) { return wa_diff_ordered(items) ? 2 * (size_t)items : 0; }
+// Fills a.order for the rows of the mask, or for its columns summed over the heads of a key head (entry t of a unit u of n
+// is item u n + t).
+hipError_t wa_launch_diff_order(const WaDiffLaunch& a, bool columns, hipStream_t stream);
+
+// How the gradient is cut: tiles of 32 * waves queries (keys), each tile's keys (queries of all heads) in so many parts.
+struct WaDiffSide {
+  int32_t waves, tiles, parts;
+  int64_t items;  // tiles of all units
+};
+WaDiffSide wa_diff_dq_side(const WaDiffLaunch& a, bool masked);
+WaDiffSide wa_diff_dkv_side(const WaDiffLaunch& a, bool masked);
+// float32 of the parts' results, 0 where there is one
+size_t wa_diff_dq_floats(const WaDiffLaunch& a, const WaDiffSide& s);
+size_t wa_diff_dkv_floats(const WaDiffLaunch& a, const WaDiffSide& s);
 
 hipError_t wa_launch_diff_attn(const WaDiffLaunch& a, hipStream_t stream);
 hipError_t wa_launch_diff_backward(const WaDiffLaunch& a, hipStream_t stream);

@@ -41,6 +41,11 @@ __device__ __forceinline__ uint32_t col_operand(int lane, int c, int j) {
   return row * RB + tile_chunk<RB>(row, 4 * c + 2 * (g & 1) + (i >> 1 & 1)) * 16 + (i & 1) * 8;
 }
 
+// The same offsets of k-step s (below 8) and of column tile c (below 4) from those of the first: the swizzle is an exclusive or of
+// the chunk's bits, so the step is too.
+__device__ __forceinline__ uint32_t row_step(uint32_t first, int s) { return first ^ 32 * s; }
+__device__ __forceinline__ uint32_t col_step(uint32_t first, int c) { return first ^ 64 * c; }
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
