@@ -28,7 +28,7 @@ using namespace wa;
 
 constexpr float kGrow = 8.f;  // log2 units
 constexpr int kAheadRows = 4, kAheadCols = 4;  // operands read ahead
-constexpr int kMaxSplits = 128;
+constexpr int kMaxSplits = 128, kFewSplits = 4;
 
 template <int D, int DV, int W>
 struct Fwd {
@@ -56,16 +56,11 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
 
   // Work item: the key range fastest, then the units of a group in turn, tile after tile; longest tiles first where
   // later queries see more keys.
-  int id = a.order ? a.order[blockIdx.x] : blockIdx.x;
-  const int chunk = id % p.splits;
-  id /= p.splits;
-  const int item = id;
-  const int first = id / (p.tiles * p.group) * p.group;  // unit
-  id -= first * p.tiles;
-  const int count = min(p.group, p.units - first);
-  const int unit = first + id % count;
-  int tile = id / count;
+  const int chunk = blockIdx.x % p.splits;
+  int unit, tile;
+  deal(a, blockIdx.x / p.splits, p.tiles, p.units, &unit, &tile);
   if (a.causal && !a.order) tile = p.tiles - 1 - tile;
+  const int64_t item = (int64_t)unit * p.tiles + tile;
   const int per_key_head = a.heads / a.kv_heads;
   const int heads = p.packed ? a.kv_heads : a.heads;
   const int b = unit / heads;
@@ -232,7 +227,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   const float l = add_halves(l_run);
   if (p.splits > 1) {
     if (!valid) return;
-    const int64_t n = (int64_t)item * p.splits + chunk, rows = 32 * W;
+    const int64_t n = item * p.splits + chunk, rows = 32 * W;
     const int64_t at = (n * 2 + map) * rows + slice * 32 + l32;
     float* out = a.part + at * DV;
 #pragma unroll
@@ -299,95 +294,149 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
     }
 }
 
-// Joins the key ranges of split tiles, in a fixed order: R wavefronts a query row, each the ranges of its number modulo R,
-// DV / 64 columns a lane. R is 4 where a row has eight ranges and more, else 1 (16 x 16 rows of 8 ranges of 128 columns: 6.1 us
-// with 1, 4.7 with 4).
-template <int DV, int R>
-__global__ __launch_bounds__(256) void diff_join_kernel(const WaDiffLaunch a, const WaDiffPlan p) {
-  constexpr int E = DV / 64;
-  typedef float cols __attribute__((ext_vector_type(E)));
-  __shared__ float weight[4][2][kMaxSplits];
-  __shared__ cols sums[4][2][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t r = (int64_t)blockIdx.x * (4 / R) + w / R;
-  const bool valid = r < (int64_t)a.batch * a.heads * a.q_len;
-  const int i = r % a.q_len;
-  const int bh = valid ? r / a.q_len : 0, b = bh / a.heads, h = bh % a.heads;
-  const int per_key_head = a.heads / a.kv_heads;
-  const int unit = p.packed ? b * a.kv_heads + h / per_key_head : bh;
-  const int row = p.packed ? h % per_key_head * a.q_len + i : i;
-  const int rows = 32 * p.waves, tile = row / rows;
-  // the tile's place in the order of the work items
-  const int first = unit / p.group * p.group, count = min(p.group, p.units - first);
-  const int64_t item = (int64_t)first * p.tiles + (int64_t)(a.causal ? p.tiles - 1 - tile : tile) * count + unit - first;
-  const float2* stat = (const float2*)(a.part + (int64_t)p.units * p.tiles * p.splits * 2 * rows * DV);
-  auto at = [&](int c, int m) { return ((item * p.splits + c) * 2 + m) * rows + row % rows; };
-  float top[2], l[2];
-  cols o[2];
+// The end of a row whose maps are whole: cols holds both maps' `E` columns from c on. top, l: of both maps; big: the
+// largest of the row's columns on every lane.
+template <int E, typename COLS>
+__device__ __forceinline__ void finish_row(const WaDiffLaunch& a, const COLS (&o)[2], const float (&top)[2], const float (&l)[2],
+                                           const float (&big)[2], int64_t bh, int i, int c, bool first) {
+  const int dv = a.value_dim;
+  if (a.maps) {
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    // a range a lane (kMaxSplits is at most twice 64)
-    float2 s[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int c = lane + 64 * x;
-      s[x] = valid && c < p.splits ? stat[at(c, m)] : make_float2(-INFINITY, 0.f);
-    }
-    top[m] = fmaxf(s[0].x, s[1].x);
-    for (int x = 32; x > 0; x >>= 1) top[m] = fmaxf(top[m], __shfl_xor(top[m], x));
-    l[m] = 0.f;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float f = s[x].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[x].x - top[m]);
-      if (lane + 64 * x < p.splits) weight[w][m][lane + 64 * x] = f;
-      l[m] += f * s[x].y;
-    }
-    for (int x = 32; x > 0; x >>= 1) l[m] += __shfl_xor(l[m], x);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[m][e] = 0.f;
-  }
-  __syncthreads();
-  if (valid) {
-#pragma unroll 4
-    for (int c = w % R; c < p.splits; c += R)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) o[m] += *(const cols*)(a.part + at(c, m) * DV + lane * E) * weight[w][m][c];
-  }
-  if constexpr (R > 1) {
-#pragma unroll
-    for (int m = 0; m < 2; ++m) sums[w][m][lane] = o[m];
-    __syncthreads();
-    if (w % R) return;
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int x = 1; x < R; ++x) o[m] += sums[w + x][m][lane];
-  }
-  if (!valid) return;
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    o[m] *= l[m] > 0.f ? 1.f / l[m] : l[m] == 0.f ? 0.f : NAN;
-    if (a.maps) {
-      float big = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) big = fmaxf(big, fabsf(o[m][e]));
-      for (int x = 32; x > 0; x >>= 1) big = fmaxf(big, __shfl_xor(big, x));
-      const RowStats s = row_stats(top[m], l[m], big);
+    for (int m = 0; m < 2; ++m) {
+      const RowStats s = row_stats(top[m], l[m], big[m]);
       const float per_step = s.step > 0.f ? 1.f / s.step : 0.f;
-      const int64_t to = ((int64_t)b * 2 * a.heads + 2 * h + m) * a.q_len + i;
+      const int64_t to = (2 * bh + m) * a.q_len + i;
 #pragma unroll
-      for (int e = 0; e < E; ++e) a.maps[to * DV + lane * E + e] = (int16_t)rintf(o[m][e] * per_step);
-      if (lane == 0) {
+      for (int e = 0; e < E; ++e) a.maps[to * dv + c + e] = (int16_t)rintf(o[m][e] * per_step);
+      if (first) {
         a.stats[3 * to] = s.lse;
         a.stats[3 * to + 1] = s.step;
         a.stats[3 * to + 2] = s.factor;
       }
     }
   }
-  const float lam = a.lam[h];
-  __bf16* out = (__bf16*)a.o + r * DV + lane * E;
+  const float lam = a.lam[bh % a.heads];
+  __bf16* out = (__bf16*)a.o + (bh * a.q_len + i) * dv + c;
 #pragma unroll
   for (int e = 0; e < E; ++e) out[e] = (__bf16)(o[0][e] - lam * o[1][e]);
+}
+
+// Where a row's partial results lie: range c of map m at at + (2 c + m) rows, in rows of DV floats (or one float2 of
+// statistics).
+struct PartRow {
+  int64_t bh, at;
+  int i, rows;
+  const float2* stat;
+  __device__ __forceinline__ PartRow(const WaDiffLaunch& a, const WaDiffPlan& p, int64_t r, int dv) {
+    i = r % a.q_len;
+    bh = r / a.q_len;
+    const int per_key_head = a.heads / a.kv_heads, h = bh % a.heads;
+    const int64_t unit = p.packed ? bh / a.heads * a.kv_heads + h / per_key_head : bh;
+    const int row = p.packed ? h % per_key_head * a.q_len + i : i;
+    rows = 32 * p.waves;
+    at = (unit * p.tiles + row / rows) * p.splits * 2 * rows + row % rows;
+    stat = (const float2*)(a.part + (int64_t)p.units * p.tiles * p.splits * 2 * rows * dv);
+  }
+};
+
+// Joins the key ranges of split tiles, in a fixed order. Few ranges: four columns a lane, DV / 4 lanes a row, every lane with the
+// row's weights.
+template <int DV>
+__global__ __launch_bounds__(256) void diff_join_few_kernel(const WaDiffLaunch a, const WaDiffPlan p) {
+  typedef float cols __attribute__((ext_vector_type(4)));
+  constexpr int L = DV / 4;
+  const int64_t r = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  if (r >= (int64_t)a.batch * a.heads * a.q_len) return;
+  const int lane = threadIdx.x % L;
+  const PartRow row(a, p, r, DV);
+  cols o[2];
+  float top[2], l[2], big[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    float2 s[kFewSplits];
+    cols x[kFewSplits];
+#pragma unroll
+    for (int c = 0; c < kFewSplits; ++c) {  // past the last range the last again, without weight
+      const int64_t at = row.at + (2 * min(c, p.splits - 1) + m) * row.rows;
+      s[c] = row.stat[at];
+      x[c] = *(const cols*)(a.part + at * DV + 4 * lane);
+    }
+    top[m] = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < kFewSplits; ++c) top[m] = fmaxf(top[m], s[c].x);
+    l[m] = 0.f;
+    o[m] = 0.f;
+#pragma unroll
+    for (int c = 0; c < kFewSplits; ++c) {
+      if (c < p.splits) {
+        const float f = s[c].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[c].x - top[m]);
+        l[m] += f * s[c].y;
+        o[m] += x[c] * f;
+      }
+    }
+    o[m] *= l[m] > 0.f ? 1.f / l[m] : l[m] == 0.f ? 0.f : NAN;
+    big[m] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) big[m] = fmaxf(big[m], fabsf(o[m][e]));
+    if (a.maps)
+      for (int y = L / 2; y > 0; y >>= 1) big[m] = fmaxf(big[m], __shfl_xor(big[m], y));
+  }
+  finish_row<4>(a, o, top, l, big, row.bh, row.i, 4 * lane, lane == 0);
+}
+
+// Many ranges: a workgroup of R wavefronts a row, each taking every R-th range, DV / 64 columns a lane. 4 wavefronts, or 16 where
+// there are more than 16 ranges (8 rows of 64 ranges of 256 columns: 8.7 us with 4, 7.9 with 16).
+template <int DV, int R>
+__global__ __launch_bounds__(64 * R) void diff_join_many_kernel(const WaDiffLaunch a, const WaDiffPlan p) {
+  constexpr int E = DV / 64;
+  typedef float cols __attribute__((ext_vector_type(E)));
+  __shared__ float weight[2][kMaxSplits];
+  __shared__ cols sums[R][2][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const PartRow row(a, p, blockIdx.x, DV);
+  float top[2], l[2], big[2];
+  cols o[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    float2 s[kMaxSplits / 64];  // a range a lane
+    top[m] = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < kMaxSplits / 64; ++x) {
+      const int c = lane + 64 * x;
+      s[x] = c < p.splits ? row.stat[row.at + (2 * c + m) * row.rows] : make_float2(-INFINITY, 0.f);
+      top[m] = fmaxf(top[m], s[x].x);
+    }
+    for (int x = 32; x > 0; x >>= 1) top[m] = fmaxf(top[m], __shfl_xor(top[m], x));
+    l[m] = 0.f;
+#pragma unroll
+    for (int x = 0; x < kMaxSplits / 64; ++x) {
+      const float f = s[x].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[x].x - top[m]);
+      if (w == 0 && lane + 64 * x < p.splits) weight[m][lane + 64 * x] = f;
+      l[m] += f * s[x].y;
+    }
+    for (int x = 32; x > 0; x >>= 1) l[m] += __shfl_xor(l[m], x);
+    o[m] = 0.f;
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int c = w; c < p.splits; c += R)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) o[m] += *(const cols*)(a.part + (row.at + (2 * c + m) * row.rows) * DV + lane * E) * weight[m][c];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) sums[w][m][lane] = o[m];
+  __syncthreads();
+  if (w) return;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    for (int x = 1; x < R; ++x) o[m] += sums[x][m][lane];
+    o[m] *= l[m] > 0.f ? 1.f / l[m] : l[m] == 0.f ? 0.f : NAN;
+    big[m] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) big[m] = fmaxf(big[m], fabsf(o[m][e]));
+    if (a.maps)
+      for (int x = 32; x > 0; x >>= 1) big[m] = fmaxf(big[m], __shfl_xor(big[m], x));
+  }
+  finish_row<E>(a, o, top, l, big, row.bh, row.i, lane * E, lane == 0);
 }
 
 template <int D, int DV>
@@ -407,10 +456,14 @@ hipError_t launch_dims(WaDiffLaunch a, const WaDiffPlan& p, hipStream_t stream) 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t rows = (int64_t)a.batch * a.heads * a.q_len;
-  if (p.splits >= 8)
-    hipLaunchKernelGGL((diff_join_kernel<DV, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a, p);
-  else
-    hipLaunchKernelGGL((diff_join_kernel<DV, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, p);
+  if (p.splits > 16) {
+    hipLaunchKernelGGL((diff_join_many_kernel<DV, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, a, p);
+  } else if (p.splits > kFewSplits) {
+    hipLaunchKernelGGL((diff_join_many_kernel<DV, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a, p);
+  } else {
+    constexpr int PER = 256 / (DV / 4);
+    hipLaunchKernelGGL(diff_join_few_kernel<DV>, dim3((unsigned)((rows + PER - 1) / PER)), dim3(256), 0, stream, a, p);
+  }
   return hipGetLastError();
 }
 
@@ -429,8 +482,6 @@ WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked) {
   // 256 keys at least.
   const int64_t slots = p.waves == 4 ? 256 : 512, items = (int64_t)p.units * p.tiles;
   p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / items, kMaxSplits), a.kv_len / 256));
-  // Heads of a mask one after another, so that one head's keys are in the caches; dense ones eight together, one an XCD.
-  p.group = masked ? 1 : 8;
   return p;
 }
 

@@ -30,12 +30,23 @@ struct Bwd {
   static constexpr int KBYTES = TB * KRB, VBYTES = TB * VRB, STAGE = 2 * KBYTES + VBYTES;
   static constexpr int DT = D / 32, VT = DV / 32, KS = D / 16, VS = DV / 16;
 };
-constexpr int kAhead = 6, kAheadCols = 4;  // operands read ahead: rows, columns
+// Operands read ahead of their products, and a fence that keeps the order of the code where a wavefront has its SIMD to itself: the
+// scheduler would sink each read to its product. With two wavefronts a SIMD the one hides the other's waits, and registers
+// of operands in flight would spill (dK and dV of 2 x 14 heads of 4,096 tokens, d 64, values 128: 646 us with 2, 723 with 3,
+// 996 with 4; 788 with one wavefront a SIMD).
+template <int WAVES>
+constexpr int kAheadRows = WAVES == 1 ? 6 : 2;
+template <int WAVES>
+constexpr int kAheadCols = WAVES == 1 ? 4 : 2;
+template <int WAVES>
+__device__ __forceinline__ void in_order() {
+  if constexpr (WAVES == 1) WA_SCHED_FENCE();
+}
 // Wavefronts a SIMD: two share its 512 registers a lane where both hold their accumulators.
 template <int D>
 constexpr int kDqWaves = D == 64 ? 2 : 1;
-template <int DV>
-constexpr int kDkvWaves = DV == 64 ? 2 : 1;
+template <int D>
+constexpr int kDkvWaves = D == 64 ? 2 : 1;
 
 __device__ __forceinline__ void fill(f32x16& x, float f) {
 #pragma unroll
@@ -84,18 +95,18 @@ __device__ __forceinline__ void store_part(float* out, const f32x16 (&acc)[T], f
 template <int D, int DV, int W>
 __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDiffLaunch a, const WaDiffSide n) {
   using C = Bwd<D, DV, W>;
-  constexpr int KB = C::TB;
+  constexpr int KB = C::TB, AHEAD = kAheadRows<kDqWaves<D>>, CAHEAD = kAheadCols<kDqWaves<D>>;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE];
   __shared__ double lam_sum[W];
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // The parts of a tile together; the longest tiles of all heads first where later queries see more keys, else head
-  // after head, or as the order says.
-  const int part = blockIdx.x % n.parts, turn = blockIdx.x / n.parts;
-  const int item = a.order ? a.order[turn] : a.causal ? turn % (a.batch * a.heads) * n.tiles + n.tiles - 1 - turn / (a.batch * a.heads) : turn;
-  const int bh = item / n.tiles, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
-  const int tile = item % n.tiles;
+  // The parts of a tile together; the longest tiles first where later queries see more keys.
+  const int part = blockIdx.x % n.parts;
+  int bh, tile;
+  deal(a, blockIdx.x / n.parts, n.tiles, a.batch * a.heads, &bh, &tile);
+  if (a.causal && !a.order) tile = n.tiles - 1 - tile;
+  const int item = bh * n.tiles + tile, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
   const int i0 = tile * 32 * W + w * 32, i = i0 + l32, i_last = a.q_len - 1;
   const bool valid = i <= i_last;
   const int keys = keys_of(a, b), start = start_of(a, b);
@@ -149,27 +160,26 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
       d[m] = dot8(dof[s], u, d[m]);
     }
   }
-  // The products start from what is subtracted from them: scores from the log-sum-exp, so P_m = exp2(c2 s), and dP from D_1;
-  // with D_1 - D_2 they are all that diff_dkv_kernel needs of a row.
+  // For the side of the keys: what its products start from, scores from the log-sum-exp, so that P_m = exp2(c2 s), and dP from
+  // -D_1; and D_1 - D_2.
   const float c2 = a.scale * kLog2e;
-  float from[2] = {0.f, 0.f}, factor = 1.f;
+  float ref[2] = {0.f, 0.f}, factor = 1.f;  // ref: log-sum-exp in log2 units
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     d[m] = add_halves(d[m]);
     if (valid) {
       const float* st = a.stats + 3 * (row0 + (int64_t)m * a.q_len);
-      from[m] = -st[0] * kLog2e / c2;
+      ref[m] = st[0] * kLog2e;
       d[m] *= st[1];
       factor = st[2];  // of the second map, in the end
     }
   }
-  const float step = d[0] - d[1];
   if (valid && hf == 0 && part == 0) {
     float* to = a.rows + (int64_t)bh * 4 * a.q_len + i;
-    to[0] = from[0];
-    to[a.q_len] = from[1];
+    to[0] = -ref[0] / c2;
+    to[a.q_len] = -ref[1] / c2;
     to[2 * (int64_t)a.q_len] = -d[0];
-    to[3 * (int64_t)a.q_len] = step;
+    to[3 * (int64_t)a.q_len] = d[0] - d[1];
   }
   const float lam = a.lam[h];
 
@@ -198,33 +208,33 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     };
     constexpr int ROWS = 2 * C::KS + C::VS, COLS = 4 * C::DT;
     f32x16 s[2], dp;
-    fill(s[0], from[0]);
-    fill(s[1], from[1]);
-    fill(dp, -d[0]);
+    fill(s[0], 0.f);
+    fill(s[1], 0.f);
+    fill(dp, 0.f);
     float p[2][16];
-    bf16x8 ring[kAhead];
+    bf16x8 ring[AHEAD];
 #pragma unroll
-    for (int x = 0; x < kAhead; ++x) ring[x] = row(x);
+    for (int x = 0; x < AHEAD; ++x) ring[x] = row(x);
 #pragma unroll
     for (int x = 0; x < ROWS; ++x) {
-      WA_SCHED_FENCE();
+      in_order<kDqWaves<D>>();
       if (x < 2 * C::KS)
-        s[x & 1] = mfma(ring[x % kAhead], qf[x & 1][x >> 1], s[x & 1]);
+        s[x & 1] = mfma(ring[x % AHEAD], qf[x & 1][x >> 1], s[x & 1]);
       else
-        dp = mfma(ring[x % kAhead], dof[x - 2 * C::KS], dp);
-      if (x + kAhead < ROWS) ring[x % kAhead] = row(x + kAhead);
+        dp = mfma(ring[x % AHEAD], dof[x - 2 * C::KS], dp);
+      if (x + AHEAD < ROWS) ring[x % AHEAD] = row(x + AHEAD);
       if (x >= 2 * C::KS) {  // the exponentials run beside the products of dP
         constexpr int PER = 32 / C::VS;
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
           const int v = (x - 2 * C::KS) * PER + e;
-          p[v >> 4][v & 15] = __builtin_amdgcn_exp2f(s[v >> 4][v & 15] * c2);
+          p[v >> 4][v & 15] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v >> 4][v & 15], c2, -ref[v >> 4]));
         }
       }
     }
-    bf16x8 cring[kAheadCols];
+    bf16x8 cring[CAHEAD];
 #pragma unroll
-    for (int x = 0; x < kAheadCols; ++x) cring[x] = col(x);
+    for (int x = 0; x < CAHEAD; ++x) cring[x] = col(x);
     if (masked) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
@@ -232,7 +242,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     }
     float dot = 0.f;
     auto dscore = [&](int m, int v) {
-      p[m][v] *= m ? dp[v] + step : dp[v];
+      p[m][v] *= dp[v] - d[m];
       if (m) dot += p[m][v];
     };
     bf16x8 ds[2];
@@ -244,12 +254,12 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     ds[1] = pack8(p[1]);
 #pragma unroll
     for (int x = 0; x < COLS; ++x) {
-      WA_SCHED_FENCE();
+      in_order<kDqWaves<D>>();
       const int m = x / C::DT & 1;
       if (x == 2 * C::DT) ds[0] = pack8(p[0] + 8);
       if (x == 3 * C::DT) ds[1] = pack8(p[1] + 8);
-      dq[m][x % C::DT] = mfma(cring[x % kAheadCols], ds[m], dq[m][x % C::DT]);
-      if (x + kAheadCols < COLS) cring[x % kAheadCols] = col(x + kAheadCols);
+      dq[m][x % C::DT] = mfma(cring[x % CAHEAD], ds[m], dq[m][x % C::DT]);
+      if (x + CAHEAD < COLS) cring[x % CAHEAD] = col(x + CAHEAD);
       if (x < 2 * C::DT) {  // dS of the second 16 keys beside the products of the first
         constexpr int PER = 16 / (2 * C::DT);
 #pragma unroll
@@ -259,7 +269,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
         }
       }
     }
-    WA_SCHED_FENCE();
+    in_order<kDqWaves<D>>();
     const float add = dot - lam_lost, grown = lam_dot + add;
     lam_lost = (grown - lam_dot) - add;
     lam_dot = grown;
@@ -317,11 +327,12 @@ __device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, const uns
 }
 
 template <int D, int DV, int W>
-__global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const WaDiffLaunch a, const WaDiffSide n, int lam_parts) {
-  // Values of 256 columns lie in LDS, where four wavefronts leave the room: with the keys and the sums of dK and dV, they
-  // do not fit 512 registers.
-  constexpr bool kValuesInLds = DV == 256 && W == 4;
+__global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const WaDiffLaunch a, const WaDiffSide n, int lam_parts) {
+  // Values lie in LDS where, with the keys and the sums of dK and dV, they do not fit the registers: twice the keys' columns, unless
+  // 256 of them leave two wavefronts a workgroup too little LDS.
+  constexpr bool kValuesInLds = DV == 2 * D && (DV == 128 || W == 4);
   using C = Bwd<D, DV, W, kValuesInLds>;
+  constexpr int AHEAD = kAheadRows<kDkvWaves<D>>, CAHEAD = kAheadCols<kDkvWaves<D>>;
   constexpr int QB = C::TB, VALUES = kValuesInLds ? 32 * W * C::VRB : 0;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE + VALUES];
   __shared__ __attribute__((aligned(1024))) float stat[2][4 * QB];  // the rows of a.rows
@@ -339,11 +350,11 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const W
     }
   }
 
-  // The parts of a tile together; the first tiles of all heads, which the most queries see, first where that differs.
-  const int part = blockIdx.x % n.parts, turn = blockIdx.x / n.parts;
-  const int item = a.order ? a.order[turn] : a.causal ? turn % (a.batch * a.kv_heads) * n.tiles + turn / (a.batch * a.kv_heads) : turn;
-  const int bh = item / n.tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
-  const int tile = item % n.tiles;
+  // The parts of a tile together; the first tiles, which the most queries see, first where that differs.
+  const int part = blockIdx.x % n.parts;
+  int bh, tile;
+  deal(a, blockIdx.x / n.parts, n.tiles, a.batch * a.kv_heads, &bh, &tile);
+  const int item = bh * n.tiles + tile, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
   const int keys = keys_of(a, b), start = start_of(a, b);
   const int k0 = tile * 32 * W + w * 32, kj = k0 + l32;
   const bool valid = kj < keys;
@@ -458,19 +469,19 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const W
         dp[4 * q4 + e] = st[2 * QB + 8 * q4 + e];
       }
     float p[2][16], pc[16];
-    bf16x8 ring[kAhead], vring[kAhead];
+    bf16x8 ring[AHEAD], vring[AHEAD];
 #pragma unroll
-    for (int x = 0; x < kAhead; ++x) ring[x] = row(x);
+    for (int x = 0; x < AHEAD; ++x) ring[x] = row(x);
 #pragma unroll
     for (int x = 0; x < ROWS; ++x) {
-      WA_SCHED_FENCE();
+      in_order<kDkvWaves<D>>();
       if (x < 2 * C::KS)
-        s[x & 1] = mfma(ring[x % kAhead], kf[x & 1][x >> 1], s[x & 1]);
+        s[x & 1] = mfma(ring[x % AHEAD], kf[x & 1][x >> 1], s[x & 1]);
       else
-        dp = mfma(ring[x % kAhead], kValuesInLds ? vring[x % kAhead] : vf[kValuesInLds ? 0 : x - 2 * C::KS], dp);
-      if (x + kAhead < ROWS) {
-        ring[x % kAhead] = row(x + kAhead);
-        if (kValuesInLds && x + kAhead >= 2 * C::KS) vring[x % kAhead] = value(x + kAhead - 2 * C::KS);
+        dp = mfma(ring[x % AHEAD], kValuesInLds ? vring[x % AHEAD] : vf[kValuesInLds ? 0 : x - 2 * C::KS], dp);
+      if (x + AHEAD < ROWS) {
+        ring[x % AHEAD] = row(x + AHEAD);
+        if (kValuesInLds && x + AHEAD >= 2 * C::KS) vring[x % AHEAD] = value(x + AHEAD - 2 * C::KS);
       }
       if (x >= 2 * C::KS) {
         constexpr int PER = 32 / C::VS;
@@ -486,9 +497,9 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const W
     for (int q4 = 0; q4 < 4; ++q4)
 #pragma unroll
       for (int e = 0; e < 4; ++e) step[4 * q4 + e] = st[3 * QB + 8 * q4 + e];
-    bf16x8 cring[kAheadCols];
+    bf16x8 cring[CAHEAD];
 #pragma unroll
-    for (int x = 0; x < kAheadCols; ++x) cring[x] = col(x);
+    for (int x = 0; x < CAHEAD; ++x) cring[x] = col(x);
     if (masked) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -510,22 +521,22 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<DV>) void diff_dkv_kernel(const W
     w8[2] = pack8(p[1]);
 #pragma unroll
     for (int x = 0; x < 2 * HALF; ++x) {
-      WA_SCHED_FENCE();
+      in_order<kDkvWaves<D>>();
       const int y = x % HALF;
       if (x == HALF) w8[0] = pack8(pc + 8);
       if (x == HALF + C::VT) w8[1] = pack8(p[0] + 8);
       if (x == HALF + C::VT + C::DT) w8[2] = pack8(p[1] + 8);
       if (y < C::VT)
-        dv[y] = mfma(cring[x % kAheadCols], w8[0], dv[y]);
+        dv[y] = mfma(cring[x % CAHEAD], w8[0], dv[y]);
       else
         dk[(y - C::VT) / C::DT][(y - C::VT) % C::DT] =
-            mfma(cring[x % kAheadCols], w8[1 + (y - C::VT) / C::DT], dk[(y - C::VT) / C::DT][(y - C::VT) % C::DT]);
-      if (x + kAheadCols < 2 * HALF) cring[x % kAheadCols] = col(x + kAheadCols);
+            mfma(cring[x % CAHEAD], w8[1 + (y - C::VT) / C::DT], dk[(y - C::VT) / C::DT][(y - C::VT) % C::DT]);
+      if (x + CAHEAD < 2 * HALF) cring[x % CAHEAD] = col(x + CAHEAD);
 #pragma unroll
       for (int v = 8; v < 16; ++v)  // the second 16 queries' beside the products of the first
         if (x == (v - 8) * HALF / 8) weigh(v);
     }
-    WA_SCHED_FENCE();
+    in_order<kDkvWaves<D>>();
   };
   bool more = advance(0);
   if (more) copy(0);
@@ -622,23 +633,25 @@ hipError_t launch_dims(WaDiffLaunch a, hipStream_t stream) {
 }
 
 // Tiles of 128 tokens, or 64 where a mask block or the sequence is no longer. A call of few tiles does each in parts, so many
-// as fill the chip's workgroups (those of one wavefront a SIMD: 256 of four, 512 of two) once; twice where the tiles are of
-// different lengths. A part is 4 tiles of 64 of the other side at least, and its float32 result is written and read once more.
-WaDiffSide side_of(const WaDiffLaunch& a, bool masked, int len, int units, int64_t other) {
+// as fill the chip's workgroups once (256 of four wavefronts, 512 of two, times per_cu); twice where the tiles are of
+// different lengths. A part is 4 tiles of 64 of the other side at least, and its float32 result is written and read once more: with
+// per_cu 2 for d 64, where two wavefronts share a SIMD, dK and dV of 2 x 16 causal heads of 2,048 tokens and 4 key heads take
+// 117 + 21 us instead of 136 + 12, but dQ 88 + 12 instead of 90.
+WaDiffSide side_of(const WaDiffLaunch& a, bool masked, int len, int units, int64_t other, int per_cu) {
   WaDiffSide s;
   s.waves = len <= 64 || (masked && a.block == 64) ? 2 : 4;
   s.tiles = (len + 32 * s.waves - 1) / (32 * s.waves);
   s.items = (int64_t)units * s.tiles;
-  const int64_t slots = (s.waves == 2 ? 512 : 256) * (a.causal || masked ? 2 : 1);
+  const int64_t slots = (s.waves == 2 ? 512 : 256) * per_cu * (a.causal || masked ? 2 : 1);
   s.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(slots / s.items, other / 256));
   return s;
 }
 
 }  // namespace
 
-WaDiffSide wa_diff_dq_side(const WaDiffLaunch& a, bool masked) { return side_of(a, masked, a.q_len, a.batch * a.heads, a.kv_len); }
+WaDiffSide wa_diff_dq_side(const WaDiffLaunch& a, bool masked) { return side_of(a, masked, a.q_len, a.batch * a.heads, a.kv_len, 1); }
 WaDiffSide wa_diff_dkv_side(const WaDiffLaunch& a, bool masked) {
-  return side_of(a, masked, a.kv_len, a.batch * a.kv_heads, (int64_t)(a.heads / a.kv_heads) * a.q_len);
+  return side_of(a, masked, a.kv_len, a.batch * a.kv_heads, (int64_t)(a.heads / a.kv_heads) * a.q_len, a.head_dim == 64 ? 2 : 1);
 }
 size_t wa_diff_dq_floats(const WaDiffLaunch& a, const WaDiffSide& s) {
   return s.parts == 1 ? 0 : (size_t)s.items * s.parts * 32 * s.waves * 2 * a.head_dim;

@@ -36,7 +36,6 @@ struct WaDiffPlan {
   int32_t units;   // (sequence, head) or, packed, (sequence, key head) pairs
   int32_t tiles;   // row tiles of a unit
   int32_t splits;  // key ranges a tile is computed in
-  int32_t group;   // units whose tiles are dealt out in turn
 };
 WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked);
 size_t wa_diff_part_floats(const WaDiffPlan& p, int value_dim);
