@@ -413,26 +413,28 @@ def sparse_attn_vt_noalloc(q, k, vt, row_ptr, col_idx, perm=None, seg=None, *, b
     return out
 
 
-def _one_device(**tensors) -> torch.device:
+def _one_device(**tensors) -> int:
     """The device that all given tensors share; work is enqueued on that device's current stream."""
-    dev = None
+    index = -1
     for name, t in tensors.items():
         if t is None:
             continue
-        if not t.is_cuda:
+        if index < 0:
+            index = t.get_device()
+        if index < 0 or not t.is_cuda:
             raise ValueError(f"{name} must be a device tensor")
-        if dev is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, the other tensors on {dev}")
-        dev = t.device
-    return dev
+        if t.get_device() != index:
+            raise ValueError(f"{name} is on {t.device}, the tensors before it on cuda:{index}")
+    return index
 
 
-def _call_on(device: torch.device, call, *args) -> None:
-    """The library call with ``device`` current and its current stream as the last argument."""
-    if device.index in (None, torch.cuda.current_device()):
-        L.check(call(*args, _stream()))
+def _call_on(index: int, call, *args) -> None:
+    """The library call with device ``index`` current and its current stream as the last argument. The raw handles are asked
+    for as torch's own extensions do: its stream and device objects take 3.5 us a call, these 0.3."""
+    if index == torch._C._cuda_getDevice():
+        L.check(call(*args, torch._C._cuda_getCurrentRawStream(index)))
         return
-    with torch.cuda.device(device):
+    with torch.cuda.device(index):
         L.check(call(*args, _stream()))
 
 
@@ -471,39 +473,38 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, inv_freq: torch
     if q.dim() != 4 or q.dtype not in _DTYPE:
         raise ValueError("q must be a bfloat16, float16 or float32 [B][H][N][d] tensor")
     b, _, n, d = q.shape
-    if k is not None and (k.dim() != 4 or k.dtype != q.dtype or (k.shape[0], k.shape[2], k.shape[3]) != (b, n, d)):
-        raise ValueError(f"k must be a {q.dtype} tensor [{b}][H][{n}][{d}], got {k.dtype} {tuple(k.shape)}")
     if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be a contiguous float64 vector")
     axis = [inv_freq.numel()] if axis_pairs is None else [int(x) for x in axis_pairs]
-    if not 1 <= len(axis) <= 3:
+    axes = len(axis)
+    if not 1 <= axes <= 3:
         raise ValueError("axis_pairs must name 1 to 3 axes")
     pos_batch = 1
     if positions is not None:
-        want = [(len(axis), 1, n), (len(axis), b, n)] + ([(n,), (b, n)] if len(axis) == 1 else [])
-        if positions.dtype != torch.int32 or tuple(positions.shape) not in want or not positions.is_contiguous():
-            raise ValueError(f"positions must be contiguous int32 of a shape in {want}, got {positions.dtype} "
-                             f"{tuple(positions.shape)}")
-        pos_batch = positions.numel() // (len(axis) * n) if n else 1
-    pairs = [(q, out_q, "q"), (k, out_k, "k")][:1 if k is None else 2]
-    for x, o, name in pairs:
-        if o is not None and (o.dtype != x.dtype or o.shape != x.shape):
-            raise ValueError(f"out_{name} must be {x.dtype} of shape {tuple(x.shape)}, got {o.dtype} {tuple(o.shape)}")
-        for y in (x, o):
-            if y is not None and d > 1 and y.stride(3) != 1:
-                raise ValueError(f"{name} and its output must have contiguous rows (last stride 1)")
-    dev = _one_device(q=q, k=k, inv_freq=inv_freq, positions=positions, out_q=out_q, out_k=out_k)
-    outs, tensors = [], (L.WaRotaryTensor * 2)()
-    for t, (x, o, _) in zip(tensors, pairs):
+        ps = tuple(positions.shape)
+        if (positions.dtype != torch.int32 or not positions.is_contiguous() or ps[-1:] != (n,)
+                or not (ps[:-1] in ((axes, 1), (axes, b)) or axes == 1 and ps[:-1] in ((), (b,)))):
+            raise ValueError(f"positions must be contiguous int32 [{axes}][1 or {b}][{n}] (of one axis also [{b}][{n}] or "
+                             f"[{n}]), got {positions.dtype} {ps}")
+        pos_batch = ps[-2] if len(ps) > 1 else 1
+    outs, tensors = [], b""
+    for x, o, name in ((q, out_q, "q"),) if k is None else ((q, out_q, "q"), (k, out_k, "k")):
+        xb, xh, xn, xd = x.shape if x.dim() == 4 else (0, 0, 0, 0)
+        if xb != b or xn != n or xd != d or x.dtype != q.dtype:
+            raise ValueError(f"{name} must be a {q.dtype} tensor [{b}][H][{n}][{d}], got {x.dtype} {tuple(x.shape)}")
         if o is None:
-            o = torch.empty(x.shape, dtype=x.dtype, device=dev)
+            o = x.new_empty((b, xh, n, d))
+        elif o.dtype != x.dtype or o.shape != x.shape:
+            raise ValueError(f"out_{name} must be {x.dtype} of shape {tuple(x.shape)}, got {o.dtype} {tuple(o.shape)}")
+        (s0, s1, s2, s3), (t0, t1, t2, t3) = x.stride(), o.stride()
+        if d > 1 and (s3 != 1 or t3 != 1):
+            raise ValueError(f"{name} and its output must have contiguous rows (last stride 1)")
         outs.append(o)
-        t.inp, t.out, t.heads = x.data_ptr(), o.data_ptr(), x.shape[1]
-        t.in_stride[:] = x.stride()[:3]
-        t.out_stride[:] = o.stride()[:3]
-    params = L.WaRotaryParams(b, n, d, _DTYPE[q.dtype], _ROTARY_LAYOUT[layout], inv_freq.numel(), len(axis),
-                              (ctypes.c_int32 * 3)(*axis), pos_batch, 1 if backward else 0, float(scale))
-    _call_on(dev, lib.wa_rotary, ctypes.byref(params), tensors, len(pairs), _ptr(inv_freq), _ptr(positions))
+        tensors += L.ROTARY_TENSOR.pack(x.data_ptr(), o.data_ptr(), xh, s0, s1, s2, t0, t1, t2)
+    index = _one_device(q=q, k=k, inv_freq=inv_freq, positions=positions, out_q=out_q, out_k=out_k)
+    params = L.ROTARY_PARAMS.pack(b, n, d, _DTYPE[q.dtype], _ROTARY_LAYOUT[layout], inv_freq.numel(), axes,
+                                  *(axis + [0, 0])[:3], pos_batch, 1 if backward else 0, float(scale))
+    _call_on(index, lib.wa_rotary, params, tensors, len(outs), _ptr(inv_freq), _ptr(positions))
     return outs[0] if k is None else tuple(outs)
 
 
@@ -566,16 +567,16 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
     _check(out, "out", torch.bfloat16, want)
     _check(workspace, "workspace", torch.uint8)
     _on_device(q=q, k=k, v=v, lam=lam, mask=mask, q_start=q_start, kv_lens=kv_lens, out=out, workspace=workspace)
-    dev = _one_device(q=q, k=k, v=v, lam=lam, mask=mask, q_start=q_start, kv_lens=kv_lens, out=out, workspace=workspace)
+    index = _one_device(q=q, k=k, v=v, lam=lam, mask=mask, q_start=q_start, kv_lens=kv_lens, out=out, workspace=workspace)
     need = diff_attn_workspace_size(shape)
     if need and (workspace is None or workspace.numel() < need):
-        workspace = _workspace(need, dev)
-    o = torch.empty(want, dtype=torch.bfloat16, device=dev) if out is None else out
+        workspace = _workspace(need, q.device)
+    o = q.new_empty(want) if out is None else out
     rows = (want[0], 2 * want[1], want[2])
-    maps = torch.empty((*rows, want[3]), dtype=torch.int16, device=dev) if return_stats else None
-    stats = torch.empty((*rows, 3), dtype=torch.float32, device=dev) if return_stats else None
+    maps = q.new_empty((*rows, want[3]), dtype=torch.int16) if return_stats else None
+    stats = q.new_empty((*rows, 3), dtype=torch.float32) if return_stats else None
     opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
-    _call_on(dev, lib.wa_diff_attn, _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(mask), _ptr(q_start), _ptr(kv_lens),
+    _call_on(index, lib.wa_diff_attn, _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(mask), _ptr(q_start), _ptr(kv_lens),
              ctypes.byref(shape), ctypes.byref(opts), _ptr(o), _ptr(maps), _ptr(stats), _ptr(workspace),
              0 if workspace is None else workspace.numel())
     return (o, maps, stats) if return_stats else o
@@ -603,13 +604,13 @@ def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     given = dict(dout=dout, q=q, k=k, v=v, lam=lam, mask=mask, maps=maps, stats=stats, q_start=q_start,
                  kv_lens=kv_lens, workspace=workspace)
     _on_device(**given)
-    dev = _one_device(**given)
+    index = _one_device(**given)
     need = diff_attn_backward_workspace_size(shape)
     if workspace is None or workspace.numel() < need:
-        workspace = _workspace(need, dev)
+        workspace = _workspace(need, q.device)
     dq, dk, dv, dlam = (torch.empty_like(t) for t in (q, k, v, lam))
     opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
-    _call_on(dev, lib.wa_diff_attn_backward, _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(maps),
+    _call_on(index, lib.wa_diff_attn_backward, _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(maps),
              _ptr(stats), _ptr(mask), _ptr(q_start), _ptr(kv_lens), ctypes.byref(shape), ctypes.byref(opts), _ptr(dq),
              _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), workspace.numel())
     return dq, dk, dv, dlam

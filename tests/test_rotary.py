@@ -69,6 +69,12 @@ def _tensor(**kw):
     return t
 
 
+def test_packed_structures_are_the_declared_ones():
+    p, t = _params(scale=2.5, axes=2, axis_pairs=(20, 12, 0)), _tensor()
+    assert bytes(p) == L.ROTARY_PARAMS.pack(2, 100, 64, L.WA_BF16, L.WA_ROTARY_HALF, 32, 2, 20, 12, 0, 1, 0, 2.5)
+    assert bytes(t) == L.ROTARY_TENSOR.pack(1 << 20, 1 << 21, 4, 25600, 6400, 64, 25600, 6400, 64)
+
+
 INVALID, ALIGN, UNSUP = L.WA_ERR_INVALID_ARG, L.WA_ERR_ALIGNMENT, L.WA_ERR_UNSUPPORTED
 
 
@@ -110,18 +116,21 @@ def test_refusals_of_pointers_and_counts():
     assert lib.wa_rotary(ctypes.byref(some), t, 1, FAKE, FAKE, None) == INVALID
 
 
-@pytest.mark.parametrize("kw", [
-    dict(inv_freq=torch.ones(8)), dict(layout="other"), dict(q=torch.zeros(2, 3, 5, 16, dtype=torch.float64)),
-    dict(k=torch.zeros(2, 3, 6, 16)), dict(k=torch.zeros(2, 3, 5, 16, dtype=torch.bfloat16)),
-    dict(positions=torch.zeros(5)), dict(positions=torch.zeros(3, 5, dtype=torch.int32)),
-    dict(positions=torch.zeros(2, 5, dtype=torch.int32), axis_pairs=[4, 4]), dict(axis_pairs=[2, 2, 2, 2]),
-    dict(out_q=torch.zeros(2, 3, 5, 8)), dict(out_k=torch.zeros(2, 3, 5, 16)),
-    dict(q=torch.zeros(2, 3, 16, 5).transpose(2, 3)), dict(),   # the last: host tensors
+@pytest.mark.parametrize("kw,says", [
+    (dict(inv_freq=torch.ones(8)), "inv_freq"), (dict(layout="other"), "layout"),
+    (dict(q=torch.zeros(2, 3, 5, 16, dtype=torch.float64)), "q must be"), (dict(k=torch.zeros(2, 3, 6, 16)), "k must be"),
+    (dict(k=torch.zeros(2, 3, 5, 16, dtype=torch.bfloat16)), "k must be"), (dict(k=torch.zeros(3, 5, 16)), "k must be"),
+    (dict(positions=torch.zeros(5)), "positions"), (dict(positions=torch.zeros(3, 5, dtype=torch.int32)), "positions"),
+    (dict(positions=torch.zeros(2, 5, dtype=torch.int32), axis_pairs=[4, 4]), "positions"),
+    (dict(positions=torch.zeros(2, 3, 5, dtype=torch.int32), axis_pairs=[4, 4]), "positions"),
+    (dict(axis_pairs=[2, 2, 2, 2]), "axis_pairs"), (dict(out_q=torch.zeros(2, 3, 5, 8)), "out_q"),
+    (dict(out_k=torch.zeros(2, 3, 5, 16)), "out_k without k"),
+    (dict(q=torch.zeros(2, 3, 16, 5).transpose(2, 3)), "contiguous rows"), (dict(), "device tensor"),
 ])
-def test_binding_refusals(kw):
+def test_binding_refusals(kw, says):
     args = dict(q=torch.zeros(2, 3, 5, 16), inv_freq=torch.ones(8, dtype=torch.float64))
     args.update(kw)
-    with pytest.raises(ValueError):
+    with pytest.raises(ValueError, match=says):
         W.rotary(args.pop("q"), args.pop("k", None), **args)
 
 
