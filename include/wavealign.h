@@ -430,7 +430,7 @@ typedef struct wa_diff_shape {
 } wa_diff_shape;
 
 typedef struct wa_diff_options {
-  float softmax_scale;  /* <= 0 selects 1/sqrt(head_dim) */
+  float softmax_scale;  /* <= 0 selects 1/sqrt(head_dim); at least 1e-30 */
   int32_t causal;       /* nonzero: query i of sequence b sees the keys j <= q_start[b] + i */
 } wa_diff_options;
 

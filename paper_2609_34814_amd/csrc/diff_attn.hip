@@ -123,14 +123,15 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   float m_run = -INFINITY, l_run = 0.f;
 
   bf16x8 qf[C::KS];
-  auto work = [&](int key, const unsigned char* t) {
-    // The operands' offsets are taken from their first in every tile (opaque, so that all of them are not held all along).
-    uint32_t kb = kbase, vb0 = vbase0, vb1 = vbase1;
+  auto work = [&](int key, uint32_t t) {
+    // The operands' offsets are taken from their first in every tile, whose place is added before, one exclusive or each (opaque, so
+    // that all of them are not held all along).
+    uint32_t kb = kbase + t, vb0 = vbase0 + t, vb1 = vbase1 + t;
     asm volatile("" : "+v"(kb), "+v"(vb0), "+v"(vb1));
-    auto row = [&](int x) { return read_row(t + row_step(kb, x / C::KT) + x % C::KT * 32 * C::KRB); };
+    auto row = [&](int x) { return read_row(lds + row_step(kb, x / C::KT) + x % C::KT * 32 * C::KRB); };
     auto col = [&](int x) {  // column tile x mod DT of 16 keys
-      const unsigned char* at = t + x / C::DT * 16 * C::VRB + (x % C::DT >> 2) * 256;
-      return read_cols(at + col_step(vb0, x % C::DT & 3), at + col_step(vb1, x % C::DT & 3));
+      const int at = x / C::DT * 16 * C::VRB + (x % C::DT >> 2) * 256;
+      return read_cols(lds + col_step(vb0, x % C::DT & 3) + at, lds + col_step(vb1, x % C::DT & 3) + at);
     };
     // Operands are read ahead of the products; fences keep the order written here (the scheduler sinks each read to its product).
     f32x16 s[C::KT];
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
     WA_WAIT_VM(0);  // this wavefront's part of the tile has arrived (and the queries, so that nothing waits for them below)
     WA_BARRIER();   // everyone's has, and everyone is done with the other buffer
     if (next < hi) copy(next, buf ^ 1);
-    if (key < some) work(key, lds + buf * C::STAGE);
+    if (key < some) work(key, buf * C::STAGE);
     key = next;
     buf ^= 1;
   }
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
 #pragma unroll
       for (int v = 0; v < 16; ++v) big = fmaxf(big, fabsf(acc[dt][v]));
     const RowStats r = row_stats(m_run, l, max_halves(big));
-    const float per_step = r.step > 0.f ? 1.f / r.step : 0.f;
+    const float per_step = steps_per_unit(r.step);
     const int64_t at = ((int64_t)b * 2 * a.heads + 2 * h + map) * a.q_len + i;
     if (valid) {
 #pragma unroll
@@ -304,7 +305,7 @@ __device__ __forceinline__ void finish_row(const WaDiffLaunch& a, const COLS (&o
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const RowStats s = row_stats(top[m], l[m], big[m]);
-      const float per_step = s.step > 0.f ? 1.f / s.step : 0.f;
+      const float per_step = steps_per_unit(s.step);
       const int64_t to = (2 * bh + m) * a.q_len + i;
 #pragma unroll
       for (int e = 0; e < E; ++e) a.maps[to * dv + c + e] = (int16_t)rintf(o[m][e] * per_step);

@@ -194,17 +194,18 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
   float lam_dot = 0.f, lam_lost = 0.f;
 
   // 32 keys; masked: this lane's query sees only `rest` of them, counted from its first register's.
-  auto work = [&](const unsigned char* t, const unsigned char* tv, bool masked, int rest) {
-    // opaque, so that the offsets of all operands are not held across the loop
-    uint32_t kr = k_row, vr = v_row, kc0 = k_col0, kc1 = k_col1;
+  auto work = [&](uint32_t t, uint32_t tv, bool masked, int rest) {
+    // The tile's place is added before the steps, one exclusive or each; opaque, so that the offsets of all operands are not held
+    // across the loop.
+    uint32_t kr = k_row + t, vr = v_row + tv, kc0 = k_col0 + t, kc1 = k_col1 + t;
     asm volatile("" : "+v"(kr), "+v"(vr), "+v"(kc0), "+v"(kc1));
     auto row = [&](int x) {  // operand of product x of the scores, then of dP
       const int y = x - 2 * C::KS;
-      return x < 2 * C::KS ? read_row(t + (x & 1) * C::KBYTES + row_step(kr, x >> 1)) : read_row(tv + row_step(vr, y & 7) + (y >> 3) * 256);
+      return x < 2 * C::KS ? read_row(lds + row_step(kr, x >> 1) + (x & 1) * C::KBYTES) : read_row(lds + row_step(vr, y & 7) + (y >> 3) * 256);
     };
     auto col = [&](int x) {  // operand of product x of dQ: 16 keys, map, 32 columns
-      const unsigned char* at = t + (x / C::DT & 1) * C::KBYTES + 16 * (x / (2 * C::DT)) * C::KRB;
-      return read_cols(at + col_step(kc0, x % C::DT), at + col_step(kc1, x % C::DT));
+      const int at = (x / C::DT & 1) * C::KBYTES + 16 * (x / (2 * C::DT)) * C::KRB;
+      return read_cols(lds + col_step(kc0, x % C::DT) + at, lds + col_step(kc1, x % C::DT) + at);
     };
     constexpr int ROWS = 2 * C::KS + C::VS, COLS = 4 * C::DT;
     f32x16 s[2], dp;
@@ -284,9 +285,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
 #pragma unroll 1
     for (int half = 0; half < end; half += 32) {
       if (key + half >= some) break;
-      const unsigned char* t = lds + buf * C::STAGE + half * C::KRB;
-      const unsigned char* tv = lds + buf * C::STAGE + half * C::VRB;
-      work(t, tv, key + half + 32 > all, limit - key - half - 4 * hf);
+      work(buf * C::STAGE + half * C::KRB, buf * C::STAGE + half * C::VRB, key + half + 32 > all, limit - key - half - 4 * hf);
     }
     key = next;
     buf ^= 1;
@@ -388,7 +387,7 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
   const uint32_t q_row = row_operand<C::KRB>(lane, 0), o_row = 2 * C::KBYTES + row_operand<C::VRB>(lane, 0);
   const uint32_t q_col0 = col_operand<C::KRB>(lane, 0, 0), q_col1 = col_operand<C::KRB>(lane, 0, 1);
   const uint32_t o_col0 = 2 * C::KBYTES + col_operand<C::VRB>(lane, 0, 0), o_col1 = 2 * C::KBYTES + col_operand<C::VRB>(lane, 0, 1);
-  const uint32_t v_row = w * 32 * C::VRB + row_operand<C::VRB>(lane, 0);
+  const uint32_t v_row = 2 * C::STAGE + w * 32 * C::VRB + row_operand<C::VRB>(lane, 0);
 
   const float c2 = a.scale * kLog2e;
   f32x16 dk[2][C::DT], dv[C::VT];
@@ -440,23 +439,22 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
     }
   };
   // 32 queries; q0: the query of this lane's first register
-  auto work = [&](const unsigned char* t, const unsigned char* to, const float* st, float lam, bool masked, int q0) {
-    uint32_t qr = q_row, orow = o_row, qc0 = q_col0, qc1 = q_col1, oc0 = o_col0, oc1 = o_col1, vr = v_row;
+  auto work = [&](uint32_t t, uint32_t to, const float* st, float lam, bool masked, int q0) {
+    uint32_t qr = q_row + t, orow = o_row + to, qc0 = q_col0 + t, qc1 = q_col1 + t, oc0 = o_col0 + to, oc1 = o_col1 + to, vr = v_row;
     asm volatile("" : "+v"(qr), "+v"(orow), "+v"(qc0), "+v"(qc1), "+v"(oc0), "+v"(oc1), "+v"(vr));
     auto row = [&](int x) {
       const int y = x - 2 * C::KS;
-      return x < 2 * C::KS ? read_row(t + (x & 1) * C::KBYTES + row_step(qr, x >> 1)) : read_row(to + row_step(orow, y & 7) + (y >> 3) * 256);
+      return x < 2 * C::KS ? read_row(lds + row_step(qr, x >> 1) + (x & 1) * C::KBYTES) : read_row(lds + row_step(orow, y & 7) + (y >> 3) * 256);
     };
-    auto value = [&](int y) { return read_row(values + row_step(vr, y & 7) + (y >> 3) * 256); };
+    auto value = [&](int y) { return read_row(lds + row_step(vr, y & 7) + (y >> 3) * 256); };
     auto col = [&](int x) {  // of the products of 16 queries: dV's column tiles, then dK's of both maps
       const int x16 = x / (C::VT + 2 * C::DT), y = x % (C::VT + 2 * C::DT);
       if (y < C::VT) {
-        const unsigned char* at = to + 16 * x16 * C::VRB + (y >> 2) * 256;
-        return read_cols(at + col_step(oc0, y & 3), at + col_step(oc1, y & 3));
+        const int at = 16 * x16 * C::VRB + (y >> 2) * 256;
+        return read_cols(lds + col_step(oc0, y & 3) + at, lds + col_step(oc1, y & 3) + at);
       }
-      const int c = (y - C::VT) % C::DT;
-      const unsigned char* at = t + (y - C::VT) / C::DT * C::KBYTES + 16 * x16 * C::KRB;
-      return read_cols(at + col_step(qc0, c), at + col_step(qc1, c));
+      const int c = (y - C::VT) % C::DT, at = (y - C::VT) / C::DT * C::KBYTES + 16 * x16 * C::KRB;
+      return read_cols(lds + col_step(qc0, c) + at, lds + col_step(qc1, c) + at);
     };
     constexpr int ROWS = 2 * C::KS + C::VS, HALF = C::VT + 2 * C::DT;
     f32x16 s[2], dp;
@@ -554,10 +552,7 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
     for (int half = 0; half < end; half += 32) {
       const int i1 = i0 + half;
       if (i1 + 32 <= some || i1 >= a.q_len) continue;
-      const unsigned char* t = lds + buf * C::STAGE + half * C::KRB;
-      const unsigned char* to = lds + buf * C::STAGE + half * C::VRB;
-      const float* st = stat[buf] + half + 4 * hf;
-      work(t, to, st, lam, !whole || i1 < all || i1 + 32 > a.q_len, i1 + 4 * hf);
+      work(buf * C::STAGE + half * C::KRB, buf * C::STAGE + half * C::VRB, stat[buf] + half + 4 * hf, lam, !whole || i1 < all || i1 + 32 > a.q_len, i1 + 4 * hf);
     }
     buf ^= 1;
   }

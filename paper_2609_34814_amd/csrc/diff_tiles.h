@@ -161,6 +161,8 @@ __device__ __forceinline__ RowStats row_stats(float top, float l, float big) {
   }
   return r;
 }
+// Steps a unit; a row of nothing but 0, or too small for its step to have a reciprocal, is held as 0.
+__device__ __forceinline__ float steps_per_unit(float step) { return step > 1e-37f ? 1.f / step : 0.f; }
 __device__ __forceinline__ uint32_t pack_steps(float x, float y, float per_step) {
   return (uint32_t)(uint16_t)(int16_t)rintf(x * per_step) | (uint32_t)(uint16_t)(int16_t)rintf(y * per_step) << 16;
 }

@@ -1,4 +1,5 @@
-// Device helpers of the kernels that copy tiles into LDS and feed them to the matrix cores.
+// Device helpers of the differential-attention kernels, which copy tiles into LDS and feed them to the matrix cores. attn_fwd.hip
+// holds the same helpers: its counter profiles are keyed to the source of that one file.
 #pragma once
 
 #include "common.h"

@@ -58,7 +58,7 @@ def test_argument_refusals():
     assert call(start=FAKE, opts=L.WaDiffOptions(0.0, 0)) == INVALID
     assert call(ws=None) == INVALID and call(size=n.value - 1) == WORK
     assert call(ws=ctypes.c_void_p((1 << 20) + 64)) == ALIGN
-    assert call(shape=_shape(block=16)) == UNSUP
+    assert call(shape=_shape(block=16)) == UNSUP and call(opts=L.WaDiffOptions(1e-38, 1)) == UNSUP
 
 
 def _host(b=1, h=2, hk=1, m=70, n=70, d=64, dv=64):
@@ -254,6 +254,40 @@ def test_one_map_less_is_attention():
     o = W.diff_attn(q, k, v, torch.zeros_like(lam), mask)
     first = W.sparse_attn(q[:, ::2].contiguous(), k[:, ::2].contiguous(), v, mask, block=128)
     assert (o.float() - first.float()).abs().max() <= 5 * 4 * 2.0 ** -8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("b,h,block", [(4, 8, 64), (8, 10, 128)])
+def test_masked_tiles_in_order_of_length(b, h, block):
+    """Enough tiles that they run longest first (more than 256, no split)."""
+    m = 5 * block - 9 if block == 128 else 9 * block
+    check_forward(make(b, h, h, m, m, 64, 64), block_mask(b, h, m, m, block, 0.4), block)
+
+
+@pytest.mark.gpu
+def test_masked_tiles_without_an_order():
+    """More than 8,192 tiles run head after head: a mask that keeps all is no mask, bit for bit (128-token blocks are the dense
+    call's tiles)."""
+    args = make(2, 820, 820, 576, 576, 64, 64)
+    ones = torch.ones((2, 820, 5, 5), dtype=torch.bool, device="cuda")
+    assert torch.equal(W.diff_attn(*args, ones), W.diff_attn(*args))
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """A cache of 3.8e9 bytes of keys and as much of values, one token: the last head is what it is alone (other key ranges, so
+    other roundings of float32 sums: 2^-11 of P |V|, within 1)."""
+    hk, n = 120, 131072
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.randn((1, 2 * hk, 1, 64), generator=g, device="cuda").to(torch.bfloat16)
+    k = torch.randn((1, 2 * hk, n, 64), generator=g, device="cuda", dtype=torch.bfloat16)
+    v = torch.randn((1, hk, n, 128), generator=g, device="cuda", dtype=torch.bfloat16)
+    assert v.numel() * 2 > 2 ** 31 and k.numel() * 2 > 2 ** 31
+    lam = torch.full((hk,), 0.5, device="cuda")
+    o = W.diff_attn(q, k, v, lam, causal=True)
+    one = W.diff_attn(q[:, -2:].contiguous(), k[:, -2:].contiguous(), v[:, -1:].contiguous(), lam[-1:], causal=True)
+    err = (o[:, -1:].float() - one.float()).abs()
+    assert torch.all(err <= 2.0 ** -11 + 2 * 2.0 ** -8 * one.float().abs()) and one.abs().max() > 1e-4
 
 
 @pytest.mark.gpu

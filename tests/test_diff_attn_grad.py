@@ -97,6 +97,23 @@ def test_block_masks(b, h, hk, m, n, d, dv, block, causal):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("b,h,hk,block", [(4, 8, 8, 64), (8, 10, 10, 128), (6, 16, 8, 64)])
+def test_masked_tiles_in_order_of_length(b, h, hk, block):
+    """More than 256 tiles of queries and of keys run longest first."""
+    m = 5 * block - 9 if block == 128 else 9 * block
+    check_gradient(make(b, h, hk, m, m, 64, 64), block_mask(b, h, m, m, block, 0.4), block)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dv", DIMS)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("h,hk,m,n", [(1, 1, 1100, 1100), (4, 1, 70, 1500), (3, 1, 1300, 60)])
+def test_tiles_in_parts(d, dv, causal, h, hk, m, n):
+    """Few tiles, so that each is computed in parts; of grouped heads they begin and end inside a head's queries."""
+    check_gradient(make(1, h, hk, m, n, d, dv), causal=causal)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d,dv", DIMS)
 def test_one_key_or_none(d, dv):
     """One key takes all: dS is 0 but for roundings, and dV is (1 - lam) dO; a mask that keeps nothing gives zeros."""

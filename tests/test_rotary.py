@@ -261,6 +261,19 @@ def test_unaligned_rows():
 
 
 @pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """2.2e9 elements: the last tokens of the last head are what they are alone."""
+    f, _ = W.rotary_frequencies(64)
+    q = torch.randn((1, 40, 430000, 128), device="cuda", dtype=torch.bfloat16)
+    assert q.numel() > 2 ** 31
+    tail = q[:, -1:, -50:].contiguous()
+    pos = torch.arange(430000, dtype=torch.int32, device="cuda")
+    want = W.rotary(tail, inv_freq=f, positions=pos[-50:].contiguous())
+    W.rotary(q, inv_freq=f, positions=pos, out_q=q)
+    assert torch.equal(q[:, -1:, -50:], want)
+
+
+@pytest.mark.gpu
 def test_gradient_is_the_transposed_map():
     """For a linear map the difference quotient is exact: <g, R(x + e) - R(x)> = <R^T g, e> up to float32 roundings
     (2^-20.5 of at most 2 |x| |g| a product, over 2 x 3 x 40 x 32 of them)."""
