@@ -458,14 +458,15 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
  *   stats    out float [B][2H][q_len][3], with maps: natural-log sum-exp of the map's scaled scores, the step, and the factor
  *            (1 but for roundings) from probabilities recomputed with that sum-exp to the exact ones
  *   workspace  >= wa_diff_attn_workspace_size(shape), 256-byte aligned; NULL if that is 0
- * How a call is cut into workgroups follows from its shape alone, so equal calls give equal bits. At most
- * 4096 blocks of queries and of keys. */
+ * How a call is cut into workgroups follows from its shape and mask, so equal calls give equal bits; how a head's sums
+ * are split may depend on the masks of the other heads. At most 4096 blocks of queries and of keys. */
 wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
                        const int32_t* q_start, const int32_t* kv_lens, const wa_diff_shape* shape,
                        const wa_diff_options* options, void* o, int16_t* maps, float* stats, void* workspace,
                        size_t workspace_bytes, void* stream);
 
-/* Workspace bytes needed by wa_diff_attn_backward: 4 B H q_len float32 of row values and a float64 per 64 queries of a head. */
+/* Workspace bytes needed by wa_diff_attn_backward: 4 B H q_len float32 of row values, parts of dlam, and the float32 results of
+ * tiles that are computed in parts (about 135 MB at most). */
 wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_t* bytes);
 
 /* Gradient of wa_diff_attn: with dO of O it writes

@@ -514,7 +514,7 @@ def diff_shape_of(batch: int, heads: int, kv_heads: int, q_len: int, kv_len: int
 
 
 def diff_attn_workspace_size(shape: L.WaDiffShape) -> int:
-    """Bytes for diff_attn (0 for calls of many rows)."""
+    """Bytes for diff_attn with or without a mask, 0 in some shapes: results of tiles computed in parts, about 135 MB at most."""
     return _size("wa_diff_attn_workspace_size", shape)
 
 

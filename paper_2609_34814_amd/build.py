@@ -30,7 +30,7 @@ SOURCES = {
     "rotary.hip": [],
     "diff_attn.hip": [],
     "diff_bwd.hip": [],
-    "diff_order.hip": [],
+    "diff_tasks.hip": [],
     "abi.cpp": [],
 }
 

@@ -328,32 +328,37 @@ wa_status check_diff_shape(const wa_diff_shape* s, WaDiffLaunch* out) {
   return WA_OK;
 }
 
-// Forward: split results, or the order of a masked call that is not split.
+// Forward: the task list of a masked call, then the results of split tiles.
+size_t diff_task_bytes(const WaDiffLaunch& a) {
+  const WaDiffPlan p = wa_diff_plan(a, true);
+  return p.splits == 1 ? align_up(4 * wa_diff_task_ints((int64_t)p.units * p.tiles, wa_diff_slots(p.waves))) : 0;
+}
 size_t diff_ws_bytes(const WaDiffLaunch& a) {
-  const WaDiffPlan dense = wa_diff_plan(a, false), masked = wa_diff_plan(a, true);
-  return align_up(4 * std::max({wa_diff_part_floats(dense, a.value_dim), wa_diff_part_floats(masked, a.value_dim),
-                                wa_diff_order_ints((int64_t)masked.units * masked.tiles)}));
+  return diff_task_bytes(a) + align_up(4 * std::max(wa_diff_part_floats(wa_diff_plan(a, false), false, a.value_dim),
+                                                    wa_diff_part_floats(wa_diff_plan(a, true), true, a.value_dim)));
 }
 
-// Gradient: two floats a row and map; the parts of dlam; the order of a masked call; the results of parts of tiles, those of the
+// Gradient: four floats a row; the parts of dlam; the task list of a masked call; the results of split tiles, those of the
 // queries and then those of the keys. Sized for either value of causal and with or without a mask.
 struct DiffBackwardWs {
-  size_t lam, order, part, total;
+  size_t lam, tasks, part, total;
 };
 DiffBackwardWs diff_backward_ws(WaDiffLaunch a) {
-  size_t lam = 0, order = 0, part = 0;
+  size_t lam = 0, tasks = 0, part = 0;
   for (int x = 0; x < 4; ++x) {
     const bool masked = x & 1;
     a.causal = x >> 1;
     const WaDiffSide q = wa_diff_dq_side(a, masked), k = wa_diff_dkv_side(a, masked);
-    lam = std::max(lam, (size_t)q.items * q.parts);
-    if (masked) order = std::max({order, wa_diff_order_ints(q.items), wa_diff_order_ints(k.items)});
-    part = std::max({part, wa_diff_dq_floats(a, q), wa_diff_dkv_floats(a, k)});
+    lam = std::max(lam, (size_t)q.items * (masked && wa_diff_has_tasks(q.items) ? kDiffMaxChunks : q.parts));
+    if (masked)
+      tasks = std::max({tasks, wa_diff_task_ints(q.items, wa_diff_slots(q.waves)), wa_diff_task_ints(k.items, wa_diff_slots(k.waves))});
+    part = std::max({part, (size_t)wa_diff_side_tiles(q, masked) * 32 * q.waves * 2 * a.head_dim,
+                     (size_t)wa_diff_side_tiles(k, masked) * 32 * k.waves * (2 * a.head_dim + a.value_dim)});
   }
   DiffBackwardWs w;
   w.lam = align_up((size_t)4 * a.batch * a.heads * a.q_len * 4);
-  w.order = w.lam + align_up(lam * 8);
-  w.part = w.order + align_up(order * 4);
+  w.tasks = w.lam + align_up(lam * 8);
+  w.part = w.tasks + align_up(tasks * 4);
   w.total = w.part + align_up(part * 4);
   return w;
 }
@@ -804,8 +809,8 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
   s = check_ws(workspace, workspace_bytes, diff_ws_bytes(a));
   if (s != WA_OK) return s;
   a.o = o; a.maps = maps; a.stats = stats;
-  a.part = (float*)workspace;
-  a.order = (int32_t*)workspace;
+  a.tasks = (int32_t*)workspace;
+  a.part = (float*)((char*)workspace + diff_task_bytes(a));
   const hipError_t e = wa_launch_diff_attn(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention launch");
   return ok();
@@ -842,7 +847,7 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
   a.dq = dq; a.dk = dk; a.dv = dv; a.dlam = dlam;
   a.rows = (float*)workspace;
   a.lam_part = (double*)((char*)workspace + L.lam);
-  a.order = (int32_t*)((char*)workspace + L.order);
+  a.tasks = (int32_t*)((char*)workspace + L.tasks);
   a.part = (float*)((char*)workspace + L.part);
   const hipError_t e = wa_launch_diff_backward(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention gradient launch");

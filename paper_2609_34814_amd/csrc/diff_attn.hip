@@ -54,13 +54,9 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int map = w / W, slice = w % W;
 
-  // Work item: the key range fastest, then the units of a group in turn, tile after tile; longest tiles first where
-  // later queries see more keys.
-  const int chunk = blockIdx.x % p.splits;
-  int unit, tile;
-  deal(a, blockIdx.x / p.splits, p.tiles, p.units, &unit, &tile);
-  if (a.causal && !a.order) tile = p.tiles - 1 - tile;
-  const int64_t item = (int64_t)unit * p.tiles + tile;
+  Task task;
+  if (!take_task(a, p.tiles, p.units, p.splits, a.causal, &task)) return;
+  const int unit = task.unit, tile = task.tile;
   const int per_key_head = a.heads / a.kv_heads;
   const int heads = p.packed ? a.kv_heads : a.heads;
   const int b = unit / heads;
@@ -80,12 +76,6 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   const int some = p.packed ? key_limit(a, keys, start, i_last) : i0 > i_last ? 0 : key_limit(a, keys, start, min(i0 + 31, i_last));
   const int all = key_limit(a, keys, start, p.packed ? 0 : min(i0, i_last));
   const int most = key_limit(a, keys, start, p.packed ? i_last : min(tile * 32 * W + 32 * W - 1, i_last));
-  // this workgroup's keys: a range of whole blocks and tiles
-  const int unit_keys = a.mask ? max(a.block, KB) : KB;
-  const int per = ((most + unit_keys - 1) / unit_keys + p.splits - 1) / p.splits;
-  const int lo = min((int64_t)chunk * per * unit_keys, (int64_t)most);
-  const int hi = min((int64_t)lo + per * unit_keys, (int64_t)most);
-
   const unsigned char* kg[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m)
@@ -97,8 +87,10 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   if (a.mask) {
     walk.at = a.mask + (((int64_t)b * a.heads + h) * a.mb + (tile * 32 * W >> shift)) * a.nb;
     walk.at = uniform_ptr(walk.at);
-    walk.entries = (hi + a.block - 1) >> shift;
   }
+  int lo, hi;  // this workgroup's keys
+  chunk_keys<KB>(a, task, walk, most, lane, &lo, &hi);
+  walk.entries = (hi + a.block - 1) >> shift;
   // first kept tile at or past `key`, a multiple of KB
   auto next_tile = [&](int key) {
     if (!a.mask || (key & (a.block - 1))) return key;
@@ -226,10 +218,9 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   }
 
   const float l = add_halves(l_run);
-  if (p.splits > 1) {
+  if (task.chunks > 1) {
     if (!valid) return;
-    const int64_t n = item * p.splits + chunk, rows = 32 * W;
-    const int64_t at = (n * 2 + map) * rows + slice * 32 + l32;
+    const int64_t rows = 32 * W, at = (task.part * 2 + map) * rows + slice * 32 + l32;
     float* out = a.part + at * DV;
 #pragma unroll
     for (int dt = 0; dt < C::DT; ++dt)
@@ -237,7 +228,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
       for (int v = 0; v < 16; v += 4)
         *(float4*)(out + dt * 32 + 2 * v + 4 * hf) = make_float4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3]);
     if (hf == 0) {
-      float2* stat = (float2*)(a.part + (int64_t)p.units * p.tiles * p.splits * 2 * rows * DV);
+      float2* stat = (float2*)(a.part + a.part_tiles * 2 * rows * DV);
       stat[at] = make_float2(m_run, l);
     }
     return;
@@ -336,7 +327,7 @@ struct PartRow {
     const int row = p.packed ? h % per_key_head * a.q_len + i : i;
     rows = 32 * p.waves;
     at = (unit * p.tiles + row / rows) * p.splits * 2 * rows + row % rows;
-    stat = (const float2*)(a.part + (int64_t)p.units * p.tiles * p.splits * 2 * rows * dv);
+    stat = (const float2*)(a.part + a.part_tiles * 2 * rows * dv);
   }
 };
 
@@ -440,24 +431,70 @@ __global__ __launch_bounds__(64 * R) void diff_join_many_kernel(const WaDiffLaun
   finish_row<E>(a, o, top, l, big, row.bh, row.i, lane * E, lane == 0);
 }
 
+// The same for the cut tiles of a list of tasks: four columns a lane, DV / 4 lanes a row.
+template <int DV>
+__global__ __launch_bounds__(256) void diff_join_cut_kernel(const WaDiffLaunch a, const WaDiffPlan p) {
+  typedef float cols __attribute__((ext_vector_type(4)));
+  constexpr int L = DV / 4, PER = 256 / L;
+  const int lane = threadIdx.x % L, rows = 32 * p.waves, all = a.tasks[1] * rows;
+  const int4* cuts = (const int4*)(a.tasks + wa_diff_cut_list(a.task_items, wa_diff_slots(p.waves)));
+  const float2* stat = (const float2*)(a.part + a.part_tiles * 2 * rows * DV);
+  for (int r = blockIdx.x * PER + threadIdx.x / L; r < all; r += gridDim.x * PER) {
+    const int4 e = cuts[r / rows];
+    const int64_t bh = e.x / p.tiles;
+    const int i = e.x % p.tiles * rows + r % rows;
+    if (i >= a.q_len) continue;
+    cols o[2];
+    float top[2], l[2], big[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      auto at = [&](int c) { return ((int64_t)(e.z + c) * 2 + m) * rows + r % rows; };
+      top[m] = -INFINITY;
+      for (int c = 0; c < e.y; ++c) top[m] = fmaxf(top[m], stat[at(c)].x);
+      l[m] = 0.f;
+      o[m] = 0.f;
+#pragma unroll 4
+      for (int c = 0; c < e.y; ++c) {
+        const float2 s = stat[at(c)];
+        const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top[m]);
+        l[m] += f * s.y;
+        o[m] += *(const cols*)(a.part + at(c) * DV + 4 * lane) * f;
+      }
+      o[m] *= l[m] > 0.f ? 1.f / l[m] : l[m] == 0.f ? 0.f : NAN;
+      big[m] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) big[m] = fmaxf(big[m], fabsf(o[m][x]));
+      if (a.maps)
+        for (int y = L / 2; y > 0; y >>= 1) big[m] = fmaxf(big[m], __shfl_xor(big[m], y));
+    }
+    finish_row<4>(a, o, top, l, big, bh, i, 4 * lane, lane == 0);
+  }
+}
+
 template <int D, int DV>
 hipError_t launch_dims(WaDiffLaunch a, const WaDiffPlan& p, hipStream_t stream) {
-  if (a.mask && p.splits == 1 && wa_diff_ordered((int64_t)p.units * p.tiles)) {
-    const hipError_t e = wa_launch_diff_order(a, false, stream);
+  const int64_t items = (int64_t)p.units * p.tiles;
+  const int slots = wa_diff_slots(p.waves);
+  if (a.mask && p.splits == 1 && wa_diff_has_tasks(items)) {
+    a.task_items = (int32_t)items;
+    a.part_tiles = 2 * slots;
+    const hipError_t e = wa_launch_diff_tasks(a, false, slots, stream);
     if (e != hipSuccess) return e;
   } else {
-    a.order = nullptr;
+    a.tasks = nullptr;
+    a.part_tiles = items * p.splits;
   }
-  const int64_t grid = (int64_t)p.units * p.tiles * p.splits;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t grid = a.tasks ? items + slots : items * p.splits;
   const dim3 g((unsigned)grid), t(128 * p.waves);
   if (p.waves == 1) hipLaunchKernelGGL((diff_fwd_kernel<D, DV, 1>), g, t, 0, stream, a, p);
   if (p.waves == 2) hipLaunchKernelGGL((diff_fwd_kernel<D, DV, 2>), g, t, 0, stream, a, p);
   if (p.waves == 4) hipLaunchKernelGGL((diff_fwd_kernel<D, DV, 4>), g, t, 0, stream, a, p);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
+  if (e != hipSuccess || (p.splits == 1 && !a.tasks)) return e;
   const int64_t rows = (int64_t)a.batch * a.heads * a.q_len;
-  if (p.splits > 16) {
+  if (a.tasks) {
+    hipLaunchKernelGGL(diff_join_cut_kernel<DV>, dim3(1024), dim3(256), 0, stream, a, p);
+  } else if (p.splits > 16) {
     hipLaunchKernelGGL((diff_join_many_kernel<DV, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, a, p);
   } else if (p.splits > kFewSplits) {
     hipLaunchKernelGGL((diff_join_many_kernel<DV, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a, p);
@@ -486,8 +523,10 @@ WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked) {
   return p;
 }
 
-size_t wa_diff_part_floats(const WaDiffPlan& p, int value_dim) {
-  return p.splits == 1 ? 0 : (size_t)p.units * p.tiles * p.splits * 2 * 32 * p.waves * (value_dim + 2);
+size_t wa_diff_part_floats(const WaDiffPlan& p, bool masked, int value_dim) {
+  const int64_t items = (int64_t)p.units * p.tiles;
+  const int64_t tiles = p.splits > 1 ? items * p.splits : masked && wa_diff_has_tasks(items) ? 2 * wa_diff_slots(p.waves) : 0;
+  return (size_t)tiles * 2 * 32 * p.waves * (value_dim + 2);
 }
 
 hipError_t wa_launch_diff_attn(const WaDiffLaunch& a, hipStream_t stream) {

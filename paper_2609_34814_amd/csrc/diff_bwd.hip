@@ -101,22 +101,16 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // The parts of a tile together; the longest tiles first where later queries see more keys.
-  const int part = blockIdx.x % n.parts;
-  int bh, tile;
-  deal(a, blockIdx.x / n.parts, n.tiles, a.batch * a.heads, &bh, &tile);
-  if (a.causal && !a.order) tile = n.tiles - 1 - tile;
-  const int item = bh * n.tiles + tile, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
+  Task task;
+  if (!take_task(a, n.tiles, a.batch * a.heads, n.parts, a.causal, &task)) return;
+  const int bh = task.unit, tile = task.tile, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
   const int i0 = tile * 32 * W + w * 32, i = i0 + l32, i_last = a.q_len - 1;
   const bool valid = i <= i_last;
   const int keys = keys_of(a, b), start = start_of(a, b);
   const int limit = valid ? key_limit(a, keys, start, i) : 0;
   const int some = i0 > i_last ? 0 : key_limit(a, keys, start, min(i0 + 31, i_last));
   const int all = key_limit(a, keys, start, min(i0, i_last));
-  // this part's keys: whole blocks and tiles
   const int most = key_limit(a, keys, start, min(tile * 32 * W + 32 * W - 1, i_last));
-  const int unit = a.mask ? max(a.block, KB) : KB, per = ((most + unit - 1) / unit + n.parts - 1) / n.parts;
-  const int lo = min((int64_t)part * per * unit, (int64_t)most), hi = min((int64_t)lo + per * unit, (int64_t)most);
 
   const unsigned char* kg = (const unsigned char*)a.k + (((int64_t)b * 2 * a.kv_heads + 2 * hk) * a.kv_len) * C::KRB;
   const unsigned char* vg = (const unsigned char*)a.v + (((int64_t)b * a.kv_heads + hk) * a.kv_len) * C::VRB;
@@ -124,8 +118,10 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
   const int shift = a.block == 128 ? 7 : 6;
   if (a.mask) {
     walk.at = uniform_ptr(a.mask + ((int64_t)bh * a.mb + (tile * 32 * W >> shift)) * a.nb);
-    walk.entries = (hi + a.block - 1) >> shift;
   }
+  int lo, hi;  // this workgroup's keys
+  chunk_keys<KB>(a, task, walk, most, lane, &lo, &hi);
+  walk.entries = (hi + a.block - 1) >> shift;
   auto next_tile = [&](int key) {
     if (!a.mask || (key & (a.block - 1))) return key;
     return walk.next(key >> shift, lane) << shift;
@@ -174,7 +170,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
       factor = st[2];  // of the second map, in the end
     }
   }
-  if (valid && hf == 0 && part == 0) {
+  if (valid && hf == 0 && task.chunk == 0) {
     float* to = a.rows + (int64_t)bh * 4 * a.q_len + i;
     to[0] = -ref[0] / c2;
     to[a.q_len] = -ref[1] / c2;
@@ -290,8 +286,8 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     key = next;
     buf ^= 1;
   }
-  if (n.parts > 1) {
-    float* to = a.part + (((int64_t)item * n.parts + part) * 32 * W + w * 32 + l32) * 2 * D;
+  if (task.chunks > 1) {
+    float* to = a.part + (task.part * 32 * W + w * 32 + l32) * 2 * D;
     store_part(to, dq[0], a.scale, hf);
     store_part(to + D, dq[1], -lam * a.scale, hf);
   } else if (valid) {
@@ -299,7 +295,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     store_row(((uint16_t*)a.dq) + (row0 + a.q_len) * D, dq[1], -lam * a.scale, hf);
   }
   // sum_j P_2 (dP - D_2), which the stored maps' steps leave of their D_2 (the sum of P_2 is 1), and that D_2
-  double lam_row = (double)lam_dot * factor + (valid && hf == 0 && part == 0 ? (double)d[1] : 0.0);
+  double lam_row = (double)lam_dot * factor + (valid && hf == 0 && task.chunk == 0 ? (double)d[1] : 0.0);
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) lam_row += __shfl_xor(lam_row, x);
   if (lane == 0) lam_sum[w] = lam_row;
@@ -307,7 +303,11 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
   if (tid == 0) {
     double sum = 0.0;
     for (int x = 0; x < W; ++x) sum += lam_sum[x];
-    a.lam_part[(int64_t)item * n.parts + part] = sum;
+    // of listed tasks, kDiffMaxChunks a tile, 0 past its chunks
+    double* to = a.lam_part + task.item * (a.tasks ? kDiffMaxChunks : n.parts);
+    to[task.chunk] = sum;
+    if (a.tasks && task.chunk == 0)
+      for (int x = task.chunks; x < kDiffMaxChunks; ++x) to[x] = 0.0;
   }
 }
 
@@ -349,11 +349,10 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
     }
   }
 
-  // The parts of a tile together; the first tiles, which the most queries see, first where that differs.
-  const int part = blockIdx.x % n.parts;
-  int bh, tile;
-  deal(a, blockIdx.x / n.parts, n.tiles, a.batch * a.kv_heads, &bh, &tile);
-  const int item = bh * n.tiles + tile, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
+  // the first tiles, which the most queries see, come first where that differs
+  Task task;
+  if (!take_task(a, n.tiles, a.batch * a.kv_heads, n.parts, false, &task)) return;
+  const int bh = task.unit, tile = task.tile, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
   const int keys = keys_of(a, b), start = start_of(a, b);
   const int k0 = tile * 32 * W + w * 32, kj = k0 + l32;
   const bool valid = kj < keys;
@@ -362,11 +361,25 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
   const int from = first_query(kj);
   const int some = first_query(k0), all = first_query(min(k0 + 31, max(keys - 1, k0)));
   const bool whole = k0 + 31 < keys;
-  // this part's tiles of queries, counted through the heads one after another
+  // this chunk's tiles of queries, counted through the heads one after another: an equal number, or that of an equal number of the
+  // column's kept blocks
   const int from0 = first_query(tile * 32 * W), first = from0 / QB * QB;
   const int q_tiles = from0 < a.q_len ? (a.q_len - first + QB - 1) / QB : 0;
   const int64_t all_tiles = (int64_t)per_key_head * q_tiles;
-  const int64_t t0 = all_tiles * part / n.parts, t1 = all_tiles * (part + 1) / n.parts;
+  const int shift = a.block == 128 ? 7 : 6;
+  MaskWalk walk;
+  int64_t t0 = all_tiles * task.chunk / task.chunks, t1 = all_tiles * (task.chunk + 1) / task.chunks;
+  if (a.tasks && task.chunks > 1) {
+    walk.at = uniform_ptr(a.mask + ((int64_t)b * a.heads + hk * per_key_head) * a.mb * a.nb + (tile * 32 * W >> shift));
+    walk.step = a.nb;
+    walk.entries = per_key_head * a.mb;  // the heads' rows lie one after another
+    auto tile_of = [&](int chunk) {
+      const int e = walk.nth((int)((int64_t)a.tasks[4 + task.item] * chunk / task.chunks), lane), head = e / a.mb;
+      return head * (int64_t)q_tiles + min(max(((e - head * a.mb) << shift) - first, 0) / QB, q_tiles);
+    };
+    t0 = task.chunk > 0 ? tile_of(task.chunk) : 0;
+    t1 = task.chunk + 1 < task.chunks ? tile_of(task.chunk + 1) : all_tiles;
+  }
 
   const int64_t krow0 = ((int64_t)b * 2 * a.kv_heads + 2 * hk) * a.kv_len + kj, vrow = (int64_t)bh * a.kv_len + kj;
   bf16x8 kf[2][C::KS], vf[kValuesInLds ? 1 : C::VS];
@@ -400,8 +413,6 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
   for (int c = 0; c < C::VT; ++c) fill(dv[c], 0.f);
 
   // One loop over the tiles of all heads: head g's run from lo to hi; i is the next one's first query.
-  const int shift = a.block == 128 ? 7 : 6;
-  MaskWalk walk;
   int g = q_tiles > 0 ? (int)(t0 / q_tiles) - 1 : per_key_head, i = 0, hi = 0;
   auto kept = [&](int x) { return a.mask && !(x & (a.block - 1)) ? walk.next(x >> shift, lane) << shift : x; };
   auto advance = [&](int from) {
@@ -556,8 +567,8 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
     }
     buf ^= 1;
   }
-  if (n.parts > 1) {
-    float* to = a.part + (((int64_t)item * n.parts + part) * 32 * W + w * 32 + l32) * (2 * D + DV);
+  if (task.chunks > 1) {
+    float* to = a.part + (task.part * 32 * W + w * 32 + l32) * (2 * D + DV);
     store_part(to, dk[0], a.scale, hf);
     store_part(to + D, dk[1], a.scale, hf);
     store_part(to + 2 * D, dv, 1.f, hf);
@@ -591,40 +602,79 @@ __global__ __launch_bounds__(256) void diff_parts_kernel(const float* part, uint
   *(uint2*)out = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
 }
 
+// The same for the cut tiles of a list of tasks.
+__global__ __launch_bounds__(256) void diff_parts_cut_kernel(const WaDiffLaunch a, const WaDiffSide n, uint16_t* maps, uint16_t* values,
+                                                             int len, int dv) {
+  const int d = a.head_dim, width = 2 * d + dv, quads = width / 4, rows = 32 * n.waves;
+  const int64_t all = (int64_t)a.tasks[1] * rows * quads;
+  const int4* cuts = (const int4*)(a.tasks + wa_diff_cut_list(a.task_items, wa_diff_slots(n.waves)));
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
+    const int r = (int)(id / quads), c = (int)(id % quads) * 4;
+    const int4 e = cuts[r / rows];
+    const int64_t unit = e.x / n.tiles;
+    const int i = e.x % n.tiles * rows + r % rows;
+    if (i >= len) continue;
+    const float* at = a.part + ((int64_t)e.z * rows + r % rows) * width + c;
+    float4 sum = *(const float4*)at;
+#pragma unroll 4
+    for (int x = 1; x < e.y; ++x) {
+      const float4 y = *(const float4*)(at + (int64_t)x * rows * width);
+      sum.x += y.x;
+      sum.y += y.y;
+      sum.z += y.z;
+      sum.w += y.w;
+    }
+    uint16_t* out = c < 2 * d ? maps + ((unit * 2 + c / d) * len + i) * d + c % d : values + (unit * len + i) * dv + c - 2 * d;
+    *(uint2*)out = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
+  }
+}
+
 hipError_t launch_parts(const WaDiffLaunch& a, const WaDiffSide& n, void* maps, void* values, int64_t rows, int len, int dv,
                         hipStream_t stream) {
-  const int64_t threads = rows * ((2 * a.head_dim + dv) / 4);
-  hipLaunchKernelGGL(diff_parts_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a.part, (uint16_t*)maps,
-                     (uint16_t*)values, rows, len, 32 * n.waves, n.tiles, n.parts, a.head_dim, dv);
+  if (a.tasks) {
+    hipLaunchKernelGGL(diff_parts_cut_kernel, dim3(1024), dim3(256), 0, stream, a, n, (uint16_t*)maps, (uint16_t*)values, len, dv);
+  } else if (n.parts > 1) {
+    const int64_t threads = rows * ((2 * a.head_dim + dv) / 4);
+    hipLaunchKernelGGL(diff_parts_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a.part, (uint16_t*)maps,
+                       (uint16_t*)values, rows, len, 32 * n.waves, n.tiles, n.parts, a.head_dim, dv);
+  }
   return hipGetLastError();
+}
+
+// a.tasks for a side, if it has a list; its workgroups
+template <bool COLUMNS>
+hipError_t start_side(WaDiffLaunch& a, int32_t* tasks, const WaDiffSide& n, unsigned* grid, hipStream_t stream) {
+  a.tasks = a.mask && n.parts == 1 && wa_diff_has_tasks(n.items) ? tasks : nullptr;
+  *grid = (unsigned)(n.items * n.parts);
+  if (!a.tasks) return hipSuccess;
+  const int slots = wa_diff_slots(n.waves);
+  a.task_items = (int32_t)n.items;
+  *grid += slots;
+  return wa_launch_diff_tasks(a, COLUMNS, slots, stream);
 }
 
 template <int D, int DV>
 hipError_t launch_dims(WaDiffLaunch a, hipStream_t stream) {
   const WaDiffSide q = wa_diff_dq_side(a, a.mask), k = wa_diff_dkv_side(a, a.mask);
-  int32_t* const order = a.order;
-  hipError_t e = hipSuccess;
-  a.order = a.mask && wa_diff_ordered(q.items) ? order : nullptr;
-  if (a.order && (e = wa_launch_diff_order(a, false, stream)) != hipSuccess) return e;
-  const dim3 gq((unsigned)(q.items * q.parts)), tq(64 * q.waves);
+  int32_t* const tasks = a.tasks;
+  unsigned grid;
+  hipError_t e = start_side<false>(a, tasks, q, &grid, stream);
+  if (e != hipSuccess) return e;
+  const int lam_parts = q.tiles * (a.tasks ? kDiffMaxChunks : q.parts);
   if (q.waves == 2)
-    hipLaunchKernelGGL((diff_dq_kernel<D, DV, 2>), gq, tq, 0, stream, a, q);
+    hipLaunchKernelGGL((diff_dq_kernel<D, DV, 2>), dim3(grid), dim3(128), 0, stream, a, q);
   else
-    hipLaunchKernelGGL((diff_dq_kernel<D, DV, 4>), gq, tq, 0, stream, a, q);
+    hipLaunchKernelGGL((diff_dq_kernel<D, DV, 4>), dim3(grid), dim3(256), 0, stream, a, q);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (q.parts > 1 && (e = launch_parts(a, q, a.dq, nullptr, (int64_t)a.batch * a.heads * a.q_len, a.q_len, 0, stream)) != hipSuccess)
-    return e;
+  if ((e = launch_parts(a, q, a.dq, nullptr, (int64_t)a.batch * a.heads * a.q_len, a.q_len, 0, stream)) != hipSuccess) return e;
 
-  a.order = a.mask && wa_diff_ordered(k.items) ? order : nullptr;
-  if (a.order && (e = wa_launch_diff_order(a, true, stream)) != hipSuccess) return e;
-  const dim3 gk((unsigned)(k.items * k.parts)), tk(64 * k.waves);
+  if ((e = start_side<true>(a, tasks, k, &grid, stream)) != hipSuccess) return e;
   if (k.waves == 2)
-    hipLaunchKernelGGL((diff_dkv_kernel<D, DV, 2>), gk, tk, 0, stream, a, k, q.tiles * q.parts);
+    hipLaunchKernelGGL((diff_dkv_kernel<D, DV, 2>), dim3(grid), dim3(128), 0, stream, a, k, lam_parts);
   else
-    hipLaunchKernelGGL((diff_dkv_kernel<D, DV, 4>), gk, tk, 0, stream, a, k, q.tiles * q.parts);
+    hipLaunchKernelGGL((diff_dkv_kernel<D, DV, 4>), dim3(grid), dim3(256), 0, stream, a, k, lam_parts);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (k.parts > 1) e = launch_parts(a, k, a.dk, a.dv, (int64_t)a.batch * a.kv_heads * a.kv_len, a.kv_len, DV, stream);
-  return e;
+  return launch_parts(a, k, a.dk, a.dv, (int64_t)a.batch * a.kv_heads * a.kv_len, a.kv_len, DV, stream);
 }
 
 // Tiles of 128 tokens, or 64 where a mask block or the sequence is no longer. A call of few tiles does each in parts, so many
@@ -648,11 +698,8 @@ WaDiffSide wa_diff_dq_side(const WaDiffLaunch& a, bool masked) { return side_of(
 WaDiffSide wa_diff_dkv_side(const WaDiffLaunch& a, bool masked) {
   return side_of(a, masked, a.kv_len, a.batch * a.kv_heads, (int64_t)(a.heads / a.kv_heads) * a.q_len, a.head_dim == 64 ? 2 : 1);
 }
-size_t wa_diff_dq_floats(const WaDiffLaunch& a, const WaDiffSide& s) {
-  return s.parts == 1 ? 0 : (size_t)s.items * s.parts * 32 * s.waves * 2 * a.head_dim;
-}
-size_t wa_diff_dkv_floats(const WaDiffLaunch& a, const WaDiffSide& s) {
-  return s.parts == 1 ? 0 : (size_t)s.items * s.parts * 32 * s.waves * (2 * a.head_dim + a.value_dim);
+int64_t wa_diff_side_tiles(const WaDiffSide& s, bool masked) {
+  return s.parts > 1 ? s.items * s.parts : masked && wa_diff_has_tasks(s.items) ? 2 * wa_diff_slots(s.waves) : 0;
 }
 
 hipError_t wa_launch_diff_backward(const WaDiffLaunch& a, hipStream_t stream) {

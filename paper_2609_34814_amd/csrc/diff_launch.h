@@ -15,8 +15,10 @@ struct WaDiffLaunch {
   void* o;            // bf16 [batch][heads][q_len][value_dim]
   int16_t* maps;      // [batch][2 heads][q_len][value_dim]: P_m V in steps of its row's, nullable
   float* stats;       // [batch][2 heads][q_len][3]: log-sum-exp, step, correction (diff_tiles.h), with maps
-  int32_t* order;     // workspace of masked calls: work items by falling length, then their lengths
-  float* part;        // workspace of split calls: partial tiles, then (forward) their statistics
+  int32_t* tasks;     // workspace of masked calls (see wa_diff_task_ints); null: tiles are dealt out by number
+  int32_t task_items; // tiles that `tasks` is about
+  float* part;        // workspace of split calls: part_tiles partial tiles, then (forward) their statistics
+  int64_t part_tiles;
   int32_t batch, heads, kv_heads, q_len, kv_len, head_dim, value_dim, block, mb, nb, causal;
   float scale;
   // backward
@@ -38,16 +40,26 @@ struct WaDiffPlan {
   int32_t splits;  // key ranges a tile is computed in
 };
 WaDiffPlan wa_diff_plan(const WaDiffLaunch& a, bool masked);
-size_t wa_diff_part_floats(const WaDiffPlan& p, int value_dim);
+size_t wa_diff_part_floats(const WaDiffPlan& p, bool masked, int value_dim);
 
-// Tiles of masked calls run longest first where there are this many of them: fewer all run at once; with more, a long one
+// Masked calls of this many tiles run a list of tasks, longest first, in which tiles of more kept blocks than a workgroup's share of
+// the call are cut into chunks. Fewer tiles all run at once (or are cut into key ranges by their number alone); with more, a long one
 // that starts late is short next to the call, and running heads one after another keeps their keys in the caches.
-constexpr int kDiffOrderMin = 257, kDiffOrderMax = 8192;
-inline bool wa_diff_ordered(int64_t items) { return items >= kDiffOrderMin && items <= kDiffOrderMax; }
-inline size_t wa_diff_order_ints(int64_t items) { return wa_diff_ordered(items) ? 2 * (size_t)items : 0; }
-// Fills a.order for the rows of the mask, or for its columns summed over the heads of a key head (entry t of a unit u of n
-// is item u n + t).
-hipError_t wa_launch_diff_order(const WaDiffLaunch& a, bool columns, hipStream_t stream);
+constexpr int kDiffTasksMin = 257, kDiffTasksMax = 8192, kDiffMaxChunks = 16;
+inline bool wa_diff_has_tasks(int64_t items) { return items >= kDiffTasksMin && items <= kDiffTasksMax; }
+// Workgroups that fill the chip, of so many wavefronts a map (or a workgroup of the gradient).
+__host__ __device__ inline int wa_diff_slots(int waves) { return waves == 4 ? 256 : 512; }
+// The list: [0] tasks, [1] cut tiles; from 4 the kept blocks of each tile; then tasks {tile, chunk, chunks, first partial tile}, at
+// most one more a slot than there are tiles; then cut tiles {tile, chunks, first partial tile, 0}, at most one a slot. Their chunks
+// are at most two a slot.
+__host__ __device__ inline int wa_diff_task_list(int items) { return 4 + (items + 3) / 4 * 4; }
+__host__ __device__ inline int wa_diff_cut_list(int items, int slots) { return wa_diff_task_list(items) + 4 * (items + slots); }
+inline size_t wa_diff_task_ints(int64_t items, int slots) {
+  return wa_diff_has_tasks(items) ? (size_t)wa_diff_cut_list((int)items, slots) + 4 * slots : 0;
+}
+// Fills a.tasks for the rows of the mask, or for its columns with the rows of all heads of a key head (entry t of a unit u of n is
+// tile u n + t).
+hipError_t wa_launch_diff_tasks(const WaDiffLaunch& a, bool columns, int slots, hipStream_t stream);
 
 // How the gradient is cut: tiles of 32 * waves queries (keys), each tile's keys (queries of all heads) in so many parts.
 struct WaDiffSide {
@@ -56,9 +68,8 @@ struct WaDiffSide {
 };
 WaDiffSide wa_diff_dq_side(const WaDiffLaunch& a, bool masked);
 WaDiffSide wa_diff_dkv_side(const WaDiffLaunch& a, bool masked);
-// float32 of the parts' results, 0 where there is one
-size_t wa_diff_dq_floats(const WaDiffLaunch& a, const WaDiffSide& s);
-size_t wa_diff_dkv_floats(const WaDiffLaunch& a, const WaDiffSide& s);
+// Partial tiles of a side: of its parts, or of its tasks; 0 where no tile is cut.
+int64_t wa_diff_side_tiles(const WaDiffSide& s, bool masked);
 
 hipError_t wa_launch_diff_attn(const WaDiffLaunch& a, hipStream_t stream);
 hipError_t wa_launch_diff_backward(const WaDiffLaunch& a, hipStream_t stream);

@@ -86,17 +86,33 @@ __device__ __forceinline__ void copy_tile(const unsigned char* tile, const unsig
   }
 }
 
-// Unit and tile number `turn`. Masked calls go by their order, or unit after unit. Others take the tiles of `group` units in turn,
-// tile after tile, then those of the next units: workgroups go round the eight XCDs, so with eight units each XCD's cache holds the
-// other side of one; causal ones take all units, so that long tiles come first (forward and dQ of 2 x 16 heads of 2,048 tokens
-// 96 and 101 us, by eights 97 and 122).
-__device__ __forceinline__ void deal(const WaDiffLaunch& a, int turn, int tiles, int units, int* unit, int* tile) {
-  if (a.order) turn = a.order[turn];
+// What a workgroup computes: chunk `chunk` of the `chunks` of a tile of a unit (a head or key head of a sequence).
+struct Task {
+  int unit, tile, chunk, chunks;
+  int64_t item, part;  // the tile's number, and the chunk's among the partial results
+};
+// The workgroup's task; false if there is none. Without a list of tasks, the chunks of a tile together, and the tiles of `group` units
+// in turn, tile after tile (backwards: from the last), then those of the next units: workgroups go round the eight XCDs, so with
+// eight units each XCD's cache holds the other side of one; causal ones take all units, so that long tiles come first (forward and
+// dQ of 2 x 16 heads of 2,048 tokens 77 and 90 us, by eights 97 and 122); masked ones go unit after unit.
+__device__ __forceinline__ bool take_task(const WaDiffLaunch& a, int tiles, int units, int chunks, bool backwards, Task* t) {
+  if (a.tasks) {
+    if ((int)blockIdx.x >= a.tasks[0]) return false;
+    const int4 e = ((const int4*)(a.tasks + wa_diff_task_list(a.task_items)))[blockIdx.x];
+    *t = {e.x / tiles, e.x % tiles, e.y, e.z, e.x, e.w + e.y};
+    return true;
+  }
+  int turn = blockIdx.x / chunks;
   const int group = a.mask ? 1 : a.causal ? units : 8;
   const int first = turn / (tiles * group) * group, count = min(group, units - first);
   turn -= first * tiles;
-  *unit = first + turn % count;
-  *tile = turn / count;
+  t->unit = first + turn % count;
+  t->tile = backwards ? tiles - 1 - turn / count : turn / count;
+  t->chunk = blockIdx.x % chunks;
+  t->chunks = chunks;
+  t->item = (int64_t)t->unit * tiles + t->tile;
+  t->part = t->item * chunks + t->chunk;
+  return true;
 }
 
 // Keys that exist for sequence b, and the first query's position; both clamped, so that no value of the device
@@ -129,14 +145,30 @@ struct MaskWalk {
   int entries = 0, word_i = -1;
   uint64_t word = 0;
 
+  __device__ __forceinline__ void load(int w, int lane) {
+    if (w == word_i) return;
+    word_i = w;
+    const int e = w * 64 + lane;
+    word = __ballot(e < entries && at[e * step] != 0);
+  }
+  // Kept entry number k, or `entries` if there are fewer.
+  __device__ __forceinline__ int nth(int k, int lane) {
+    for (int w = 0; w * 64 < entries; ++w) {
+      load(w, lane);
+      const int n = __popcll(word);
+      if (k < n) {
+        uint64_t rest = word;
+        for (; k > 0; --k) rest &= rest - 1;
+        return w * 64 + __builtin_ctzll(rest);
+      }
+      k -= n;
+    }
+    return entries;
+  }
   // First kept entry at or past j, or a value >= entries.
   __device__ __forceinline__ int next(int j, int lane) {
     while (j < entries) {
-      if (j >> 6 != word_i) {
-        word_i = j >> 6;
-        const int e = word_i * 64 + lane;
-        word = __ballot(e < entries && at[e * step] != 0);
-      }
+      load(j >> 6, lane);
       const uint64_t rest = word >> (j & 63);
       if (rest) return j + __builtin_ctzll(rest);
       j = (word_i + 1) * 64;
@@ -165,6 +197,26 @@ __device__ __forceinline__ RowStats row_stats(float top, float l, float big) {
 __device__ __forceinline__ float steps_per_unit(float step) { return step > 1e-37f ? 1.f / step : 0.f; }
 __device__ __forceinline__ uint32_t pack_steps(float x, float y, float per_step) {
   return (uint32_t)(uint16_t)(int16_t)rintf(x * per_step) | (uint32_t)(uint16_t)(int16_t)rintf(y * per_step) << 16;
+}
+
+// The keys [*lo, *hi) of a chunk of a row tile that sees keys below `most`: of a listed task an equal number of the row's kept blocks,
+// else equal ranges of whole blocks and tiles of KB.
+template <int KB>
+__device__ __forceinline__ void chunk_keys(const WaDiffLaunch& a, const Task& t, MaskWalk& walk, int most, int lane, int* lo, int* hi) {
+  *lo = 0;
+  *hi = most;
+  if (t.chunks == 1) return;
+  if (a.tasks) {
+    const int shift = a.block == 128 ? 7 : 6, kept = a.tasks[4 + t.item];
+    walk.entries = a.nb;
+    if (t.chunk > 0) *lo = min(walk.nth(kept * t.chunk / t.chunks, lane) << shift, most);
+    if (t.chunk + 1 < t.chunks) *hi = min(walk.nth(kept * (t.chunk + 1) / t.chunks, lane) << shift, most);
+    walk.word_i = -1;
+    return;
+  }
+  const int unit = a.mask ? max(a.block, KB) : KB, per = ((most + unit - 1) / unit + t.chunks - 1) / t.chunks;
+  *lo = min((int64_t)t.chunk * per * unit, (int64_t)most);
+  *hi = min((int64_t)*lo + per * unit, (int64_t)most);
 }
 
 // The value of lane % 32 and that of lane % 32 + 32. In assembly: the compiler reads both results of its builtin from
