@@ -434,8 +434,8 @@ typedef struct wa_diff_options {
   int32_t causal;       /* nonzero: query i of sequence b sees the keys j <= q_start[b] + i */
 } wa_diff_options;
 
-/* Workspace bytes needed by wa_diff_attn: partial results of calls with few rows, whose keys are split over
- * workgroups; 0 for others. Calls that share a workspace must not overlap, captured ones included. */
+/* Workspace bytes needed by wa_diff_attn, with or without a mask: the float32 results of tiles whose keys are split over
+ * workgroups (about 135 MB at most) and the order of a mask's tiles; 0 for some shapes. Calls that share a workspace must not overlap, captured ones included. */
 wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes);
 
 /* Differential attention forward: head h has two softmax maps over the same kept keys,

@@ -14,7 +14,7 @@ struct WaDiffLaunch {
   const int32_t* kv_lens;  // [batch], null: kv_len
   void* o;            // bf16 [batch][heads][q_len][value_dim]
   int16_t* maps;      // [batch][2 heads][q_len][value_dim]: P_m V in steps of its row's, nullable
-  float* stats;       // [batch][2 heads][q_len][3]: log-sum-exp, step, correction (diff_tiles.h), with maps
+  float* stats;       // [batch][2 heads][q_len][3]: log-sum-exp, step, factor (diff_tiles.h), with maps
   int32_t* tasks;     // workspace of masked calls (see wa_diff_task_ints); null: tiles are dealt out by number
   int32_t task_items; // tiles that `tasks` is about
   float* part;        // workspace of split calls: part_tiles partial tiles, then (forward) their statistics
@@ -31,7 +31,7 @@ struct WaDiffLaunch {
   double* lam_part;   // workspace: [batch][heads][tiles of q_len][parts] partial sums for dlam
 };
 
-// How a forward call is cut into workgroups (see diff_plan in diff_attn.hip).
+// How a forward call is cut into workgroups (see wa_diff_plan in diff_attn.hip).
 struct WaDiffPlan {
   int32_t waves;   // wavefronts a map of a workgroup, 32 query rows each: 1, 2 or 4
   int32_t packed;  // 1: the rows of a tile run over the queries of all heads of a key head
