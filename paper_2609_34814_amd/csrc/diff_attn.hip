@@ -55,7 +55,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   const int map = w / W, slice = w % W;
 
   Task task;
-  if (!take_task(a, p.tiles, p.units, p.splits, a.causal, &task)) return;
+  if (!take_task<D == 64 && DV == 64 ? 2 : 1>(a, p.tiles, p.units, p.splits, a.causal, &task)) return;
   const int unit = task.unit, tile = task.tile;
   const int per_key_head = a.heads / a.kv_heads;
   const int heads = p.packed ? a.kv_heads : a.heads;

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   Task task;
-  if (!take_task(a, n.tiles, a.batch * a.heads, n.parts, a.causal, &task)) return;
+  if (!take_task<kDqWaves<D>>(a, n.tiles, a.batch * a.heads, n.parts, a.causal, &task)) return;
   const int bh = task.unit, tile = task.tile, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
   const int i0 = tile * 32 * W + w * 32, i = i0 + l32, i_last = a.q_len - 1;
   const bool valid = i <= i_last;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
 
   // the first tiles, which the most queries see, come first where that differs
   Task task;
-  if (!take_task(a, n.tiles, a.batch * a.kv_heads, n.parts, false, &task)) return;
+  if (!take_task<kDkvWaves<D>>(a, n.tiles, a.batch * a.kv_heads, n.parts, false, &task)) return;
   const int bh = task.unit, tile = task.tile, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
   const int keys = keys_of(a, b), start = start_of(a, b);
   const int k0 = tile * 32 * W + w * 32, kj = k0 + l32;

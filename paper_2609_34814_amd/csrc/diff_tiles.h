@@ -91,10 +91,12 @@ struct Task {
   int unit, tile, chunk, chunks;
   int64_t item, part;  // the tile's number, and the chunk's among the partial results
 };
-// The workgroup's task; false if there is none. Without a list of tasks, the chunks of a tile together, and the tiles of `group` units
-// in turn, tile after tile (backwards: from the last), then those of the next units: workgroups go round the eight XCDs, so with
-// eight units each XCD's cache holds the other side of one; causal ones take all units, so that long tiles come first (forward and
-// dQ of 2 x 16 heads of 2,048 tokens 77 and 90 us, by eights 97 and 122); masked ones go unit after unit.
+// The workgroup's task; false if there is none. PER_CU: workgroups that a compute unit holds. Without a list of tasks, the chunks of a
+// tile together, and the tiles of `group` units in turn, tile after tile (backwards: from the last), then those of the next units:
+// workgroups go round the eight XCDs, so with eight units each XCD's cache holds the other side of one; causal ones take all units, so
+// that long tiles come first (forward and dQ of 2 x 16 heads of 2,048 tokens 77 and 90 us, by eights 97 and 122); masked ones go unit
+// after unit.
+template <int PER_CU>
 __device__ __forceinline__ bool take_task(const WaDiffLaunch& a, int tiles, int units, int chunks, bool backwards, Task* t) {
   if (a.tasks) {
     if ((int)blockIdx.x >= a.tasks[0]) return false;
@@ -102,13 +104,17 @@ __device__ __forceinline__ bool take_task(const WaDiffLaunch& a, int tiles, int 
     *t = {e.x / tiles, e.x % tiles, e.y, e.z, e.x, e.w + e.y};
     return true;
   }
-  int turn = blockIdx.x / chunks;
+  int id = blockIdx.x;
+  // Causal tiles that all run at once, two a compute unit: the second ones shortest first, so that long ones share with short ones
+  // (2 x 16 heads of 2,048 tokens, d 64, values 64: forward 61 -> 55 us, dQ 83 -> 80; 24 heads 57 -> 51, 80 -> 75).
+  if (PER_CU == 2 && a.causal && !a.mask && gridDim.x <= 512 && id >= 256) id = 255 + gridDim.x - id;
+  int turn = id / chunks;
   const int group = a.mask ? 1 : a.causal ? units : 8;
   const int first = turn / (tiles * group) * group, count = min(group, units - first);
   turn -= first * tiles;
   t->unit = first + turn % count;
   t->tile = backwards ? tiles - 1 - turn / count : turn / count;
-  t->chunk = blockIdx.x % chunks;
+  t->chunk = id % chunks;
   t->chunks = chunks;
   t->item = (int64_t)t->unit * tiles + t->tile;
   t->part = t->item * chunks + t->chunk;

@@ -9,7 +9,8 @@ torch = pytest.importorskip("torch")
 import paper_2609_34814_amd as W                                     # noqa: E402
 from paper_2609_34814_amd import _lib as L                           # noqa: E402
 from tests.test_abi import FAKE, _lib                                # noqa: E402
-from tests.test_diff_attn import DIMS, INVALID, ALIGN, WORK, UNSUP, _host, _shape, block_mask, make, reference  # noqa: E402
+from tests.test_diff_attn import (DIMS, INVALID, ALIGN, WORK, UNSUP, _host, _shape, block_mask, check_forward,  # noqa: E402
+                                  make, reference)
 
 
 def test_argument_refusals():
@@ -111,6 +112,14 @@ def test_masked_tiles_in_order_of_length(b, h, hk, block):
 def test_tiles_in_parts(d, dv, causal, h, hk, m, n):
     """Few tiles, so that each is computed in parts; of grouped heads they begin and end inside a head's queries."""
     check_gradient(make(1, h, hk, m, n, d, dv), causal=causal)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("h,m", [(86, 300), (101, 300), (128, 470), (129, 470)])
+def test_causal_tiles_that_run_at_once(h, m):
+    """257 to 512 tiles, of which the second ones of a compute unit run in the other order, and more."""
+    check_gradient(make(1, h, h, m, m, 64, 64), causal=True)
+    check_forward(make(1, h, h, m, m, 64, 64), causal=True)
 
 
 @pytest.mark.gpu
