@@ -9,6 +9,9 @@
 // maps with their accumulators in registers (for d 128 one wavefront a SIMD, which may use 512), and the other side's tiles pass
 // through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are.
+// What bounds it (d 128): of a wavefront's time 60% is instructions issued one after another (16 cycles a product, 4 to 8 a vector
+// instruction, 6 of those a product), 20% waits for the matrix core and 18% for LDS and barriers; the matrix cores are busy 38%. One
+// map a wavefront, so that two share a SIMD, makes a fifth to a third more products (dP twice) and is no faster.
 // dlam is the sum of D_2 from the stored maps and of the float32 P_2 (dP - D_2), which takes their steps' error back: over a
 // lane's keys with the roundings carried along, over queries in float64.
 
@@ -54,6 +57,31 @@ __device__ __forceinline__ void fill(f32x16& x, float f) {
 }
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// Products whose results the vector unit reads. A kernel of one wavefront a SIMD has its accumulators in the 256 accumulation
+// registers, and the compiler puts every product's result there: the scores and dP would be moved out one by one, and where the
+// accumulators fill them (d 128, values 256) three of those to and fro as well, 96 moves beside 64 products. Written out, these
+// results are in vector registers (dK and dV of 2 x 8 heads of 4,096 tokens, d 128, values 256: 670 -> 619 us; values 128, 16 heads:
+// 1,033 -> 1,011; dQ 860 -> 846). The compiler does not see these products' latency: two wait states stand before each, for an
+// operand that the vector unit has just written, and settled() has to stand before a result is read (12 states, 8 passes).
+template <int WAVES, bool ZERO>
+__device__ __forceinline__ void product(bf16x8 a, bf16x8 b, f32x16& c) {
+  if constexpr (WAVES > 1) {
+    if constexpr (ZERO) fill(c, 0.f);
+    c = mfma(a, b, c);
+  } else if constexpr (ZERO) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b));
+  } else {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+&v"(c) : "v"(a), "v"(b));
+  }
+}
+template <int WAVES>
+__device__ __forceinline__ void settled(f32x16& c) {
+  if constexpr (WAVES == 1) asm volatile("s_nop 11" : "+v"(c));
+}
+template <int WAVES>
+__device__ __forceinline__ void settled(f32x16& c, f32x16& d) {
+  if constexpr (WAVES == 1) asm volatile("s_nop 11" : "+v"(c), "+v"(d));
 }
 // Registers 8 s to 8 s + 7 of a product as an operand over its rows.
 __device__ __forceinline__ bf16x8 pack8(const float* p) {
@@ -205,9 +233,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     };
     constexpr int ROWS = 2 * C::KS + C::VS, COLS = 4 * C::DT;
     f32x16 s[2], dp;
-    fill(s[0], 0.f);
-    fill(s[1], 0.f);
-    fill(dp, 0.f);
+    constexpr int WV = kDqWaves<D>;
     float p[2][16];
     bf16x8 ring[AHEAD];
 #pragma unroll
@@ -215,10 +241,15 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
 #pragma unroll
     for (int x = 0; x < ROWS; ++x) {
       in_order<kDqWaves<D>>();
-      if (x < 2 * C::KS)
-        s[x & 1] = mfma(ring[x % AHEAD], qf[x & 1][x >> 1], s[x & 1]);
+      if (x < 2)
+        product<WV, true>(ring[x % AHEAD], qf[x & 1][x >> 1], s[x & 1]);
+      else if (x < 2 * C::KS)
+        product<WV, false>(ring[x % AHEAD], qf[x & 1][x >> 1], s[x & 1]);
+      else if (x == 2 * C::KS)
+        product<WV, true>(ring[x % AHEAD], dof[x - 2 * C::KS], dp);
       else
-        dp = mfma(ring[x % AHEAD], dof[x - 2 * C::KS], dp);
+        product<WV, false>(ring[x % AHEAD], dof[x - 2 * C::KS], dp);
+      if (x == 2 * C::KS) settled<WV>(s[0], s[1]);
       if (x + AHEAD < ROWS) ring[x % AHEAD] = row(x + AHEAD);
       if (x >= 2 * C::KS) {  // the exponentials run beside the products of dP
         constexpr int PER = 32 / C::VS;
@@ -232,6 +263,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     bf16x8 cring[CAHEAD];
 #pragma unroll
     for (int x = 0; x < CAHEAD; ++x) cring[x] = col(x);
+    settled<WV>(dp);
     if (masked) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
@@ -477,6 +509,7 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
         s[1][4 * q4 + e] = st[QB + 8 * q4 + e];
         dp[4 * q4 + e] = st[2 * QB + 8 * q4 + e];
       }
+    constexpr int WV = kDkvWaves<D>;
     float p[2][16], pc[16];
     bf16x8 ring[AHEAD], vring[AHEAD];
 #pragma unroll
@@ -485,9 +518,10 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
     for (int x = 0; x < ROWS; ++x) {
       in_order<kDkvWaves<D>>();
       if (x < 2 * C::KS)
-        s[x & 1] = mfma(ring[x % AHEAD], kf[x & 1][x >> 1], s[x & 1]);
+        product<WV, false>(ring[x % AHEAD], kf[x & 1][x >> 1], s[x & 1]);
       else
-        dp = mfma(ring[x % AHEAD], kValuesInLds ? vring[x % AHEAD] : vf[kValuesInLds ? 0 : x - 2 * C::KS], dp);
+        product<WV, false>(ring[x % AHEAD], kValuesInLds ? vring[x % AHEAD] : vf[kValuesInLds ? 0 : x - 2 * C::KS], dp);
+      if (x == 2 * C::KS) settled<WV>(s[0], s[1]);
       if (x + AHEAD < ROWS) {
         ring[x % AHEAD] = row(x + AHEAD);
         if (kValuesInLds && x + AHEAD >= 2 * C::KS) vring[x % AHEAD] = value(x + AHEAD - 2 * C::KS);
@@ -509,6 +543,7 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
     bf16x8 cring[CAHEAD];
 #pragma unroll
     for (int x = 0; x < CAHEAD; ++x) cring[x] = col(x);
+    settled<WV>(dp);
     if (masked) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
