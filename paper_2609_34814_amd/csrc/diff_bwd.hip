@@ -9,11 +9,12 @@
 // maps with their accumulators in registers (for d 128 one wavefront a SIMD, which may use 512), and the other side's tiles pass
 // through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are.
-// What bounds it (d 128): of a wavefront's time 60% is instructions issued one after another (16 cycles a product, 4 to 8 a vector
-// instruction, 6 of those a product), 20% waits for the matrix core and 18% for LDS and barriers; the matrix cores are busy 38%. One
-// map a wavefront, so that two share a SIMD, makes a fifth to a third more products (dP twice) and is no faster.
 // dlam is the sum of D_2 from the stored maps and of the float32 P_2 (dP - D_2), which takes their steps' error back: over a
 // lane's keys with the roundings carried along, over queries in float64.
+// What bounds it (d 128, values 256, 2 x 8 heads of 4,096 tokens): dQ 429 and dK with dV 564 us where each runs alone at 2.3 GHz
+// (matrix cores 40% busy; a wavefront issues 55% of its time, waits 20% for the matrix core and 25% for LDS, copies and barriers),
+// 497 and 694 one after another, when the power limit lowers the clock. One map a wavefront, so that two share a SIMD, makes a
+// fifth to a third more products (dP twice) and is no faster.
 
 #include "diff_tiles.h"
 #include "wavealign.h"
