@@ -351,6 +351,7 @@ __device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, const uns
   asm volatile(
       "s_mov_b32 %0, m0\n\t"
       "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
       "global_load_lds_dword %2, %3\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)
