@@ -118,13 +118,14 @@ struct Cfg {
 // One 16-byte-per-lane copy from global memory (uniform base + per-lane byte offset) into LDS at the
 // uniform address lds (lane i writes lds + 16 i). Written as inline assembly so that only the
 // explicit vmcnt waits of the pipeline order it against LDS reads of the other tile; M0 (the LDS
-// base of the copy) is restored afterwards.
+// base of the copy), which a copy may read one wait state after it is written, is restored afterwards.
 __device__ __forceinline__ void dma16(const void* gbase, uint32_t voff, const unsigned char* lds) {
   const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds);
   uint32_t saved;
   asm volatile(
       "s_mov_b32 %0, m0\n\t"
       "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
       "global_load_lds_dwordx4 %2, %3\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)

@@ -50,7 +50,7 @@ def test_the_check_sees_faults():
 
 
 @pytest.mark.skipif(not os.path.exists("/opt/rocm/bin/hipcc"), reason="no compiler")
-@pytest.mark.parametrize("source", ["diff_attn.hip", "diff_bwd.hip"])
+@pytest.mark.parametrize("source", ["diff_attn.hip", "diff_bwd.hip", "attn_fwd.hip"])
 def test_copies(source, tmp_path):
     out = tmp_path / "listing.s"
     flags = [x for x in build.COMMON + build.SOURCES[source] if x != "-fPIC"]
