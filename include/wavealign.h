@@ -443,7 +443,8 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
  * A key j of sequence b is kept for query i if j < kv_lens[b], the mask keeps its block, and, with
  * `causal`, j <= q_start[b] + i. A query with no kept key gets O = 0 and a sum-exp of -inf. bf16 inputs, float32
  * scores, sums and O, probabilities rounded to bf16 for the product with V, bf16 output.
- * Values must be finite in the keys below kv_lens[b]; memory past them is not used, whatever it holds.
+ * Values must be finite in the keys below kv_lens[b], with `causal` of those up to the last query's; memory past them
+ * (room of a cache that is not written yet) and blocks that the masks drop are not used, whatever they hold.
  *   q        bf16 [B][2H][q_len][d], 16-byte aligned: the maps of head h are 2h and 2h + 1
  *   k        bf16 [B][2Hk][kv_len][d], likewise
  *   v        bf16 [B][Hk][kv_len][value_dim]
@@ -474,8 +475,8 @@ wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_
  *   dQ_m = scale dS_m K_m, dK_m = sum of scale dS_m^T Q_m, dlam[h] = -sum over b, i of dO_i . (P_2 V)_i,
  *   dS_1 = P_1 (dP - dO . O_1), dS_2 = -lam P_2 (dP - dO . O_2), dP = dO V^T,
  * probabilities recomputed in float32 from stats, sums in float32 (dlam over queries in float64), P and dS rounded to
- * bf16 for the matrix products. Every output is overwritten; keys at or past kv_lens[b] get 0, and so do queries
- * with no kept key. Nothing is added with atomics: equal calls give equal bits.
+ * bf16 for the matrix products. Every output is overwritten; keys at or past kv_lens[b] or behind the last
+ * query's limit get 0, and so do queries with no kept key. Nothing is added with atomics: equal calls give equal bits.
  *   dout     bf16 [B][H][q_len][value_dim], 16-byte aligned
  *   q, k, v, lam, mask, q_start, kv_lens, shape, options   as given to wa_diff_attn
  *   maps, stats  what that call wrote

@@ -556,8 +556,9 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
               2h and 2h + 1, and H / Hk heads in a row share keys and values
     lam       float32 [H]
     mask      uint8 or bool [B][H][ceil(M/block)][ceil(N/block)] of kept blocks; None keeps all
-    causal    query i of sequence b sees the keys up to q_start[b] + i (q_start int32 [B]; None: N - M)
-    kv_lens   int32 [B]: keys each sequence holds; what lies behind them is not used
+    causal    query i of sequence b sees the keys up to q_start[b] + i (q_start int32 [B]; None: N - M); what lies behind
+              the last query's is not used
+    kv_lens   int32 [B]: keys each sequence holds; what lies behind them is not used, all before has to be finite
     return_stats  also (maps, stats), which diff_attn_backward takes: each P_m V int16 [B][2H][M][dv] in steps of 1/32767 of
               its row's largest magnitude, and float32 [B][2H][M][3]: the log-sum-exp of the scaled scores, the step, and a
               factor of roundings"""
@@ -592,7 +593,7 @@ def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
                        q_start: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None,
                        workspace: Optional[torch.Tensor] = None):
     """(dq, dk, dv bf16, dlam float32) from dout, the gradient of diff_attn's O: the other arguments as that call had
-    them, maps and stats as it returned them with return_stats. Keys past kv_lens get 0. Equal calls give equal bits."""
+    them, maps and stats as it returned them with return_stats. Keys past kv_lens, or behind every query, get 0. Equal calls give equal bits."""
     lib = L.load()
     shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)
     want = (shape.batch, shape.heads, shape.q_len, shape.value_dim)

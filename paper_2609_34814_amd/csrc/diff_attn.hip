@@ -74,7 +74,7 @@ __global__ __launch_bounds__(128 * W, 2) void diff_fwd_kernel(const WaDiffLaunch
   const bool valid = p.packed ? sub < per_key_head : i < a.q_len;
 
   // limits: of this lane's query, of the wavefront's (all below `some`, all at or past `all`), of the workgroup's
-  const int keys = keys_of(a, b), start = start_of(a, b);
+  const int start = start_of(a, b), keys = keys_of(a, b, start);
   const int limit = valid ? key_limit(a, keys, start, i) : 0;
   const int i0 = tile * 32 * W + slice * 32;  // not packed: the wavefront's first query
   const int i_last = a.q_len - 1;

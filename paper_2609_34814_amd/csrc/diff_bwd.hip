@@ -135,7 +135,7 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
   const int bh = task.unit, tile = task.tile, b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
   const int i0 = tile * 32 * W + w * 32, i = i0 + l32, i_last = a.q_len - 1;
   const bool valid = i <= i_last;
-  const int keys = keys_of(a, b), start = start_of(a, b);
+  const int start = start_of(a, b), keys = keys_of(a, b, start);
   const int limit = valid ? key_limit(a, keys, start, i) : 0;
   const int some = i0 > i_last ? 0 : key_limit(a, keys, start, min(i0 + 31, i_last));
   const int all = key_limit(a, keys, start, min(i0, i_last));
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
   Task task;
   if (!take_task<kDkvWaves<D>>(a, n.tiles, a.batch * a.kv_heads, n.parts, false, &task)) return;
   const int bh = task.unit, tile = task.tile, b = bh / a.kv_heads, hk = bh % a.kv_heads, per_key_head = a.heads / a.kv_heads;
-  const int keys = keys_of(a, b), start = start_of(a, b);
+  const int start = start_of(a, b), keys = keys_of(a, b, start);
   const int k0 = tile * 32 * W + w * 32, kj = k0 + l32;
   const bool valid = kj < keys;
   // first query that sees this lane's key, the wavefront's first key, its last, the workgroup's first
@@ -626,7 +626,7 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
     store_part(to, dk[0], a.scale, hf);
     store_part(to + D, dk[1], a.scale, hf);
     store_part(to + 2 * D, dv, 1.f, hf);
-  } else if (kj < a.kv_len) {  // keys that the sequence does not hold get 0
+  } else if (kj < a.kv_len) {  // keys that the sequence does not hold, or no query sees, get 0
     store_row((uint16_t*)a.dk + krow0 * D, dk[0], a.scale, hf);
     store_row((uint16_t*)a.dk + (krow0 + a.kv_len) * D, dk[1], a.scale, hf);
     store_row((uint16_t*)a.dv + vrow * DV, dv, 1.f, hf);

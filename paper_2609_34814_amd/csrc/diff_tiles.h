@@ -123,17 +123,19 @@ __device__ __forceinline__ bool take_task(const WaDiffLaunch& a, int tiles, int 
   return true;
 }
 
-// Keys that exist for sequence b, and the first query's position; both clamped, so that no value of the device
-// arrays leads out of a tensor.
-__device__ __forceinline__ int keys_of(const WaDiffLaunch& a, int b) {
-  return a.kv_lens ? min(max(a.kv_lens[b], 0), a.kv_len) : a.kv_len;
-}
+// The first query's position, taken so that no value of the device array leads out of a tensor.
 __device__ __forceinline__ int start_of(const WaDiffLaunch& a, int b) {
   return a.q_start ? min(max(a.q_start[b], -a.q_len), a.kv_len) : a.kv_len - a.q_len;
 }
 // Query i sees the keys below this.
 __device__ __forceinline__ int key_limit(const WaDiffLaunch& a, int keys, int start, int i) {
   return a.causal ? min(keys, max(start + i + 1, 0)) : keys;
+}
+// Keys of sequence b that its last query may see, so that any does: those behind them are neither read nor part of a tile, whatever
+// they hold.
+__device__ __forceinline__ int keys_of(const WaDiffLaunch& a, int b, int start) {
+  const int keys = a.kv_lens ? min(max(a.kv_lens[b], 0), a.kv_len) : a.kv_len;
+  return key_limit(a, keys, start, a.q_len - 1);
 }
 
 // A pointer that is the same in every lane, as scalar registers (the builtin returns signed words).
