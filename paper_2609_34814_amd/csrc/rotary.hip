@@ -23,6 +23,7 @@ constexpr int kThreads = 256;
 // Heads a thread walks over, at most; fewer while the launch would leave compute units empty.
 constexpr int kMaxHeads = 16;
 constexpr int64_t kFullThreads = 256 * 1024;  // four wavefronts a SIMD on 256 compute units
+constexpr int64_t kMaxGrid = 1 << 22;
 
 template <typename T>
 struct Chunk;  // 16 bytes <-> floats
@@ -98,7 +99,8 @@ template <typename T, typename C, bool ILV, typename W>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const WaRotaryLaunch a, int rot_units, int units, int per,
                                                           W threads) {
   constexpr int V = C::N;
-  const W id = (W)blockIdx.x * kThreads + threadIdx.x;
+  W id = (W)blockIdx.x * kThreads + threadIdx.x;
+  if constexpr (sizeof(W) == 8) id += (W)blockIdx.y * gridDim.x * kThreads;
   if (id >= threads) return;
   const int unit = (int)(id % (W)units);
   W rest = id / (W)units;
@@ -153,13 +155,15 @@ hipError_t launch_units(const WaRotaryLaunch& a, hipStream_t stream) {
   const int per = (int)std::min<int64_t>(kMaxHeads, std::max<int64_t>(1, rows * heads / kFullThreads));
   const int64_t threads = rows * ((heads + per - 1) / per);
   const int64_t grid = (threads + kThreads - 1) / kThreads;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (threads < ((int64_t)1 << 31))
+  if (threads < ((int64_t)1 << 31)) {
     hipLaunchKernelGGL((rotary_kernel<T, C, ILV, uint32_t>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a, rot, units,
                        per, (uint32_t)threads);
-  else
-    hipLaunchKernelGGL((rotary_kernel<T, C, ILV, uint64_t>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a, rot, units,
-                       per, (uint64_t)threads);
+  } else {
+    // a dimension of a launch holds fewer than 2^32 threads, so rows of kMaxGrid workgroups
+    const dim3 rows_of((unsigned)kMaxGrid, (unsigned)((grid + kMaxGrid - 1) / kMaxGrid));
+    hipLaunchKernelGGL((rotary_kernel<T, C, ILV, uint64_t>), rows_of, dim3(kThreads), 0, stream, a, rot, units, per,
+                       (uint64_t)threads);
+  }
   return hipGetLastError();
 }
 
