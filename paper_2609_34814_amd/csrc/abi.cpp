@@ -328,6 +328,27 @@ wa_status check_diff_shape(const wa_diff_shape* s, WaDiffLaunch* out) {
   return WA_OK;
 }
 
+// A dimension of a launch holds fewer than 2^32 threads: whether a call of either direction, with or without a mask, stays below.
+wa_status check_diff_grid(int64_t workgroups, int threads) {
+  if (workgroups * threads < (int64_t(1) << 32)) return WA_OK;
+  return fail(WA_ERR_UNSUPPORTED, "%lld workgroups of %d threads exceed a launch", (long long)workgroups, threads);
+}
+wa_status check_diff_forward(const wa_diff_shape* shape, WaDiffLaunch* a) {
+  wa_status s = check_diff_shape(shape, a);
+  for (int masked = 0; masked < 2 && s == WA_OK; ++masked) {
+    const WaDiffPlan p = wa_diff_plan(*a, masked);
+    s = check_diff_grid((int64_t)p.units * p.tiles * p.splits, 128 * p.waves);
+  }
+  return s;
+}
+wa_status check_diff_backward(const wa_diff_shape* shape, WaDiffLaunch* a) {
+  wa_status s = check_diff_shape(shape, a);
+  for (int masked = 0; masked < 2 && s == WA_OK; ++masked)
+    for (const WaDiffSide& side : {wa_diff_dq_side(*a, masked), wa_diff_dkv_side(*a, masked)})
+      if (s == WA_OK) s = check_diff_grid(side.items * side.parts, 64 * side.waves);
+  return s;
+}
+
 // Forward: the task list of a masked call, then the results of split tiles.
 size_t diff_task_bytes(const WaDiffLaunch& a) {
   const WaDiffPlan p = wa_diff_plan(a, true);
@@ -786,7 +807,7 @@ wa_status wa_rotary_frequencies(int32_t pairs, double base, const wa_rotary_scal
 
 wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes) {
   WaDiffLaunch a{};
-  wa_status s = check_diff_shape(shape, &a);
+  wa_status s = check_diff_forward(shape, &a);
   if (s != WA_OK) return s;
   if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
   *bytes = diff_ws_bytes(a);
@@ -798,7 +819,7 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
                        const wa_diff_options* options, void* o, int16_t* maps, float* stats, void* workspace,
                        size_t workspace_bytes, void* stream) {
   WaDiffLaunch a{};
-  wa_status s = check_diff_shape(shape, &a);
+  wa_status s = check_diff_forward(shape, &a);
   if (s != WA_OK) return s;
   s = check_diff_args(q, k, v, lam, mask, q_start, kv_lens, options, &a);
   if (s != WA_OK) return s;
@@ -818,7 +839,7 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
 
 wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_t* bytes) {
   WaDiffLaunch a{};
-  wa_status s = check_diff_shape(shape, &a);
+  wa_status s = check_diff_backward(shape, &a);
   if (s != WA_OK) return s;
   if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
   *bytes = diff_backward_ws(a).total;
@@ -831,7 +852,7 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
                                 const wa_diff_options* options, void* dq, void* dk, void* dv, float* dlam,
                                 void* workspace, size_t workspace_bytes, void* stream) {
   WaDiffLaunch a{};
-  wa_status s = check_diff_shape(shape, &a);
+  wa_status s = check_diff_backward(shape, &a);
   if (s != WA_OK) return s;
   s = check_diff_args(q, k, v, lam, mask, q_start, kv_lens, options, &a);
   if (s != WA_OK) return s;
