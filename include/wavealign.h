@@ -430,7 +430,7 @@ typedef struct wa_diff_shape {
 } wa_diff_shape;
 
 typedef struct wa_diff_options {
-  float softmax_scale;  /* <= 0 selects 1/sqrt(head_dim); at least 1e-30 */
+  float softmax_scale;  /* finite; <= 0 selects 1/sqrt(head_dim); else 1e-30..1e30 */
   int32_t causal;       /* nonzero: query i of sequence b sees the keys j <= q_start[b] + i */
 } wa_diff_options;
 
@@ -442,7 +442,7 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
  *   P_m = softmax(scale Q_m K_m^T), m = 1, 2,   O = P_1 V - lam[h] P_2 V.
  * A key j of sequence b is kept for query i if j < kv_lens[b], the mask keeps its block, and, with
  * `causal`, j <= q_start[b] + i. A query with no kept key gets O = 0 and a sum-exp of -inf. bf16 inputs, float32
- * scores, sums and O, probabilities rounded to bf16 for the product with V, bf16 output.
+ * scores (so a probability is off by some 2^-24 of the row's largest scaled score), sums and O, probabilities rounded to bf16 for the product with V, bf16 output.
  * Values must be finite in the keys below kv_lens[b], with `causal` of those up to the last query's; memory past them
  * (room of a cache that is not written yet) and blocks that the masks drop are not used, whatever they hold.
  *   q        bf16 [B][2H][q_len][d], 16-byte aligned: the maps of head h are 2h and 2h + 1

@@ -546,6 +546,16 @@ def _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens):
     return diff_shape_of(b, h, hk, m, n, d, dv, block), mask
 
 
+def _diff_scale(scale: Optional[float]) -> float:
+    """The C ABI's softmax_scale, whose 0 is the default."""
+    if scale is None:
+        return 0.0
+    value = ctypes.c_float(scale).value
+    if not 0.0 < value < math.inf:
+        raise ValueError(f"scale must be positive and finite in float32 (None: 1 / sqrt(d)), got {scale}")
+    return value
+
+
 def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor, mask: Optional[torch.Tensor] = None,
               *, block: int = 128, scale: Optional[float] = None, causal: bool = False,
               q_start: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None, return_stats: bool = False,
@@ -556,6 +566,7 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
               2h and 2h + 1, and H / Hk heads in a row share keys and values
     lam       float32 [H]
     mask      uint8 or bool [B][H][ceil(M/block)][ceil(N/block)] of kept blocks; None keeps all
+    scale     positive; None: 1 / sqrt(d)
     causal    query i of sequence b sees the keys up to q_start[b] + i (q_start int32 [B]; None: N - M); what lies behind
               the last query's is not used
     kv_lens   int32 [B]: keys each sequence holds; what lies behind them is not used, all before has to be finite
@@ -563,6 +574,7 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
               its row's largest magnitude, and float32 [B][2H][M][3]: the log-sum-exp of the scaled scores, the step, and a
               factor of roundings"""
     lib = L.load()
+    softmax_scale = _diff_scale(scale)
     shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)
     want = (shape.batch, shape.heads, shape.q_len, shape.value_dim)
     _check(out, "out", torch.bfloat16, want)
@@ -576,7 +588,7 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
     rows = (want[0], 2 * want[1], want[2])
     maps = q.new_empty((*rows, want[3]), dtype=torch.int16) if return_stats else None
     stats = q.new_empty((*rows, 3), dtype=torch.float32) if return_stats else None
-    opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
+    opts = L.WaDiffOptions(softmax_scale, 1 if causal else 0)
     _call_on(index, lib.wa_diff_attn, _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(mask), _ptr(q_start), _ptr(kv_lens),
              ctypes.byref(shape), ctypes.byref(opts), _ptr(o), _ptr(maps), _ptr(stats), _ptr(workspace),
              0 if workspace is None else workspace.numel())
@@ -595,6 +607,7 @@ def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     """(dq, dk, dv bf16, dlam float32) from dout, the gradient of diff_attn's O: the other arguments as that call had
     them, maps and stats as it returned them with return_stats. Keys past kv_lens, or behind every query, get 0. Equal calls give equal bits."""
     lib = L.load()
+    softmax_scale = _diff_scale(scale)
     shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)
     want = (shape.batch, shape.heads, shape.q_len, shape.value_dim)
     rows = (want[0], 2 * want[1], want[2])
@@ -610,7 +623,7 @@ def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     if workspace is None or workspace.numel() < need:
         workspace = _workspace(need, q.device)
     dq, dk, dv, dlam = (torch.empty_like(t) for t in (q, k, v, lam))
-    opts = L.WaDiffOptions(float(scale or 0.0), 1 if causal else 0)
+    opts = L.WaDiffOptions(softmax_scale, 1 if causal else 0)
     _call_on(index, lib.wa_diff_attn_backward, _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(maps),
              _ptr(stats), _ptr(mask), _ptr(q_start), _ptr(kv_lens), ctypes.byref(shape), ctypes.byref(opts), _ptr(dq),
              _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), workspace.numel())

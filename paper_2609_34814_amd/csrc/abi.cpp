@@ -397,9 +397,11 @@ wa_status check_diff_args(const void* q, const void* k, const void* v, const flo
   a->q = q; a->k = k; a->v = v; a->lam = lam; a->mask = mask; a->q_start = q_start; a->kv_lens = kv_lens;
   a->causal = options->causal ? 1 : 0;
   const float scale = options->softmax_scale;
-  // the gradient divides log-sum-exps by it
-  if (scale > 0.f && scale < 1e-30f) return fail(WA_ERR_UNSUPPORTED, "softmax_scale %g is below 1e-30", scale);
-  a->scale = scale > 0.f && std::isfinite(scale) ? scale : (float)(1.0 / std::sqrt((double)a->head_dim));
+  if (!std::isfinite(scale)) return fail(WA_ERR_INVALID_ARG, "softmax_scale must be finite");
+  // the gradient divides log-sum-exps by it, and its product with log2 e is a float32
+  if (scale > 0.f && (scale < 1e-30f || scale > 1e30f))
+    return fail(WA_ERR_UNSUPPORTED, "softmax_scale %g is outside 1e-30..1e30", scale);
+  a->scale = scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)a->head_dim));
   return WA_OK;
 }
 

@@ -31,3 +31,28 @@ def _sizes(**kw):
 ])
 def test_workgroups_fit_a_launch(kw, want):
     assert _sizes(**kw) == want
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf")])
+def test_scales_that_are_no_numbers(scale):
+    lib, shape, opts = _lib(), _shape(), L.WaDiffOptions(scale, 0)
+    size = 1 << 40
+    assert lib.wa_diff_attn(*[FAKE] * 4, None, None, None, ctypes.byref(shape), ctypes.byref(opts), FAKE, None, None, FAKE, size,
+                            None) == INVALID
+    assert b"softmax_scale" in lib.wa_last_error()
+    assert lib.wa_diff_attn_backward(*[FAKE] * 7, None, None, None, ctypes.byref(shape), ctypes.byref(opts), *[FAKE] * 5, size,
+                                     None) == INVALID
+    assert b"softmax_scale" in lib.wa_last_error()
+    opts.softmax_scale = 2e30
+    assert lib.wa_diff_attn(*[FAKE] * 4, None, None, None, ctypes.byref(shape), ctypes.byref(opts), FAKE, None, None, FAKE, size,
+                            None) == UNSUP
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.125, 1e-50, float("nan"), float("inf"), 1e39])
+def test_scales_of_the_binding(scale):
+    """None is the default; another value that the kernels cannot take is not replaced by it."""
+    with pytest.raises(ValueError, match="scale"):
+        W.diff_attn(**_host(), scale=scale)
+    with pytest.raises(ValueError, match="scale"):
+        W.diff_attn_backward(torch.zeros(1, 2, 70, 64, dtype=torch.bfloat16), **_host(), mask=None,
+                             maps=torch.zeros(1, 4, 70, 64, dtype=torch.int16), stats=torch.zeros(1, 4, 70, 3), scale=scale)
