@@ -442,7 +442,8 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
  *   P_m = softmax(scale Q_m K_m^T), m = 1, 2,   O = P_1 V - lam[h] P_2 V.
  * A key j of sequence b is kept for query i if j < kv_lens[b], the mask keeps its block, and, with
  * `causal`, j <= q_start[b] + i. A query with no kept key gets O = 0 and a sum-exp of -inf. bf16 inputs, float32
- * scores (so a probability is off by some 2^-24 of the row's largest scaled score), sums and O, probabilities rounded to bf16 for the product with V, bf16 output.
+ * scores (so a probability is off by some 2^-24 of the row's largest scaled score), sums and O, probabilities
+ * rounded to bf16 for the product with V, bf16 output.
  * Values must be finite in the keys below kv_lens[b], with `causal` of those up to the last query's; memory past them
  * (room of a cache that is not written yet) and blocks that the masks drop are not used, whatever they hold.
  *   q        bf16 [B][2H][q_len][d], 16-byte aligned: the maps of head h are 2h and 2h + 1
@@ -459,6 +460,7 @@ wa_status wa_diff_attn_workspace_size(const wa_diff_shape* shape, size_t* bytes)
  *   stats    out float [B][2H][q_len][3], with maps: natural-log sum-exp of the map's scaled scores, the step, and the factor
  *            (1 but for roundings) from probabilities recomputed with that sum-exp to the exact ones
  *   workspace  >= wa_diff_attn_workspace_size(shape), 256-byte aligned; NULL if that is 0
+ * Outputs and workspace overlap neither inputs nor each other (refused).
  * How a call is cut into workgroups follows from its shape and mask, so equal calls give equal bits; how a head's sums
  * are split may depend on the masks of the other heads. At most 4096 blocks of queries and of keys. */
 wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float* lam, const uint8_t* mask,
@@ -482,7 +484,8 @@ wa_status wa_diff_attn_backward_workspace_size(const wa_diff_shape* shape, size_
  *   maps, stats  what that call wrote
  *   dq, dk, dv   out bf16, shaped as q, k and v, 16-byte aligned
  *   dlam         out float [H]
- *   workspace    >= wa_diff_attn_backward_workspace_size(shape), 256-byte aligned */
+ *   workspace    >= wa_diff_attn_backward_workspace_size(shape), 256-byte aligned
+ * Outputs and workspace overlap neither inputs nor each other (refused). */
 wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, const void* v, const float* lam,
                                 const int16_t* maps, const float* stats, const uint8_t* mask, const int32_t* q_start,
                                 const int32_t* kv_lens, const wa_diff_shape* shape,

@@ -8,6 +8,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 
 #include "common.h"
 #include "diff_launch.h"
@@ -404,6 +405,36 @@ wa_status check_diff_args(const void* q, const void* k, const void* v, const flo
   a->scale = scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)a->head_dim));
   return WA_OK;
 }
+
+// Memory of a differential-attention call. Workgroups read inputs that others have finished with at any time, so nothing that a call
+// writes may lie in what it reads or writes elsewhere.
+struct DiffSpan {
+  const char* name;
+  const void* at;  // null: not given
+  size_t bytes;
+  bool written;
+};
+wa_status check_diff_spans(std::initializer_list<DiffSpan> spans) {
+  for (const DiffSpan& x : spans)
+    for (const DiffSpan& y : spans) {
+      const uintptr_t p = (uintptr_t)x.at, q = (uintptr_t)y.at;
+      if (x.written && &x != &y && x.at && y.at && p < q + y.bytes && q < p + x.bytes)
+        return fail(WA_ERR_INVALID_ARG, "%s overlaps %s", x.name, y.name);
+    }
+  return WA_OK;
+}
+// Bytes of the tensors: bf16 of a query's or key's maps, of values and of rows of O.
+struct DiffBytes {
+  size_t q, k, v, o, lam, mask, batch;
+  explicit DiffBytes(const WaDiffLaunch& a)
+      : q((size_t)a.batch * 2 * a.heads * a.q_len * a.head_dim * 2),
+        k((size_t)a.batch * 2 * a.kv_heads * a.kv_len * a.head_dim * 2),
+        v((size_t)a.batch * a.kv_heads * a.kv_len * a.value_dim * 2),
+        o((size_t)a.batch * a.heads * a.q_len * a.value_dim * 2),
+        lam((size_t)a.heads * 4),
+        mask((size_t)a.batch * a.heads * a.mb * a.nb),
+        batch((size_t)a.batch * 4) {}
+};
 
 }  // namespace
 
@@ -829,7 +860,14 @@ wa_status wa_diff_attn(const void* q, const void* k, const void* v, const float*
   if (!maps != !stats) return fail(WA_ERR_INVALID_ARG, "maps and stats go together");
   if (!aligned(o, 16) || !aligned(maps, 16)) return fail(WA_ERR_ALIGNMENT, "o and maps must be 16-byte aligned");
   if (!aligned(stats, 4)) return fail(WA_ERR_ALIGNMENT, "stats must be 4-byte aligned");
-  s = check_ws(workspace, workspace_bytes, diff_ws_bytes(a));
+  const size_t need = diff_ws_bytes(a);
+  s = check_ws(workspace, workspace_bytes, need);
+  if (s != WA_OK) return s;
+  const DiffBytes n(a);
+  s = check_diff_spans({{"o", o, n.o, true}, {"maps", maps, 2 * n.o, true}, {"stats", stats, (size_t)a.batch * 2 * a.heads * a.q_len * 12, true},
+                        {"workspace", need ? workspace : nullptr, need, true}, {"q", q, n.q, false}, {"k", k, n.k, false},
+                        {"v", v, n.v, false}, {"lam", lam, n.lam, false}, {"mask", mask, n.mask, false},
+                        {"q_start", q_start, n.batch, false}, {"kv_lens", kv_lens, n.batch, false}});
   if (s != WA_OK) return s;
   a.o = o; a.maps = maps; a.stats = stats;
   a.tasks = (int32_t*)workspace;
@@ -865,6 +903,13 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
   if (!aligned(stats, 4) || !aligned(dlam, 4)) return fail(WA_ERR_ALIGNMENT, "stats and dlam must be 4-byte aligned");
   const DiffBackwardWs L = diff_backward_ws(a);
   s = check_ws(workspace, workspace_bytes, L.total);
+  if (s != WA_OK) return s;
+  const DiffBytes n(a);
+  s = check_diff_spans({{"dq", dq, n.q, true}, {"dk", dk, n.k, true}, {"dv", dv, n.v, true}, {"dlam", dlam, n.lam, true},
+                        {"workspace", workspace, L.total, true}, {"dout", dout, n.o, false}, {"q", q, n.q, false},
+                        {"k", k, n.k, false}, {"v", v, n.v, false}, {"lam", lam, n.lam, false}, {"maps", maps, 2 * n.o, false},
+                        {"stats", stats, (size_t)a.batch * 2 * a.heads * a.q_len * 12, false}, {"mask", mask, n.mask, false},
+                        {"q_start", q_start, n.batch, false}, {"kv_lens", kv_lens, n.batch, false}});
   if (s != WA_OK) return s;
   a.dout = dout; a.maps = const_cast<int16_t*>(maps); a.stats = const_cast<float*>(stats);
   a.dq = dq; a.dk = dk; a.dv = dv; a.dlam = dlam;

@@ -56,3 +56,30 @@ def test_scales_of_the_binding(scale):
     with pytest.raises(ValueError, match="scale"):
         W.diff_attn_backward(torch.zeros(1, 2, 70, 64, dtype=torch.bfloat16), **_host(), mask=None,
                              maps=torch.zeros(1, 4, 70, 64, dtype=torch.int16), stats=torch.zeros(1, 4, 70, 3), scale=scale)
+
+
+def _span_call(backward, **at):
+    """A call whose tensors lie 1 GiB apart, but for those that `at` places."""
+    lib, shape = _lib(), _shape(batch=1, heads=2, kv_heads=2, q_len=1, kv_len=8192, head_dim=64, value_dim=64)
+    ins = ["dout", "q", "k", "v", "lam", "maps", "stats", "mask", "start", "lens"] if backward else \
+        ["q", "k", "v", "lam", "mask", "start", "lens"]
+    outs = ["dq", "dk", "dv", "dlam", "ws"] if backward else ["o", "maps", "stats", "ws"]
+    a = {x: (i + 1) << 30 for i, x in enumerate(ins + outs)}
+    for x, (other, bytes_on) in at.items():
+        a[x] = a[other] + bytes_on
+    opts, p = L.WaDiffOptions(0.0, 1), [ctypes.c_void_p(a[x]) for x in ins + outs]
+    call = lib.wa_diff_attn_backward if backward else lib.wa_diff_attn
+    return call(*p[:len(ins)], ctypes.byref(shape), ctypes.byref(opts), *p[len(ins):], 1 << 28, None)
+
+
+@pytest.mark.parametrize("backward,at,says", [
+    # 2 x 8192 values of 64 columns are 2 MiB, keys twice that
+    (False, dict(o=("v", 0)), "o overlaps v"), (False, dict(o=("k", (4 << 20) - 256)), "o overlaps k"),
+    (False, dict(maps=("o", 16)), "o overlaps maps"), (False, dict(stats=("lens", 0)), "stats overlaps kv_lens"),
+    (False, dict(ws=("q", 256)), "workspace overlaps q"), (False, dict(v=("ws", 512)), "workspace overlaps v"),
+    (True, dict(dq=("q", 0)), "dq overlaps q"), (True, dict(dv=("v", 0)), "dv overlaps v"), (True, dict(dk=("dv", 16)), "dk overlaps dv"),
+    (True, dict(dlam=("lam", 4)), "dlam overlaps lam"), (True, dict(ws=("maps", 256)), "workspace overlaps maps"),
+])
+def test_overlapping_memory(backward, at, says):
+    assert _span_call(backward, **at) == INVALID
+    assert _lib().wa_last_error().decode() == says
