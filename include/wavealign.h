@@ -411,7 +411,8 @@ typedef struct wa_rotary_scaling {
  *   LINEAR  divided by factor
  *   NTK     with base * factor^(pairs / (pairs - 1)): the first pair unchanged, the last divided by factor
  *   YARN    f (w + (1 - w) / factor) with w rising from 0 at beta_slow to 1 at beta_fast turns
- *           original_len f / 2 pi; *scale = 0.1 ln(factor) + 1
+ *           original_len f / 2 pi, linearly in the turns; *scale = 0.1 ln(factor) + 1. Frequencies of a model whose
+ *           ramp is linear in the pair's index instead are not these: pass its own to wa_rotary
  * *scale (nullable) is 1 otherwise. scaling NULL: PLAIN. */
 wa_status wa_rotary_frequencies(int32_t pairs, double base, const wa_rotary_scaling* scaling, double* inv_freq,
                                 double* scale);

@@ -442,7 +442,8 @@ def rotary_frequencies(pairs: int, *, base: float = 10000.0, scaling: str = "non
                        original_len: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda"):
     """(inv_freq float64 [pairs] on ``device``, scale) of one position axis for ``rotary``: base^(-i / pairs), for
     contexts ``factor`` times the trained length divided by it ("linear"), with a larger base ("ntk") or by the pair's
-    turns over ``original_len`` ("yarn", which also grows the values by scale). Axes are concatenated by the caller."""
+    turns over ``original_len`` ("yarn", linear in the turns, not in the pair's index; it also grows the values by scale). Axes are
+    concatenated by the caller."""
     if scaling not in _ROTARY_SCALING:
         raise ValueError(f"scaling must be one of {sorted(_ROTARY_SCALING)}")
     freq, scale = (ctypes.c_double * max(int(pairs), 1))(), ctypes.c_double(1.0)
@@ -464,7 +465,9 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, inv_freq: torch
     layout     "half" (pair i: columns i and i + P) or "interleaved" (2i and 2i + 1)
     axis_pairs pairs of each position axis (None: one axis)
     scale      factor of the rotated values
-    backward   the transposed map: gradients of the outputs in, gradients of q and k out"""
+    backward   the transposed map: gradients of the outputs in, gradients of q and k out
+
+    No autograd graph is recorded, also where q requires a gradient: the caller makes the backward call."""
     lib = L.load()
     if layout not in _ROTARY_LAYOUT:
         raise ValueError(f"layout must be one of {sorted(_ROTARY_LAYOUT)}")
@@ -572,7 +575,9 @@ def diff_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tens
     kv_lens   int32 [B]: keys each sequence holds; what lies behind them is not used, all before has to be finite
     return_stats  also (maps, stats), which diff_attn_backward takes: each P_m V int16 [B][2H][M][dv] in steps of 1/32767 of
               its row's largest magnitude, and float32 [B][2H][M][3]: the log-sum-exp of the scaled scores, the step, and a
-              factor of roundings"""
+              factor of roundings
+
+    No autograd graph is recorded, also where an input requires a gradient: the caller makes the backward call."""
     lib = L.load()
     softmax_scale = _diff_scale(scale)
     shape, mask = _diff_args(q, k, v, lam, mask, block, causal, q_start, kv_lens)

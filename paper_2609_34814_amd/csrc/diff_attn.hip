@@ -16,9 +16,9 @@
 // split over workgroups whose partial results a second kernel joins in key order, so a result does not depend on
 // the order in which workgroups run.
 //
-// What bounds it: many rows of d 128, values 256 the power limit (2 x 8 heads of 4,096 tokens 381 us alone, 1.08 PFLOP/s, matrix
-// cores 51% busy at 2.0 GHz; 411 in a row); of d 64 the exponentials beside the few products (values 64, 16 heads: 299 us,
-// 0.92 PFLOP/s, vector unit 72% busy, matrix cores 45%); few rows the memory (one token of 16 sequences, 201 MB of keys and values:
+// What bounds it: many rows of d 128, values 256 the power limit (2 x 8 heads of 4,096 tokens 392 us alone, 1.05 PFLOP/s, matrix
+// cores 50% busy at 2.0 GHz; 441 in a row); of d 64 the exponentials beside the few products (values 64, 16 heads: 301 us,
+// 0.91 PFLOP/s, vector unit 70% busy, matrix cores 44%); few rows the memory (one token of 16 sequences, 201 MB of keys and values:
 // 36 us, 5.6 TB/s, and 4 for the join).
 
 #include "diff_tiles.h"

@@ -11,9 +11,9 @@
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are.
 // dlam is the sum of D_2 from the stored maps and of the float32 P_2 (dP - D_2), which takes their steps' error back: over a
 // lane's keys with the roundings carried along, over queries in float64.
-// What bounds it (d 128, values 256, 2 x 8 heads of 4,096 tokens): dQ 429 and dK with dV 564 us where each runs alone at 2.3 GHz
+// What bounds it (d 128, values 256, 2 x 8 heads of 4,096 tokens): dQ 437 and dK with dV 583 us where each runs alone at 2.3 GHz
 // (matrix cores 40% busy; a wavefront issues 55% of its time, waits 20% for the matrix core and 25% for LDS, copies and barriers),
-// 497 and 694 one after another, when the power limit lowers the clock. One map a wavefront, so that two share a SIMD, makes a
+// 514 and 728 one after another, when the power limit lowers the clock. One map a wavefront, so that two share a SIMD, makes a
 // fifth to a third more products (dP twice) and is no faster.
 
 #include "diff_tiles.h"
@@ -367,8 +367,9 @@ __global__ __launch_bounds__(64 * W, kDkvWaves<D>) void diff_dkv_kernel(const Wa
   using C = Bwd<D, DV, W, kValuesInLds>;
   constexpr int AHEAD = kAheadRows<kDkvWaves<D>>, CAHEAD = kAheadCols<kDkvWaves<D>>;
   // Keys that do not fit the registers either (d 64) lie in LDS by the lane, as many as leave a compute unit its two workgroups of four
-  // wavefronts (three of two): the compiler's own spills are reloaded in the loop, which waits for the next tile's copies too. 2 x 14
-  // heads of 4,096 tokens, values 128: 669 -> 636 us, causal 16 heads over 4 of 2,048: 120 -> 114.
+  // wavefronts (three of two): the compiler's own spills are reloaded in the loop, which waits for the next tile's copies too (5 registers
+  // of two wavefronts and one of four are left). 2 x 14 heads of 4,096 tokens, values 128: 669 -> 636 us, causal 16 heads over 4 of 2,048:
+  // 120 -> 114.
   constexpr int KEPT = !kValuesInLds || D != 64 ? 0 : W == 4 ? 3 : 2;
   constexpr int QB = C::TB, VALUES = kValuesInLds ? 32 * W * C::VRB : 0;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * C::STAGE + VALUES + KEPT * 1024 * W];

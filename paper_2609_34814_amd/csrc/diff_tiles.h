@@ -94,9 +94,9 @@ struct Task {
 // The workgroup's task; false if there is none. PER_CU: workgroups that a compute unit holds. Without a list of tasks, the chunks of a
 // tile together, and the tiles of `group` units in turn, tile after tile (backwards: from the last), then those of the next units:
 // workgroups go round the eight XCDs, so with eight units each XCD's cache holds the other side of one; causal ones take all units, so
-// that long tiles come first (forward and dQ of 2 x 16 heads of 2,048 tokens 77 and 90 us, by eights 97 and 122), with neighbouring units,
-// which may share keys, on one XCD (forward and gradient of 32 heads over 8 of 16,384 tokens, d and values 128: 17.46 -> 16.88 ms); masked
-// ones go unit after unit.
+// that long tiles come first (2 x 16 heads of 2,048 tokens, d 64, values 64: forward 55 us, dQ 78, dK and dV 88; by eights 58, 80 and
+// 96), with neighbouring units, which may share keys, on one XCD where eight divides their number (forward and gradient of 32 heads over
+// 8 of 16,384 tokens, d and values 128: 17.46 -> 16.88 ms); masked ones go unit after unit.
 template <int PER_CU>
 __device__ __forceinline__ bool take_task(const WaDiffLaunch& a, int tiles, int units, int chunks, bool backwards, Task* t) {
   if (a.tasks) {
