@@ -493,6 +493,185 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
                                 const wa_diff_options* options, void* dq, void* dk, void* dv, float* dlam,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- packed sequences ---- */
+
+/* Rows [tokens][heads][head_dim] of 16-bit values; element (t, h, c) lies at t token_stride + h head_stride + c elements, so a
+ * tensor may be a part of a fused projection's output, or head-major. `at` is 16-byte aligned, strides are multiples of 8, token
+ * strides of keys and values below 2^24. An input's stride may be 0; elements of an output may not coincide. */
+typedef struct wa_token_rows {
+  void* at;               /* inputs are only read */
+  int64_t token_stride;
+  int64_t head_stride;
+} wa_token_rows;
+
+typedef struct wa_seq_shape {
+  int32_t batch;      /* sequences */
+  int32_t tokens;     /* rows of the tensors of queries (packed: of all tensors); 0: nothing to do */
+  int32_t heads;      /* H, a multiple of kv_heads */
+  int32_t kv_heads;   /* Hk: heads h with equal h / (H / Hk) share keys and values */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t dtype;      /* WA_BF16 or WA_F16, of every tensor of rows and pages */
+} wa_seq_shape;
+
+typedef struct wa_seq_options {
+  float softmax_scale;  /* finite; <= 0 selects 1/sqrt(head_dim); else 1e-30..1e30 */
+  int32_t causal;       /* nonzero: a query sees no key behind its own position */
+} wa_seq_options;
+
+/* Workspace bytes needed by wa_packed_attn and by wa_paged_attn: float32 results of query tiles that several workgroups compute
+ * (about 70 MB at most) and 8 bytes a row of O. Calls that share a workspace must not overlap, captured ones included. */
+wa_status wa_seq_attn_workspace_size(const wa_seq_shape* shape, size_t* bytes);
+
+/* Attention over packed sequences: sequence b has the tokens starts[b] to starts[b + 1] - 1 and attends to itself,
+ *   O = softmax(scale Q K^T) V, with `causal` over the keys up to each query's own.
+ * float32 scores (so a probability is off by some 2^-24 of the row's largest scaled score), sums and O, probabilities
+ * rounded to the tensors' type for the product with V (in fp16 down to 2^-21 of the row's largest with all bits). Keys and values of a
+ * sequence's tokens have to be finite; rows of no sequence are not read (but the last row of a sequence may be read again in their place), and
+ * their outputs are left as they were.
+ *   q, o       [tokens][H][d];  k, v  [tokens][Hk][d]
+ *   starts     int32 [batch + 1], device, ascending; values are taken into 0..tokens. A sequence may be empty
+ *   lse        out float [H][tokens], nullable: natural-log sum-exp of a query's scaled scores, for the gradient
+ *   workspace  >= wa_seq_attn_workspace_size(shape), 256-byte aligned
+ * Outputs and workspace overlap neither inputs nor each other (refused; outputs may interleave in one tensor of equal token strides).
+ * How the work is cut follows from the lengths, so equal calls give equal bits; the bits of a sequence may
+ * depend on the lengths of the others. */
+wa_status wa_packed_attn(const wa_token_rows* q, const wa_token_rows* k, const wa_token_rows* v, const int32_t* starts,
+                         const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* o, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes needed by wa_packed_attn_backward: 2 H tokens float32, and float32 results of key tiles that are computed in parts. */
+wa_status wa_packed_attn_backward_workspace_size(const wa_seq_shape* shape, size_t* bytes);
+
+/* Gradient of wa_packed_attn, bf16 only (dS = P (dP - dO . O) lies below fp16's range): with dO of O it writes
+ *   dV = P^T dO, dQ = scale dS K, dK = scale dS^T Q, dP = dO V^T, dV and dK summed over the heads of a key head,
+ * probabilities recomputed in float32 from lse, sums in float32, P and dS rounded to bf16 for the matrix products, dO . O taken of
+ * the bf16 O. Rows of no sequence are left as they were. Nothing is added with atomics: equal calls give equal bits.
+ *   dout, o, lse   dO [tokens][H][d]; what wa_packed_attn wrote
+ *   dq, dk, dv     out, shaped as q, k and v
+ *   workspace      >= wa_packed_attn_backward_workspace_size(shape), 256-byte aligned
+ * Outputs and workspace overlap neither inputs nor each other (as above). */
+wa_status wa_packed_attn_backward(const wa_token_rows* dout, const wa_token_rows* q, const wa_token_rows* k,
+                                  const wa_token_rows* v, const wa_token_rows* o, const float* lse, const int32_t* starts,
+                                  const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* dq,
+                                  const wa_token_rows* dk, const wa_token_rows* dv, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+/* ---- a paged cache ---- */
+
+/* Bits that calls add to a paged call's status word (device int32; the caller zeroes it). */
+enum {
+  WA_PAGE_BAD_INDEX = 1,  /* a page or sequence number outside what there is; its part of the work is left out */
+  WA_PAGE_EXHAUSTED = 2,  /* no free page was left, or no room in a table */
+  WA_PAGE_BUSY = 4        /* page_fork: a child that holds tokens, or is named twice */
+};
+
+/* Keys or values in pages, [pages][Hk][page][head_dim]: element (p, h, i, c) lies at p page_stride + h head_stride +
+ * i token_stride + c elements, so keys and values may share a pool in any order. `at` is 16-byte aligned, strides are
+ * multiples of 8, token strides below 2^24. */
+typedef struct wa_pages {
+  void* at;
+  int64_t page_stride;
+  int64_t head_stride;
+  int64_t token_stride;
+} wa_pages;
+
+/* Which pages sequences hold: token i of sequence b lies in row i % page of page tables[b table_stride + i / page]. */
+typedef struct wa_page_tables {
+  const int32_t* tables;   /* device; entries behind a sequence's last page are not used */
+  int64_t table_stride;    /* table_width at least, or 0 where all sequences share one */
+  int32_t table_width;     /* entries of a sequence */
+  int32_t n_pages;         /* pages of the pool */
+  int32_t page;            /* tokens a page: a power of two, 16..4096 */
+} wa_page_tables;
+
+/* Attention of new tokens over a paged cache: sequence b's n = starts[b + 1] - starts[b] queries (one in a decoding step, a
+ * chunk of a prompt, none) are its last n of kv_lens[b] tokens, whose keys and values all lie in the pages (wa_page_store puts the
+ * new ones there). Query i sees the keys up to kv_lens[b] - n + i, without `causal` all kv_lens[b]; one that sees none gets O = 0 and
+ * a sum-exp of -inf. Arithmetic, o, lse, workspace and order as for wa_packed_attn.
+ *   q, o      [tokens][H][d]
+ *   k, v      pages of Hk heads; what lies behind a sequence's last token is not used, all before has to be finite
+ *   starts    int32 [batch + 1], device, ascending; values are taken into 0..tokens
+ *   kv_lens   int32 [batch], device: taken into 0..table_width * page
+ *   status    device int32, nullable: WA_PAGE_BAD_INDEX is added where a sequence's table names a page outside
+ *             0..n_pages - 1; keys of such a page are left out */
+wa_status wa_paged_attn(const wa_token_rows* q, const wa_pages* k, const wa_pages* v, const wa_page_tables* tables,
+                        const int32_t* starts, const int32_t* kv_lens, const wa_seq_shape* shape,
+                        const wa_seq_options* options, const wa_token_rows* o, float* lse, int32_t* status,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Keys and values of new tokens to their places: row starts[b] + i of k and v to token kv_lens[b] - n + i of sequence b
+ * (n = starts[b + 1] - starts[b]; kv_lens counts the new tokens). Places before token 0 are left out. Two sequences must not
+ * store into one page's row.
+ *   k, v      [tokens][Hk][d] rows (shape->heads is not used)
+ *   k_pages, v_pages   out; they overlap neither inputs nor each other (but may interleave, page by page or token by token,
+ *             with equal strides)
+ *   status    as for wa_paged_attn; rows without a page are left out */
+wa_status wa_page_store(const wa_token_rows* k, const wa_token_rows* v, const wa_pages* k_pages, const wa_pages* v_pages,
+                        const wa_page_tables* tables, const int32_t* starts, const int32_t* kv_lens,
+                        const wa_seq_shape* shape, int32_t* status, void* stream);
+
+/* A pool's pages and who holds them, on the device. A page is free where refs is 0. Sequence s holds the first
+ * ceil(lens[s] / page) pages of its table, each counted in refs; entries behind them are left as they are. The calls below keep a state
+ * so that is so; of one that is not, no call reads or writes outside the arrays. */
+typedef struct wa_page_state {
+  int32_t* refs;          /* [n_pages] */
+  int32_t* tables;        /* [sequences][table_width] */
+  int32_t* lens;          /* [sequences]: tokens */
+  int32_t n_pages;
+  int32_t sequences;
+  int32_t table_width;
+  int32_t page;           /* tokens a page: a power of two, 1..4096 */
+} wa_page_state;
+
+/* Contents of the pages: planes (keys and values of every layer) of n_pages pages of page_bytes, one behind another. */
+typedef struct wa_page_pool {
+  void* at;               /* 16-byte aligned */
+  int64_t page_bytes;     /* a multiple of 16 */
+  int32_t planes;
+} wa_page_pool;
+
+/* Workspace bytes needed by wa_page_grow and wa_page_compact (entries 0) and by wa_page_fork of `entries` children. */
+wa_status wa_page_workspace_size(const wa_page_state* state, int32_t entries, size_t* bytes);
+
+/* Grows sequences to new lengths: sequence s to max(lens[s], new_lens[s]) tokens. The pages that it needs are the lowest free
+ * ones, in the order of the sequences and of their tables. A sequence that would find no free page, or no
+ * room in its table, keeps its length, takes none and adds WA_PAGE_EXHAUSTED; those behind it go on with the
+ * pages that are left.
+ *   new_lens   int32 [sequences], device */
+wa_status wa_page_grow(const wa_page_state* state, const int32_t* new_lens, int32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Makes sequence children[i] a copy of sequence parents[i], for all i at once: full pages are shared, a last one
+ * that is not full is copied, in every plane, to a page of its own: the lowest free ones in the order of i. Children are empty
+ * before (their lens 0) and named once: one that is not, or is named before, is left out and adds WA_PAGE_BUSY; numbers outside
+ * 0..sequences - 1 are left out and add WA_PAGE_BAD_INDEX, as are parents whose last page, where it is to be copied, is none of the
+ * pool (other entries of that kind are handed on, uncounted, and add the bit); a child without a free page stays empty and adds
+ * WA_PAGE_EXHAUSTED. Parents may repeat; all entries read the state before the call.
+ *   parents, children   int32 [entries], device */
+wa_status wa_page_fork(const wa_page_state* state, const wa_page_pool* pool, const int32_t* parents,
+                       const int32_t* children, int32_t entries, int32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Gives the pages of sequences back: their references go down by one and their lens to 0; tables and contents stay.
+ * A sequence named twice is freed once; numbers outside 0..sequences - 1 add WA_PAGE_BAD_INDEX.
+ *   slots   int32 [entries], device */
+wa_status wa_page_free(const wa_page_state* state, const int32_t* slots, int32_t entries, int32_t* status, void* stream);
+
+/* Moves the pages in use to the front of the pool: of u pages in use those numbered u and above move, in order, into
+ * the free ones below u, in every plane; refs and tables follow. What the moved pages held stays where it was too, so with
+ * out_refs and out_tables of its own a call in flight may go on with the old ones until those pages are dealt out again.
+ *   out_refs, out_tables   as refs and tables: the same memory, or apart from them; entries behind a sequence's last page
+ *                          are copied. Entries that name no page of the pool are copied and add WA_PAGE_BAD_INDEX
+ *   used                   out int32, device, nullable: u */
+wa_status wa_page_compact(const wa_page_state* state, const wa_page_pool* pool, int32_t* out_refs, int32_t* out_tables,
+                          int32_t* used, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies pages, in every plane: page from[i] to page to[i]. No page is both, and none is in `to` twice. Pairs with a number outside
+ * 0..n_pages - 1 are left out and add WA_PAGE_BAD_INDEX.
+ *   from, to   int32 [entries], device */
+wa_status wa_page_copy(const wa_page_pool* pool, int32_t n_pages, const int32_t* from, const int32_t* to, int32_t entries,
+                       int32_t* status, void* stream);
+
 /* ---- diagnostics (used by the test suite; not needed by callers) ---- */
 
 /* Evaluates on the GPU the fp64 operations the exact permutation relies on, for

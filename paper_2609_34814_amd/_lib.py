@@ -23,6 +23,7 @@ WA_PRODUCE_WAIT_EXPIRED = 1
 WA_HEADS_IN_ORDER, WA_HEADS_INTERLEAVED = 0, 1
 WA_NOALLOC_SCRATCH_BYTES = 4 * 1024 * 1024
 WA_BF16, WA_F16, WA_F32 = 0, 1, 2
+WA_PAGE_BAD_INDEX, WA_PAGE_EXHAUSTED, WA_PAGE_BUSY = 1, 2, 4
 WA_ROTARY_HALF, WA_ROTARY_INTERLEAVED = 0, 1
 WA_ROTARY_PLAIN, WA_ROTARY_LINEAR, WA_ROTARY_NTK, WA_ROTARY_YARN = 0, 1, 2, 3
 
@@ -79,6 +80,17 @@ class WaDiffOptions(ctypes.Structure):
     _fields_ = [("softmax_scale", c_float), ("causal", c_int32)]
 
 
+# The structures of packed sequences and of the paged cache as bytes (see ROTARY_PARAMS): wa_token_rows, wa_seq_shape, wa_seq_options,
+# wa_pages, wa_page_tables, wa_page_state, wa_page_pool.
+TOKEN_ROWS = struct.Struct("@Pqq")
+SEQ_SHAPE = struct.Struct("@6i")
+SEQ_OPTIONS = struct.Struct("@fi")
+PAGES = struct.Struct("@Pqqq")
+PAGE_TABLES = struct.Struct("@Pq3i4x")
+PAGE_STATE = struct.Struct("@3P4i")
+PAGE_POOL = struct.Struct("@Pqi4x")
+
+
 class WaError(RuntimeError):
     def __init__(self, status: int, detail: str):
         super().__init__(f"wavealign error {status}: {detail}")
@@ -126,6 +138,18 @@ _SIGNATURES = {
     "wa_diff_attn_backward_workspace_size": (c_int32, [POINTER(WaDiffShape), POINTER(c_size_t)]),
     "wa_diff_attn_backward": (c_int32, [c_void_p] * 10 + [POINTER(WaDiffShape), POINTER(WaDiffOptions)] + [c_void_p] * 5
                               + [c_size_t, c_void_p]),
+    "wa_seq_attn_workspace_size": (c_int32, [c_void_p, POINTER(c_size_t)]),
+    "wa_packed_attn": (c_int32, [c_void_p] * 9 + [c_size_t, c_void_p]),
+    "wa_packed_attn_backward_workspace_size": (c_int32, [c_void_p, POINTER(c_size_t)]),
+    "wa_packed_attn_backward": (c_int32, [c_void_p] * 13 + [c_size_t, c_void_p]),
+    "wa_paged_attn": (c_int32, [c_void_p] * 12 + [c_size_t, c_void_p]),
+    "wa_page_store": (c_int32, [c_void_p] * 10),
+    "wa_page_workspace_size": (c_int32, [c_void_p, c_int32, POINTER(c_size_t)]),
+    "wa_page_grow": (c_int32, [c_void_p] * 4 + [c_size_t, c_void_p]),
+    "wa_page_fork": (c_int32, [c_void_p] * 4 + [c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "wa_page_free": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p, c_void_p]),
+    "wa_page_compact": (c_int32, [c_void_p] * 7 + [c_size_t, c_void_p]),
+    "wa_page_copy": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p]),
     "wa_fp64_probe": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p]),
     "wa_xcc_probe": (c_int32, [c_void_p, c_int32, c_void_p]),
 }

@@ -6,6 +6,7 @@ device memory and the current HIP stream.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 from typing import Optional
 
@@ -633,6 +634,304 @@ def diff_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
              _ptr(stats), _ptr(mask), _ptr(q_start), _ptr(kv_lens), ctypes.byref(shape), ctypes.byref(opts), _ptr(dq),
              _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), workspace.numel())
     return dq, dk, dv, dlam
+
+
+_SEQ_DTYPE = {torch.bfloat16: L.WA_BF16, torch.float16: L.WA_F16}
+
+
+def _rows(t: torch.Tensor, name: str, dtype, shape) -> bytes:
+    """wa_token_rows of a tensor [T][H][d] with free strides and whole rows."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        raise ValueError(f"{name} must have contiguous rows (last stride 1)")
+    return L.TOKEN_ROWS.pack(t.data_ptr(), s0, s1)
+
+
+def _int32(t: Optional[torch.Tensor], name: str, shape) -> None:
+    """A contiguous int32 tensor; a None in ``shape`` takes any size."""
+    if t is None:
+        return
+    if t.dtype != torch.int32 or t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        want = "".join("[any]" if w is None else f"[{w}]" for w in shape)
+        raise ValueError(f"{name} must be int32 {want}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _seq_args(q: torch.Tensor, kv_heads: int, starts: torch.Tensor, name: str = "q"):
+    """(wa_seq_shape, tokens, heads, head_dim) of a call whose rows of queries are q [T][H][d]."""
+    if q.dim() != 3 or q.dtype not in _SEQ_DTYPE:
+        raise ValueError(f"{name} must be a bfloat16 or float16 [T][H][d] tensor, got {q.dtype} {tuple(q.shape)}")
+    _int32(starts, "starts", (None,))
+    t, h, d = q.shape
+    return L.SEQ_SHAPE.pack(starts.numel() - 1, t, h, kv_heads, d, _SEQ_DTYPE[q.dtype]), t, h, d
+
+
+@functools.lru_cache(maxsize=1024)
+def _seq_size(call: str, shape: bytes, *more) -> int:
+    n = ctypes.c_size_t(0)
+    L.check(getattr(L.load(), call)(shape, *more, ctypes.byref(n)))
+    return n.value
+
+
+def _room(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    _check(workspace, "workspace", torch.uint8)
+    return _workspace(need, device) if workspace is None or workspace.numel() < need else workspace
+
+
+def packed_attn_workspace_size(tokens: int, batch: int, heads: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16) -> int:
+    """Bytes for packed_attn and paged_attn of ``batch`` sequences with ``tokens`` queries in all."""
+    return _seq_size("wa_seq_attn_workspace_size", L.SEQ_SHAPE.pack(batch, tokens, heads, kv_heads, head_dim, _SEQ_DTYPE[dtype]))
+
+
+def packed_attn_backward_workspace_size(tokens: int, batch: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return _seq_size("wa_packed_attn_backward_workspace_size",
+                     L.SEQ_SHAPE.pack(batch, tokens, heads, kv_heads, head_dim, L.WA_BF16))
+
+
+def packed_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, *, causal: bool = True,
+                scale: Optional[float] = None, return_lse: bool = False, out: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None):
+    """Attention over packed sequences: O = softmax(scale Q K^T) V [T][H][d], each sequence over its own tokens.
+
+    q, k, v   bfloat16 or float16 [T][H][d], [T][Hk][d], [T][Hk][d], d 64 or 128, of any strides (multiples of 8) with whole
+              rows: parts of one projection's output will do; H / Hk heads in a row share keys and values
+    starts    int32 [B + 1], ascending: sequence b has the rows starts[b] to starts[b + 1] - 1 and may be empty
+    causal    each query sees the keys up to its own
+    scale     positive; None: 1 / sqrt(d)
+    return_lse  also float32 [H][T], the log-sum-exps of the scaled scores, which packed_attn_backward takes
+    out       as q, of any strides; None: a new contiguous tensor. Rows of no sequence keep what they hold (in a new
+              tensor and in the log-sum-exps: anything)
+
+    A sequence's keys and values have to be finite. No autograd graph is recorded: the caller makes the backward call."""
+    lib = L.load()
+    softmax_scale = _diff_scale(scale)
+    if k.dim() != 3:
+        raise ValueError(f"k must have shape [T][Hk][d], got {tuple(k.shape)}")
+    shape, t, h, d = _seq_args(q, k.shape[1], starts)
+    o = q.new_empty((t, h, d)) if out is None else out
+    kv = (t, k.shape[1], d)
+    rows = (_rows(q, "q", q.dtype, q.shape), _rows(k, "k", q.dtype, kv), _rows(v, "v", q.dtype, kv))
+    to = _rows(o, "out", q.dtype, q.shape)
+    index = _one_device(q=q, k=k, v=v, starts=starts, out=out, workspace=workspace)
+    need = _seq_size("wa_seq_attn_workspace_size", shape)
+    workspace = _room(workspace, need, q.device)
+    lse = q.new_empty((h, t), dtype=torch.float32) if return_lse else None
+    _call_on(index, lib.wa_packed_attn, *rows, starts.data_ptr(), shape, L.SEQ_OPTIONS.pack(softmax_scale, 1 if causal else 0), to,
+             _ptr(lse), workspace.data_ptr(), workspace.numel())
+    return (o, lse) if return_lse else o
+
+
+def packed_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+                         lse: torch.Tensor, starts: torch.Tensor, *, causal: bool = True, scale: Optional[float] = None,
+                         out=None, workspace: Optional[torch.Tensor] = None):
+    """(dq, dk, dv) from dout, the gradient of packed_attn's O: the other arguments as that call had them, o and lse as it
+    returned them. bfloat16 only. out: (dq, dk, dv) tensors of any strides (parts of one tensor will do); rows of no sequence
+    keep what they hold (in new tensors: anything). Equal calls give equal bits."""
+    lib = L.load()
+    softmax_scale = _diff_scale(scale)
+    if k.dim() != 3:
+        raise ValueError(f"k must have shape [T][Hk][d], got {tuple(k.shape)}")
+    shape, t, h, d = _seq_args(q, k.shape[1], starts)
+    kv = (t, k.shape[1], d)
+    bf = torch.bfloat16
+    rows = [_rows(x, n, bf, w) for x, n, w in ((dout, "dout", q.shape), (q, "q", q.shape), (k, "k", kv), (v, "v", kv), (o, "o", q.shape))]
+    if lse.dtype != torch.float32 or lse.shape != (h, t) or not lse.is_contiguous():
+        raise ValueError(f"lse must be contiguous float32 [{h}][{t}], got {lse.dtype} {tuple(lse.shape)}")
+    if out is None:
+        out = (q.new_empty(q.shape), q.new_empty(kv), q.new_empty(kv))
+    dq, dk, dv = out
+    to = (_rows(dq, "dq", bf, q.shape), _rows(dk, "dk", bf, kv), _rows(dv, "dv", bf, kv))
+    index = _one_device(dout=dout, q=q, k=k, v=v, o=o, lse=lse, starts=starts, dq=dq, dk=dk, dv=dv, workspace=workspace)
+    workspace = _room(workspace, _seq_size("wa_packed_attn_backward_workspace_size", shape), q.device)
+    _call_on(index, lib.wa_packed_attn_backward, *rows, lse.data_ptr(), starts.data_ptr(), shape,
+             L.SEQ_OPTIONS.pack(softmax_scale, 1 if causal else 0), *to, workspace.data_ptr(), workspace.numel())
+    return dq, dk, dv
+
+
+def _pages(t: torch.Tensor, name: str, dtype, kv_heads: int, d: int) -> bytes:
+    """wa_pages of a tensor [pages][Hk][page][d] with free strides and whole rows."""
+    if t.dtype != dtype or t.dim() != 4 or t.shape[1] != kv_heads or t.shape[3] != d:
+        raise ValueError(f"{name} must be {dtype} [pages][{kv_heads}][page][{d}], got {t.dtype} {tuple(t.shape)}")
+    s0, s1, s2, s3 = t.stride()
+    if s3 != 1:
+        raise ValueError(f"{name} must have contiguous rows (last stride 1)")
+    return L.PAGES.pack(t.data_ptr(), s0, s1, s2)
+
+
+def _page_tables(tables: torch.Tensor, kv_lens: torch.Tensor, batch: int, n_pages: int, page: int) -> bytes:
+    if tables.dtype != torch.int32 or tables.dim() != 2 or tables.shape[0] != batch or (tables.shape[1] > 1 and tables.stride(1) != 1):
+        raise ValueError(f"tables must be int32 [{batch}][pages] with contiguous rows, got {tables.dtype} {tuple(tables.shape)}")
+    _int32(kv_lens, "kv_lens", (batch,))
+    return L.PAGE_TABLES.pack(tables.data_ptr(), tables.stride(0) if batch > 1 else 0, tables.shape[1], n_pages, page)
+
+
+def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, tables: torch.Tensor, starts: torch.Tensor,
+               kv_lens: torch.Tensor, *, causal: bool = True, scale: Optional[float] = None, return_lse: bool = False,
+               out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None):
+    """Attention of new tokens over a paged cache: O [T][H][d]. Sequence b's n = starts[b + 1] - starts[b] queries (one, a chunk
+    of a prompt, none) are its last n of kv_lens[b] tokens, whose keys and values lie in the pages already (page_store).
+
+    q         bfloat16 or float16 [T][H][d], d 64 or 128, of any strides (multiples of 8) with whole rows
+    k_pages, v_pages  as q [pages][Hk][page][d], page a power of two from 16 to 4096, of any strides with whole rows: a pool of
+              both, or a layer of one, will do
+    tables    int32 [B][any]: token i of sequence b lies in row i % page of page tables[b][i // page]
+    starts    int32 [B + 1], ascending; kv_lens int32 [B]: tokens of each sequence, the new ones counted
+    causal    query i of n sees the keys up to kv_lens[b] - n + i; else all kv_lens[b]. One that sees none gets 0
+    status    int32 [1], to which WA_PAGE_BAD_INDEX (1) is added if a table names a page that there is not: its keys are left out
+    scale, return_lse, out   as for packed_attn
+
+    What lies behind a sequence's last token is not used; all before has to be finite."""
+    lib = L.load()
+    softmax_scale = _diff_scale(scale)
+    if k_pages.dim() != 4:
+        raise ValueError(f"k_pages must have shape [pages][Hk][page][d], got {tuple(k_pages.shape)}")
+    n_pages, hk, page, _ = k_pages.shape
+    shape, t, h, d = _seq_args(q, hk, starts)
+    o = q.new_empty((t, h, d)) if out is None else out
+    if v_pages.shape != k_pages.shape:
+        raise ValueError(f"v_pages must have k_pages' shape {tuple(k_pages.shape)}, got {tuple(v_pages.shape)}")
+    args = (_rows(q, "q", q.dtype, q.shape), _pages(k_pages, "k_pages", q.dtype, hk, d), _pages(v_pages, "v_pages", q.dtype, hk, d),
+            _page_tables(tables, kv_lens, starts.numel() - 1, n_pages, page))
+    to = _rows(o, "out", q.dtype, q.shape)
+    _int32(status, "status", (1,))
+    index = _one_device(q=q, k_pages=k_pages, v_pages=v_pages, tables=tables, starts=starts, kv_lens=kv_lens, out=out,
+                        status=status, workspace=workspace)
+    workspace = _room(workspace, _seq_size("wa_seq_attn_workspace_size", shape), q.device)
+    lse = q.new_empty((h, t), dtype=torch.float32) if return_lse else None
+    _call_on(index, lib.wa_paged_attn, *args, starts.data_ptr(), kv_lens.data_ptr(), shape,
+             L.SEQ_OPTIONS.pack(softmax_scale, 1 if causal else 0), to, _ptr(lse), _ptr(status), workspace.data_ptr(),
+             workspace.numel())
+    return (o, lse) if return_lse else o
+
+
+def page_store(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, tables: torch.Tensor,
+               starts: torch.Tensor, kv_lens: torch.Tensor, *, status: Optional[torch.Tensor] = None) -> None:
+    """Puts keys and values of new tokens into their pages: rows starts[b] to starts[b + 1] - 1 of k and v [T][Hk][d] (any
+    strides, whole rows) are the last tokens of sequence b's kv_lens[b]. Pages, tables and status as for paged_attn."""
+    lib = L.load()
+    if k_pages.dim() != 4:
+        raise ValueError(f"k_pages must have shape [pages][Hk][page][d], got {tuple(k_pages.shape)}")
+    n_pages, hk, page, d = k_pages.shape
+    shape, t, _, _ = _seq_args(k, hk, starts, "k")
+    if v_pages.shape != k_pages.shape:
+        raise ValueError(f"v_pages must have k_pages' shape {tuple(k_pages.shape)}, got {tuple(v_pages.shape)}")
+    args = (_rows(k, "k", k.dtype, (t, hk, d)), _rows(v, "v", k.dtype, (t, hk, d)), _pages(k_pages, "k_pages", k.dtype, hk, d),
+            _pages(v_pages, "v_pages", k.dtype, hk, d), _page_tables(tables, kv_lens, starts.numel() - 1, n_pages, page))
+    _int32(status, "status", (1,))
+    index = _one_device(k=k, v=v, k_pages=k_pages, v_pages=v_pages, tables=tables, starts=starts, kv_lens=kv_lens, status=status)
+    _call_on(index, lib.wa_page_store, *args, starts.data_ptr(), kv_lens.data_ptr(), shape, _ptr(status))
+
+
+def _page_state(refs, tables, lens, page: int) -> bytes:
+    _int32(refs, "refs", (None,))
+    _int32(tables, "tables", (None, None))
+    _int32(lens, "lens", (tables.shape[0],))
+    return L.PAGE_STATE.pack(refs.data_ptr(), tables.data_ptr(), lens.data_ptr(), refs.numel(), tables.shape[0], tables.shape[1], page)
+
+
+def _page_sizes(refs, tables, page: int) -> bytes:
+    return L.PAGE_STATE.pack(0, 0, 0, refs.numel(), tables.shape[0], tables.shape[1], page)
+
+
+def _page_pool(pool: torch.Tensor, n_pages: int) -> bytes:
+    if pool.dim() < 3 or pool.shape[1] != n_pages or not pool.is_contiguous():
+        raise ValueError(f"pool must be contiguous [planes][{n_pages}][...], got {tuple(pool.shape)}")
+    size = pool.element_size()
+    for n in pool.shape[2:]:
+        size *= n
+    return L.PAGE_POOL.pack(pool.data_ptr(), size, pool.shape[0])
+
+
+def page_workspace_size(n_pages: int, sequences: int, table_width: int, *, page: int, entries: int = 0) -> int:
+    """Bytes for page_grow and page_compact, and for page_fork of ``entries`` children."""
+    return _seq_size("wa_page_workspace_size", L.PAGE_STATE.pack(0, 0, 0, n_pages, sequences, table_width, page), entries)
+
+
+def page_grow(refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, new_lens: torch.Tensor, *, page: int,
+              status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Grows sequence s to max(lens[s], new_lens[s]) tokens, in place: the pages it needs are the lowest free ones, in
+    the order of the sequences. One that finds too few, or no room in its table, keeps its length and adds WA_PAGE_EXHAUSTED (2).
+
+    refs      int32 [pages]: how many sequences hold each page; 0: free
+    tables    int32 [S][any]; sequence s holds the first ceil(lens[s] / page) pages of its row
+    lens, new_lens   int32 [S]: tokens
+    page      tokens a page, a power of two
+    status    int32 [1], to which bits are added"""
+    lib = L.load()
+    state = _page_state(refs, tables, lens, page)
+    _int32(new_lens, "new_lens", (tables.shape[0],))
+    _int32(status, "status", (1,))
+    index = _one_device(refs=refs, tables=tables, lens=lens, new_lens=new_lens, status=status, workspace=workspace)
+    workspace = _room(workspace, _seq_size("wa_page_workspace_size", _page_sizes(refs, tables, page), 0), refs.device)
+    _call_on(index, lib.wa_page_grow, state, new_lens.data_ptr(), _ptr(status), workspace.data_ptr(), workspace.numel())
+
+
+def page_fork(pool: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, parents: torch.Tensor,
+              children: torch.Tensor, *, page: int, status: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None) -> None:
+    """Makes sequence children[i] a copy of parents[i], in place: full pages are shared, a last one that is not full is copied to
+    the lowest free page. Children are empty before and named once (else left out, WA_PAGE_BUSY, 4); one without a free
+    page stays empty (WA_PAGE_EXHAUSTED, 2).
+
+    pool      [planes][pages][...] contiguous, any type: keys and values of every layer; pages are multiples of 16 bytes
+    parents, children   int32 [n]; refs, tables, lens, page, status   as for page_grow"""
+    lib = L.load()
+    state, at = _page_state(refs, tables, lens, page), _page_pool(pool, refs.numel())
+    _int32(parents, "parents", (None,))
+    n = parents.numel()
+    _int32(children, "children", (n,))
+    _int32(status, "status", (1,))
+    index = _one_device(pool=pool, refs=refs, tables=tables, lens=lens, parents=parents, children=children, status=status,
+                        workspace=workspace)
+    workspace = _room(workspace, _seq_size("wa_page_workspace_size", _page_sizes(refs, tables, page), n), refs.device)
+    _call_on(index, lib.wa_page_fork, state, at, parents.data_ptr(), children.data_ptr(), n, _ptr(status), workspace.data_ptr(),
+             workspace.numel())
+
+
+def page_free(refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, slots: torch.Tensor, *, page: int,
+              status: Optional[torch.Tensor] = None) -> None:
+    """Gives the pages of the sequences slots (int32 [n]) back, in place: refs go down, lens to 0; tables and contents stay."""
+    lib = L.load()
+    state = _page_state(refs, tables, lens, page)
+    _int32(slots, "slots", (None,))
+    _int32(status, "status", (1,))
+    index = _one_device(refs=refs, tables=tables, lens=lens, slots=slots, status=status)
+    _call_on(index, lib.wa_page_free, state, slots.data_ptr(), slots.numel(), _ptr(status))
+
+
+def page_compact(pool: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, *, page: int,
+                 out_refs: Optional[torch.Tensor] = None, out_tables: Optional[torch.Tensor] = None,
+                 used: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None) -> None:
+    """Moves the pages in use to the front of the pool: of u in use those numbered u and above go, in order, to the free ones
+    below u. out_refs and out_tables take the new state (None: in place); with their own, calls in flight may go on with the
+    old one, since what a page held stays where it was until the page is dealt out again. used: int32 [1], u."""
+    lib = L.load()
+    state, at = _page_state(refs, tables, lens, page), _page_pool(pool, refs.numel())
+    _int32(out_refs, "out_refs", refs.shape)
+    _int32(out_tables, "out_tables", tables.shape)
+    _int32(used, "used", (1,))
+    _int32(status, "status", (1,))
+    index = _one_device(pool=pool, refs=refs, tables=tables, lens=lens, out_refs=out_refs, out_tables=out_tables, used=used,
+                        status=status, workspace=workspace)
+    workspace = _room(workspace, _seq_size("wa_page_workspace_size", _page_sizes(refs, tables, page), 0), refs.device)
+    _call_on(index, lib.wa_page_compact, state, at, _ptr(refs if out_refs is None else out_refs),
+             _ptr(tables if out_tables is None else out_tables), _ptr(used), _ptr(status), workspace.data_ptr(), workspace.numel())
+
+
+def page_copy(pool: torch.Tensor, source: torch.Tensor, target: torch.Tensor, *, status: Optional[torch.Tensor] = None) -> None:
+    """Copies page source[i] to page target[i] (int32 [n]) in every plane of the pool; no page is both, or a target twice."""
+    lib = L.load()
+    at = _page_pool(pool, pool.shape[1] if pool.dim() > 1 else 0)
+    _int32(source, "source", (None,))
+    _int32(target, "target", (source.numel(),))
+    _int32(status, "status", (1,))
+    index = _one_device(pool=pool, source=source, target=target, status=status)
+    _call_on(index, lib.wa_page_copy, at, pool.shape[1], source.data_ptr(), target.data_ptr(), source.numel(), _ptr(status))
 
 
 def fp64_probe(a: torch.Tensor, b: torch.Tensor, c: torch.Tensor) -> torch.Tensor:

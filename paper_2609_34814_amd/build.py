@@ -31,6 +31,10 @@ SOURCES = {
     "diff_attn.hip": [],
     "diff_bwd.hip": [],
     "diff_tasks.hip": [],
+    "packed_attn.hip": [],
+    "packed_bwd.hip": [],
+    "paged_attn.hip": [],
+    "pages.hip": [],
     "abi.cpp": [],
 }
 

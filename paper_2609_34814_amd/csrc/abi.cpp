@@ -12,9 +12,11 @@
 
 #include "common.h"
 #include "diff_launch.h"
+#include "pages_launch.h"
 #include "perm_launch.h"
 #include "producer_launch.h"
 #include "rotary_launch.h"
+#include "seq_launch.h"
 #include "wavealign.h"
 
 namespace {
@@ -435,6 +437,207 @@ struct DiffBytes {
         mask((size_t)a.batch * a.heads * a.mb * a.nb),
         batch((size_t)a.batch * 4) {}
 };
+
+
+// ---- packed sequences and the paged cache ----
+
+constexpr int kMaxTokens = 1 << 26, kMaxKeys = 1 << 30;
+
+wa_status check_seq_shape(const wa_seq_shape* s, WaSeqLaunch* a) {
+  if (!s) return fail(WA_ERR_INVALID_ARG, "shape is null");
+  if (s->batch < 1 || s->tokens < 0 || s->heads < 1 || s->kv_heads < 1)
+    return fail(WA_ERR_INVALID_ARG, "batch, heads and kv_heads must be >= 1 and tokens >= 0 (got %d, %d, %d, %d)", s->batch, s->heads,
+                s->kv_heads, s->tokens);
+  if (s->heads % s->kv_heads) return fail(WA_ERR_INVALID_ARG, "%d heads are not a multiple of %d key heads", s->heads, s->kv_heads);
+  if (s->head_dim != 64 && s->head_dim != 128)
+    return fail(WA_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", s->head_dim);
+  if (s->dtype != WA_BF16 && s->dtype != WA_F16) return fail(WA_ERR_UNSUPPORTED, "dtype %d not supported (bf16 or fp16)", s->dtype);
+  // a dimension of a launch holds fewer than 2^32 threads: a wavefront a stored token, a lane a joined row
+  if (s->tokens >= kMaxTokens || s->batch >= kMaxTokens || (int64_t)s->tokens * s->heads >= (int64_t(1) << 31))
+    return fail(WA_ERR_UNSUPPORTED, "tokens and batch must be < 2^26 and tokens * heads < 2^31 (got %d, %d, %d heads)", s->tokens,
+                s->batch, s->heads);
+  a->batch = s->batch; a->tokens = s->tokens; a->heads = s->heads; a->kv_heads = s->kv_heads; a->head_dim = s->head_dim;
+  a->half = s->dtype == WA_F16;
+  return WA_OK;
+}
+
+size_t seq_cut_bytes(const WaSeqLaunch& a) { return align_up((size_t)a.tokens * a.heads * 8); }
+size_t seq_ws_bytes(const WaSeqLaunch& a) {
+  return a.tokens == 0 ? 0 : seq_cut_bytes(a) + align_up(wa_seq_part_floats(wa_seq_plan(a), a.head_dim) * 4);
+}
+// bf16, and a workgroup a tile of 128 queries and head in a dimension of a launch
+wa_status check_seq_backward(const WaSeqLaunch& a) {
+  if (a.half) return fail(WA_ERR_UNSUPPORTED, "the gradient is bf16 only");
+  if (wa_packed_backward_tiles(a) * a.heads >= (int64_t(1) << 24))
+    return fail(WA_ERR_UNSUPPORTED, "%d tokens of %d sequences and %d heads exceed a launch", a.tokens, a.batch, a.heads);
+  return WA_OK;
+}
+size_t seq_rows_bytes(const WaSeqLaunch& a) { return align_up((size_t)2 * a.heads * a.tokens * 4); }
+size_t seq_backward_bytes(WaSeqLaunch a) {
+  const size_t parts = wa_packed_backward_parts(a);
+  return a.tokens == 0 ? 0 : seq_rows_bytes(a) + (parts > 1 ? align_up(parts * a.tokens * a.kv_heads * 2 * a.head_dim * 4) : 0);
+}
+
+wa_status check_seq_options(const wa_seq_options* o, WaSeqLaunch* a) {
+  if (!o) return fail(WA_ERR_INVALID_ARG, "options is null");
+  const float scale = o->softmax_scale;
+  if (!std::isfinite(scale)) return fail(WA_ERR_INVALID_ARG, "softmax_scale must be finite");
+  if (scale > 0.f && (scale < 1e-30f || scale > 1e30f))
+    return fail(WA_ERR_UNSUPPORTED, "softmax_scale %g is outside 1e-30..1e30", scale);
+  a->scale = scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)a->head_dim));
+  a->causal = o->causal ? 1 : 0;
+  return WA_OK;
+}
+
+// Memory of a tensor: `count` blocks of `inner` bytes, `step` bytes apart. Vectors are one block.
+struct SeqSpan {
+  const char* name;
+  const void* at;  // null: not given
+  size_t inner, step, count;
+  bool written;
+  size_t fine = 0, fine_step = 0;  // the same memory as smaller blocks, 0: none
+  size_t bytes() const { return count ? (count - 1) * step + inner : 0; }
+};
+bool spans_meet(const SeqSpan& x, const SeqSpan& y) {
+  const uintptr_t p = (uintptr_t)x.at, q = (uintptr_t)y.at;
+  if (!x.at || !y.at || !x.bytes() || !y.bytes() || p >= q + y.bytes() || q >= p + x.bytes()) return false;
+  // blocks of equal steps: apart where each fits beside the other, in every round of the step
+  auto apart = [&](size_t step, size_t one, size_t other) {
+    if (!step) return false;
+    const size_t ahead = (size_t)(q > p ? q - p : p - q) % step, off = q >= p ? ahead : (step - ahead) % step;
+    return off >= one && off + other <= step;
+  };
+  if (x.count > 1 && y.count > 1 && x.step == y.step && apart(x.step, x.inner, y.inner)) return false;
+  return !(x.fine_step == y.fine_step && apart(x.fine_step, x.fine, y.fine));
+}
+wa_status check_seq_spans(std::initializer_list<SeqSpan> spans) {
+  for (const SeqSpan& x : spans)
+    for (const SeqSpan& y : spans)
+      if (x.written && &x != &y && spans_meet(x, y)) return fail(WA_ERR_INVALID_ARG, "%s overlaps %s", x.name, y.name);
+  return WA_OK;
+}
+SeqSpan flat(const char* name, const void* at, size_t bytes, bool written) { return {name, at, bytes, bytes, 1, written}; }
+
+constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxTokenStride = int64_t(1) << 24;
+
+// Rows [tokens][heads][d], checked; *span: their memory.
+wa_status check_rows(const wa_token_rows* r, const char* name, int tokens, int heads, int d, bool written, WaSeqRows* out, SeqSpan* span) {
+  if (!r || !r->at) return fail(WA_ERR_INVALID_ARG, "%s must be non-null", name);
+  if (!aligned(r->at, 16)) return fail(WA_ERR_ALIGNMENT, "%s must be 16-byte aligned", name);
+  const int64_t t = tokens > 1 ? r->token_stride : 0, h = heads > 1 ? r->head_stride : 0;
+  if (t < 0 || h < 0 || t >= kMaxTokenStride || h >= kMaxStride)
+    return fail(WA_ERR_UNSUPPORTED, "%s: strides %lld and %lld are outside 0..2^24 and 0..2^40", name, (long long)t, (long long)h);
+  if (t % 8 || h % 8) return fail(WA_ERR_ALIGNMENT, "%s: strides %lld and %lld are not multiples of 8", name, (long long)t, (long long)h);
+  const int64_t row = (heads - 1) * h + d, head = (tokens - 1) * t + d;
+  const bool by_token = tokens < 2 || t >= row, by_head = heads < 2 || h >= head;
+  if (written && !((by_token && (heads < 2 || h >= d)) || (by_head && (tokens < 2 || t >= d))))
+    return fail(WA_ERR_INVALID_ARG, "%s: elements of an output coincide (strides %lld and %lld)", name, (long long)t, (long long)h);
+  *out = {r->at, t, h};
+  if (by_token && tokens > 1)
+    *span = {name, r->at, (size_t)row * 2, (size_t)t * 2, (size_t)tokens, written};
+  else if (by_head && heads > 1)
+    *span = {name, r->at, (size_t)head * 2, (size_t)h * 2, (size_t)heads, written};
+  else
+    *span = flat(name, r->at, (size_t)((tokens - 1) * t + row) * 2, written);
+  return WA_OK;
+}
+
+wa_status check_tables(const wa_page_tables* t, const int32_t* kv_lens, WaSeqLaunch* a) {
+  if (!t) return fail(WA_ERR_INVALID_ARG, "tables is null");
+  if (!t->tables || !kv_lens) return fail(WA_ERR_INVALID_ARG, "tables and kv_lens must be non-null");
+  if (!aligned(t->tables, 4) || !aligned(kv_lens, 4)) return fail(WA_ERR_ALIGNMENT, "tables and kv_lens must be 4-byte aligned");
+  if (t->page < 16 || t->page > 4096 || (t->page & (t->page - 1)))
+    return fail(WA_ERR_UNSUPPORTED, "page %d not supported (a power of two, 16..4096)", t->page);
+  if (t->table_width < 1 || t->n_pages < 1)
+    return fail(WA_ERR_INVALID_ARG, "table_width and n_pages must be >= 1 (got %d, %d)", t->table_width, t->n_pages);
+  if ((int64_t)t->table_width * t->page > kMaxKeys)
+    return fail(WA_ERR_UNSUPPORTED, "a table of %d pages of %d tokens exceeds 2^30 tokens", t->table_width, t->page);
+  if (t->table_stride < 0 || t->table_stride >= kMaxStride || (t->table_stride && t->table_stride < t->table_width && a->batch > 1))
+    return fail(WA_ERR_INVALID_ARG, "table_stride %lld is below table_width %d", (long long)t->table_stride, t->table_width);
+  a->tables = t->tables; a->table_stride = t->table_stride; a->table_width = t->table_width; a->n_pages = t->n_pages;
+  a->page_shift = 0;
+  while ((1 << a->page_shift) < t->page) ++a->page_shift;
+  a->kv_lens = kv_lens;
+  return WA_OK;
+}
+SeqSpan table_span(const WaSeqLaunch& a) {
+  return flat("tables", a.tables, (size_t)((a.batch - 1) * a.table_stride + a.table_width) * 4, false);
+}
+
+// Pages [n_pages][kv_heads][page][d], checked; *span: their memory.
+wa_status check_pages(const wa_pages* p, const char* name, const WaSeqLaunch& a, bool written, WaSeqPages* out, SeqSpan* span) {
+  if (!p || !p->at) return fail(WA_ERR_INVALID_ARG, "%s must be non-null", name);
+  if (!aligned(p->at, 16)) return fail(WA_ERR_ALIGNMENT, "%s must be 16-byte aligned", name);
+  const int64_t s = a.n_pages > 1 ? p->page_stride : 0, h = a.kv_heads > 1 ? p->head_stride : 0, t = p->token_stride;
+  if (s < 0 || h < 0 || t < 0 || s >= kMaxStride || h >= kMaxStride || t >= kMaxTokenStride)
+    return fail(WA_ERR_UNSUPPORTED, "%s: strides %lld, %lld and %lld are outside 0..2^40, 0..2^40 and 0..2^24", name, (long long)s,
+                (long long)h, (long long)t);
+  if (s % 8 || h % 8 || t % 8)
+    return fail(WA_ERR_ALIGNMENT, "%s: strides %lld, %lld and %lld are not multiples of 8", name, (long long)s, (long long)h, (long long)t);
+  const int64_t tokens = int64_t(1) << a.page_shift, head = (tokens - 1) * t + a.head_dim, row = (a.kv_heads - 1) * h + a.head_dim;
+  const int64_t page = (tokens - 1) * t + row;
+  const bool nested = (t >= a.head_dim && (a.kv_heads < 2 || h >= head)) || (t >= row && (a.kv_heads < 2 || h >= a.head_dim));
+  if (written && !(nested && (a.n_pages < 2 || s >= page)))
+    return fail(WA_ERR_INVALID_ARG, "%s: elements of an output coincide (strides %lld, %lld and %lld)", name, (long long)s, (long long)h,
+                (long long)t);
+  *out = {p->at, s, h, t};
+  *span = {name, p->at, (size_t)page * 2, (size_t)s * 2, (size_t)a.n_pages, written};
+  if (t >= row && s % t == 0) span->fine = (size_t)row * 2, span->fine_step = (size_t)t * 2;
+  return WA_OK;
+}
+
+wa_status check_starts(const int32_t* starts, WaSeqLaunch* a) {
+  if (!starts) return fail(WA_ERR_INVALID_ARG, "starts must be non-null");
+  if (!aligned(starts, 4)) return fail(WA_ERR_ALIGNMENT, "starts must be 4-byte aligned");
+  a->starts = starts;
+  return WA_OK;
+}
+
+// A pool's state, checked; spans: refs, tables and lens.
+wa_status check_page_state(const wa_page_state* s, WaPageLaunch* a) {
+  if (!s) return fail(WA_ERR_INVALID_ARG, "state is null");
+  if (s->n_pages < 1 || s->sequences < 1 || s->table_width < 1)
+    return fail(WA_ERR_INVALID_ARG, "n_pages, sequences and table_width must be >= 1 (got %d, %d, %d)", s->n_pages, s->sequences,
+                s->table_width);
+  if (s->page < 1 || s->page > 4096 || (s->page & (s->page - 1)))
+    return fail(WA_ERR_UNSUPPORTED, "page %d not supported (a power of two, 1..4096)", s->page);
+  if (s->n_pages > (1 << 24) || s->sequences > (1 << 24) || s->table_width > (1 << 20))
+    return fail(WA_ERR_UNSUPPORTED, "%d pages, %d sequences or tables of %d exceed 2^24, 2^24 and 2^20", s->n_pages, s->sequences,
+                s->table_width);
+  a->refs = s->refs; a->tables = s->tables; a->lens = s->lens;
+  a->n_pages = s->n_pages; a->sequences = s->sequences; a->width = s->table_width;
+  a->shift = 0;
+  while ((1 << a->shift) < s->page) ++a->shift;
+  return WA_OK;
+}
+wa_status check_page_arrays(const WaPageLaunch& a, const int32_t* status) {
+  if (!a.refs || !a.tables || !a.lens) return fail(WA_ERR_INVALID_ARG, "refs, tables and lens must be non-null");
+  if (!aligned(a.refs, 4) || !aligned(a.tables, 4) || !aligned(a.lens, 4) || !aligned(status, 4))
+    return fail(WA_ERR_ALIGNMENT, "refs, tables, lens and status must be 4-byte aligned");
+  return WA_OK;
+}
+wa_status check_page_pool(const wa_page_pool* p, WaPageLaunch* a) {
+  if (!p || !p->at) return fail(WA_ERR_INVALID_ARG, "pool must be non-null");
+  if (!aligned(p->at, 16)) return fail(WA_ERR_ALIGNMENT, "pool must be 16-byte aligned");
+  if (p->page_bytes < 16 || p->planes < 1) return fail(WA_ERR_INVALID_ARG, "page_bytes and planes must be positive");
+  if (p->page_bytes % 16) return fail(WA_ERR_ALIGNMENT, "page_bytes %lld is not a multiple of 16", (long long)p->page_bytes);
+  if (p->page_bytes >= (int64_t(1) << 32) || (double)p->page_bytes * a->n_pages * p->planes >= 1099511627776.0)
+    return fail(WA_ERR_UNSUPPORTED, "pool too large");
+  a->pool = (unsigned char*)p->at; a->page_bytes = p->page_bytes; a->planes = p->planes;
+  return WA_OK;
+}
+// Workgroups that copy `entries` pages.
+wa_status check_page_copies(const WaPageLaunch& a, int32_t entries) {
+  if (entries < 0) return fail(WA_ERR_INVALID_ARG, "entries %d is negative", entries);
+  const int64_t wgs = entries * (a.planes * ((a.page_bytes + 16383) / 16384) + 1);
+  if (wgs >= (int64_t(1) << 24)) return fail(WA_ERR_UNSUPPORTED, "%d pages of %lld bytes in %d planes exceed a launch", entries,
+                                             (long long)a.page_bytes, a.planes);
+  return WA_OK;
+}
+SeqSpan refs_span(const WaPageLaunch& a) { return flat("refs", a.refs, (size_t)a.n_pages * 4, true); }
+SeqSpan tables_span(const WaPageLaunch& a, bool written) { return flat("tables", a.tables, (size_t)a.sequences * a.width * 4, written); }
+SeqSpan lens_span(const WaPageLaunch& a, bool written) { return flat("lens", a.lens, (size_t)a.sequences * 4, written); }
+SeqSpan pool_span(const WaPageLaunch& a) { return flat("pool", a.pool, (size_t)a.planes * a.n_pages * a.page_bytes, true); }
 
 }  // namespace
 
@@ -919,6 +1122,267 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
   a.part = (float*)((char*)workspace + L.part);
   const hipError_t e = wa_launch_diff_backward(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "differential attention gradient launch");
+  return ok();
+}
+
+wa_status wa_seq_attn_workspace_size(const wa_seq_shape* shape, size_t* bytes) {
+  WaSeqLaunch a{};
+  wa_status s = check_seq_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
+  *bytes = seq_ws_bytes(a);
+  return ok();
+}
+
+wa_status wa_packed_attn(const wa_token_rows* q, const wa_token_rows* k, const wa_token_rows* v, const int32_t* starts,
+                         const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* o, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  WaSeqLaunch a{};
+  SeqSpan sq, sk, sv, so;
+  wa_status s = check_seq_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_seq_options(options, &a)) != WA_OK) return s;
+  if (a.tokens == 0) return ok();
+  if ((s = check_rows(q, "q", a.tokens, a.heads, a.head_dim, false, &a.q, &sq)) != WA_OK) return s;
+  if ((s = check_rows(k, "k", a.tokens, a.kv_heads, a.head_dim, false, &a.k, &sk)) != WA_OK) return s;
+  if ((s = check_rows(v, "v", a.tokens, a.kv_heads, a.head_dim, false, &a.v, &sv)) != WA_OK) return s;
+  if ((s = check_rows(o, "o", a.tokens, a.heads, a.head_dim, true, &a.o, &so)) != WA_OK) return s;
+  if ((s = check_starts(starts, &a)) != WA_OK) return s;
+  if (!aligned(lse, 4)) return fail(WA_ERR_ALIGNMENT, "lse must be 4-byte aligned");
+  const size_t need = seq_ws_bytes(a);
+  if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
+  s = check_seq_spans({so, flat("lse", lse, (size_t)a.heads * a.tokens * 4, true), flat("workspace", workspace, need, true), sq, sk, sv,
+                       flat("starts", starts, (size_t)(a.batch + 1) * 4, false)});
+  if (s != WA_OK) return s;
+  a.lse = lse;
+  a.cuts = (int2*)workspace;
+  a.part = (float*)((char*)workspace + seq_cut_bytes(a));
+  const hipError_t e = wa_launch_packed_attn(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "packed attention launch");
+  return ok();
+}
+
+wa_status wa_packed_attn_backward_workspace_size(const wa_seq_shape* shape, size_t* bytes) {
+  WaSeqLaunch a{};
+  wa_status s = check_seq_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_seq_backward(a)) != WA_OK) return s;
+  if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
+  *bytes = seq_backward_bytes(a);
+  return ok();
+}
+
+wa_status wa_packed_attn_backward(const wa_token_rows* dout, const wa_token_rows* q, const wa_token_rows* k,
+                                  const wa_token_rows* v, const wa_token_rows* o, const float* lse, const int32_t* starts,
+                                  const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* dq,
+                                  const wa_token_rows* dk, const wa_token_rows* dv, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+  WaSeqLaunch a{};
+  SeqSpan sg, sq, sk, sv, so, gq, gk, gv;
+  wa_status s = check_seq_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_seq_backward(a)) != WA_OK) return s;
+  if ((s = check_seq_options(options, &a)) != WA_OK) return s;
+  if (a.tokens == 0) return ok();
+  if ((s = check_rows(dout, "dout", a.tokens, a.heads, a.head_dim, false, &a.dout, &sg)) != WA_OK) return s;
+  if ((s = check_rows(q, "q", a.tokens, a.heads, a.head_dim, false, &a.q, &sq)) != WA_OK) return s;
+  if ((s = check_rows(k, "k", a.tokens, a.kv_heads, a.head_dim, false, &a.k, &sk)) != WA_OK) return s;
+  if ((s = check_rows(v, "v", a.tokens, a.kv_heads, a.head_dim, false, &a.v, &sv)) != WA_OK) return s;
+  if ((s = check_rows(o, "o", a.tokens, a.heads, a.head_dim, false, &a.o, &so)) != WA_OK) return s;
+  if ((s = check_rows(dq, "dq", a.tokens, a.heads, a.head_dim, true, &a.dq, &gq)) != WA_OK) return s;
+  if ((s = check_rows(dk, "dk", a.tokens, a.kv_heads, a.head_dim, true, &a.dk, &gk)) != WA_OK) return s;
+  if ((s = check_rows(dv, "dv", a.tokens, a.kv_heads, a.head_dim, true, &a.dv, &gv)) != WA_OK) return s;
+  if ((s = check_starts(starts, &a)) != WA_OK) return s;
+  if (!lse) return fail(WA_ERR_INVALID_ARG, "lse must be non-null");
+  if (!aligned(lse, 4)) return fail(WA_ERR_ALIGNMENT, "lse must be 4-byte aligned");
+  const size_t need = seq_backward_bytes(a);
+  if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
+  s = check_seq_spans({gq, gk, gv, flat("workspace", workspace, need, true), sg, sq, sk, sv, so,
+                       flat("lse", lse, (size_t)a.heads * a.tokens * 4, false), flat("starts", starts, (size_t)(a.batch + 1) * 4, false)});
+  if (s != WA_OK) return s;
+  a.lse_in = lse;
+  a.parts = wa_packed_backward_parts(a);
+  a.rows = (float*)workspace;
+  a.part = (float*)((char*)workspace + seq_rows_bytes(a));
+  const hipError_t e = wa_launch_packed_backward(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "packed attention gradient launch");
+  return ok();
+}
+
+wa_status wa_paged_attn(const wa_token_rows* q, const wa_pages* k, const wa_pages* v, const wa_page_tables* tables,
+                        const int32_t* starts, const int32_t* kv_lens, const wa_seq_shape* shape,
+                        const wa_seq_options* options, const wa_token_rows* o, float* lse, int32_t* status,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  WaSeqLaunch a{};
+  SeqSpan sq, sk, sv, so;
+  wa_status s = check_seq_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_seq_options(options, &a)) != WA_OK) return s;
+  if (a.tokens == 0) return ok();
+  if ((s = check_tables(tables, kv_lens, &a)) != WA_OK) return s;
+  if ((s = check_rows(q, "q", a.tokens, a.heads, a.head_dim, false, &a.q, &sq)) != WA_OK) return s;
+  if ((s = check_pages(k, "k", a, false, &a.kp, &sk)) != WA_OK) return s;
+  if ((s = check_pages(v, "v", a, false, &a.vp, &sv)) != WA_OK) return s;
+  if ((s = check_rows(o, "o", a.tokens, a.heads, a.head_dim, true, &a.o, &so)) != WA_OK) return s;
+  if ((s = check_starts(starts, &a)) != WA_OK) return s;
+  if (!aligned(lse, 4) || !aligned(status, 4)) return fail(WA_ERR_ALIGNMENT, "lse and status must be 4-byte aligned");
+  const size_t need = seq_ws_bytes(a);
+  if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
+  s = check_seq_spans({so, flat("lse", lse, (size_t)a.heads * a.tokens * 4, true), flat("workspace", workspace, need, true),
+                       flat("status", status, 4, true), sq, sk, sv, table_span(a), flat("starts", starts, (size_t)(a.batch + 1) * 4, false),
+                       flat("kv_lens", kv_lens, (size_t)a.batch * 4, false)});
+  if (s != WA_OK) return s;
+  a.lse = lse;
+  a.status = status;
+  a.cuts = (int2*)workspace;
+  a.part = (float*)((char*)workspace + seq_cut_bytes(a));
+  const hipError_t e = wa_launch_paged_attn(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "paged attention launch");
+  return ok();
+}
+
+wa_status wa_page_store(const wa_token_rows* k, const wa_token_rows* v, const wa_pages* k_pages, const wa_pages* v_pages,
+                        const wa_page_tables* tables, const int32_t* starts, const int32_t* kv_lens,
+                        const wa_seq_shape* shape, int32_t* status, void* stream) {
+  WaSeqLaunch a{};
+  SeqSpan sk, sv, pk, pv;
+  wa_status s = check_seq_shape(shape, &a);
+  if (s != WA_OK) return s;
+  if (a.tokens == 0) return ok();
+  if ((s = check_tables(tables, kv_lens, &a)) != WA_OK) return s;
+  if ((s = check_rows(k, "k", a.tokens, a.kv_heads, a.head_dim, false, &a.k, &sk)) != WA_OK) return s;
+  if ((s = check_rows(v, "v", a.tokens, a.kv_heads, a.head_dim, false, &a.v, &sv)) != WA_OK) return s;
+  if ((s = check_pages(k_pages, "k_pages", a, true, &a.kp, &pk)) != WA_OK) return s;
+  if ((s = check_pages(v_pages, "v_pages", a, true, &a.vp, &pv)) != WA_OK) return s;
+  if ((s = check_starts(starts, &a)) != WA_OK) return s;
+  if (!aligned(status, 4)) return fail(WA_ERR_ALIGNMENT, "status must be 4-byte aligned");
+  s = check_seq_spans({pk, pv, flat("status", status, 4, true), sk, sv, table_span(a),
+                       flat("starts", starts, (size_t)(a.batch + 1) * 4, false), flat("kv_lens", kv_lens, (size_t)a.batch * 4, false)});
+  if (s != WA_OK) return s;
+  a.status = status;
+  const hipError_t e = wa_launch_page_store(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "page store launch");
+  return ok();
+}
+
+wa_status wa_page_workspace_size(const wa_page_state* state, int32_t entries, size_t* bytes) {
+  WaPageLaunch a{};
+  wa_status s = check_page_state(state, &a);
+  if (s != WA_OK) return s;
+  if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
+  if (entries < 0) return fail(WA_ERR_INVALID_ARG, "entries %d is negative", entries);
+  a.entries = entries;
+  *bytes = align_up(wa_page_ws_ints(a) * 4);
+  return ok();
+}
+
+wa_status wa_page_grow(const wa_page_state* state, const int32_t* new_lens, int32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  WaPageLaunch a{};
+  wa_status s = check_page_state(state, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_page_arrays(a, status)) != WA_OK) return s;
+  if (!new_lens) return fail(WA_ERR_INVALID_ARG, "new_lens must be non-null");
+  if (!aligned(new_lens, 4)) return fail(WA_ERR_ALIGNMENT, "new_lens must be 4-byte aligned");
+  const size_t need = align_up(wa_page_ws_ints(a) * 4);
+  if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
+  s = check_seq_spans({refs_span(a), tables_span(a, true), lens_span(a, true), flat("status", status, 4, true),
+                       flat("workspace", workspace, need, true), flat("new_lens", new_lens, (size_t)a.sequences * 4, false)});
+  if (s != WA_OK) return s;
+  a.first = new_lens; a.status = status; a.ws = (int32_t*)workspace;
+  const hipError_t e = wa_launch_page_grow(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "page grow launch");
+  return ok();
+}
+
+wa_status wa_page_fork(const wa_page_state* state, const wa_page_pool* pool, const int32_t* parents,
+                       const int32_t* children, int32_t entries, int32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  WaPageLaunch a{};
+  wa_status s = check_page_state(state, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_page_arrays(a, status)) != WA_OK) return s;
+  if ((s = check_page_pool(pool, &a)) != WA_OK) return s;
+  if ((s = check_page_copies(a, entries)) != WA_OK) return s;
+  if (entries == 0) return ok();
+  if (!parents || !children) return fail(WA_ERR_INVALID_ARG, "parents and children must be non-null");
+  if (!aligned(parents, 4) || !aligned(children, 4)) return fail(WA_ERR_ALIGNMENT, "parents and children must be 4-byte aligned");
+  a.entries = entries;
+  const size_t need = align_up(wa_page_ws_ints(a) * 4);
+  if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
+  s = check_seq_spans({refs_span(a), tables_span(a, true), lens_span(a, true), pool_span(a), flat("status", status, 4, true),
+                       flat("workspace", workspace, need, true), flat("parents", parents, (size_t)entries * 4, false),
+                       flat("children", children, (size_t)entries * 4, false)});
+  if (s != WA_OK) return s;
+  a.first = parents; a.second = children; a.status = status; a.ws = (int32_t*)workspace;
+  const hipError_t e = wa_launch_page_fork(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "page fork launch");
+  return ok();
+}
+
+wa_status wa_page_free(const wa_page_state* state, const int32_t* slots, int32_t entries, int32_t* status, void* stream) {
+  WaPageLaunch a{};
+  wa_status s = check_page_state(state, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_page_arrays(a, status)) != WA_OK) return s;
+  if (entries < 0) return fail(WA_ERR_INVALID_ARG, "entries %d is negative", entries);
+  if (entries >= (1 << 24)) return fail(WA_ERR_UNSUPPORTED, "%d entries exceed a launch", entries);
+  if (entries == 0) return ok();
+  if (!slots) return fail(WA_ERR_INVALID_ARG, "slots must be non-null");
+  if (!aligned(slots, 4)) return fail(WA_ERR_ALIGNMENT, "slots must be 4-byte aligned");
+  s = check_seq_spans({refs_span(a), lens_span(a, true), flat("status", status, 4, true), tables_span(a, false),
+                       flat("slots", slots, (size_t)entries * 4, false)});
+  if (s != WA_OK) return s;
+  a.first = slots; a.entries = entries; a.status = status;
+  const hipError_t e = wa_launch_page_free(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "page free launch");
+  return ok();
+}
+
+wa_status wa_page_compact(const wa_page_state* state, const wa_page_pool* pool, int32_t* out_refs, int32_t* out_tables,
+                          int32_t* used, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  WaPageLaunch a{};
+  wa_status s = check_page_state(state, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_page_arrays(a, status)) != WA_OK) return s;
+  if ((s = check_page_pool(pool, &a)) != WA_OK) return s;
+  if (!out_refs || !out_tables) return fail(WA_ERR_INVALID_ARG, "out_refs and out_tables must be non-null");
+  if (!aligned(out_refs, 4) || !aligned(out_tables, 4) || !aligned(used, 4))
+    return fail(WA_ERR_ALIGNMENT, "out_refs, out_tables and used must be 4-byte aligned");
+  const size_t need = align_up(wa_page_ws_ints(a) * 4);
+  if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
+  // in place the outputs are the inputs
+  s = check_seq_spans({flat("out_refs", out_refs, (size_t)a.n_pages * 4, true),
+                       flat("refs", out_refs == a.refs ? nullptr : a.refs, (size_t)a.n_pages * 4, false),
+                       flat("out_tables", out_tables, (size_t)a.sequences * a.width * 4, true),
+                       flat("tables", out_tables == a.tables ? nullptr : a.tables, (size_t)a.sequences * a.width * 4, false),
+                       lens_span(a, false), pool_span(a), flat("used", used, 4, true), flat("status", status, 4, true),
+                       flat("workspace", workspace, need, true)});
+  if (s != WA_OK) return s;
+  a.out_refs = out_refs; a.out_tables = out_tables; a.used = used; a.status = status; a.ws = (int32_t*)workspace;
+  const hipError_t e = wa_launch_page_compact(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "page compaction launch");
+  return ok();
+}
+
+wa_status wa_page_copy(const wa_page_pool* pool, int32_t n_pages, const int32_t* from, const int32_t* to, int32_t entries,
+                       int32_t* status, void* stream) {
+  WaPageLaunch a{};
+  if (n_pages < 1) return fail(WA_ERR_INVALID_ARG, "n_pages must be >= 1 (got %d)", n_pages);
+  a.n_pages = n_pages;
+  wa_status s = check_page_pool(pool, &a);
+  if (s != WA_OK) return s;
+  if ((s = check_page_copies(a, entries)) != WA_OK) return s;
+  if (entries == 0) return ok();
+  if (!from || !to) return fail(WA_ERR_INVALID_ARG, "from and to must be non-null");
+  if (!aligned(from, 4) || !aligned(to, 4) || !aligned(status, 4))
+    return fail(WA_ERR_ALIGNMENT, "from, to and status must be 4-byte aligned");
+  s = check_seq_spans({pool_span(a), flat("status", status, 4, true), flat("from", from, (size_t)entries * 4, false),
+                       flat("to", to, (size_t)entries * 4, false)});
+  if (s != WA_OK) return s;
+  a.first = from; a.second = to; a.entries = entries; a.status = status;
+  const hipError_t e = wa_launch_page_copy(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "page copy launch");
   return ok();
 }
 

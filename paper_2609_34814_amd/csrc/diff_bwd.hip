@@ -52,10 +52,6 @@ constexpr int kDqWaves = D == 64 ? 2 : 1;
 template <int D>
 constexpr int kDkvWaves = D == 64 ? 2 : 1;
 
-__device__ __forceinline__ void fill(f32x16& x, float f) {
-#pragma unroll
-  for (int v = 0; v < 16; ++v) x[v] = f;
-}
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -84,10 +80,6 @@ template <int WAVES>
 __device__ __forceinline__ void settled(f32x16& c, f32x16& d) {
   if constexpr (WAVES == 1) asm volatile("s_nop 11" : "+v"(c), "+v"(d));
 }
-// Registers 8 s to 8 s + 7 of a product as an operand over its rows.
-__device__ __forceinline__ bf16x8 pack8(const float* p) {
-  return as_bf16x8(make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
-}
 __device__ __forceinline__ float dot8(bf16x8 a, uint4 b, float sum) {
   typedef short s16x8 __attribute__((ext_vector_type(8)));
   const s16x8 n = __builtin_bit_cast(s16x8, b);
@@ -95,32 +87,6 @@ __device__ __forceinline__ float dot8(bf16x8 a, uint4 b, float sum) {
   for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)a[i], (float)n[i], sum);
   return sum;
 }
-__device__ __forceinline__ bf16x8 load8(const uint16_t* p, bool ok) {
-  uint4 u = make_uint4(0, 0, 0, 0);
-  if (ok) u = *(const uint4*)p;
-  return as_bf16x8(u);
-}
-// acc (rows: columns of the output) to the lane's output row, times f
-template <int T>
-__device__ __forceinline__ void store_row(uint16_t* out, const f32x16 (&acc)[T], float f, int hf) {
-#pragma unroll
-  for (int t = 0; t < T; ++t)
-#pragma unroll
-    for (int v = 0; v < 16; v += 4)
-      *(uint2*)(out + t * 32 + 2 * v + 4 * hf) =
-          make_uint2(pack_bf16x2(acc[t][v] * f, acc[t][v + 1] * f), pack_bf16x2(acc[t][v + 2] * f, acc[t][v + 3] * f));
-}
-
-// the same unrounded, as a row of a part's result
-template <int T>
-__device__ __forceinline__ void store_part(float* out, const f32x16 (&acc)[T], float f, int hf) {
-#pragma unroll
-  for (int t = 0; t < T; ++t)
-#pragma unroll
-    for (int v = 0; v < 16; v += 4)
-      *(float4*)(out + t * 32 + 2 * v + 4 * hf) = make_float4(acc[t][v] * f, acc[t][v + 1] * f, acc[t][v + 2] * f, acc[t][v + 3] * f);
-}
-
 template <int D, int DV, int W>
 __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDiffLaunch a, const WaDiffSide n) {
   using C = Bwd<D, DV, W>;
@@ -342,21 +308,6 @@ __global__ __launch_bounds__(64 * W, kDqWaves<D>) void diff_dq_kernel(const WaDi
     if (a.tasks && task.chunk == 0)
       for (int x = task.chunks; x < kDiffMaxChunks; ++x) to[x] = 0.0;
   }
-}
-
-// One 4-byte-a-lane copy from global memory into LDS at the uniform address lds (lane i writes lds + 4 i).
-__device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, const unsigned char* lds) {
-  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds);
-  uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %1\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dword %2, %3\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "s"(m0), "v"(voff), "s"(gbase)
-      : "memory");
 }
 
 template <int D, int DV, int W>

@@ -246,4 +246,69 @@ __device__ __forceinline__ float add_halves(float x) {
   return v[0] + v[1];
 }
 
+// Helpers of the gradients.
+__device__ __forceinline__ void fill(f32x16& x, float f) {
+#pragma unroll
+  for (int v = 0; v < 16; ++v) x[v] = f;
+}
+// Registers 8 s to 8 s + 7 of a product as an operand over its rows.
+__device__ __forceinline__ bf16x8 pack8(const float* p) {
+  return as_bf16x8(make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
+}
+__device__ __forceinline__ bf16x8 load8(const uint16_t* p, bool ok) {
+  uint4 u = make_uint4(0, 0, 0, 0);
+  if (ok) u = *(const uint4*)p;
+  return as_bf16x8(u);
+}
+// acc (rows: columns of the output) to the lane's output row, times f
+template <int T>
+__device__ __forceinline__ void store_row(uint16_t* out, const f32x16 (&acc)[T], float f, int hf) {
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4)
+      *(uint2*)(out + t * 32 + 2 * v + 4 * hf) =
+          make_uint2(pack_bf16x2(acc[t][v] * f, acc[t][v + 1] * f), pack_bf16x2(acc[t][v + 2] * f, acc[t][v + 3] * f));
+}
+
+// the same unrounded, as a row of a part's result
+template <int T>
+__device__ __forceinline__ void store_part(float* out, const f32x16 (&acc)[T], float f, int hf) {
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4)
+      *(float4*)(out + t * 32 + 2 * v + 4 * hf) = make_float4(acc[t][v] * f, acc[t][v + 1] * f, acc[t][v + 2] * f, acc[t][v + 3] * f);
+}
+
+// One 4-byte-a-lane copy from global memory into LDS at the uniform address lds (lane i writes lds + 4 i).
+__device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, const unsigned char* lds) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %2, %3\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(m0), "v"(voff), "s"(gbase)
+      : "memory");
+}
+
+// The same from an address of the lane's own.
+__device__ __forceinline__ void dma4_at(const void* from, const unsigned char* lds) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %2, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(m0), "v"(from)
+      : "memory");
+}
+
 }  // namespace wa
