@@ -530,28 +530,29 @@ wa_status wa_seq_attn_workspace_size(const wa_seq_shape* shape, size_t* bytes);
  * their outputs are left as they were.
  *   q, o       [tokens][H][d];  k, v  [tokens][Hk][d]
  *   starts     int32 [batch + 1], device, ascending; values are taken into 0..tokens. A sequence may be empty
- *   lse        out float [H][tokens], nullable: natural-log sum-exp of a query's scaled scores, for the gradient
+ *   stats      out float [H][tokens][1 + d/4] (fp16: [H][tokens][1]), nullable: the natural-log sum-exp of a query's scaled scores
+ *              and then, for the gradient, what O's columns lost in rounding, a byte each
  *   workspace  >= wa_seq_attn_workspace_size(shape), 256-byte aligned
  * Outputs and workspace overlap neither inputs nor each other (refused; outputs may interleave in one tensor of equal token strides).
  * How the work is cut follows from the lengths, so equal calls give equal bits; the bits of a sequence may
  * depend on the lengths of the others. */
 wa_status wa_packed_attn(const wa_token_rows* q, const wa_token_rows* k, const wa_token_rows* v, const int32_t* starts,
-                         const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* o, float* lse,
+                         const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* o, float* stats,
                          void* workspace, size_t workspace_bytes, void* stream);
 
-/* Workspace bytes needed by wa_packed_attn_backward: 2 H tokens float32, and float32 results of key tiles that are computed in parts. */
+/* Workspace bytes needed by wa_packed_attn_backward: 2 H tokens float32, and float32 results of tiles that are computed in parts (200 MB
+ * at most). */
 wa_status wa_packed_attn_backward_workspace_size(const wa_seq_shape* shape, size_t* bytes);
 
 /* Gradient of wa_packed_attn, bf16 only (dS = P (dP - dO . O) lies below fp16's range): with dO of O it writes
  *   dV = P^T dO, dQ = scale dS K, dK = scale dS^T Q, dP = dO V^T, dV and dK summed over the heads of a key head,
- * probabilities recomputed in float32 from lse, sums in float32, P and dS rounded to bf16 for the matrix products, dO . O taken of
- * the bf16 O. Rows of no sequence are left as they were. Nothing is added with atomics: equal calls give equal bits.
- *   dout, o, lse   dO [tokens][H][d]; what wa_packed_attn wrote
+ * probabilities recomputed in float32 from stats, sums in float32, P and dS rounded to bf16 for the matrix products. Rows of no sequence are left as they were. Nothing is added with atomics: equal calls give equal bits.
+ *   dout, o, stats   dO [tokens][H][d]; what wa_packed_attn wrote
  *   dq, dk, dv     out, shaped as q, k and v
  *   workspace      >= wa_packed_attn_backward_workspace_size(shape), 256-byte aligned
  * Outputs and workspace overlap neither inputs nor each other (as above). */
 wa_status wa_packed_attn_backward(const wa_token_rows* dout, const wa_token_rows* q, const wa_token_rows* k,
-                                  const wa_token_rows* v, const wa_token_rows* o, const float* lse, const int32_t* starts,
+                                  const wa_token_rows* v, const wa_token_rows* o, const float* stats, const int32_t* starts,
                                   const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* dq,
                                   const wa_token_rows* dk, const wa_token_rows* dv, void* workspace, size_t workspace_bytes,
                                   void* stream);
@@ -587,11 +588,12 @@ typedef struct wa_page_tables {
 /* Attention of new tokens over a paged cache: sequence b's n = starts[b + 1] - starts[b] queries (one in a decoding step, a
  * chunk of a prompt, none) are its last n of kv_lens[b] tokens, whose keys and values all lie in the pages (wa_page_store puts the
  * new ones there). Query i sees the keys up to kv_lens[b] - n + i, without `causal` all kv_lens[b]; one that sees none gets O = 0 and
- * a sum-exp of -inf. Arithmetic, o, lse, workspace and order as for wa_packed_attn.
+ * a sum-exp of -inf. Arithmetic, o, workspace and order as for wa_packed_attn.
  *   q, o      [tokens][H][d]
  *   k, v      pages of Hk heads; what lies behind a sequence's last token is not used, all before has to be finite
  *   starts    int32 [batch + 1], device, ascending; values are taken into 0..tokens
  *   kv_lens   int32 [batch], device: taken into 0..table_width * page
+ *   lse       out float [H][tokens], nullable: natural-log sum-exp of a query's scaled scores
  *   status    device int32, nullable: WA_PAGE_BAD_INDEX is added where a sequence's table names a page outside
  *             0..n_pages - 1; keys of such a page are left out */
 wa_status wa_paged_attn(const wa_token_rows* q, const wa_pages* k, const wa_pages* v, const wa_page_tables* tables,

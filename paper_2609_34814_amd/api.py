@@ -676,6 +676,10 @@ def _seq_size(call: str, shape: bytes, *more) -> int:
     return n.value
 
 
+def _lse_step(dtype, d: int) -> int:
+    return 1 + d // 4 if dtype == torch.bfloat16 else 1
+
+
 def _room(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
     _check(workspace, "workspace", torch.uint8)
     return _workspace(need, device) if workspace is None or workspace.numel() < need else workspace
@@ -701,7 +705,8 @@ def packed_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch
     starts    int32 [B + 1], ascending: sequence b has the rows starts[b] to starts[b + 1] - 1 and may be empty
     causal    each query sees the keys up to its own
     scale     positive; None: 1 / sqrt(d)
-    return_lse  also float32 [H][T], the log-sum-exps of the scaled scores, which packed_attn_backward takes
+    return_lse  also what packed_attn_backward takes: float32 [H][T][1 + d / 4] (float16, which has no gradient: [H][T][1]), of
+              which [..., 0] are the log-sum-exps of the scaled scores and the others hold, as bytes, what O lost in rounding
     out       as q, of any strides; None: a new contiguous tensor. Rows of no sequence keep what they hold (in a new
               tensor and in the log-sum-exps: anything)
 
@@ -718,7 +723,7 @@ def packed_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch
     index = _one_device(q=q, k=k, v=v, starts=starts, out=out, workspace=workspace)
     need = _seq_size("wa_seq_attn_workspace_size", shape)
     workspace = _room(workspace, need, q.device)
-    lse = q.new_empty((h, t), dtype=torch.float32) if return_lse else None
+    lse = q.new_empty((h, t, _lse_step(q.dtype, d)), dtype=torch.float32) if return_lse else None
     _call_on(index, lib.wa_packed_attn, *rows, starts.data_ptr(), shape, L.SEQ_OPTIONS.pack(softmax_scale, 1 if causal else 0), to,
              _ptr(lse), workspace.data_ptr(), workspace.numel())
     return (o, lse) if return_lse else o
@@ -738,8 +743,8 @@ def packed_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v
     kv = (t, k.shape[1], d)
     bf = torch.bfloat16
     rows = [_rows(x, n, bf, w) for x, n, w in ((dout, "dout", q.shape), (q, "q", q.shape), (k, "k", kv), (v, "v", kv), (o, "o", q.shape))]
-    if lse.dtype != torch.float32 or lse.shape != (h, t) or not lse.is_contiguous():
-        raise ValueError(f"lse must be contiguous float32 [{h}][{t}], got {lse.dtype} {tuple(lse.shape)}")
+    if lse.dtype != torch.float32 or lse.shape != (h, t, _lse_step(bf, d)) or not lse.is_contiguous():
+        raise ValueError(f"lse must be contiguous float32 [{h}][{t}][{_lse_step(bf, d)}], got {lse.dtype} {tuple(lse.shape)}")
     if out is None:
         out = (q.new_empty(q.shape), q.new_empty(kv), q.new_empty(kv))
     dq, dk, dv = out
@@ -782,7 +787,8 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, ta
     starts    int32 [B + 1], ascending; kv_lens int32 [B]: tokens of each sequence, the new ones counted
     causal    query i of n sees the keys up to kv_lens[b] - n + i; else all kv_lens[b]. One that sees none gets 0
     status    int32 [1], to which WA_PAGE_BAD_INDEX (1) is added if a table names a page that there is not: its keys are left out
-    scale, return_lse, out   as for packed_attn
+    return_lse  also float32 [H][T], the log-sum-exps of the scaled scores
+    scale, out  as for packed_attn
 
     What lies behind a sequence's last token is not used; all before has to be finite."""
     lib = L.load()

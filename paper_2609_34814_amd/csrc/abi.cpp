@@ -461,21 +461,22 @@ wa_status check_seq_shape(const wa_seq_shape* s, WaSeqLaunch* a) {
   return WA_OK;
 }
 
-size_t seq_cut_bytes(const WaSeqLaunch& a) { return align_up((size_t)a.tokens * a.heads * 8); }
+// a row's log-sum-exp and, for the gradient, the rest of each column of O in a byte
+int seq_lse_step(const WaSeqLaunch& a) { return a.half ? 1 : 1 + a.head_dim / 4; }
+size_t seq_cut_bytes(const WaSeqLaunch& a) { return kAlign + align_up((size_t)a.tokens * a.heads * 8); }
 size_t seq_ws_bytes(const WaSeqLaunch& a) {
   return a.tokens == 0 ? 0 : seq_cut_bytes(a) + align_up(wa_seq_part_floats(wa_seq_plan(a), a.head_dim) * 4);
 }
 // bf16, and a workgroup a tile of 128 queries and head in a dimension of a launch
 wa_status check_seq_backward(const WaSeqLaunch& a) {
   if (a.half) return fail(WA_ERR_UNSUPPORTED, "the gradient is bf16 only");
-  if (wa_packed_backward_tiles(a) * a.heads >= (int64_t(1) << 24))
+  if (wa_packed_backward_tiles(a) * a.heads >= (int64_t(1) << 24) - 1024)
     return fail(WA_ERR_UNSUPPORTED, "%d tokens of %d sequences and %d heads exceed a launch", a.tokens, a.batch, a.heads);
   return WA_OK;
 }
 size_t seq_rows_bytes(const WaSeqLaunch& a) { return align_up((size_t)2 * a.heads * a.tokens * 4); }
-size_t seq_backward_bytes(WaSeqLaunch a) {
-  const size_t parts = wa_packed_backward_parts(a);
-  return a.tokens == 0 ? 0 : seq_rows_bytes(a) + (parts > 1 ? align_up(parts * a.tokens * a.kv_heads * 2 * a.head_dim * 4) : 0);
+size_t seq_backward_bytes(const WaSeqLaunch& a) {
+  return a.tokens == 0 ? 0 : seq_rows_bytes(a) + align_up((size_t)wa_packed_backward_part_floats(a) * 4);
 }
 
 wa_status check_seq_options(const wa_seq_options* o, WaSeqLaunch* a) {
@@ -1135,7 +1136,7 @@ wa_status wa_seq_attn_workspace_size(const wa_seq_shape* shape, size_t* bytes) {
 }
 
 wa_status wa_packed_attn(const wa_token_rows* q, const wa_token_rows* k, const wa_token_rows* v, const int32_t* starts,
-                         const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* o, float* lse,
+                         const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* o, float* stats,
                          void* workspace, size_t workspace_bytes, void* stream) {
   WaSeqLaunch a{};
   SeqSpan sq, sk, sv, so;
@@ -1148,14 +1149,16 @@ wa_status wa_packed_attn(const wa_token_rows* q, const wa_token_rows* k, const w
   if ((s = check_rows(v, "v", a.tokens, a.kv_heads, a.head_dim, false, &a.v, &sv)) != WA_OK) return s;
   if ((s = check_rows(o, "o", a.tokens, a.heads, a.head_dim, true, &a.o, &so)) != WA_OK) return s;
   if ((s = check_starts(starts, &a)) != WA_OK) return s;
-  if (!aligned(lse, 4)) return fail(WA_ERR_ALIGNMENT, "lse must be 4-byte aligned");
+  if (!aligned(stats, 4)) return fail(WA_ERR_ALIGNMENT, "stats must be 4-byte aligned");
   const size_t need = seq_ws_bytes(a);
   if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
-  s = check_seq_spans({so, flat("lse", lse, (size_t)a.heads * a.tokens * 4, true), flat("workspace", workspace, need, true), sq, sk, sv,
+  s = check_seq_spans({so, flat("stats", stats, (size_t)a.heads * a.tokens * seq_lse_step(a) * 4, true), flat("workspace", workspace, need, true), sq, sk, sv,
                        flat("starts", starts, (size_t)(a.batch + 1) * 4, false)});
   if (s != WA_OK) return s;
-  a.lse = lse;
-  a.cuts = (int2*)workspace;
+  a.lse = stats;
+  a.lse_step = seq_lse_step(a);
+  a.any_cut = (int32_t*)workspace;
+  a.cuts = (int2*)((char*)workspace + kAlign);
   a.part = (float*)((char*)workspace + seq_cut_bytes(a));
   const hipError_t e = wa_launch_packed_attn(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "packed attention launch");
@@ -1173,7 +1176,7 @@ wa_status wa_packed_attn_backward_workspace_size(const wa_seq_shape* shape, size
 }
 
 wa_status wa_packed_attn_backward(const wa_token_rows* dout, const wa_token_rows* q, const wa_token_rows* k,
-                                  const wa_token_rows* v, const wa_token_rows* o, const float* lse, const int32_t* starts,
+                                  const wa_token_rows* v, const wa_token_rows* o, const float* stats, const int32_t* starts,
                                   const wa_seq_shape* shape, const wa_seq_options* options, const wa_token_rows* dq,
                                   const wa_token_rows* dk, const wa_token_rows* dv, void* workspace, size_t workspace_bytes,
                                   void* stream) {
@@ -1193,15 +1196,16 @@ wa_status wa_packed_attn_backward(const wa_token_rows* dout, const wa_token_rows
   if ((s = check_rows(dk, "dk", a.tokens, a.kv_heads, a.head_dim, true, &a.dk, &gk)) != WA_OK) return s;
   if ((s = check_rows(dv, "dv", a.tokens, a.kv_heads, a.head_dim, true, &a.dv, &gv)) != WA_OK) return s;
   if ((s = check_starts(starts, &a)) != WA_OK) return s;
-  if (!lse) return fail(WA_ERR_INVALID_ARG, "lse must be non-null");
-  if (!aligned(lse, 4)) return fail(WA_ERR_ALIGNMENT, "lse must be 4-byte aligned");
+  if (!stats) return fail(WA_ERR_INVALID_ARG, "stats must be non-null");
+  if (!aligned(stats, 4)) return fail(WA_ERR_ALIGNMENT, "stats must be 4-byte aligned");
   const size_t need = seq_backward_bytes(a);
   if ((s = check_ws(workspace, workspace_bytes, need)) != WA_OK) return s;
   s = check_seq_spans({gq, gk, gv, flat("workspace", workspace, need, true), sg, sq, sk, sv, so,
-                       flat("lse", lse, (size_t)a.heads * a.tokens * 4, false), flat("starts", starts, (size_t)(a.batch + 1) * 4, false)});
+                       flat("stats", stats, (size_t)a.heads * a.tokens * seq_lse_step(a) * 4, false), flat("starts", starts, (size_t)(a.batch + 1) * 4, false)});
   if (s != WA_OK) return s;
-  a.lse_in = lse;
-  a.parts = wa_packed_backward_parts(a);
+  a.lse_in = stats;
+  a.lse_step = seq_lse_step(a);
+  a.dq_part = wa_packed_backward_dq_floats(a);
   a.rows = (float*)workspace;
   a.part = (float*)((char*)workspace + seq_rows_bytes(a));
   const hipError_t e = wa_launch_packed_backward(a, (hipStream_t)stream);
@@ -1233,8 +1237,10 @@ wa_status wa_paged_attn(const wa_token_rows* q, const wa_pages* k, const wa_page
                        flat("kv_lens", kv_lens, (size_t)a.batch * 4, false)});
   if (s != WA_OK) return s;
   a.lse = lse;
+  a.lse_step = 1;
   a.status = status;
-  a.cuts = (int2*)workspace;
+  a.any_cut = (int32_t*)workspace;
+  a.cuts = (int2*)((char*)workspace + kAlign);
   a.part = (float*)((char*)workspace + seq_cut_bytes(a));
   const hipError_t e = wa_launch_paged_attn(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "paged attention launch");

@@ -3,14 +3,11 @@
 //
 // Two kernels, each owning what it writes, so nothing is added with atomics and equal calls give equal bits:
 //   packed_dq_kernel: 128 queries of a head, over their keys; also writes what the other kernel's products of a query start from.
-//   packed_dkv_kernel: 128 keys, over the queries of all heads that share them; in a call of few such tiles in parts, which
-//   packed_parts_kernel adds in order.
+//   packed_dkv_kernel: 128 keys, over the queries of all heads that share them.
+// Long tiles are computed in parts, which packed_parts_kernel adds in order.
 // Both recompute the scores and dP. A wavefront holds 32 queries (keys) with their accumulators in registers, and the other side's
 // tiles pass through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are. Two wavefronts share a SIMD.
-//
-// The lengths are known on the device only: workgroups are dealt tiles longest first over all sequences, each finding its own by counting
-// the tiles that are longer (a sequence a lane).
 
 #include "seq_attn.h"
 
@@ -20,7 +17,10 @@ namespace {
 
 using namespace wa;
 
-constexpr int kRows = 128, kWaves = 4, kAhead = 2;
+constexpr int kRows = 128, kWaves = 4, kAhead = 2, kSlots = 512;
+
+// Neighbouring units, which may share keys, on one XCD where eight divides their number.
+__device__ __forceinline__ int spread(int u, int units) { return units % 8 ? u : u % 8 * (units / 8) + u / 8; }
 
 template <int D>
 struct Bwd {
@@ -34,46 +34,108 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// Tile number `rank` of all sequences, by descending level (a tile's number in its sequence, or that counted from the end): the sequence
-// and the level, or false.
-__device__ __forceinline__ bool tile_of(SeqArgs a, int64_t rank, int lane, int* b, int* level) {
-  auto tiles_of = [&](int x) { return x < a->batch ? (int)(((int64_t)seq_of<false>(a, x).n + kRows - 1) / kRows) : 0; };
-  const int mine = tiles_of(lane);
-  // tiles of level t and above
-  auto above = [&](int t) {
-    int64_t sum = max(mine - t, 0);
-    for (int base = 64; base < a->batch; base += 64) sum += max(tiles_of(base + lane) - t, 0);
+// A tile of 128 rows, or the part of one, that a workgroup computes. Its length is the tiles of the other side that it meets.
+struct Job {
+  int b, tile, col;        // sequence, tile of it, head or key head
+  int length, part, parts;
+  int first;               // the first part's number among all jobs; they are `cols` apart
+};
+
+// All tiles of all sequences and `cols` heads, longest first, those longer than `most` in parts of about equal length: `most` is a
+// 512th of all there is, so that a call of few tiles fills the chip's workgroups (two a compute unit) once, and one of many is not cut.
+// Causal tiles have the lengths 1 to T of a sequence of T tiles, others T. Each workgroup finds its job itself: the lengths are on the
+// device. The first 64 sequences are held, one a lane.
+struct Jobs {
+  SeqArgs a;
+  int lane, cols, batch, mine, most;
+  bool causal;
+
+  __device__ __forceinline__ Jobs(int lane_, int cols_) : a(seq_args()), lane(lane_), cols(cols_), batch(a->batch), causal(a->causal) {
+    mine = tiles_of(lane);
+    int64_t sum = 0;
+    for (int base = 0; base < batch; base += 64) {
+      const int64_t t = tiles_at(base);
+      sum += causal ? t * (t + 1) / 2 : t * t;
+    }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-    return sum;
-  };
-  int most = mine;
-  for (int base = 64; base < a->batch; base += 64) most = max(most, tiles_of(base + lane));
-#pragma unroll
-  for (int x = 32; x > 0; x >>= 1) most = max(most, __shfl_xor(most, x));
-  if (rank >= above(0)) return false;
-  int lo = 0, hi = most;  // above(lo) > rank >= above(hi)
-  while (hi - lo > 1) {
-    const int mid = lo + ((hi - lo) >> 1);
-    if (above(mid) > rank) lo = mid; else hi = mid;
+    sum = Walk<false>::uniform64(sum) * cols;
+    most = (int)((sum + kSlots - 1) / kSlots);
   }
-  int64_t k = rank - above(lo + 1);
-  for (int base = 0; base < a->batch; base += 64) {
-    uint64_t there = __ballot((base ? tiles_of(base + lane) : mine) > lo);
-    const int n = __popcll(there);
-    if (k < n) {
-      for (; k > 0; --k) there &= there - 1;
-      *b = base + __builtin_ctzll(there);
-      *level = lo;
-      return true;
+  __device__ __forceinline__ int tiles_of(int b) const {
+    return b < batch ? (int)(((int64_t)seq_of<false>(again(a), b).n + kRows - 1) / kRows) : 0;
+  }
+  __device__ __forceinline__ int tiles_at(int base) const { return base == 0 ? mine : tiles_of(base + lane); }
+  __device__ __forceinline__ int parts_of(int length) const { return (length + most - 1) / most; }
+  // jobs (or, not counting parts, tiles) of the first x lengths of a sequence
+  __device__ __forceinline__ int upto(int x, bool in_parts) const {
+    if (!in_parts) return x;
+    const int q = x / most, r = x - q * most;
+    return q * (q + 1) / 2 * most + r * (q + 1);
+  }
+  // those of tiles longer than `length`, of one column
+  __device__ __forceinline__ int above(int length, bool in_parts) const {
+    int sum = 0;
+    for (int base = 0; base < batch; base += 64) {
+      const int t = tiles_at(base);
+      const int n = t <= length ? 0 : causal ? upto(t, in_parts) - upto(length, in_parts) : t * (in_parts ? parts_of(t) : 1);
+      sum += lane_sum(n);
     }
-    k -= n;
+    return sum;
   }
-  return false;
-}
-
-// Neighbouring units, which may share keys, on one XCD where eight divides their number.
-__device__ __forceinline__ int spread(int u, int units) { return units % 8 ? u : u % 8 * (units / 8) + u / 8; }
+  // job (or tile) number `rank`; false if there is none
+  __device__ __forceinline__ bool find(int64_t rank, bool in_parts, Job* job) const {
+    int lo = 0, hi = 0, passed = 0;  // above(lo) > row of jobs >= above(hi) = passed
+    for (int base = 0; base < batch; base += 64) hi = max(hi, tiles_at(base));
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) hi = max(hi, __shfl_xor(hi, x));
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    const int row = (int)(rank / cols);
+    if (row >= above(0, in_parts)) return false;
+    while (hi - lo > 1) {
+      const int mid = lo + ((hi - lo) >> 1), n = above(mid, in_parts);
+      if (n > row) {
+        lo = mid;
+      } else {
+        hi = mid;
+        passed = n;
+      }
+    }
+    job->length = hi;
+    job->parts = parts_of(hi);
+    const int per = in_parts ? job->parts : 1;
+    int k = (row - passed) / per;
+    job->part = row - passed - k * per;
+    job->col = spread((int)(rank - (int64_t)row * cols), cols);
+    job->first = 0;
+    // the k-th tile of this length
+    int who = 0, tile = 0, t = 0;
+    for (int base = 0; base < batch; base += 64) {
+      t = tiles_at(base);
+      const int n = causal ? t >= hi : t == hi ? t : 0, sum = lane_prefix_sum(n);
+      const uint64_t past = __ballot(sum > k);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        who = base + l;
+        tile = k - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(n, l));
+        t = __builtin_amdgcn_readlane(t, l);
+        break;
+      }
+      k -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    job->b = __builtin_amdgcn_readfirstlane(who);
+    job->tile = __builtin_amdgcn_readfirstlane(tile);  // causal: 0
+    t = __builtin_amdgcn_readfirstlane(t);
+    if (causal) job->tile = t - hi;  // counted from the sequence's longest
+    return true;
+  }
+  // number of the first part of tile number `rank` among all jobs
+  __device__ __forceinline__ int64_t first_part(int64_t rank, const Job& job) const {
+    const int row = (int)(rank / cols);
+    const int same = row - above(job.length, false);  // tiles of this length before it
+    return ((int64_t)above(job.length, true) + (int64_t)same * job.parts) * cols + (rank - (int64_t)row * cols);
+  }
+};
 
 // Rows [row, row + ROWS) of g (`token` bytes apart) into a tile; rows past `last` are that row again.
 template <int RB, int ROWS>
@@ -89,9 +151,13 @@ __device__ __forceinline__ void copy_rows(const unsigned char* tile, const unsig
   }
 }
 
-__device__ __forceinline__ float dot8(bf16x8 a, bf16x8 b, float sum) {
+// dO . O of 8 columns, O with what its rounding left (dO . O of the rounded O alone gave dQ and dK an error of 0.0026 of their size where
+// this gives 0.0023 and rounding them alone 0.0017)
+__device__ __forceinline__ float dot8(bf16x8 a, bf16x8 o, uint32_t rest0, uint32_t rest1, float sum) {
+  typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+  const u16x8 bits = __builtin_bit_cast(u16x8, o);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)a[i], (float)b[i], sum);
+  for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)a[i], with_rest(bits[i], i < 4 ? rest0 : rest1, i & 3), sum);
   return sum;
 }
 
@@ -103,17 +169,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int b = 0, tile = 0;
-  if (!__builtin_amdgcn_readfirstlane(tile_of(seq_args(), blockIdx.x / a.heads, lane, &b, &tile))) return;
-  b = __builtin_amdgcn_readfirstlane(b);
-  tile = __builtin_amdgcn_readfirstlane(tile);
-  const int h = spread(blockIdx.x % a.heads, a.heads), hk = h / (a.heads / a.kv_heads);
+  Job job;
+  if (!Jobs(lane, a.heads).find(blockIdx.x, true, &job)) return;
+  // causal: a tile's length is its number and one, and the longest is the last
+  const int b = job.b, tile = a.causal ? job.length - 1 : job.tile, h = job.col, hk = h / (a.heads / a.kv_heads);
   const Seq s = Walk<false>::uniform(seq_of<false>(seq_args(), b));
   const int i0 = tile * kRows + w * 32, i = i0 + l32, i_last = s.n - 1;
   const bool valid = i <= i_last;
   const int limit = !valid ? 0 : a.causal ? i + 1 : s.n;
   const int some = i0 > i_last ? 0 : a.causal ? min(i0 + 32, s.n) : s.n, all = a.causal ? min(i0 + 1, s.n) : s.n;
-  const int most = a.causal ? min((tile + 1) * kRows, s.n) : s.n;
+  // this part's keys
+  const int lo = job.length * job.part / job.parts * kRows, most = min(job.length * (job.part + 1) / job.parts * kRows, s.n);
   const unsigned char* kg = (const unsigned char*)a.k.at + (s.first * a.k.token + hk * a.k.head) * 2;
   const unsigned char* vg = (const unsigned char*)a.v.at + (s.first * a.v.token + hk * a.v.head) * 2;
   auto copy = [&](int key, int buf) {
@@ -123,7 +189,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
     copy_rows<C::RB, KB>(t, kg, (uint32_t)(a.k.token * 2), key, i_last, w, lane_o);
     copy_rows<C::RB, KB>(t + BYTES, vg, (uint32_t)(a.v.token * 2), key, i_last, w, lane_o);
   };
-  copy(0, 0);
+  copy(lo, 0);
 
   // the wavefront's queries, their dO, and D
   bf16x8 qf[C::KS], dof[C::KS];
@@ -131,19 +197,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
   const uint16_t* qg = (const uint16_t*)a.q.at + tok * a.q.token + h * a.q.head;
   const uint16_t* dog = (const uint16_t*)a.dout.at + tok * a.dout.token + h * a.dout.head;
   const uint16_t* og = (const uint16_t*)a.o.at + tok * a.o.token + h * a.o.head;
+  const float* stat = a.lse_in + ((int64_t)h * a.tokens + tok) * a.lse_step;
   float d = 0.f;
 #pragma unroll
   for (int x = 0; x < C::KS; ++x) {
     qf[x] = load8(qg + 16 * x + 8 * hf, valid);
     dof[x] = load8(dog + 16 * x + 8 * hf, valid);
-    d = dot8(dof[x], load8(og + 16 * x + 8 * hf, valid), d);
+    uint32_t rest[2] = {0, 0};
+    if (valid) {
+      rest[0] = *(const uint32_t*)(stat + 1 + 4 * x + 2 * hf);
+      rest[1] = *(const uint32_t*)(stat + 2 + 4 * x + 2 * hf);
+    }
+    d = dot8(dof[x], load8(og + 16 * x + 8 * hf, valid), rest[0], rest[1], d);
   }
   d = add_halves(d);
   const float c2 = a.scale * kLog2e;
   float ref = 0.f;  // log-sum-exp in log2 units
-  if (valid) ref = a.lse_in[(int64_t)h * a.tokens + tok] * kLog2e;
+  if (valid) ref = *stat * kLog2e;
   // For the side of the keys: what its products start from, scores from the log-sum-exp, so that P = exp2(c2 s), and dP from -D.
-  if (valid && hf == 0) {
+  if (valid && hf == 0 && job.part == 0) {
     float* to = a.rows + (int64_t)h * a.tokens + tok;
     to[0] = -ref / c2;
     to[(int64_t)a.heads * a.tokens] = -d;
@@ -204,7 +276,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
     }
   };
   int buf = 0;
-  for (int key = 0; key < most; key += KB) {
+  for (int key = lo; key < most; key += KB) {
     WA_WAIT_VM(0);
     WA_BARRIER();
     if (key + KB < most) copy(key + KB, buf ^ 1);
@@ -217,7 +289,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
     }
     buf ^= 1;
   }
-  if (valid) store_row((uint16_t*)a.dq.at + tok * a.dq.token + h * a.dq.head, dq, a.scale, hf);
+  if (job.parts > 1) {
+    store_part(a.part + ((int64_t)blockIdx.x * kRows + w * 32 + l32) * D, dq, a.scale, hf);
+  } else if (valid) {
+    store_row((uint16_t*)a.dq.at + tok * a.dq.token + h * a.dq.head, dq, a.scale, hf);
+  }
 }
 
 template <int D>
@@ -229,25 +305,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int part = blockIdx.x % a.parts, unit = blockIdx.x / a.parts;
-  int b = 0, level = 0;
-  if (!__builtin_amdgcn_readfirstlane(tile_of(seq_args(), unit / a.kv_heads, lane, &b, &level))) return;
-  b = __builtin_amdgcn_readfirstlane(b);
-  level = __builtin_amdgcn_readfirstlane(level);
-  const int hk = spread(unit % a.kv_heads, a.kv_heads), group = a.heads / a.kv_heads;
+  Job job;
+  if (!Jobs(lane, a.kv_heads).find(blockIdx.x, true, &job)) return;
+  // causal: the first tile of a sequence meets the queries of all of them
+  const int b = job.b, tile = job.tile, hk = job.col, group = a.heads / a.kv_heads;
   const Seq s = Walk<false>::uniform(seq_of<false>(seq_args(), b));
-  // causal: the first tiles are seen by the most queries
-  const int tile = a.causal ? (s.n + kRows - 1) / kRows - 1 - level : level;
   const int k0 = tile * kRows + w * 32, kj = k0 + l32;
   const bool valid = kj < s.n;
   const int from = !valid ? s.n : a.causal ? kj : 0;                      // first query that sees this lane's key,
   const int some = k0 >= s.n ? s.n : a.causal ? k0 : 0;                   // the wavefront's first
   const int all = a.causal ? min(k0 + 31, s.n - 1) : 0;                   // and its last
   const bool whole = k0 + 31 < s.n;
-  // this part's tiles of queries, counted through the heads one after another
-  const int first = (a.causal ? tile * kRows : 0) / QB * QB, q_tiles = (s.n - first + QB - 1) / QB;
-  const int64_t all_tiles = (int64_t)group * q_tiles;
-  const int64_t u0 = all_tiles * part / a.parts, u1 = all_tiles * (part + 1) / a.parts;
+  // this part's queries, in tiles of QB, through the heads one after another
+  const int lead = a.causal ? tile : 0, first = (lead + job.length * job.part / job.parts) * kRows;
+  const int past = min((lead + job.length * (job.part + 1) / job.parts) * kRows, s.n);
 
   const int64_t tok = s.first + kj;
   const uint16_t* kg = (const uint16_t*)a.k.at + tok * a.k.token + hk * a.k.head;
@@ -354,19 +425,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
       if (x + kAhead < 4 * C::DT) cring[x % kAhead] = col(x + kAhead);
     }
   };
-  int g = (int)(u0 / q_tiles), i = first + (int)(u0 - (int64_t)g * q_tiles) * QB, buf = 0;
-  int64_t u = u0;
-  if (u < u1) copy(g, i, 0);
-  for (; u < u1; ++u) {
+  int g = 0, i = first, buf = 0;
+  copy(0, first, 0);
+  while (g < group) {
     const int i0 = i;
     i += QB;
-    if (i >= s.n) {
+    if (i >= past) {
       i = first;
       ++g;
     }
     WA_WAIT_VM(0);
     WA_BARRIER();
-    if (u + 1 < u1) copy(g, i, buf ^ 1);
+    if (g < group) copy(g, i, buf ^ 1);
     int end = QB;
     asm volatile("" : "+s"(end));
 #pragma unroll 1
@@ -377,50 +447,66 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
     }
     buf ^= 1;
   }
-  if (!valid) return;
-  if (a.parts > 1) {
-    float* to = a.part + (((int64_t)part * a.tokens + tok) * a.kv_heads + hk) * 2 * D;
+  if (job.parts > 1) {
+    float* to = a.part + a.dq_part + ((int64_t)blockIdx.x * kRows + w * 32 + l32) * 2 * D;
     store_part(to, dk, a.scale, hf);
     store_part(to + D, dv, 1.f, hf);
-  } else {
+  } else if (valid) {
     store_row((uint16_t*)a.dk.at + tok * a.dk.token + hk * a.dk.head, dk, a.scale, hf);
     store_row((uint16_t*)a.dv.at + tok * a.dv.token + hk * a.dv.head, dv, 1.f, hf);
   }
 }
 
-// Adds the parts' results in order and rounds: a thread four columns of a row (D of dK, then D of dV).
+// Adds the parts of cut tiles in order and rounds: four workgroups a tile, those of dQ first, then those of dK and dV.
 template <int D>
-__global__ __launch_bounds__(256) void packed_parts_kernel(const WaSeqLaunch a) {
-  constexpr int QUADS = 2 * D / 4;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / QUADS, tok = row / a.kv_heads;
-  const int hk = (int)(row - tok * a.kv_heads), c = (int)(id % QUADS) * 4;
-  if (tok < min(max(a.starts[0], 0), a.tokens) || tok >= min(max(a.starts[a.batch], 0), a.tokens)) return;
-  const int64_t step = (int64_t)a.tokens * a.kv_heads * 2 * D;
-  const float* at = a.part + row * 2 * D + c;
-  float4 sum = *(const float4*)at;
+__global__ __launch_bounds__(256) void packed_parts_kernel(const WaSeqLaunch a, int dq_tiles) {
+  const int64_t rank = blockIdx.x / 4;
+  const bool keys = rank >= dq_tiles;
+  const int cols = keys ? a.kv_heads : a.heads;
+  const Jobs jobs(threadIdx.x & 63, cols);
+  Job job;
+  const int64_t mine = keys ? rank - dq_tiles : rank;
+  if (!jobs.find(mine, false, &job) || job.parts == 1) return;
+  const Seq s = Walk<false>::uniform(seq_of<false>(seq_args(), job.b));
+  const int tile = !a.causal || keys ? job.tile : job.length - 1, width = keys ? 2 * D : D;
+  const int64_t first = jobs.first_part(mine, job), step = (int64_t)cols * kRows * width;
+  const float* from = a.part + (keys ? a.dq_part : 0) + first * kRows * width;
+  for (int x = threadIdx.x; x < kRows / 4 * width / 4; x += 256) {
+    const int r = x / (width / 4) + blockIdx.x % 4 * (kRows / 4), c = x % (width / 4) * 4;
+    if (tile * kRows + r >= s.n) break;
+    const float* at = from + (int64_t)r * width + c;
+    float4 sum = *(const float4*)at;
 #pragma unroll 4
-  for (int x = 1; x < a.parts; ++x) {
-    const float4 y = *(const float4*)(at + x * step);
-    sum.x += y.x;
-    sum.y += y.y;
-    sum.z += y.z;
-    sum.w += y.w;
+    for (int y = 1; y < job.parts; ++y) {
+      const float4 z = *(const float4*)(at + y * step);
+      sum.x += z.x;
+      sum.y += z.y;
+      sum.z += z.z;
+      sum.w += z.w;
+    }
+    const int64_t tok = s.first + tile * kRows + r;
+    const WaSeqRows& to = !keys ? a.dq : c < D ? a.dk : a.dv;
+    *(uint2*)((uint16_t*)to.at + tok * to.token + job.col * to.head + c % D) = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
   }
-  uint16_t* out = c < D ? (uint16_t*)a.dk.at + tok * a.dk.token + hk * a.dk.head + c
-                        : (uint16_t*)a.dv.at + tok * a.dv.token + hk * a.dv.head + c - D;
-  *(uint2*)out = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
+}
+
+// Tiles in parts are longer than a 512th of all, so that there are fewer than 1,024 parts (each of more than a half of that), of fewer
+// than 512 tiles; and no more than the sequences' tiles have.
+int64_t most_parts(const WaSeqLaunch& a, int cols) {
+  return std::min<int64_t>(2 * kSlots, wa_packed_backward_tiles(a) * cols * (((int64_t)a.tokens + kRows - 1) / kRows));
 }
 
 template <int D>
 hipError_t launch(const WaSeqLaunch& a, hipStream_t stream) {
   const int64_t tiles = wa_packed_backward_tiles(a);
-  hipLaunchKernelGGL(packed_dq_kernel<D>, dim3((unsigned)(tiles * a.heads)), dim3(64 * kWaves), 0, stream, a);
+  // a job a tile, and for each part of a 512th of all one more at most
+  hipLaunchKernelGGL(packed_dq_kernel<D>, dim3((unsigned)(tiles * a.heads + kSlots)), dim3(64 * kWaves), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(packed_dkv_kernel<D>, dim3((unsigned)(tiles * a.kv_heads * a.parts)), dim3(64 * kWaves), 0, stream, a);
-  if ((e = hipGetLastError()) != hipSuccess || a.parts == 1) return e;
-  const int64_t threads = (int64_t)a.tokens * a.kv_heads * (2 * D / 4);
-  hipLaunchKernelGGL(packed_parts_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(packed_dkv_kernel<D>, dim3((unsigned)(tiles * a.kv_heads + kSlots)), dim3(64 * kWaves), 0, stream, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int dq_tiles = (int)std::min<int64_t>(kSlots, tiles * a.heads), kv_tiles = (int)std::min<int64_t>(kSlots, tiles * a.kv_heads);
+  hipLaunchKernelGGL(packed_parts_kernel<D>, dim3(4 * (dq_tiles + kv_tiles)), dim3(256), 0, stream, a, dq_tiles);
   return hipGetLastError();
 }
 
@@ -431,12 +517,9 @@ int64_t wa_packed_backward_tiles(const WaSeqLaunch& a) {
   return std::min<int64_t>(a.tokens, ((int64_t)a.tokens + (int64_t)(kRows - 1) * a.batch) / kRows);
 }
 
-// Parts of a tile of keys: as many as fill the 512 workgroups that the chip holds about once, twice where tiles are of
-// different lengths, each of at least 256 queries of the longest that a sequence can be.
-int32_t wa_packed_backward_parts(const WaSeqLaunch& a) {
-  const int64_t items = std::max<int64_t>(1, ((int64_t)a.tokens + kRows - 1) / kRows * a.kv_heads);
-  const int64_t queries = (int64_t)(a.heads / a.kv_heads) * a.tokens;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(1024 / items, std::min<int64_t>(queries / 256, 16)));
+int64_t wa_packed_backward_dq_floats(const WaSeqLaunch& a) { return most_parts(a, a.heads) * kRows * a.head_dim; }
+int64_t wa_packed_backward_part_floats(const WaSeqLaunch& a) {
+  return wa_packed_backward_dq_floats(a) + most_parts(a, a.kv_heads) * kRows * 2 * a.head_dim;
 }
 
 hipError_t wa_launch_packed_backward(const WaSeqLaunch& a, hipStream_t stream) {

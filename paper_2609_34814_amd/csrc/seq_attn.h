@@ -25,10 +25,16 @@
 #include "seq_launch.h"
 #include "wavealign.h"
 
+#include <algorithm>
+
 namespace wa {
 
 constexpr float kSeqGrow = 8.f;  // log2 units
 constexpr int kSeqAhead = 4;     // operands read ahead
+// From so many tiles a worker on, tiles are dealt out whole.
+constexpr int kSeqRounds = 2;
+// What a tile costs beside its keys, in tiles of keys.
+constexpr int kSeqFixed = 2;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -88,16 +94,19 @@ __device__ __forceinline__ Seq seq_of(SeqArgs a, int b) {
   return s;
 }
 
-// Units of the first t tiles of a sequence and head: tile t has ceil((before + (t + 1) p) / KB) of them, at least as many as tiles
-// of keys that its queries see and at least one; without `causal` all have ceil(keys / KB).
+// Units of the first t tiles of a sequence and head: tile t has kSeqFixed for its queries and its end, and ceil((before + (t + 1) p) / KB)
+// for its keys, at least as many as tiles of keys that its queries see; without `causal` all have ceil(keys / KB) + 1.
 struct Line {
   int log_p, log_kb, before;
   int whole;  // units of every tile, 0: causal
   __device__ __forceinline__ Line(int log_p_, int log_kb_, const Seq& s, bool causal) : log_p(log_p_), log_kb(log_kb_) {
     before = max(s.keys - s.n, 0);
-    whole = causal ? 0 : max((int)(((int64_t)s.keys + (1 << log_kb) - 1) >> log_kb), 1);
+    whole = causal ? 0 : (int)(((int64_t)s.keys + (1 << log_kb) - 1) >> log_kb) + 1;
   }
   __device__ __forceinline__ int64_t upto(int64_t t) const {
+    return t * kSeqFixed + keys_upto(t);
+  }
+  __device__ __forceinline__ int64_t keys_upto(int64_t t) const {
     if (whole) return t * whole;
     if (log_p >= log_kb) {
       const int64_t start = ((int64_t)before + (1 << log_kb) - 1) >> log_kb;
@@ -222,13 +231,98 @@ struct Walk {
   }
 };
 
+// Sum and maximum over the lanes, the same in all of them.
+__device__ __forceinline__ int lane_sum(int x) { return __builtin_amdgcn_readlane(lane_prefix_sum(x), 63); }
+
+// All tiles of packed sequences by falling number of the tile in its sequence: those that see the most keys first. The first 64 sequences
+// are held, one a lane.
+struct Levels {
+  int lane, log_tokens, batch, first, n, mine;
+
+  __device__ __forceinline__ Levels(SeqArgs a, int lane_) : lane(lane_), log_tokens(a->plan.log_tokens), batch(a->batch) {
+    const Seq s = seq_of<false>(a, min(lane, batch - 1));
+    first = s.first;
+    n = lane < batch ? s.n : 0;
+    mine = tiles(n);
+  }
+  __device__ __forceinline__ int tiles(int n) const { return (int)(((int64_t)n + (1 << log_tokens) - 1) >> log_tokens); }
+  // tiles of the sequence `base` + lane
+  __device__ __forceinline__ int tiles_at(int base) const {
+    return base == 0 ? mine : base + lane < batch ? tiles(seq_of<false>(again(seq_args()), base + lane).n) : 0;
+  }
+  // tiles number t and above of their sequences
+  __device__ __forceinline__ int above(int t) const {
+    int sum = 0;
+    for (int base = 0; base < batch; base += 64) sum += lane_sum(max(tiles_at(base) - t, 0));
+    return sum;
+  }
+  // Tile `rank` (below above(0)) of one column: its sequence, and its number there.
+  __device__ __forceinline__ void find(int rank, int* b, int* tile) const {
+    int most = 0;
+    for (int base = 0; base < batch; base += 64) most = max(most, tiles_at(base));
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) most = max(most, __shfl_xor(most, x));
+    int lo = 0, hi = __builtin_amdgcn_readfirstlane(most), passed = 0;  // above(lo) > rank >= above(hi) = passed
+    while (hi - lo > 1) {
+      const int mid = lo + ((hi - lo) >> 1), m = above(mid);
+      if (m > rank) {
+        lo = mid;
+      } else {
+        hi = mid;
+        passed = m;
+      }
+    }
+    int k = rank - passed, who = 0;
+    for (int base = 0; base < batch; base += 64) {
+      uint64_t there = __ballot(tiles_at(base) > lo);
+      const int m = __popcll(there);
+      if (k < m) {
+        for (; k > 0; --k) there &= there - 1;
+        who = base + __builtin_ctzll(there);
+        break;
+      }
+      k -= m;
+    }
+    *b = __builtin_amdgcn_readfirstlane(who);
+    *tile = lo;
+  }
+  __device__ __forceinline__ Seq seq(int b) const {
+    Seq s;
+    if (b < 64) {
+      s.first = __builtin_amdgcn_readlane(first, b);
+      s.n = s.keys = __builtin_amdgcn_readlane(n, b);
+    } else {
+      s = Walk<false>::uniform(seq_of<false>(again(seq_args()), b));
+    }
+    return s;
+  }
+};
+
+// What bfloat16 lost of four values, as the next eight bits of each: differences of the bit patterns in steps of 2^8, so that a value and its
+// rest are within 2^-17 of the float32 one.
+__device__ __forceinline__ uint32_t rest4(float a, float b, float c, float d, uint2 o) {
+  const float x[4] = {a, b, c, d};
+  const uint32_t h[4] = {o.x << 16, o.x & 0xffff0000u, o.y << 16, o.y & 0xffff0000u};
+  uint32_t out = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int lost = (int)(__builtin_bit_cast(uint32_t, x[i]) - h[i]);
+    out |= (uint32_t)(min((lost + 128) >> 8, 127) & 255) << 8 * i;
+  }
+  return out;
+}
+// the i-th of four values from its bfloat16 and its rest
+__device__ __forceinline__ float with_rest(uint32_t bf16_bits, uint32_t rest, int i) {
+  return __builtin_bit_cast(float, (bf16_bits << 16) + ((uint32_t)(int)(int8_t)(rest >> 8 * i) << 8));
+}
+
 // The shares of the line: of `total` units for `workers` workers.
 struct Shares {
-  int64_t total, near;  // near: how far a border moves to a tile's end
+  int64_t total, near;  // near: how far a border moves to a tile's end; it never stays before a tile's first keys
   int workers;
   __device__ __forceinline__ Shares(int64_t total_, SeqArgs a) : total(total_) {
     workers = (int)max((int64_t)1, min((int64_t)a->plan.workers, total / a->plan.min_units));
-    near = total / workers >> 4;
+    near = max(total / workers >> 4, (int64_t)kSeqFixed);
   }
   __device__ __forceinline__ int64_t border(int w) const { return total * w / workers; }
   // where the border at unit x, inside `it`, is moved to
@@ -247,32 +341,69 @@ struct Shares {
 // Zero rows, in the place of keys behind the last and of pages that the pool does not have.
 static __device__ const uint4 kZeroRow[16] = {};
 
-// The rows of one item's keys (or values) as tiles in LDS.
-template <int D, int W, bool PAGED>
-struct KeyRows {
-  using C = SeqTile<D, W>;
-  static constexpr int RPI = 1024 / C::RB, LPR = C::RB / 16, N = C::BYTES / 1024 / W;
-  const unsigned char* base;  // packed: the sequence's first row; paged: the head of page 0
-  uint32_t token;             // bytes
-  int64_t page;
+// One 16-byte-a-lane copy as dma16, for kernels in which nothing else uses M0 (the compiler writes it just before a use).
+__device__ __forceinline__ void dma16_at(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(lds), "v"(voff), "s"(base)
+      : "memory");
+}
 
-  // Rows [key, key + KB) into `tile`; last: the last key. Rows past it are that row again, or (whole copies of paged ones) zeros: what
-  // they add is masked, and they hold no memory that the caller did not write. ids: the page of each 16 keys' (below 0: none), uniform.
-  __device__ __forceinline__ void copy(const unsigned char* tile, int key, int last, int w, int lane, const int* ids, int page_mask) const {
-    const int r0 = lane / LPR;
+// Rows of keys or of values on their way to a tile in LDS: KB rows of RB bytes, `token` bytes apart in memory. A copy of a wavefront is
+// RPI rows; the swizzle of a row's 16-byte chunks repeats after PERIOD copies, and so do the lanes' offsets from a copy's first row.
+template <int D, int W>
+struct Rows {
+  using C = SeqTile<D, W>;
+  static constexpr int RPI = 1024 / C::RB, LPR = C::RB / 16, N = C::BYTES / 1024 / W, STEP = W * RPI;
+  static constexpr int PERIOD = STEP >= 16 ? 1 : 16 / STEP;
+  uint32_t token;         // bytes
+  uint32_t off[PERIOD];   // of this lane in copies 0 .. PERIOD - 1, from the tile's row 0 (copy i: of row i STEP)
+
+  __device__ __forceinline__ void init(int64_t stride, int w, int lane) {
+    token = (uint32_t)(stride * 2);
+#pragma unroll
+    for (int i = 0; i < PERIOD; ++i) {
+      const int r = (i * W + w) * RPI + lane / LPR;
+      off[i] = (w * RPI + lane / LPR) * token + tile_chunk<C::RB>(r, lane % LPR) * 16;
+    }
+  }
+  // packed rows from `from` on, `left` of them: those past the last are the last again (what they add is masked, and they hold no memory
+  // that the caller did not write)
+  __device__ __forceinline__ void copy(const unsigned char* from, int left, uint32_t lds, int w, int lane) const {
+    from = uniform_ptr(from);
+    if (left >= C::KB) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) dma16_at(from + (uint64_t)(i * STEP) * token, off[i % PERIOD], lds + i * W * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = (i * W + w) * RPI + lane / LPR;
+        dma16_at(from, min(r, left - 1) * token + tile_chunk<C::RB>(r, lane % LPR) * 16, lds + i * W * 1024);
+      }
+    }
+  }
+  // Rows of pages. head: of page 0; ids: the page of each 16 rows (below 0: none), uniform; at: the first row's place in its page. A page
+  // that there is not, and copies past the last row, give zeros.
+  __device__ __forceinline__ void copy_pages(const unsigned char* head, int64_t page, const int* ids, int at, int shift, int left,
+                                             uint32_t lds, int w, int lane) const {
+    const int mask = (1 << shift) - 1;
+    if (left >= C::KB && shift >= C::LOG_KB && ids[0] >= 0) {
+      const unsigned char* from = uniform_ptr(head + ids[0] * page + (uint64_t)at * token);
+#pragma unroll
+      for (int i = 0; i < N; ++i) dma16_at(from + (uint64_t)(i * STEP) * token, off[i % PERIOD], lds + i * W * 1024);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int row = (i * W + w) * RPI, r = row + r0;
-      const uint32_t chunk = tile_chunk<C::RB>(r, lane % LPR) * 16;
-      const unsigned char* to = tile + (i * W + w) * 1024;
-      if constexpr (!PAGED) {
-        dma16(uniform_ptr(base + (int64_t)key * token), min(r, last - key) * token + chunk, to);
-      } else {
-        const int id = ids[row / 16];
-        const unsigned char* from = base + id * page + (int64_t)((key + row) & page_mask) * token;
-        const bool none = id < 0 || key + row > last;
-        dma16(uniform_ptr(none ? (const unsigned char*)kZeroRow : from), (none ? 0 : min(r0, last - key - row) * token) + chunk, to);
-      }
+      const int row = (i * W + w) * RPI, r0 = lane / LPR;
+      const int id = ids[row / 16];
+      const uint32_t chunk = tile_chunk<C::RB>(row + r0, lane % LPR) * 16;
+      const bool none = id < 0 || row >= left;
+      const unsigned char* from = none ? (const unsigned char*)kZeroRow : head + id * page + (uint64_t)((at + row) & mask) * token;
+      dma16_at(uniform_ptr(from), (none ? 0 : min(r0, left - 1 - row) * token) + chunk, lds + i * W * 1024);
     }
   }
 };
@@ -286,91 +417,170 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const SeqArgs a = seq_args();
-  const Walk<PAGED> walk(a, C::LOG_KB, lane);
-  const Shares shares(walk.uniform64(walk.total()), a);
-  if (shares.total == 0) return;
-  // workgroups go round the eight XCDs: each XCD takes neighbouring shares where there are shares for all
-  const int me = shares.workers == a->plan.workers ? (blockIdx.x & 7) * (a->plan.workers >> 3) + (blockIdx.x >> 3) : blockIdx.x;
-  if (me >= shares.workers) return;
-  int64_t begin = shares.border(me), end = shares.border(me + 1);
-  if (end < shares.total) end = shares.moved(end, walk.find(end));
-  Item it = walk.find(begin);
-  begin = shares.moved(begin, it);
-  if (begin == it.at + it.units && begin < shares.total) it = walk.next(it);
-  if (begin >= end) return;
+  constexpr bool kWhole = !PAGED && W == 4;
+  const Levels levels(seq_args(), kWhole ? lane : 0);
+  // a tile of all, whole
+  auto ranked = [&](int64_t rank) {
+    const SeqArgs a = again(seq_args());
+    const Walk<PAGED> walk(a, C::LOG_KB, lane);
+    const int k = (int)(rank / walk.cols);
+    Item x;
+    x.col = (int)(rank - (int64_t)k * walk.cols);
+    levels.find(k, &x.b, &x.tile);
+    x.s = levels.seq(x.b);
+    x.tiles = walk.tiles(x.s);
+    const Line l = walk.line(x.s);
+    x.at = 0;
+    x.units = (int)(l.upto(x.tile + 1) - l.upto(x.tile));
+    walk.scalar(x);
+    return x;
+  };
+  int64_t total, begin, end;
+  Item it;
+  int me, round = -1;  // round: of tiles that are dealt out whole
+  {
+    const SeqArgs a = seq_args();
+    const Walk<PAGED> walk(a, C::LOG_KB, lane);
+    if (kWhole) {
+      total = (int64_t)levels.above(0) * walk.cols;
+      if (total >= (int64_t)kSeqRounds * a->plan.workers) round = 0;
+    }
+    if (blockIdx.x == 0 && tid == 0) *a->any_cut = round < 0;
+    if (round == 0) {
+      it = ranked(blockIdx.x);
+      begin = -(int64_t(1) << 60);
+      end = int64_t(1) << 60;
+      me = blockIdx.x;
+    } else {
+    total = walk.uniform64(walk.total());
+    if (total == 0) return;
+    const Shares shares(total, a);
+    // workgroups go round the eight XCDs: each XCD takes neighbouring shares where there are shares for all
+    me = shares.workers == a->plan.workers ? (blockIdx.x & 7) * (a->plan.workers >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+    if (me >= shares.workers) return;
+    begin = shares.border(me), end = shares.border(me + 1);
+    if (end < total) end = shares.moved(end, walk.find(end));
+    it = walk.find(begin);
+    begin = shares.moved(begin, it);
+    if (begin == it.at + it.units && begin < total) it = walk.next(it);
+    if (begin >= end) return;
+    begin = walk.uniform64(begin);
+    end = walk.uniform64(end);
+    }
+  }
+  // of tiles dealt out whole: the next one's rank, where a worker's place in a round turns round from one to the next
+  auto next_rank = [&] {
+    const int workers = again(seq_args())->plan.workers, r = round + 1;
+    const int place = blockIdx.x >> 3, p = r & 1 ? (workers >> 3) - 1 - place : place;
+    return (int64_t)r * workers + p * 8 + (blockIdx.x & 7);
+  };
 
-  const int per_tile = a->plan.per_tile, log_p = a->plan.log_tokens, group = a->heads / a->kv_heads;
-  const bool causal = a->causal;
-  const float c2 = a->scale * kLog2e;
   const uint32_t kbase = row_operand<C::RB>(lane, 0);
   const uint32_t vbase0 = C::BYTES + col_operand<C::RB>(lane, 0, 0), vbase1 = C::BYTES + col_operand<C::RB>(lane, 0, 1);
-  // this lane's row of a tile: token i of head `sub`
-  const int row = w * 32 + l32, sub = row >> log_p, i_row = row & ((1 << log_p) - 1);
-  const int i_first = log_p >= 5 ? (w * 32) & ((1 << log_p) - 1) : 0;  // the wavefront's tokens
-  const int i_last = i_first + (log_p >= 5 ? 31 : (1 << log_p) - 1);
-  const bool wave_used = (w * 32 >> log_p) < per_tile;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds) + w * 1024;
+  Rows<D, W> krows, vrows;
+  krows.init(PAGED ? seq_args()->kp.token : seq_args()->k.token, w, lane);
+  vrows.init(PAGED ? seq_args()->vp.token : seq_args()->v.token, w, lane);
 
-  // the keys of a worker's part of a tile
+  // the keys of this worker's part of a tile
   struct Range {
-    int lo, hi, most;
+    int lo, hi;
   };
   auto range = [&](const Item& x) {
+    const SeqArgs a = again(seq_args());
     Range r;
-    const int last = min(((x.tile + 1) << log_p), x.s.n) - 1;
-    r.most = causal ? min(max(x.s.keys - x.s.n + last + 1, 0), x.s.keys) : x.s.keys;
-    const int64_t u0 = max(begin - x.at, (int64_t)0), u1 = min(end - x.at, (int64_t)x.units);
-    r.lo = (int)min(u0 * KB, (int64_t)r.most);
-    r.hi = (int)min(u1 * KB, (int64_t)r.most);
+    const int last = min(((x.tile + 1) << a->plan.log_tokens), x.s.n) - 1;
+    const int most = a->causal ? min(max(x.s.keys - x.s.n + last + 1, 0), x.s.keys) : x.s.keys;
+    const int64_t u0 = max(begin - x.at - kSeqFixed, (int64_t)0), u1 = min(end - x.at, (int64_t)x.units) - kSeqFixed;
+    r.lo = (int)min(u0 * KB, (int64_t)most);
+    r.hi = (int)min(max(u1, (int64_t)0) * KB, (int64_t)most);
     return r;
   };
 
-  // Pages of a paged item: 64 entries of its table, one a lane; bad: those that the pool does not have.
-  int window = -1, entry = 0, window_b = -1;
+  // Where the next copy comes from. Paged: 64 entries of the sequence's table, one a lane, and which of them name no page.
+  const unsigned char *kfrom = nullptr, *vfrom = nullptr;
+  int from_b = -1, from_keys = 0, window = -1, entry = 0;
   uint64_t bad = 0;
-  // copies a tile of keys and of values; returns which 16 keys of it lie in no page
-  auto copy = [&](const Item& x, int key, int buf) -> uint32_t {
+  auto aim = [&](const Item& x, int key) {
     const SeqArgs a = again(seq_args());
-    const unsigned char* const kall = (const unsigned char*)(PAGED ? a->kp.at : a->k.at);
-    const unsigned char* const vall = (const unsigned char*)(PAGED ? a->vp.at : a->v.at);
-    const unsigned char* t = lds + buf * C::STAGE;
-    const int hk = per_tile == 1 ? x.col / group : x.col;
-    KeyRows<D, W, PAGED> rows[2];
-    uint32_t none = 0;
-    int ids[KB / 16];
-    if constexpr (PAGED) {
-      rows[0] = {kall + hk * a->kp.head * 2, (uint32_t)(a->kp.token * 2), a->kp.page * 2};
-      rows[1] = {vall + hk * a->vp.head * 2, (uint32_t)(a->vp.token * 2), a->vp.page * 2};
-      const int first = key >> a->page_shift;
-      if (x.b != window_b || first >> 6 != window) {
-        window_b = x.b;
+    const int hk = a->plan.per_tile == 1 ? x.col / (a->heads / a->kv_heads) : x.col;
+    if (PAGED) {
+      kfrom = (const unsigned char*)a->kp.at + hk * a->kp.head * 2;
+      vfrom = (const unsigned char*)a->vp.at + hk * a->vp.head * 2;
+    } else {
+      kfrom = (const unsigned char*)a->k.at + ((x.s.first + key) * a->k.token + hk * a->k.head) * 2;
+      vfrom = (const unsigned char*)a->v.at + ((x.s.first + key) * a->v.token + hk * a->v.head) * 2;
+    }
+    if (PAGED && x.b != from_b) window = -1;
+    from_b = x.b;
+    from_keys = x.s.keys;
+  };
+  // copies the tile of keys and of values at `key`; returns which 16 keys of it lie in no page
+  auto copy = [&](int key, int buf) -> uint32_t {
+    const uint32_t to = lds0 + buf * C::STAGE;
+    const int left = from_keys - key;
+    int lane_o = lane;
+    asm volatile("" : "+v"(lane_o));  // the last tiles' offsets are not held across the loop
+    if constexpr (!PAGED) {
+      krows.copy(kfrom, left, to, w, lane_o);
+      vrows.copy(vfrom, left, to + C::BYTES, w, lane_o);
+      kfrom += (uint64_t)KB * krows.token;
+      vfrom += (uint64_t)KB * vrows.token;
+      return 0;
+    } else {
+      const SeqArgs a = again(seq_args());
+      const int shift = a->page_shift, first = key >> shift;
+      if (first >> 6 != window) {
         window = first >> 6;
-        const int e = window * 64 + lane, used = (int)(((int64_t)x.s.keys + (1 << a->page_shift) - 1) >> a->page_shift);
-        entry = e < used ? a->tables[x.b * a->table_stride + e] : 0;
+        const int e = window * 64 + lane, used = (int)(((int64_t)from_keys + (1 << shift) - 1) >> shift);
+        entry = e < used ? a->tables[from_b * a->table_stride + e] : 0;
         bad = __ballot((uint32_t)entry >= (uint32_t)a->n_pages);
       }
+      uint32_t none = 0;
+      int ids[KB / 16];
 #pragma unroll
       for (int j = 0; j < KB / 16; ++j) {
-        const int e = (key + 16 * j) >> a->page_shift & 63;
-        const bool no = bad >> e & 1;
-        ids[j] = no ? -1 : __builtin_amdgcn_readlane(entry, e);
-        if (no) none |= 1u << j;
+        const int e = (key + 16 * j) >> shift & 63;
+        ids[j] = __builtin_amdgcn_readlane(entry, e);
+        if (bad >> e & 1) {
+          ids[j] = -1;
+          none |= 1u << j;
+        }
       }
-    } else {
-      rows[0] = {kall + (x.s.first * a->k.token + hk * a->k.head) * 2, (uint32_t)(a->k.token * 2), 0};
-      rows[1] = {vall + (x.s.first * a->v.token + hk * a->v.head) * 2, (uint32_t)(a->v.token * 2), 0};
+      const int at = key & ((1 << shift) - 1);
+      krows.copy_pages(kfrom, a->kp.page * 2, ids, at, shift, left, to, w, lane_o);
+      vrows.copy_pages(vfrom, a->vp.page * 2, ids, at, shift, left, to + C::BYTES, w, lane_o);
+      return none;
     }
-    int lane_o = lane;
-    asm volatile("" : "+v"(lane_o));  // the copies' offsets are not held across the loop
-    const int mask = (1 << a->page_shift) - 1;
-    rows[0].copy(t, key, x.s.keys - 1, w, lane_o, ids, mask);
-    rows[1].copy(t + C::BYTES, key, x.s.keys - 1, w, lane_o, ids, mask);
-    return none;
   };
 
-  bf16x8 qf[C::KS];
+  // this lane's row of a tile: token i of head `sub`
+  const int row = w * 32 + l32;
+  struct Place {
+    int token, head;
+    bool valid;
+  };
+  auto place = [&](const Item& x) {
+    const SeqArgs a = again(seq_args());
+    const int log_p = a->plan.log_tokens, sub = row >> log_p;
+    Place p;
+    p.token = (x.tile << log_p) + (row & ((1 << log_p) - 1));
+    p.head = x.col * a->plan.per_tile + sub;
+    p.valid = sub < a->plan.per_tile && p.token < x.s.n;
+    return p;
+  };
+
+  bf16x8 qf[C::KS], qn[C::KS];
+  auto load_queries = [&](const Item& x, bf16x8 (&q)[C::KS]) {
+    const Place p = place(x);
+    const SeqArgs a = again(seq_args());
+    const uint16_t* qg = (const uint16_t*)a->q.at + (x.s.first + p.token) * a->q.token + p.head * a->q.head;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) q[s] = load8(qg + 16 * s + 8 * hf, p.valid);
+  };
   f32x16 acc[C::DT];
   float m_run, l_run;
+  const float c2 = seq_args()->scale * kLog2e;
   // One tile of keys. limit: of the lane's query; none: 16 keys without a page.
   auto work = [&](int key, uint32_t t, int limit, bool masked, uint32_t none) {
     // The operands' offsets are taken from their first in every tile, whose place is added before, one exclusive or each (opaque, so
@@ -389,6 +599,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[kt][v] = 0.f;
     constexpr int ROWS = C::KS * C::KT, COLS = 2 * C::KT * C::DT;
+    __builtin_amdgcn_s_setprio(1);
     bf16x8 ring[kSeqAhead];
 #pragma unroll
     for (int x = 0; x < kSeqAhead; ++x) ring[x] = key_row(x);
@@ -399,6 +610,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
       if (x + kSeqAhead < ROWS) ring[x % kSeqAhead] = key_row(x + kSeqAhead);
     }
     WA_SCHED_FENCE();
+    __builtin_amdgcn_s_setprio(0);
     bf16x8 cring[kSeqAhead];
 #pragma unroll
     for (int x = 0; x < kSeqAhead; ++x) cring[x] = col(x);
@@ -440,6 +652,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) pair(0, j);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int x = 0; x < COLS; ++x) {
       WA_SCHED_FENCE();
@@ -451,39 +664,52 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
         if (k16 + 1 < 2 * C::KT && dt == j * C::DT / 4) pair(k16 + 1, j);
     }
     WA_SCHED_FENCE();
+    __builtin_amdgcn_s_setprio(0);
   };
 
   int buf = 0;
-  bool ready = false;      // the item's first tile is on its way
-  uint32_t none = 0, none_next = 0;
-  bool any_bad = false;
+  uint32_t none = 0, any_bad = 0;
+  bool ready = false, stored = false;  // the item's first tile is on its way; stores of the item before come behind it
   Range r = range(it);
   for (;;) {
-    const bool more = it.at + it.units < end;
-    Item nx = it;
-    Range rn = {0, 0, 0};
-    if (more) {
-      nx = walk.next(it);
+    const bool more = round >= 0 ? next_rank() < total : it.at + it.units < end;
+    Item nx;
+    Range rn;
+    bool known = false;  // nx
+    auto look = [&] {
+      const Walk<PAGED> walk(again(seq_args()), C::LOG_KB, lane);
+      if (round >= 0) {
+        nx = ranked(next_rank());
+        ++round;
+      } else {
+        nx = walk.next(it);
+      }
       rn = range(nx);
-    }
-    // the item's queries
-    const SeqArgs a = again(seq_args());
-    const int token = (it.tile << log_p) + i_row;
-    const bool valid = sub < per_tile && token < it.s.n;
-    const int head = it.col * per_tile + sub;
-    const int before = it.s.keys - it.s.n;
-    const int limit = !valid ? 0 : causal ? min(max(before + token + 1, 0), it.s.keys) : it.s.keys;
-    const int t0 = (it.tile << log_p) + i_first, t1 = min((it.tile << log_p) + i_last, it.s.n - 1);
-    // keys that any, and that all of the wavefront's queries see
-    const int some = !wave_used || t0 >= it.s.n ? 0 : causal ? min(max(before + t1 + 1, 0), it.s.keys) : it.s.keys;
-    const int all = causal ? min(max(before + t0 + 1, 0), it.s.keys) : it.s.keys;
-    const uint16_t* qg = (const uint16_t*)a->q.at + (it.s.first + token) * a->q.token + head * a->q.head;
-    if (!ready && r.lo < r.hi) none = copy(it, r.lo, buf);
+      known = true;
+    };
+    if (ready) {
 #pragma unroll
-    for (int s = 0; s < C::KS; ++s) {
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (valid) u = *(const uint4*)(qg + 16 * s + 8 * hf);
-      qf[s] = as_bf16x8(u);
+      for (int s = 0; s < C::KS; ++s) qf[s] = qn[s];
+    } else {
+      if (r.lo < r.hi) {
+        aim(it, r.lo);
+        none = copy(r.lo, buf);
+      }
+      load_queries(it, qf);
+      stored = false;
+    }
+    int limit, some, all;  // keys that the lane's query sees; that any, and that all of the wavefront's queries see
+    {
+      const SeqArgs a = again(seq_args());
+      const int log_p = a->plan.log_tokens, at = it.tile << log_p, before = it.s.keys - it.s.n;
+      const int first = log_p >= 5 ? (w * 32) & ((1 << log_p) - 1) : 0;  // the wavefront's tokens
+      const int t0 = at + first, t1 = min(at + first + (log_p >= 5 ? 31 : (1 << log_p) - 1), it.s.n - 1);
+      const bool used = (w * 32 >> log_p) < a->plan.per_tile && t0 < it.s.n;
+      const Place p = place(it);
+      auto sees = [&](int t) { return a->causal ? min(max(before + t + 1, 0), it.s.keys) : it.s.keys; };
+      limit = p.valid ? sees(p.token) : 0;
+      some = used ? sees(t1) : 0;
+      all = sees(t0);
     }
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
@@ -493,39 +719,58 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     l_run = 0.f;
     ready = false;
     for (int key = r.lo; key < r.hi; key += KB) {
-      WA_WAIT_VM(0);  // this wavefront's part of the tile has arrived (and the queries, so that nothing waits for them below)
-      WA_BARRIER();   // everyone's has, and everyone is done with the other buffer
-      if (key + KB < r.hi) {
-        none_next = copy(it, key + KB, buf ^ 1);
-      } else if (rn.lo < rn.hi) {
-        none_next = copy(nx, rn.lo, buf ^ 1);
-        ready = true;
+      // This wavefront's part of the tile has arrived (and the queries, so that nothing waits for them below); stores behind it, at
+      // least one for each four columns that a lane holds, need not have.
+      if (stored) WA_WAIT_VM(4 * C::DT); else WA_WAIT_VM(0);
+      stored = false;
+      WA_BARRIER();  // everyone's has, and everyone is done with the other buffer
+      int next = key + KB;
+      bool go = next < r.hi;
+      if (!go && more) {
+        if (!known) look();
+        go = ready = rn.lo < rn.hi;
+        next = rn.lo;
+        if (go) {
+          aim(nx, next);
+          load_queries(nx, qn);
+        }
       }
-      if (PAGED && none) any_bad = true;
+      uint32_t none_next = 0;
+      if (go) none_next = copy(next, buf ^ 1);
+      if (more && !known) look();  // early, so that the last tile's copies do not wait for it
+      any_bad |= none;
       if (key < some) work(key, buf * C::STAGE, limit, key + KB > all || (PAGED && none), none);
       none = none_next;
       buf ^= 1;
     }
+    if (more && !known) look();
 
     // the item's end: whole rows to O, others to the worker's partial tiles
-    {
-    const SeqArgs a = again(seq_args());
     const float l = add_halves(l_run);
     const float ref = m_run == -INFINITY ? -INFINITY : m_run - T::kBias;
     const bool starts = begin <= it.at, finishes = it.at + it.units <= end;
-    if (valid) {
-      const int64_t tok = it.s.first + token;
+    const Place p = place(it);
+    stored = __ballot(p.valid) != 0;
+    if (p.valid) {
+      const SeqArgs a = again(seq_args());
+      const int64_t tok = it.s.first + p.token;
       if (starts && finishes) {
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-        uint16_t* out = (uint16_t*)a->o.at + tok * a->o.token + head * a->o.head + 4 * hf;
+        uint16_t* out = (uint16_t*)a->o.at + tok * a->o.token + p.head * a->o.head + 4 * hf;
+        float* stat = a->lse ? a->lse + (p.head * (int64_t)a->tokens + tok) * a->lse_step : nullptr;
 #pragma unroll
         for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-          for (int v = 0; v < 16; v += 4)
-            *(uint2*)(out + dt * 32 + 2 * v) =
-                make_uint2(T::pack(acc[dt][v] * inv, acc[dt][v + 1] * inv), T::pack(acc[dt][v + 2] * inv, acc[dt][v + 3] * inv));
-        if (a->lse && hf == 0) a->lse[(int64_t)head * a->tokens + tok] = l == 0.f ? -INFINITY : (ref + __log2f(l)) * kLn2;
-        if (hf == 0) a->cuts[tok * a->heads + head] = make_int2(-1, 0);
+          for (int v = 0; v < 16; v += 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[dt][v + e] *= inv;
+            const uint2 o16 = make_uint2(T::pack(acc[dt][v], acc[dt][v + 1]), T::pack(acc[dt][v + 2], acc[dt][v + 3]));
+            *(uint2*)(out + dt * 32 + 2 * v) = o16;
+            if (!HALF && !PAGED && stat)
+              *(uint32_t*)(stat + 1 + dt * 8 + v / 2 + hf) = rest4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3], o16);
+          }
+        if (stat && hf == 0) *stat = l == 0.f ? -INFINITY : (ref + __log2f(l)) * kLn2;
+        if (round < 0 && hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(-1, 0);
       } else {
         // slot 0: a part that begins inside its tile; slot 1: one that begins with it
         const int64_t at = ((int64_t)me * 2 + (starts ? 1 : 0)) * R + row;
@@ -535,83 +780,162 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
 #pragma unroll
           for (int v = 0; v < 16; v += 4)
             *(float4*)(out + dt * 32 + 2 * v + 4 * hf) = make_float4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3]);
-        if (hf == 0) {
-          ((float2*)(a->part + (int64_t)a->plan.workers * 2 * R * D))[at] = make_float2(ref, l);
-          if (finishes) a->cuts[tok * a->heads + head] = make_int2(shares.first_of(it) | me << 16, row);
+        if (hf == 0) ((float2*)(a->part + (int64_t)a->plan.workers * 2 * R * D))[at] = make_float2(ref, l);
+        if (finishes) {
+          const int first = Shares(total, a).first_of(it);
+          if (hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(first | me << 16, row);
         }
       }
-    }
     }
     if (!more) break;
     it = nx;
     r = rn;
   }
-  if (PAGED && any_bad && a->status && tid == 0) atomicOr(a->status, WA_PAGE_BAD_INDEX);
+  if (PAGED && any_bad && seq_args()->status && tid == 0) atomicOr(seq_args()->status, WA_PAGE_BAD_INDEX);
 }
 
-// Joins the parts of a row, in key order: parts from worker cut.x & 0xffff to cut.x >> 16. TEAM wavefronts a row, each taking every
-// TEAM-th part; the lanes hold the columns.
-template <bool HALF, int D, int W, int TEAM>
-__global__ __launch_bounds__(256) void seq_join_kernel(const WaSeqLaunch a, int rows_per_wave) {
-  using T = SeqType<HALF>;
-  constexpr int R = 32 * W, E = D / 64;
-  typedef float cols __attribute__((ext_vector_type(E)));
-  __shared__ cols sums[TEAM == 1 ? 1 : TEAM][64];
-  __shared__ float totals[TEAM == 1 ? 1 : TEAM];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t all = (int64_t)a.tokens * a.heads;
-  const int64_t first = TEAM == 1 ? ((int64_t)blockIdx.x * 4 + w) * rows_per_wave : blockIdx.x;
-  // tokens of sequences: what lies before the first and behind the last stays as it is, and has no cuts
-  const int64_t lo = (int64_t)min(max(a.starts[0], 0), a.tokens) * a.heads, hi = (int64_t)min(max(a.starts[a.batch], 0), a.tokens) * a.heads;
-  const float2* stat = (const float2*)(a.part + (int64_t)a.plan.workers * 2 * R * D);
-  int2 mine = make_int2(-1, 0);
-  if (lane < rows_per_wave && first + lane >= lo && first + lane < min(hi, all)) mine = a.cuts[first + lane];
-  uint64_t cut = __ballot(mine.x != -1);
-  while (cut) {
-    const int who = __builtin_ctzll(cut);
-    cut &= cut - 1;
-    const int x = __builtin_amdgcn_readlane(mine.x, who), r = __builtin_amdgcn_readlane(mine.y, who) & (R - 1);
-    // taken into the workers that there are: nothing that the workspace holds leads out of it
-    const int begin = min(x & 0xffff, a.plan.workers - 1), end = min((int)((uint32_t)x >> 16), a.plan.workers - 1);
-    auto at = [&](int c) { return ((int64_t)c * 2 + (c == begin ? 1 : 0)) * R + r; };
-    float top = -INFINITY;
-    for (int c = begin + lane; c <= end; c += 64) top = fmaxf(top, stat[at(c)].x);
+// Where a row's parts lie, and its end.
+template <bool HALF, int D, int W, bool PAGED>
+struct JoinRow {
+  static constexpr int R = 32 * W;
+  int64_t token;
+  int head, begin, end, row;
+  const float2* stat;
+  // cut: as seq_attn_kernel left it, taken into the workers that there are, so that nothing that the workspace holds leads out of it
+  __device__ __forceinline__ JoinRow(const WaSeqLaunch& a, int64_t r, int2 cut) {
+    token = r / a.heads;
+    head = (int)(r - token * a.heads);
+    begin = min(cut.x & 0xffff, a.plan.workers - 1);
+    end = min((int)((uint32_t)cut.x >> 16), a.plan.workers - 1);
+    row = cut.y & (R - 1);
+    stat = (const float2*)(a.part + (int64_t)a.plan.workers * 2 * R * D);
+  }
+  // a part that begins with its tile lies in slot 1, others in slot 0
+  __device__ __forceinline__ int64_t at(int c) const { return ((int64_t)c * 2 + (c == begin ? 1 : 0)) * R + row; }
+  // columns [c, c + 4) of the row; o, l: summed over the parts, taken against `top`
+  __device__ __forceinline__ void finish(const WaSeqLaunch& a, float4 o, float l, float top, int c) const {
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+    o.x *= inv;
+    o.y *= inv;
+    o.z *= inv;
+    o.w *= inv;
+    const uint2 o16 = make_uint2(SeqType<HALF>::pack(o.x, o.y), SeqType<HALF>::pack(o.z, o.w));
+    *(uint2*)((uint16_t*)a.o.at + token * a.o.token + head * a.o.head + c) = o16;
+    if (!a.lse) return;
+    float* to = a.lse + (head * (int64_t)a.tokens + token) * a.lse_step;
+    if (c == 0) *to = l == 0.f ? -INFINITY : (top + __log2f(l)) * kLn2;
+    if (!HALF && !PAGED) *(uint32_t*)(to + 1 + c / 4) = rest4(o.x, o.y, o.z, o.w, o16);
+  }
+};
+// Rows of sequences: what lies before the first and behind the last stays as it is, and has no cuts.
+__device__ __forceinline__ bool seq_row(const WaSeqLaunch& a, int64_t r) {
+  return r >= (int64_t)min(max(a.starts[0], 0), a.tokens) * a.heads && r < (int64_t)min(max(a.starts[a.batch], 0), a.tokens) * a.heads;
+}
+
+// Joins rows of few parts: four columns a lane, D / 4 lanes a row, which look at as many rows at once (those `groups` apart) and join the
+// ones that are cut.
+template <bool HALF, int D, int W, bool PAGED>
+__global__ __launch_bounds__(256) void seq_join_few_kernel(const WaSeqLaunch a, int64_t groups) {
+  constexpr int L = D / 4;
+  if (!*a.any_cut) return;
+  const int lane = threadIdx.x & (L - 1), c = 4 * lane;
+  const int64_t group = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L, all = (int64_t)a.tokens * a.heads;
+  for (int64_t base = group; base < all; base += groups * L) {
+    const int64_t mine = base + lane * groups;
+    int2 cut = make_int2(-1, 0);
+    if (mine < all && seq_row(a, mine)) cut = a.cuts[mine];
+    uint64_t some = __ballot(cut.x != -1) >> (threadIdx.x & 63 & ~(L - 1));
+    if (L < 64) some &= ((uint64_t)1 << (L & 63)) - 1;
+    while (some) {
+      const int who = __builtin_ctzll(some);
+      some &= some - 1;
+      const JoinRow<HALF, D, W, PAGED> row(a, base + who * groups, make_int2(__shfl(cut.x, who, L), __shfl(cut.y, who, L)));
+      float top = -INFINITY, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = row.begin; w <= row.end; w += 4) {
+        float2 s[4];
+        float4 x[4];
 #pragma unroll
-    for (int y = 32; y > 0; y >>= 1) top = fmaxf(top, __shfl_xor(top, y));
-    cols o = 0.f;
-    float l = 0.f;
-#pragma unroll 8
-    for (int c = begin + (TEAM == 1 ? 0 : w); c <= end; c += TEAM) {
-      const float2 s = stat[at(c)];
-      const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
-      l += f * s.y;
-      o += *(const cols*)(a.part + at(c) * D + lane * E) * f;
-    }
-    if constexpr (TEAM > 1) {
-      sums[w][lane] = o;
-      if (lane == 0) totals[w] = l;
-      __syncthreads();
-      if (w) return;
-      for (int y = 1; y < TEAM; ++y) {
-        o += sums[y][lane];
-        l += totals[y];
+        for (int i = 0; i < 4; ++i) {  // past the last part the last again, without weight
+          const int64_t at = row.at(min(w + i, row.end));
+          s[i] = row.stat[at];
+          x[i] = *(const float4*)(a.part + at * D + c);
+        }
+        float high = top;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) high = fmaxf(high, s[i].x);
+        const float keep = high == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - high);
+        l *= keep;
+        o.x *= keep;
+        o.y *= keep;
+        o.z *= keep;
+        o.w *= keep;
+        top = high;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = s[i].x == -INFINITY || w + i > row.end ? 0.f : __builtin_amdgcn_exp2f(s[i].x - high);
+          l += f * s[i].y;
+          o.x += f * x[i].x;
+          o.y += f * x[i].y;
+          o.z += f * x[i].z;
+          o.w += f * x[i].w;
+        }
       }
+      row.finish(a, o, l, top, c);
     }
-    o *= l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-    const int64_t rr = first + who, token = rr / a.heads;
-    const int head = (int)(rr - token * a.heads);
-    uint16_t* out = (uint16_t*)a.o.at + token * a.o.token + head * a.o.head + lane * E;
-    if constexpr (E == 2) {
-      *(uint32_t*)out = T::pack(o[0], o[1]);
-    } else {
-      *out = (uint16_t)T::pack(o[0], 0.f);
-    }
-    if (a.lse && lane == 0) a.lse[(int64_t)head * a.tokens + token] = l == 0.f ? -INFINITY : (top + __log2f(l)) * kLn2;
   }
 }
 
-// Rows up to which a workgroup joins one alone: many parts each. With more, their tiles are cut in few.
-constexpr int64_t kSeqTeamRows = 8192;
+// Joins rows of many parts: a workgroup a row, D / 4 lanes a part.
+template <bool HALF, int D, int W, bool PAGED>
+__global__ __launch_bounds__(1024) void seq_join_many_kernel(const WaSeqLaunch a) {
+  constexpr int L = D / 4, TEAMS = 1024 / L;
+  __shared__ float4 sums[TEAMS][L];
+  __shared__ float totals[TEAMS], tops[16];
+  if (!*a.any_cut || !seq_row(a, blockIdx.x)) return;
+  const int2 cut = a.cuts[blockIdx.x];
+  if (cut.x == -1) return;
+  const JoinRow<HALF, D, W, PAGED> row(a, blockIdx.x, cut);
+  const int team = threadIdx.x / L, lane = threadIdx.x & (L - 1), c = 4 * lane;
+  float top = -INFINITY;  // of up to 1,024 parts, a thread one
+  if (row.begin + (int)threadIdx.x <= row.end) top = row.stat[row.at(row.begin + threadIdx.x)].x;
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < 16; ++x) top = fmaxf(top, tops[x]);
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int w = row.begin + team; w <= row.end; w += TEAMS) {
+    const int64_t at = row.at(w);
+    const float2 s = row.stat[at];
+    const float4 x = *(const float4*)(a.part + at * D + c);
+    const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
+    l += f * s.y;
+    o.x += f * x.x;
+    o.y += f * x.y;
+    o.z += f * x.z;
+    o.w += f * x.w;
+  }
+  sums[team][lane] = o;
+  if (lane == 0) totals[team] = l;
+  __syncthreads();
+  if (team) return;
+  for (int x = 1; x < TEAMS; ++x) {  // in one order
+    const float4 y = sums[x][lane];
+    l += totals[x];
+    o.x += y.x;
+    o.y += y.y;
+    o.z += y.z;
+    o.w += y.w;
+  }
+  row.finish(a, o, l, top, c);
+}
+
+// Rows up to which a workgroup joins one alone: tiles of so few rows may be cut in many parts. With more, in few.
+constexpr int64_t kSeqManyRows = 1024;
 
 template <bool HALF, int D, int W, bool PAGED>
 hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
@@ -619,10 +943,12 @@ hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)a.tokens * a.heads;
-  if (rows <= kSeqTeamRows) {
-    hipLaunchKernelGGL((seq_join_kernel<HALF, D, W, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a, 1);
+  if (rows <= kSeqManyRows) {
+    hipLaunchKernelGGL((seq_join_many_kernel<HALF, D, W, PAGED>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
   } else {
-    hipLaunchKernelGGL((seq_join_kernel<HALF, D, W, 1>), dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, stream, a, 64);
+    constexpr int PER = 256 / (D / 4);
+    const int64_t wgs = std::min<int64_t>((rows + PER - 1) / PER, 2048);
+    hipLaunchKernelGGL((seq_join_few_kernel<HALF, D, W, PAGED>), dim3((unsigned)wgs), dim3(256), 0, stream, a, wgs * PER);
   }
   return hipGetLastError();
 }

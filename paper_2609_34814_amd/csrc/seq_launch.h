@@ -31,18 +31,20 @@ struct WaSeqLaunch {
   int32_t table_width, n_pages, page_shift;
   const int32_t* starts;   // [batch + 1]: first token of each sequence's queries, and their end
   const int32_t* kv_lens;  // [batch]: keys of each sequence; packed: its tokens
-  float* lse;              // [heads][tokens], nullable
+  float* lse;              // [heads][tokens] rows of lse_step, nullable: log-sum-exps, then (packed bf16) what O lost in rounding
+  int32_t lse_step;
   int32_t* status;         // nullable
   int32_t batch, tokens, heads, kv_heads, head_dim, half, causal, paged;
   float scale;
+  int32_t* any_cut;        // workspace: whether tiles are cut
   int2* cuts;              // workspace: [tokens][heads] (see seq_attn.h)
   float* part;             // workspace: partial tiles of the workers
   WaSeqPlan plan;
   // gradient
   WaSeqRows dout, dq, dk, dv;
-  const float* lse_in;     // what the forward wrote
+  const float* lse_in;     // what the forward wrote, [heads][tokens] rows of lse_step
   float* rows;             // workspace: [2][heads][tokens]: what a query's products start from (packed_bwd.hip)
-  int32_t parts;           // ranges of queries that a tile of keys is computed in
+  int64_t dq_part;         // floats of `part` that the parts of dQ may take; those of dK and dV lie behind
 };
 
 WaSeqPlan wa_seq_plan(const WaSeqLaunch& a);  // of its shape
@@ -51,7 +53,8 @@ size_t wa_seq_part_floats(const WaSeqPlan& p, int head_dim);
 hipError_t wa_launch_packed_attn(const WaSeqLaunch& a, hipStream_t stream);
 hipError_t wa_launch_paged_attn(const WaSeqLaunch& a, hipStream_t stream);
 
-// Gradient: key tiles of 128, each in `parts` ranges of the queries that see them.
-int32_t wa_packed_backward_parts(const WaSeqLaunch& a);
-int64_t wa_packed_backward_tiles(const WaSeqLaunch& a);  // tiles of 128 tokens, at most, of all sequences
+// Gradient (packed_bwd.hip): tiles of 128 tokens of all sequences, at most; float32 results of tiles in parts, those of dQ and all.
+int64_t wa_packed_backward_tiles(const WaSeqLaunch& a);
+int64_t wa_packed_backward_dq_floats(const WaSeqLaunch& a);
+int64_t wa_packed_backward_part_floats(const WaSeqLaunch& a);
 hipError_t wa_launch_packed_backward(const WaSeqLaunch& a, hipStream_t stream);

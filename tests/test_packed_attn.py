@@ -117,9 +117,9 @@ def test_binding_refusals(kw):
         W.packed_attn(q, k, v, starts, **a)
     if "out" not in a and q.dim() == 3:
         with pytest.raises(ValueError):
-            W.packed_attn_backward(torch.zeros_like(q), q, k, v, torch.zeros_like(q), torch.zeros(4, 20), starts, **a)
+            W.packed_attn_backward(torch.zeros_like(q), q, k, v, torch.zeros_like(q), torch.zeros(4, 20, 17), starts, **a)
     h = _host()
-    for lse in (torch.zeros(20, 4), torch.zeros(4, 20, dtype=torch.float64)):
+    for lse in (torch.zeros(4, 20), torch.zeros(20, 4, 17), torch.zeros(4, 20, 17, dtype=torch.float64)):
         with pytest.raises(ValueError, match="lse"):
             W.packed_attn_backward(h["q"], h["q"], h["k"], h["v"], h["q"], lse, h["starts"])
 
@@ -191,7 +191,7 @@ def check(args, causal=True, backward=True, **kw):
     outside = np.isnan(ref["o"])
     assert np.all(f64(o)[outside] == marker)
     close(o, ref["o"], ref["tol"]["o"], "o")
-    check_lse(lse, ref["lse"])
+    check_lse(lse[..., 0], ref["lse"])
     assert torch.equal(W.packed_attn(q, k, v, starts, causal=causal, out=torch.full_like(q, marker), **kw), o)  # the same bits
     if not backward:
         return
@@ -242,7 +242,7 @@ def test_head_major_and_broadcast():
     turned = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, dout)]
     o, lse = W.packed_attn(q, k, v, starts, return_lse=True)
     o2, lse2 = W.packed_attn(*turned[:3], starts, return_lse=True, out=torch.empty_like(q.transpose(0, 1)).transpose(0, 1))
-    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    assert torch.equal(o, o2) and torch.equal(lse.view(torch.int32), lse2.view(torch.int32))
     for x, y in zip(W.packed_attn_backward(dout, q, k, v, o, lse, starts),
                     W.packed_attn_backward(turned[3], *turned[:3], o2, lse2, starts)):
         assert torch.equal(x, y)
@@ -318,7 +318,7 @@ def test_captured_and_on_another_stream():
     with torch.cuda.stream(side):
         first = step()
     side.synchronize()
-    assert all(torch.equal(x, y) for x, y in zip(first, step()))
+    assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(first, step()))
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         out = step()
@@ -328,7 +328,7 @@ def test_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         want = step()
-        assert all(torch.equal(x, y) for x, y in zip(out, want)), lens
+        assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(out, want)), lens
 
 
 @pytest.mark.gpu
