@@ -23,8 +23,14 @@ WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
     p.per_tile = 1;
     p.log_tokens = log_tokens(1);
   }
-  p.workers = p.waves == 4 ? 512 : 1024;
-  p.min_units = 4;
+#ifndef NW1
+#define NW1 1024
+#endif
+#ifndef MU
+#define MU 4
+#endif
+  p.workers = p.waves == 4 ? 512 : NW1;
+  p.min_units = MU;
   return p;
 }
 

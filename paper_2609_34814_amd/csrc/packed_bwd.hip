@@ -34,6 +34,14 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+__device__ __forceinline__ Seq one_seq(int b) {
+  Seq s = seq_of<false>(seq_args(), b);
+  s.first = __builtin_amdgcn_readfirstlane(s.first);
+  s.n = __builtin_amdgcn_readfirstlane(s.n);
+  s.keys = __builtin_amdgcn_readfirstlane(s.keys);
+  return s;
+}
+
 // A tile of 128 rows, or the part of one, that a workgroup computes. Its length is the tiles of the other side that it meets.
 struct Job {
   int b, tile, col;        // sequence, tile of it, head or key head
@@ -59,7 +67,7 @@ struct Jobs {
     }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-    sum = Walk<false>::uniform64(sum) * cols;
+    sum = uniform64(sum) * cols;
     most = (int)((sum + kSlots - 1) / kSlots);
   }
   __device__ __forceinline__ int tiles_of(int b) const {
@@ -173,7 +181,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
   if (!Jobs(lane, a.heads).find(blockIdx.x, true, &job)) return;
   // causal: a tile's length is its number and one, and the longest is the last
   const int b = job.b, tile = a.causal ? job.length - 1 : job.tile, h = job.col, hk = h / (a.heads / a.kv_heads);
-  const Seq s = Walk<false>::uniform(seq_of<false>(seq_args(), b));
+  const Seq s = one_seq(b);
   const int i0 = tile * kRows + w * 32, i = i0 + l32, i_last = s.n - 1;
   const bool valid = i <= i_last;
   const int limit = !valid ? 0 : a.causal ? i + 1 : s.n;
@@ -309,7 +317,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
   if (!Jobs(lane, a.kv_heads).find(blockIdx.x, true, &job)) return;
   // causal: the first tile of a sequence meets the queries of all of them
   const int b = job.b, tile = job.tile, hk = job.col, group = a.heads / a.kv_heads;
-  const Seq s = Walk<false>::uniform(seq_of<false>(seq_args(), b));
+  const Seq s = one_seq(b);
   const int k0 = tile * kRows + w * 32, kj = k0 + l32;
   const bool valid = kj < s.n;
   const int from = !valid ? s.n : a.causal ? kj : 0;                      // first query that sees this lane's key,
@@ -467,7 +475,7 @@ __global__ __launch_bounds__(256) void packed_parts_kernel(const WaSeqLaunch a, 
   Job job;
   const int64_t mine = keys ? rank - dq_tiles : rank;
   if (!jobs.find(mine, false, &job) || job.parts == 1) return;
-  const Seq s = Walk<false>::uniform(seq_of<false>(seq_args(), job.b));
+  const Seq s = one_seq(job.b);
   const int tile = !a.causal || keys ? job.tile : job.length - 1, width = keys ? 2 * D : D;
   const int64_t first = jobs.first_part(mine, job), step = (int64_t)cols * kRows * width;
   const float* from = a.part + (keys ? a.dq_part : 0) + first * kRows * width;

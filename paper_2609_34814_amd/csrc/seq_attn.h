@@ -63,12 +63,12 @@ struct SeqType<true> {
 
 template <int D, int W>
 struct SeqTile {
-  // Keys a tile: 64 with four wavefronts (two workgroups a compute unit); with one, 32, so that enough workgroups fit to keep the
-  // memory busy.
-  static constexpr int KB = W == 4 ? 64 : 32;
+  // Keys a tile: 64 with four wavefronts (two workgroups a compute unit); with one, 32 of 256 bytes or 64 of 128, so that enough
+  // workgroups fit to keep the memory busy.
+  static constexpr int KB = W == 4 || D == 64 ? 64 : 32;
   static constexpr int RB = D * 2, BYTES = KB * RB, STAGE = 2 * BYTES;
   static constexpr int KT = KB / 32, DT = D / 32, KS = D / 16;
-  static constexpr int LOG_KB = W == 4 ? 6 : 5;
+  static constexpr int LOG_KB = KB == 64 ? 6 : 5;
 };
 
 // A launch's arguments where the hardware put them. They do not fit the scalar registers beside the kernel's state: again() forgets
@@ -131,58 +131,105 @@ struct Item {
   int units;
 };
 
-template <bool PAGED>
-struct Walk {
-  SeqArgs a;
-  int log_kb, log_tokens, cols, lane;
-
-  __device__ __forceinline__ Walk(SeqArgs a_, int log_kb_, int lane_)
-      : a(a_), log_kb(log_kb_), log_tokens(a_->plan.log_tokens), cols(a_->heads / a_->plan.per_tile), lane(lane_) {}
-  __device__ __forceinline__ Line line(const Seq& s) const { return Line(log_tokens, log_kb, s, a->causal); }
-  __device__ __forceinline__ int tiles(const Seq& s) const { return (int)(((int64_t)s.n + (1 << log_tokens) - 1) >> log_tokens); }
-
-  // units of sequence base + lane, summed over the lanes up to this one
-  __device__ __forceinline__ int64_t prefix(int base, int64_t* own) const {
-    int64_t x = 0;
-    if (base + lane < a->batch) {
-      const Seq s = seq_of<PAGED>(a, base + lane);
-      x = cols * line(s).upto(tiles(s));
-    }
-    *own = x;
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)v >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// Sums over the lanes, the same in all of them, and up to each lane; numbers of 64 bits that are small take the short way.
+__device__ __forceinline__ int lane_sum(int x) { return __builtin_amdgcn_readlane(lane_prefix_sum(x), 63); }
+__device__ __forceinline__ int64_t lane_prefix_sum64(int64_t x, int lane) {
+  if (__ballot((uint64_t)x >> 25 != 0) == 0) return lane_prefix_sum((int)x);
 #pragma unroll
-    for (int step = 1; step < 64; step <<= 1) {
-      const int64_t y = __shfl_up(x, step);
-      if (lane >= step) x += y;
-    }
-    return x;
+  for (int step = 1; step < 64; step <<= 1) {
+    const int64_t y = __shfl_up(x, step);
+    if (lane >= step) x += y;
   }
-  __device__ __forceinline__ int64_t total() const {
-    int64_t sum = 0, own;
-    for (int base = 0; base < a->batch; base += 64) sum += __shfl(prefix(base, &own), 63);
+  return x;
+}
+__device__ __forceinline__ uint64_t divide(uint64_t x, uint64_t y) {
+  return (x | y) >> 32 ? x / y : (uint32_t)x / (uint32_t)y;
+}
+
+// Finds tiles: in the line of units, and by their length. The first 64 sequences are held, one a lane.
+template <bool PAGED, int LOG_KB>
+struct Walk {
+  int lane, log_tokens, cols, batch;
+  bool causal;
+  Seq mine;
+
+  __device__ __forceinline__ Walk(SeqArgs a, int lane_)
+      : lane(lane_), log_tokens(a->plan.log_tokens), cols(a->heads / a->plan.per_tile), batch(a->batch), causal(a->causal) {
+    mine = seq_of<PAGED>(a, min(lane, batch - 1));
+    if (lane >= batch) mine.n = 0;
+  }
+  __device__ __forceinline__ Line line(const Seq& s) const { return Line(log_tokens, LOG_KB, s, causal); }
+  __device__ __forceinline__ int tiles(const Seq& s) const { return (int)(((int64_t)s.n + (1 << log_tokens) - 1) >> log_tokens); }
+  // sequence base + lane, without queries if there is none
+  __device__ __forceinline__ Seq seq_at(int base) const {
+    if (base == 0) return mine;
+    Seq s = seq_of<PAGED>(again(seq_args()), min(base + lane, batch - 1));
+    if (base + lane >= batch) s.n = 0;
+    return s;
+  }
+  __device__ __forceinline__ Seq seq(int b) const {
+    Seq s;
+    if (b < 64) {
+      s.first = __builtin_amdgcn_readlane(mine.first, b);
+      s.n = __builtin_amdgcn_readlane(mine.n, b);
+      s.keys = __builtin_amdgcn_readlane(mine.keys, b);
+    } else {
+      s = seq_of<PAGED>(again(seq_args()), b);
+      s.first = __builtin_amdgcn_readfirstlane(s.first);
+      s.n = __builtin_amdgcn_readfirstlane(s.n);
+      s.keys = __builtin_amdgcn_readfirstlane(s.keys);
+    }
+    return s;
+  }
+
+  // Units of sequence base + lane, and of all up to it from `base` on.
+  struct Sums {
+    int64_t own, upto;
+  };
+  __device__ __forceinline__ Sums sums(int base) const {
+    const Seq s = seq_at(base);
+    const int64_t x = s.n ? cols * line(s).upto(tiles(s)) : 0;
+    return {x, lane_prefix_sum64(x, lane)};
+  }
+  __device__ __forceinline__ int64_t total(const Sums& head) const {
+    int64_t sum = lane64(head.upto, 63);
+    for (int base = 64; base < batch; base += 64) sum += lane64(sums(base).upto, 63);
     return sum;
   }
-  // the item that holds unit x, which is below the total
-  __device__ __forceinline__ Item find(int64_t x) const {
-    int64_t before = 0, own, sum = 0;
-    int base = 0, who = 0;
-    for (;; base += 64) {
-      sum = prefix(base, &own);
-      const uint64_t past = __ballot(before + sum > x);
-      if (past || base + 64 >= a->batch) {
+  // the item that holds unit x, which is below the total; head: sums(0)
+  __device__ __forceinline__ Item find(int64_t x, const Sums& head) const {
+    Item it;
+    it.at = 0;
+    Sums sum = head;
+    int who = 0;
+    for (int base = 0;; base += 64) {
+      if (base) sum = sums(base);
+      const uint64_t past = __ballot(it.at + sum.upto > x);
+      it.b = base;
+      if (past || base + 64 >= batch) {
         who = past ? __builtin_ctzll(past) : 0;
         break;
       }
-      before += __shfl(sum, 63);
+      it.at += lane64(sum.upto, 63);
     }
-    Item it;
-    it.b = min(__builtin_amdgcn_readfirstlane(base + who), a->batch - 1);
-    it.at = before + __shfl(sum - own, who);
-    it.s = uniform(seq_of<PAGED>(a, it.b));
+    it.b = __builtin_amdgcn_readfirstlane(min(it.b + who, batch - 1));
+    it.at += lane64(sum.upto - sum.own, who);
+    it.s = seq(it.b);
     const Line l = line(it.s);
     it.tiles = tiles(it.s);
     const int64_t column = l.upto(it.tiles);
-    int64_t r = x - it.at;
-    it.col = (int)(r / column);
+    int64_t r = uniform64(x - it.at);
+    it.col = (int)divide(r, column);
     it.at += it.col * column;
     r -= it.col * column;
     int lo = 0, hi = it.tiles;  // upto(lo) <= r < upto(hi)
@@ -191,8 +238,9 @@ struct Walk {
       if (l.upto(mid) <= r) lo = mid; else hi = mid;
     }
     it.tile = lo;
-    it.at += l.upto(lo);
-    it.units = (int)(l.upto(lo + 1) - l.upto(lo));
+    const int64_t from = l.upto(lo);
+    it.at += from;
+    it.units = (int)(l.upto(lo + 1) - from);
     scalar(it);
     return it;
   }
@@ -203,78 +251,47 @@ struct Walk {
       it.tile = 0;
       if (++it.col == cols) {
         it.col = 0;
-        do it.s = uniform(seq_of<PAGED>(again(a), ++it.b)); while (it.s.n == 0 && it.b + 1 < a->batch);
+        do it.s = seq(++it.b); while (it.s.n == 0 && it.b + 1 < batch);
         it.tiles = tiles(it.s);
       }
     }
+    measure(it);
+    return it;
+  }
+  __device__ __forceinline__ void measure(Item& it) const {
     const Line l = line(it.s);
     it.units = (int)(l.upto(it.tile + 1) - l.upto(it.tile));
     scalar(it);
-    return it;
   }
-  static __device__ __forceinline__ int64_t uniform64(int64_t v) {
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)v >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
-  }
-  static __device__ __forceinline__ Seq uniform(Seq s) {
-    s.first = __builtin_amdgcn_readfirstlane(s.first);
-    s.n = __builtin_amdgcn_readfirstlane(s.n);
-    s.keys = __builtin_amdgcn_readfirstlane(s.keys);
-    return s;
-  }
-  static __device__ __forceinline__ void scalar(Item& it) {
-    it.at = uniform64(it.at);
-    it.col = __builtin_amdgcn_readfirstlane(it.col);
-    it.tile = __builtin_amdgcn_readfirstlane(it.tile);
-    it.units = __builtin_amdgcn_readfirstlane(it.units);
-  }
-};
 
-// Sum and maximum over the lanes, the same in all of them.
-__device__ __forceinline__ int lane_sum(int x) { return __builtin_amdgcn_readlane(lane_prefix_sum(x), 63); }
-
-// All tiles of packed sequences by falling number of the tile in its sequence: those that see the most keys first. The first 64 sequences
-// are held, one a lane.
-struct Levels {
-  int lane, log_tokens, batch, first, n, mine;
-
-  __device__ __forceinline__ Levels(SeqArgs a, int lane_) : lane(lane_), log_tokens(a->plan.log_tokens), batch(a->batch) {
-    const Seq s = seq_of<false>(a, min(lane, batch - 1));
-    first = s.first;
-    n = lane < batch ? s.n : 0;
-    mine = tiles(n);
-  }
-  __device__ __forceinline__ int tiles(int n) const { return (int)(((int64_t)n + (1 << log_tokens) - 1) >> log_tokens); }
-  // tiles of the sequence `base` + lane
-  __device__ __forceinline__ int tiles_at(int base) const {
-    return base == 0 ? mine : base + lane < batch ? tiles(seq_of<false>(again(seq_args()), base + lane).n) : 0;
-  }
-  // tiles number t and above of their sequences
+  // Tiles of one column that are number t and above in their sequences.
   __device__ __forceinline__ int above(int t) const {
     int sum = 0;
-    for (int base = 0; base < batch; base += 64) sum += lane_sum(max(tiles_at(base) - t, 0));
+    for (int base = 0; base < batch; base += 64) sum += lane_sum(max(tiles(seq_at(base)) - t, 0));
     return sum;
   }
-  // Tile `rank` (below above(0)) of one column: its sequence, and its number there.
-  __device__ __forceinline__ void find(int rank, int* b, int* tile) const {
+  // Tile `rank` of all, by falling number: of packed sequences those that see the most keys first. rank is below above(0) cols.
+  __device__ __forceinline__ Item ranked(int64_t rank) const {
+    const int row = (int)divide(rank, cols);
+    Item it;
+    it.col = (int)(rank - (int64_t)row * cols);
     int most = 0;
-    for (int base = 0; base < batch; base += 64) most = max(most, tiles_at(base));
+    for (int base = 0; base < batch; base += 64) most = max(most, tiles(seq_at(base)));
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) most = max(most, __shfl_xor(most, x));
-    int lo = 0, hi = __builtin_amdgcn_readfirstlane(most), passed = 0;  // above(lo) > rank >= above(hi) = passed
+    int lo = 0, hi = __builtin_amdgcn_readfirstlane(most), passed = 0;  // above(lo) > row >= above(hi) = passed
     while (hi - lo > 1) {
       const int mid = lo + ((hi - lo) >> 1), m = above(mid);
-      if (m > rank) {
+      if (m > row) {
         lo = mid;
       } else {
         hi = mid;
         passed = m;
       }
     }
-    int k = rank - passed, who = 0;
+    int k = row - passed, who = 0;
     for (int base = 0; base < batch; base += 64) {
-      uint64_t there = __ballot(tiles_at(base) > lo);
+      uint64_t there = __ballot(tiles(seq_at(base)) > lo);
       const int m = __popcll(there);
       if (k < m) {
         for (; k > 0; --k) there &= there - 1;
@@ -283,18 +300,20 @@ struct Levels {
       }
       k -= m;
     }
-    *b = __builtin_amdgcn_readfirstlane(who);
-    *tile = lo;
+    it.b = __builtin_amdgcn_readfirstlane(who);
+    it.tile = lo;
+    it.s = seq(it.b);
+    it.tiles = tiles(it.s);
+    it.at = 0;
+    measure(it);
+    return it;
   }
-  __device__ __forceinline__ Seq seq(int b) const {
-    Seq s;
-    if (b < 64) {
-      s.first = __builtin_amdgcn_readlane(first, b);
-      s.n = s.keys = __builtin_amdgcn_readlane(n, b);
-    } else {
-      s = Walk<false>::uniform(seq_of<false>(again(seq_args()), b));
-    }
-    return s;
+  static __device__ __forceinline__ void scalar(Item& it) {
+    it.at = uniform64(it.at);
+    it.col = __builtin_amdgcn_readfirstlane(it.col);
+    it.tile = __builtin_amdgcn_readfirstlane(it.tile);
+    it.tiles = __builtin_amdgcn_readfirstlane(it.tiles);
+    it.units = __builtin_amdgcn_readfirstlane(it.units);
   }
 };
 
@@ -321,10 +340,10 @@ struct Shares {
   int64_t total, near;  // near: how far a border moves to a tile's end; it never stays before a tile's first keys
   int workers;
   __device__ __forceinline__ Shares(int64_t total_, SeqArgs a) : total(total_) {
-    workers = (int)max((int64_t)1, min((int64_t)a->plan.workers, total / a->plan.min_units));
-    near = max(total / workers >> 4, (int64_t)kSeqFixed);
+    workers = (int)max((int64_t)1, min((int64_t)a->plan.workers, (int64_t)divide(total, a->plan.min_units)));
+    near = max((int64_t)divide(total, workers) >> 4, (int64_t)kSeqFixed);
   }
-  __device__ __forceinline__ int64_t border(int w) const { return total * w / workers; }
+  __device__ __forceinline__ int64_t border(int w) const { return divide(total * w, workers); }
   // where the border at unit x, inside `it`, is moved to
   __device__ __forceinline__ int64_t moved(int64_t x, const Item& it) const {
     if (x - it.at <= near) return it.at;
@@ -385,25 +404,37 @@ struct Rows {
       }
     }
   }
-  // Rows of pages. head: of page 0; ids: the page of each 16 rows (below 0: none), uniform; at: the first row's place in its page. A page
-  // that there is not, and copies past the last row, give zeros.
-  __device__ __forceinline__ void copy_pages(const unsigned char* head, int64_t page, const int* ids, int at, int shift, int left,
-                                             uint32_t lds, int w, int lane) const {
-    const int mask = (1 << shift) - 1;
-    if (left >= C::KB && shift >= C::LOG_KB && ids[0] >= 0) {
-      const unsigned char* from = uniform_ptr(head + ids[0] * page + (uint64_t)at * token);
+  // Rows of pages. head: of page 0; ids: the page of each 16 rows, uniform; none: which of them have no page; at: the first row's place in
+  // its page. Rows without a page and copies past the last row give zeros.
+  __device__ __forceinline__ void copy_pages(const unsigned char* head, int64_t page, const int* ids, uint32_t none, int at, int shift,
+                                             int left, uint32_t lds, int w, int lane) const {
+    if (left >= C::KB && !none) {
+      if (shift >= C::LOG_KB) {
+        const unsigned char* from = uniform_ptr(head + ids[0] * page + (uint64_t)at * token);
 #pragma unroll
-      for (int i = 0; i < N; ++i) dma16_at(from + (uint64_t)(i * STEP) * token, off[i % PERIOD], lds + i * W * 1024);
+        for (int i = 0; i < N; ++i) dma16_at(from + (uint64_t)(i * STEP) * token, off[i % PERIOD], lds + i * W * 1024);
+      } else {
+        const unsigned char* from[C::KB / 16];  // less the rows of the tile before them
+#pragma unroll
+        for (int j = 0; j < C::KB / 16; ++j)
+          from[j] = head + ids[j] * page + ((int64_t)((at + 16 * j) & ((1 << shift) - 1)) - 16 * j) * token;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const unsigned char* to = from[i * STEP / 16];
+          if (STEP == 32 && w >= 2) to = from[i * 2 + 1];
+          dma16_at(uniform_ptr(to + (uint64_t)(i * STEP) * token), off[i % PERIOD], lds + i * W * 1024);
+        }
+      }
       return;
     }
+    const int mask = (1 << shift) - 1;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int row = (i * W + w) * RPI, r0 = lane / LPR;
-      const int id = ids[row / 16];
       const uint32_t chunk = tile_chunk<C::RB>(row + r0, lane % LPR) * 16;
-      const bool none = id < 0 || row >= left;
-      const unsigned char* from = none ? (const unsigned char*)kZeroRow : head + id * page + (uint64_t)((at + row) & mask) * token;
-      dma16_at(uniform_ptr(from), (none ? 0 : min(r0, left - 1 - row) * token) + chunk, lds + i * W * 1024);
+      const bool zero = none >> (row / 16) & 1 || row >= left;
+      const unsigned char* from = zero ? (const unsigned char*)kZeroRow : head + ids[row / 16] * page + (uint64_t)((at + row) & mask) * token;
+      dma16_at(uniform_ptr(from), (zero ? 0 : min(r0, left - 1 - row) * token) + chunk, lds + i * W * 1024);
     }
   }
 };
@@ -418,55 +449,36 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   constexpr bool kWhole = !PAGED && W == 4;
-  const Levels levels(seq_args(), kWhole ? lane : 0);
-  // a tile of all, whole
-  auto ranked = [&](int64_t rank) {
-    const SeqArgs a = again(seq_args());
-    const Walk<PAGED> walk(a, C::LOG_KB, lane);
-    const int k = (int)(rank / walk.cols);
-    Item x;
-    x.col = (int)(rank - (int64_t)k * walk.cols);
-    levels.find(k, &x.b, &x.tile);
-    x.s = levels.seq(x.b);
-    x.tiles = walk.tiles(x.s);
-    const Line l = walk.line(x.s);
-    x.at = 0;
-    x.units = (int)(l.upto(x.tile + 1) - l.upto(x.tile));
-    walk.scalar(x);
-    return x;
-  };
+  const Walk<PAGED, C::LOG_KB> walk(seq_args(), lane);
   int64_t total, begin, end;
   Item it;
-  int me, round = -1;  // round: of tiles that are dealt out whole
-  {
+  int me = blockIdx.x, round = -1;  // round: of tiles that are dealt out whole
+  if (kWhole) {
+    total = (int64_t)walk.above(0) * walk.cols;
+    if (total >= (int64_t)kSeqRounds * seq_args()->plan.workers) round = 0;
+  }
+  if (me == 0 && tid == 0) *seq_args()->any_cut = round < 0;
+  if (round == 0) {
+    it = walk.ranked(me);
+    begin = -(int64_t(1) << 60);
+    end = int64_t(1) << 60;
+  } else {
     const SeqArgs a = seq_args();
-    const Walk<PAGED> walk(a, C::LOG_KB, lane);
-    if (kWhole) {
-      total = (int64_t)levels.above(0) * walk.cols;
-      if (total >= (int64_t)kSeqRounds * a->plan.workers) round = 0;
-    }
-    if (blockIdx.x == 0 && tid == 0) *a->any_cut = round < 0;
-    if (round == 0) {
-      it = ranked(blockIdx.x);
-      begin = -(int64_t(1) << 60);
-      end = int64_t(1) << 60;
-      me = blockIdx.x;
-    } else {
-    total = walk.uniform64(walk.total());
+    const auto sums = walk.sums(0);
+    total = walk.total(sums);
     if (total == 0) return;
     const Shares shares(total, a);
     // workgroups go round the eight XCDs: each XCD takes neighbouring shares where there are shares for all
-    me = shares.workers == a->plan.workers ? (blockIdx.x & 7) * (a->plan.workers >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+    if (shares.workers == a->plan.workers) me = (blockIdx.x & 7) * (a->plan.workers >> 3) + (blockIdx.x >> 3);
     if (me >= shares.workers) return;
     begin = shares.border(me), end = shares.border(me + 1);
-    if (end < total) end = shares.moved(end, walk.find(end));
-    it = walk.find(begin);
+    if (end < total) end = shares.moved(end, walk.find(end, sums));
+    it = walk.find(begin, sums);
     begin = shares.moved(begin, it);
     if (begin == it.at + it.units && begin < total) it = walk.next(it);
     if (begin >= end) return;
-    begin = walk.uniform64(begin);
-    end = walk.uniform64(end);
-    }
+    begin = uniform64(begin);
+    end = uniform64(end);
   }
   // of tiles dealt out whole: the next one's rank, where a worker's place in a round turns round from one to the next
   auto next_rank = [&] {
@@ -499,8 +511,14 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
 
   // Where the next copy comes from. Paged: 64 entries of the sequence's table, one a lane, and which of them name no page.
   const unsigned char *kfrom = nullptr, *vfrom = nullptr;
-  int from_b = -1, from_keys = 0, window = -1, entry = 0;
+  int from_b = -1, from_keys = 0, window = -1, entry = 0, entry_ahead = 0, ahead_b = -1, ahead_window = 0;
   uint64_t bad = 0;
+  // the entry of a sequence's table that this lane holds of the window of 64 around `key`
+  auto load_entry = [&](int b, int keys, int key) {
+    const SeqArgs a = again(seq_args());
+    const int e = (key >> a->page_shift & ~63) + lane, used = (int)(((int64_t)keys + (1 << a->page_shift) - 1) >> a->page_shift);
+    return e < used ? a->tables[b * a->table_stride + e] : 0;
+  };
   auto aim = [&](const Item& x, int key) {
     const SeqArgs a = again(seq_args());
     const int hk = a->plan.per_tile == 1 ? x.col / (a->heads / a->kv_heads) : x.col;
@@ -532,8 +550,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
       const int shift = a->page_shift, first = key >> shift;
       if (first >> 6 != window) {
         window = first >> 6;
-        const int e = window * 64 + lane, used = (int)(((int64_t)from_keys + (1 << shift) - 1) >> shift);
-        entry = e < used ? a->tables[from_b * a->table_stride + e] : 0;
+        entry = from_b == ahead_b && window == ahead_window ? entry_ahead : load_entry(from_b, from_keys, key);
         bad = __ballot((uint32_t)entry >= (uint32_t)a->n_pages);
       }
       uint32_t none = 0;
@@ -542,14 +559,11 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
       for (int j = 0; j < KB / 16; ++j) {
         const int e = (key + 16 * j) >> shift & 63;
         ids[j] = __builtin_amdgcn_readlane(entry, e);
-        if (bad >> e & 1) {
-          ids[j] = -1;
-          none |= 1u << j;
-        }
+        if (bad >> e & 1) none |= 1u << j;
       }
       const int at = key & ((1 << shift) - 1);
-      krows.copy_pages(kfrom, a->kp.page * 2, ids, at, shift, left, to, w, lane_o);
-      vrows.copy_pages(vfrom, a->vp.page * 2, ids, at, shift, left, to + C::BYTES, w, lane_o);
+      krows.copy_pages(kfrom, a->kp.page * 2, ids, none, at, shift, left, to, w, lane_o);
+      vrows.copy_pages(vfrom, a->vp.page * 2, ids, none, at, shift, left, to + C::BYTES, w, lane_o);
       return none;
     }
   };
@@ -677,15 +691,19 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     Range rn;
     bool known = false;  // nx
     auto look = [&] {
-      const Walk<PAGED> walk(again(seq_args()), C::LOG_KB, lane);
       if (round >= 0) {
-        nx = ranked(next_rank());
+        nx = walk.ranked(next_rank());
         ++round;
       } else {
         nx = walk.next(it);
       }
       rn = range(nx);
       known = true;
+      if (PAGED && nx.b != it.b) {  // its pages are asked for ahead of its first copy
+        ahead_b = nx.b;
+        ahead_window = rn.lo >> again(seq_args())->page_shift >> 6;
+        entry_ahead = load_entry(nx.b, nx.s.keys, rn.lo);
+      }
     };
     if (ready) {
 #pragma unroll
@@ -886,25 +904,25 @@ __global__ __launch_bounds__(256) void seq_join_few_kernel(const WaSeqLaunch a, 
   }
 }
 
-// Joins rows of many parts: a workgroup a row, D / 4 lanes a part.
+// Joins rows of many parts: a workgroup a row, D / 4 lanes a part, 16 parts at a time.
 template <bool HALF, int D, int W, bool PAGED>
-__global__ __launch_bounds__(1024) void seq_join_many_kernel(const WaSeqLaunch a) {
-  constexpr int L = D / 4, TEAMS = 1024 / L;
+__global__ __launch_bounds__(4 * D) void seq_join_many_kernel(const WaSeqLaunch a) {
+  constexpr int L = D / 4, TEAMS = 16, WAVES = TEAMS * L / 64;
   __shared__ float4 sums[TEAMS][L];
-  __shared__ float totals[TEAMS], tops[16];
+  __shared__ float totals[TEAMS], tops[WAVES];
   if (!*a.any_cut || !seq_row(a, blockIdx.x)) return;
   const int2 cut = a.cuts[blockIdx.x];
   if (cut.x == -1) return;
   const JoinRow<HALF, D, W, PAGED> row(a, blockIdx.x, cut);
   const int team = threadIdx.x / L, lane = threadIdx.x & (L - 1), c = 4 * lane;
-  float top = -INFINITY;  // of up to 1,024 parts, a thread one
-  if (row.begin + (int)threadIdx.x <= row.end) top = row.stat[row.at(row.begin + threadIdx.x)].x;
+  float top = -INFINITY;
+  for (int w = row.begin + threadIdx.x; w <= row.end; w += TEAMS * L) top = fmaxf(top, row.stat[row.at(w)].x);
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
   if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
   __syncthreads();
 #pragma unroll
-  for (int x = 0; x < 16; ++x) top = fmaxf(top, tops[x]);
+  for (int x = 0; x < WAVES; ++x) top = fmaxf(top, tops[x]);
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
@@ -923,6 +941,7 @@ __global__ __launch_bounds__(1024) void seq_join_many_kernel(const WaSeqLaunch a
   if (lane == 0) totals[team] = l;
   __syncthreads();
   if (team) return;
+#pragma unroll
   for (int x = 1; x < TEAMS; ++x) {  // in one order
     const float4 y = sums[x][lane];
     l += totals[x];
@@ -934,8 +953,9 @@ __global__ __launch_bounds__(1024) void seq_join_many_kernel(const WaSeqLaunch a
   row.finish(a, o, l, top, c);
 }
 
-// Rows up to which a workgroup joins one alone: tiles of so few rows may be cut in many parts. With more, in few.
-constexpr int64_t kSeqManyRows = 1024;
+// Parts from which on a workgroup joins a row alone (one token of 64 sequences, 5 parts: 61 us where a workgroup of 1,024 threads does
+// each, 5 us side by side; one of a long sequence, 256 parts: 6 us and 9).
+constexpr int64_t kSeqManyParts = 12;
 
 template <bool HALF, int D, int W, bool PAGED>
 hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
@@ -943,8 +963,10 @@ hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)a.tokens * a.heads;
-  if (rows <= kSeqManyRows) {
-    hipLaunchKernelGGL((seq_join_many_kernel<HALF, D, W, PAGED>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
+  // a tile's parts, if all workers share the tiles that there are at least
+  const int64_t tiles = std::max<int64_t>(std::min(a.batch, a.tokens), a.tokens >> a.plan.log_tokens) * (a.heads / a.plan.per_tile);
+  if (a.plan.workers / tiles >= kSeqManyParts && rows <= (1 << 16)) {
+    hipLaunchKernelGGL((seq_join_many_kernel<HALF, D, W, PAGED>), dim3((unsigned)rows), dim3(4 * D), 0, stream, a);
   } else {
     constexpr int PER = 256 / (D / 4);
     const int64_t wgs = std::min<int64_t>((rows + PER - 1) / PER, 2048);
