@@ -461,6 +461,14 @@ wa_status check_seq_shape(const wa_seq_shape* s, WaSeqLaunch* a) {
   return WA_OK;
 }
 
+// The forward calls run a workgroup a tile in a dimension of a launch.
+wa_status check_seq_forward(const wa_seq_shape* shape, WaSeqLaunch* a) {
+  const wa_status s = check_seq_shape(shape, a);
+  if (s != WA_OK) return s;
+  if (wa_seq_most_tiles(*a, wa_seq_plan(*a)) >= (int64_t(1) << 24))
+    return fail(WA_ERR_UNSUPPORTED, "%d tokens of %d sequences and %d heads exceed a launch", a->tokens, a->batch, a->heads);
+  return WA_OK;
+}
 // a row's log-sum-exp and, for the gradient, the rest of each column of O in a byte
 int seq_lse_step(const WaSeqLaunch& a) { return a.half ? 1 : 1 + a.head_dim / 4; }
 size_t seq_cut_bytes(const WaSeqLaunch& a) { return kAlign + align_up((size_t)a.tokens * a.heads * 8); }
@@ -1128,7 +1136,7 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
 
 wa_status wa_seq_attn_workspace_size(const wa_seq_shape* shape, size_t* bytes) {
   WaSeqLaunch a{};
-  wa_status s = check_seq_shape(shape, &a);
+  wa_status s = check_seq_forward(shape, &a);
   if (s != WA_OK) return s;
   if (!bytes) return fail(WA_ERR_INVALID_ARG, "bytes is null");
   *bytes = seq_ws_bytes(a);
@@ -1140,7 +1148,7 @@ wa_status wa_packed_attn(const wa_token_rows* q, const wa_token_rows* k, const w
                          void* workspace, size_t workspace_bytes, void* stream) {
   WaSeqLaunch a{};
   SeqSpan sq, sk, sv, so;
-  wa_status s = check_seq_shape(shape, &a);
+  wa_status s = check_seq_forward(shape, &a);
   if (s != WA_OK) return s;
   if ((s = check_seq_options(options, &a)) != WA_OK) return s;
   if (a.tokens == 0) return ok();
@@ -1219,11 +1227,12 @@ wa_status wa_paged_attn(const wa_token_rows* q, const wa_pages* k, const wa_page
                         void* workspace, size_t workspace_bytes, void* stream) {
   WaSeqLaunch a{};
   SeqSpan sq, sk, sv, so;
-  wa_status s = check_seq_shape(shape, &a);
+  wa_status s = check_seq_forward(shape, &a);
   if (s != WA_OK) return s;
   if ((s = check_seq_options(options, &a)) != WA_OK) return s;
   if (a.tokens == 0) return ok();
   if ((s = check_tables(tables, kv_lens, &a)) != WA_OK) return s;
+  a.paged = 1;
   if ((s = check_rows(q, "q", a.tokens, a.heads, a.head_dim, false, &a.q, &sq)) != WA_OK) return s;
   if ((s = check_pages(k, "k", a, false, &a.kp, &sk)) != WA_OK) return s;
   if ((s = check_pages(v, "v", a, false, &a.vp, &sv)) != WA_OK) return s;

@@ -23,15 +23,21 @@ WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
     p.per_tile = 1;
     p.log_tokens = log_tokens(1);
   }
-#ifndef NW1
-#define NW1 1024
-#endif
-#ifndef MU
-#define MU 4
-#endif
-  p.workers = p.waves == 4 ? 512 : NW1;
-  p.min_units = MU;
+  // Workgroups that the chip holds: two a compute unit of four wavefronts, four of one (a fifth does not fit beside the LDS of four: one
+  // token of 32 sequences 162 us with 1,024, 197 with 1,280).
+  p.workers = p.waves == 4 ? 512 : 1024;
+  p.min_units = 4;
+  // Few keys a tile take less time than a join (one wavefront: 100 sequences of up to 300 keys 23.5 -> 19.7 us, but 16 of 500 19.6 ->
+  // 24.6; four: 512 tokens of 32 heads 25.0 -> 18.0, 1,000 of 16 sequences 21.7 -> 14.4, of one 24.7 -> 27.4).
+  const int64_t keys = a.paged ? (int64_t)a.table_width << a.page_shift : a.tokens;
+  p.whole = p.waves == 4 || !a.paged ? keys <= 512 || (!a.paged && mean <= 128)
+                                     : keys <= 256 || (keys <= 512 && wa_seq_most_tiles(a, p) >= 256);
   return p;
+}
+
+// Sequences of n_b queries have sum ceil(n_b / p) tiles of p tokens.
+int64_t wa_seq_most_tiles(const WaSeqLaunch& a, const WaSeqPlan& p) {
+  return ((a.tokens >> p.log_tokens) + std::min(a.batch, a.tokens)) * (int64_t)(a.heads / p.per_tile);
 }
 
 size_t wa_seq_part_floats(const WaSeqPlan& p, int head_dim) { return (size_t)p.workers * 2 * 32 * p.waves * (head_dim + 2); }

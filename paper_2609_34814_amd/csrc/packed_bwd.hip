@@ -7,7 +7,8 @@
 // Long tiles are computed in parts, which packed_parts_kernel adds in order.
 // Both recompute the scores and dP. A wavefront holds 32 queries (keys) with their accumulators in registers, and the other side's
 // tiles pass through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
-// registers, so P and dS, rounded to bf16, are operands of the following products as they are. Two wavefronts share a SIMD.
+// registers, so P and dS, rounded to bf16, are operands of the following products as they are. Two wavefronts share a SIMD; the one that is
+// at scores and dP goes first (16,384 tokens, 32 heads over 8, d 128: 7.24 -> 6.65 ms).
 
 #include "seq_attn.h"
 
@@ -253,6 +254,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
     bf16x8 ring[kAhead];
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) ring[x] = row(x);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int x = 0; x < 2 * C::KS; ++x) {
       if (x < C::KS) sc = mfma(ring[x % kAhead], qf[x], sc); else dp = mfma(ring[x % kAhead], dof[x - C::KS], dp);
@@ -266,6 +268,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
         }
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     bf16x8 cring[kAhead];
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) cring[x] = col(x);
@@ -324,7 +327,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
   const int some = k0 >= s.n ? s.n : a.causal ? k0 : 0;                   // the wavefront's first
   const int all = a.causal ? min(k0 + 31, s.n - 1) : 0;                   // and its last
   const bool whole = k0 + 31 < s.n;
-  // this part's queries, in tiles of QB, through the heads one after another
+  // this part's queries, in tiles of QB from the last on, of each tile all heads: so key tiles of different numbers, which begin with
+  // different queries, meet the same ones at the same time, and the caches hold them
   const int lead = a.causal ? tile : 0, first = (lead + job.length * job.part / job.parts) * kRows;
   const int past = min((lead + job.length * (job.part + 1) / job.parts) * kRows, s.n);
 
@@ -391,6 +395,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
     bf16x8 ring[kAhead], vring[kAhead];
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) ring[x] = row(x);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int x = 0; x < 2 * C::KS; ++x) {
       if (x < C::KS)
@@ -410,6 +415,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
         }
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     bf16x8 cring[kAhead];
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) cring[x] = col(x);
@@ -433,18 +439,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
       if (x + kAhead < 4 * C::DT) cring[x % kAhead] = col(x + kAhead);
     }
   };
-  int g = 0, i = first, buf = 0;
-  copy(0, first, 0);
-  while (g < group) {
+  int g = 0, i = first + (past - first - 1) / QB * QB, buf = 0;
+  copy(0, i, 0);
+  while (i >= first) {
     const int i0 = i;
-    i += QB;
-    if (i >= past) {
-      i = first;
-      ++g;
+    if (++g == group) {
+      g = 0;
+      i -= QB;
     }
     WA_WAIT_VM(0);
     WA_BARRIER();
-    if (g < group) copy(g, i, buf ^ 1);
+    if (i >= first) copy(g, i, buf ^ 1);
     int end = QB;
     asm volatile("" : "+s"(end));
 #pragma unroll 1

@@ -13,12 +13,17 @@
 // precision, and after a row's first tiles it hardly ever happens. In fp16 they are held 2^7 times larger (up to 2^15), so that
 // those down to 2^-21 of the largest keep all their bits.
 //
-// Who computes what: the work is a line of units, one for each tile of keys of each query tile, sequence after sequence and within
-// one key head after key head. Worker w of G takes the units [w U / G, (w + 1) U / G), so all workers have the same to do whatever
-// the lengths are, and neighbours (on one XCD) read the same keys. The lengths are known on the device only: each workgroup sums them
-// itself, a sequence a lane, and finds its place in a sequence by a closed form, which costs no launch before this one. A border within
-// a sixteenth of a share of a tile's end is moved there. A tile that several workers compute is joined by a second kernel, in key order: nothing
-// is added with atomics, and equal calls give equal bits.
+// Who computes what. The lengths are known on the device only; each workgroup finds its work itself from the lengths, a sequence a lane,
+// which costs no launch before this one.
+//   Many tiles of packed sequences: a workgroup a tile, those with the most keys first, so that the chip stays full to the end, and
+//   those that run together read the same keys at about the same time (one prompt of 32,768 tokens, 32 heads over 8, d 128: 9.6 ms where
+//   equal shares of the work begin anywhere in a tile, 8.2 so).
+//   Few tiles, and those of a paged cache: the work is a line of units, one for each tile of keys of each query tile and two for its
+//   beginning and end, sequence after sequence and within one key head after key head. Worker w of G takes the units [w U / G, (w + 1) U / G),
+//   found by a closed form, so all workers have the same to do whatever the lengths are. A border within a sixteenth of a share of a tile's
+//   end is moved there. A tile that several workers compute is joined by a second kernel, in key order: nothing is added with
+//   atomics, and equal calls give equal bits.
+//   Calls of few keys: a workgroup a tile, without the second kernel.
 #pragma once
 
 #include "diff_tiles.h"
@@ -31,8 +36,8 @@ namespace wa {
 
 constexpr float kSeqGrow = 8.f;  // log2 units
 constexpr int kSeqAhead = 4;     // operands read ahead
-// From so many tiles a worker on, tiles are dealt out whole.
-constexpr int kSeqRounds = 2;
+// Packed tiles are dealt out whole where there are so many times the workers of them.
+constexpr int kSeqWhole = 2;
 // What a tile costs beside its keys, in tiles of keys.
 constexpr int kSeqFixed = 2;
 
@@ -360,11 +365,22 @@ struct Shares {
 // Zero rows, in the place of keys behind the last and of pages that the pool does not have.
 static __device__ const uint4 kZeroRow[16] = {};
 
-// One 16-byte-a-lane copy as dma16, for kernels in which nothing else uses M0 (the compiler writes it just before a use).
+// One 16-byte-a-lane copy as dma16, for kernels in which nothing else uses M0 (the compiler writes it just before a use). The copy may
+// read M0 one state after it is written, and an address five after the vector unit wrote it (a page's, read from a lane): the
+// compiler does not look inside for that.
 __device__ __forceinline__ void dma16_at(const void* base, uint32_t voff, uint32_t lds) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(lds), "v"(voff), "s"(base)
+      : "memory");
+}
+__device__ __forceinline__ void dma16_late(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 3\n\t"
       "global_load_lds_dwordx4 %1, %2"
       :
       : "s"(lds), "v"(voff), "s"(base)
@@ -412,7 +428,7 @@ struct Rows {
       if (shift >= C::LOG_KB) {
         const unsigned char* from = uniform_ptr(head + ids[0] * page + (uint64_t)at * token);
 #pragma unroll
-        for (int i = 0; i < N; ++i) dma16_at(from + (uint64_t)(i * STEP) * token, off[i % PERIOD], lds + i * W * 1024);
+        for (int i = 0; i < N; ++i) dma16_late(from + (uint64_t)(i * STEP) * token, off[i % PERIOD], lds + i * W * 1024);
       } else {
         const unsigned char* from[C::KB / 16];  // less the rows of the tile before them
 #pragma unroll
@@ -422,7 +438,7 @@ struct Rows {
         for (int i = 0; i < N; ++i) {
           const unsigned char* to = from[i * STEP / 16];
           if (STEP == 32 && w >= 2) to = from[i * 2 + 1];
-          dma16_at(uniform_ptr(to + (uint64_t)(i * STEP) * token), off[i % PERIOD], lds + i * W * 1024);
+          dma16_late(uniform_ptr(to + (uint64_t)(i * STEP) * token), off[i % PERIOD], lds + i * W * 1024);
         }
       }
       return;
@@ -434,7 +450,7 @@ struct Rows {
       const uint32_t chunk = tile_chunk<C::RB>(row + r0, lane % LPR) * 16;
       const bool zero = none >> (row / 16) & 1 || row >= left;
       const unsigned char* from = zero ? (const unsigned char*)kZeroRow : head + ids[row / 16] * page + (uint64_t)((at + row) & mask) * token;
-      dma16_at(uniform_ptr(from), (zero ? 0 : min(r0, left - 1 - row) * token) + chunk, lds + i * W * 1024);
+      dma16_late(uniform_ptr(from), (zero ? 0 : min(r0, left - 1 - row) * token) + chunk, lds + i * W * 1024);
     }
   }
 };
@@ -448,20 +464,21 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  constexpr bool kWhole = !PAGED && W == 4;
   const Walk<PAGED, C::LOG_KB> walk(seq_args(), lane);
   int64_t total, begin, end;
   Item it;
-  int me = blockIdx.x, round = -1;  // round: of tiles that are dealt out whole
-  if (kWhole) {
+  int me = blockIdx.x;
+  bool whole = seq_args()->plan.whole;
+  if (whole || !PAGED) {
     total = (int64_t)walk.above(0) * walk.cols;
-    if (total >= (int64_t)kSeqRounds * seq_args()->plan.workers) round = 0;
+    whole |= total >= (int64_t)kSeqWhole * seq_args()->plan.workers;
   }
-  if (me == 0 && tid == 0) *seq_args()->any_cut = round < 0;
-  if (round == 0) {
+  if (me == 0 && tid == 0) *seq_args()->any_cut = !whole;
+  if (whole) {
+    if (me >= total) return;
     it = walk.ranked(me);
-    begin = -(int64_t(1) << 60);
-    end = int64_t(1) << 60;
+    begin = 0;
+    end = it.units;
   } else {
     const SeqArgs a = seq_args();
     const auto sums = walk.sums(0);
@@ -470,7 +487,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     const Shares shares(total, a);
     // workgroups go round the eight XCDs: each XCD takes neighbouring shares where there are shares for all
     if (shares.workers == a->plan.workers) me = (blockIdx.x & 7) * (a->plan.workers >> 3) + (blockIdx.x >> 3);
-    if (me >= shares.workers) return;
+    if (blockIdx.x >= a->plan.workers || me >= shares.workers) return;
     begin = shares.border(me), end = shares.border(me + 1);
     if (end < total) end = shares.moved(end, walk.find(end, sums));
     it = walk.find(begin, sums);
@@ -480,13 +497,6 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     begin = uniform64(begin);
     end = uniform64(end);
   }
-  // of tiles dealt out whole: the next one's rank, where a worker's place in a round turns round from one to the next
-  auto next_rank = [&] {
-    const int workers = again(seq_args())->plan.workers, r = round + 1;
-    const int place = blockIdx.x >> 3, p = r & 1 ? (workers >> 3) - 1 - place : place;
-    return (int64_t)r * workers + p * 8 + (blockIdx.x & 7);
-  };
-
   const uint32_t kbase = row_operand<C::RB>(lane, 0);
   const uint32_t vbase0 = C::BYTES + col_operand<C::RB>(lane, 0, 0), vbase1 = C::BYTES + col_operand<C::RB>(lane, 0, 1);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds) + w * 1024;
@@ -686,17 +696,12 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
   bool ready = false, stored = false;  // the item's first tile is on its way; stores of the item before come behind it
   Range r = range(it);
   for (;;) {
-    const bool more = round >= 0 ? next_rank() < total : it.at + it.units < end;
+    const bool more = it.at + it.units < end;
     Item nx;
     Range rn;
     bool known = false;  // nx
     auto look = [&] {
-      if (round >= 0) {
-        nx = walk.ranked(next_rank());
-        ++round;
-      } else {
-        nx = walk.next(it);
-      }
+      nx = walk.next(it);
       rn = range(nx);
       known = true;
       if (PAGED && nx.b != it.b) {  // its pages are asked for ahead of its first copy
@@ -788,7 +793,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
               *(uint32_t*)(stat + 1 + dt * 8 + v / 2 + hf) = rest4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3], o16);
           }
         if (stat && hf == 0) *stat = l == 0.f ? -INFINITY : (ref + __log2f(l)) * kLn2;
-        if (round < 0 && hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(-1, 0);
+        if (!whole && hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(-1, 0);
       } else {
         // slot 0: a part that begins inside its tile; slot 1: one that begins with it
         const int64_t at = ((int64_t)me * 2 + (starts ? 1 : 0)) * R + row;
@@ -959,9 +964,12 @@ constexpr int64_t kSeqManyParts = 12;
 
 template <bool HALF, int D, int W, bool PAGED>
 hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
-  hipLaunchKernelGGL((seq_attn_kernel<HALF, D, W, PAGED>), dim3(a.plan.workers), dim3(64 * W), 0, stream, a);
+  const int64_t most = wa_seq_most_tiles(a, a.plan);
+  const bool whole = a.plan.whole || (!PAGED && most >= (int64_t)kSeqWhole * a.plan.workers);
+  const int64_t grid = a.plan.whole ? most : whole ? std::max<int64_t>(most, a.plan.workers) : a.plan.workers;
+  hipLaunchKernelGGL((seq_attn_kernel<HALF, D, W, PAGED>), dim3((unsigned)grid), dim3(64 * W), 0, stream, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.plan.whole) return e;
   const int64_t rows = (int64_t)a.tokens * a.heads;
   // a tile's parts, if all workers share the tiles that there are at least
   const int64_t tiles = std::max<int64_t>(std::min(a.batch, a.tokens), a.tokens >> a.plan.log_tokens) * (a.heads / a.plan.per_tile);

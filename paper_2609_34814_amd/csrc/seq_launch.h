@@ -22,6 +22,7 @@ struct WaSeqPlan {
   int32_t log_tokens; // log2 of the tokens of a tile
   int32_t workers;    // workgroups, a multiple of 8
   int32_t min_units;  // tiles of keys that a worker gets at least
+  int32_t whole;      // 1: no tile is cut
 };
 struct WaSeqLaunch {
   WaSeqRows q, k, v, o;    // k, v: of packed sequences
@@ -48,6 +49,7 @@ struct WaSeqLaunch {
 };
 
 WaSeqPlan wa_seq_plan(const WaSeqLaunch& a);  // of its shape
+int64_t wa_seq_most_tiles(const WaSeqLaunch& a, const WaSeqPlan& p);  // of all sequences and heads, at most
 size_t wa_seq_part_floats(const WaSeqPlan& p, int head_dim);
 
 hipError_t wa_launch_packed_attn(const WaSeqLaunch& a, hipStream_t stream);

@@ -33,6 +33,7 @@ def test_shape_refusals(kw, code):
         assert call(None, ctypes.byref(n)) == INVALID and call(_shape(), None) == INVALID
     assert lib.wa_packed_attn_backward_workspace_size(_shape(dtype=L.WA_F16), ctypes.byref(n)) == UNSUP
     assert lib.wa_packed_attn_backward_workspace_size(_shape(tokens=1 << 25, heads=64, kv_heads=64), ctypes.byref(n)) == UNSUP
+    assert lib.wa_seq_attn_workspace_size(_shape(batch=1 << 25, tokens=1 << 25, heads=32, kv_heads=32), ctypes.byref(n)) == UNSUP
     assert lib.wa_seq_attn_workspace_size(_shape(tokens=0), ctypes.byref(n)) == 0 and n.value == 0
 
 
