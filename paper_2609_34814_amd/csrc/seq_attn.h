@@ -912,49 +912,62 @@ __global__ __launch_bounds__(256) void seq_join_few_kernel(const WaSeqLaunch a, 
 // Joins rows of many parts: a workgroup a row, D / 4 lanes a part, 16 parts at a time.
 template <bool HALF, int D, int W, bool PAGED>
 __global__ __launch_bounds__(4 * D) void seq_join_many_kernel(const WaSeqLaunch a) {
-  constexpr int L = D / 4, TEAMS = 16, WAVES = TEAMS * L / 64;
+  constexpr int L = D / 4, TEAMS = 16, AHEAD = 8;
   __shared__ float4 sums[TEAMS][L];
-  __shared__ float totals[TEAMS], tops[WAVES];
-  if (!*a.any_cut || !seq_row(a, blockIdx.x)) return;
+  __shared__ float2 stats[TEAMS];
+  const int any = *a.any_cut;
   const int2 cut = a.cuts[blockIdx.x];
-  if (cut.x == -1) return;
+  if (!any || !seq_row(a, blockIdx.x) || cut.x == -1) return;
   const JoinRow<HALF, D, W, PAGED> row(a, blockIdx.x, cut);
   const int team = threadIdx.x / L, lane = threadIdx.x & (L - 1), c = 4 * lane;
-  float top = -INFINITY;
-  for (int w = row.begin + threadIdx.x; w <= row.end; w += TEAMS * L) top = fmaxf(top, row.stat[row.at(w)].x);
-#pragma unroll
-  for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int x = 0; x < WAVES; ++x) top = fmaxf(top, tops[x]);
-  float l = 0.f;
+  float top = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int w = row.begin + team; w <= row.end; w += TEAMS) {
-    const int64_t at = row.at(w);
-    const float2 s = row.stat[at];
-    const float4 x = *(const float4*)(a.part + at * D + c);
-    const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
+  auto add = [&](float high, const float2& s, const float4& x) {  // both taken against `high`
+    const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - high);
     l += f * s.y;
     o.x += f * x.x;
     o.y += f * x.y;
     o.z += f * x.z;
     o.w += f * x.w;
+  };
+  auto raise = [&](float high) {
+    const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - high);
+    l *= keep;
+    o.x *= keep;
+    o.y *= keep;
+    o.z *= keep;
+    o.w *= keep;
+    top = high;
+  };
+  for (int w = row.begin + team; w <= row.end; w += AHEAD * TEAMS) {
+    float2 s[AHEAD];
+    float4 x[AHEAD];
+    float high = top;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {  // past the last part the last again, without weight
+      const int64_t at = row.at(min(w + i * TEAMS, row.end));
+      s[i] = row.stat[at];
+      x[i] = *(const float4*)(a.part + at * D + c);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (w + i * TEAMS > row.end) s[i] = make_float2(-INFINITY, 0.f);
+      high = fmaxf(high, s[i].x);
+    }
+    raise(high);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) add(high, s[i], x[i]);
   }
   sums[team][lane] = o;
-  if (lane == 0) totals[team] = l;
+  if (lane == 0) stats[team] = make_float2(top, l);
   __syncthreads();
   if (team) return;
+  float high = top;
 #pragma unroll
-  for (int x = 1; x < TEAMS; ++x) {  // in one order
-    const float4 y = sums[x][lane];
-    l += totals[x];
-    o.x += y.x;
-    o.y += y.y;
-    o.z += y.z;
-    o.w += y.w;
-  }
+  for (int x = 1; x < TEAMS; ++x) high = fmaxf(high, stats[x].x);
+  raise(high);
+#pragma unroll
+  for (int x = 1; x < TEAMS; ++x) add(high, stats[x], sums[x][lane]);  // in one order
   row.finish(a, o, l, top, c);
 }
 
