@@ -18,7 +18,8 @@ namespace {
 
 using namespace wa;
 
-constexpr int kRows = 128, kWaves = 4, kAhead = 2, kSlots = 512;
+constexpr int kRows = 128, kWaves = 4, kAhead = 2;
+constexpr uint32_t kSlots = 512;
 
 // Neighbouring units, which may share keys, on one XCD where eight divides their number.
 __device__ __forceinline__ int spread(int u, int units) { return units % 8 ? u : u % 8 * (units / 8) + u / 8; }
@@ -66,10 +67,8 @@ struct Jobs {
       const int64_t t = tiles_at(base);
       sum += causal ? t * (t + 1) / 2 : t * t;
     }
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-    sum = uniform64(sum) * cols;
-    most = (int)((sum + kSlots - 1) / kSlots);
+    sum = lane64(lane_prefix_sum64(sum, lane), 63) * cols;
+    most = (int)((uint64_t)(sum + kSlots - 1) / kSlots);
   }
   __device__ __forceinline__ int tiles_of(int b) const {
     return b < batch ? (int)(((int64_t)seq_of<false>(again(a), b).n + kRows - 1) / kRows) : 0;
@@ -96,9 +95,7 @@ struct Jobs {
   __device__ __forceinline__ bool find(int64_t rank, bool in_parts, Job* job) const {
     int lo = 0, hi = 0, passed = 0;  // above(lo) > row of jobs >= above(hi) = passed
     for (int base = 0; base < batch; base += 64) hi = max(hi, tiles_at(base));
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) hi = max(hi, __shfl_xor(hi, x));
-    hi = __builtin_amdgcn_readfirstlane(hi);
+    hi = lane_max(hi);
     const int row = (int)(rank / cols);
     if (row >= above(0, in_parts)) return false;
     while (hi - lo > 1) {
@@ -489,7 +486,7 @@ __global__ __launch_bounds__(256) void packed_parts_kernel(const WaSeqLaunch a, 
     if (tile * kRows + r >= s.n) break;
     const float* at = from + (int64_t)r * width + c;
     float4 sum = *(const float4*)at;
-#pragma unroll 4
+#pragma unroll 8
     for (int y = 1; y < job.parts; ++y) {
       const float4 z = *(const float4*)(at + y * step);
       sum.x += z.x;

@@ -148,6 +148,16 @@ __device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
 }
 // Sums over the lanes, the same in all of them, and up to each lane; numbers of 64 bits that are small take the short way.
 __device__ __forceinline__ int lane_sum(int x) { return __builtin_amdgcn_readlane(lane_prefix_sum(x), 63); }
+// The largest of numbers that are not negative.
+__device__ __forceinline__ int lane_max(int x) {
+  x = max(x, dpp32<0x111, 0xf>(0, x));  // as lane_prefix_sum
+  x = max(x, dpp32<0x112, 0xf>(0, x));
+  x = max(x, dpp32<0x114, 0xf>(0, x));
+  x = max(x, dpp32<0x118, 0xf>(0, x));
+  x = max(x, dpp32<0x142, 0xa>(0, x));
+  x = max(x, dpp32<0x143, 0xc>(0, x));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ int64_t lane_prefix_sum64(int64_t x, int lane) {
   if (__ballot((uint64_t)x >> 25 != 0) == 0) return lane_prefix_sum((int)x);
 #pragma unroll
@@ -282,9 +292,7 @@ struct Walk {
     it.col = (int)(rank - (int64_t)row * cols);
     int most = 0;
     for (int base = 0; base < batch; base += 64) most = max(most, tiles(seq_at(base)));
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) most = max(most, __shfl_xor(most, x));
-    int lo = 0, hi = __builtin_amdgcn_readfirstlane(most), passed = 0;  // above(lo) > row >= above(hi) = passed
+    int lo = 0, hi = lane_max(most), passed = 0;  // above(lo) > row >= above(hi) = passed
     while (hi - lo > 1) {
       const int mid = lo + ((hi - lo) >> 1), m = above(mid);
       if (m > row) {
