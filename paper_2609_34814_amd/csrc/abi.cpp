@@ -478,13 +478,14 @@ size_t seq_ws_bytes(const WaSeqLaunch& a) {
 // bf16, and a workgroup a tile of 128 queries and head in a dimension of a launch
 wa_status check_seq_backward(const WaSeqLaunch& a) {
   if (a.half) return fail(WA_ERR_UNSUPPORTED, "the gradient is bf16 only");
-  if (wa_packed_backward_tiles(a) * a.heads >= (int64_t(1) << 24) - 1024)
+  if (wa_packed_backward_tiles(a) * ((int64_t)a.heads + a.kv_heads) >= (int64_t(1) << 24) - 2048 ||
+      ((int64_t)a.tokens + 15) / 16 * a.heads >= (int64_t(1) << 25))
     return fail(WA_ERR_UNSUPPORTED, "%d tokens of %d sequences and %d heads exceed a launch", a.tokens, a.batch, a.heads);
   return WA_OK;
 }
 size_t seq_rows_bytes(const WaSeqLaunch& a) { return align_up((size_t)2 * a.heads * a.tokens * 4); }
 size_t seq_backward_bytes(const WaSeqLaunch& a) {
-  return a.tokens == 0 ? 0 : seq_rows_bytes(a) + align_up((size_t)wa_packed_backward_part_floats(a) * 4);
+  return a.tokens == 0 ? 0 : align_up(wa_packed_backward_cut_bytes()) + seq_rows_bytes(a) + align_up((size_t)wa_packed_backward_part_floats(a) * 4);
 }
 
 wa_status check_seq_options(const wa_seq_options* o, WaSeqLaunch* a) {
@@ -1214,8 +1215,9 @@ wa_status wa_packed_attn_backward(const wa_token_rows* dout, const wa_token_rows
   a.lse_in = stats;
   a.lse_step = seq_lse_step(a);
   a.dq_part = wa_packed_backward_dq_floats(a);
-  a.rows = (float*)workspace;
-  a.part = (float*)((char*)workspace + seq_rows_bytes(a));
+  a.cut_tiles = workspace;
+  a.rows = (float*)((char*)workspace + align_up(wa_packed_backward_cut_bytes()));
+  a.part = (float*)((char*)a.rows + seq_rows_bytes(a));
   const hipError_t e = wa_launch_packed_backward(a, (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "packed attention gradient launch");
   return ok();

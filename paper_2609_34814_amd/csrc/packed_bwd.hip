@@ -1,10 +1,13 @@
 // Gradient of attention over packed sequences for gfx950 (MI355X). With P recomputed from the forward's log-sum-exps,
 //   dP = dO V^T,   D = dO . O,   dS = P (dP - D),   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO.
 //
-// Two kernels, each owning what it writes, so nothing is added with atomics and equal calls give equal bits:
-//   packed_dq_kernel: 128 queries of a head, over their keys; also writes what the other kernel's products of a query start from.
-//   packed_dkv_kernel: 128 keys, over the queries of all heads that share them.
-// Long tiles are computed in parts, which packed_parts_kernel adds in order.
+// Three kernels. packed_rows_kernel: what the products of a query start from, its log-sum-exp and D. packed_grad_kernel: jobs of two kinds,
+// each owning what it writes, so nothing is added with atomics and equal calls give equal bits:
+//   keys     128 keys, over the queries of all heads that share them: dK and dV.
+//   queries  128 queries of a head, over their keys: dQ.
+// They run in one launch, those of keys first, which take longer, so that the others fill the chip while the last of them end (8,192 tokens of 8
+// documents, 16 heads over 4, d 128: 163 + 121 us one after another). Long tiles are computed in parts, which packed_parts_kernel adds
+// in order.
 // Both recompute the scores and dP. A wavefront holds 32 queries (keys) with their accumulators in registers, and the other side's
 // tiles pass through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are. Two wavefronts share a SIMD; the one that is
@@ -19,7 +22,7 @@ namespace {
 using namespace wa;
 
 constexpr int kRows = 128, kWaves = 4, kAhead = 2;
-constexpr uint32_t kSlots = 512;
+constexpr uint32_t kSlots = 512, kMostParts = 2 * kSlots;
 
 // Neighbouring units, which may share keys, on one XCD where eight divides their number.
 __device__ __forceinline__ int spread(int u, int units) { return units % 8 ? u : u % 8 * (units / 8) + u / 8; }
@@ -47,20 +50,23 @@ __device__ __forceinline__ Seq one_seq(int b) {
 // A tile of 128 rows, or the part of one, that a workgroup computes. Its length is the tiles of the other side that it meets.
 struct Job {
   int b, tile, col;        // sequence, tile of it, head or key head
-  int length, part, parts;
-  int first;               // the first part's number among all jobs; they are `cols` apart
+  int length, part, parts;  // the numbers of a tile's parts among all jobs are `cols` apart
+  int number;               // the tile's, among all: those in parts come first
 };
 
-// All tiles of all sequences and `cols` heads, longest first, those longer than `most` in parts of about equal length: `most` is a
-// 512th of all there is, so that a call of few tiles fills the chip's workgroups (two a compute unit) once, and one of many is not cut.
+// All tiles of all sequences and `cols` heads, longest first, those longer than `most` in parts of about equal length: `most` takes as
+// long as a 512th of all work, so that a call of few tiles fills the chip's workgroups (two a compute unit) once, and one of many is not cut.
+// A pair of a key and a query takes four products for dK and dV and three for dQ.
 // Causal tiles have the lengths 1 to T of a sequence of T tiles, others T. Each workgroup finds its job itself: the lengths are on the
 // device. The first 64 sequences are held, one a lane.
 struct Jobs {
   SeqArgs a;
   int lane, cols, batch, mine, most;
-  bool causal;
+  bool causal, queries;
 
-  __device__ __forceinline__ Jobs(int lane_, int cols_) : a(seq_args()), lane(lane_), cols(cols_), batch(a->batch), causal(a->causal) {
+  // share: of the kind of jobs in all work, in sevenths
+  __device__ __forceinline__ Jobs(int lane_, int cols_, int share, bool queries_)
+      : a(seq_args()), lane(lane_), cols(cols_), batch(a->batch), causal(a->causal), queries(queries_) {
     mine = tiles_of(lane);
     int64_t sum = 0;
     for (int base = 0; base < batch; base += 64) {
@@ -68,38 +74,45 @@ struct Jobs {
       sum += causal ? t * (t + 1) / 2 : t * t;
     }
     sum = lane64(lane_prefix_sum64(sum, lane), 63) * cols;
-    most = (int)((uint64_t)(sum + kSlots - 1) / kSlots);
+    most = (int)((uint64_t)(7 * sum + share * kSlots - 1) / (share * kSlots));
   }
   __device__ __forceinline__ int tiles_of(int b) const {
     return b < batch ? (int)(((int64_t)seq_of<false>(again(a), b).n + kRows - 1) / kRows) : 0;
   }
   __device__ __forceinline__ int tiles_at(int base) const { return base == 0 ? mine : tiles_of(base + lane); }
   __device__ __forceinline__ int parts_of(int length) const { return (length + most - 1) / most; }
-  // jobs (or, not counting parts, tiles) of the first x lengths of a sequence
-  __device__ __forceinline__ int upto(int x, bool in_parts) const {
-    if (!in_parts) return x;
+  // jobs of the first x lengths of a sequence
+  __device__ __forceinline__ int upto(int x) const {
     const int q = x / most, r = x - q * most;
     return q * (q + 1) / 2 * most + r * (q + 1);
   }
   // those of tiles longer than `length`, of one column
-  __device__ __forceinline__ int above(int length, bool in_parts) const {
+  __device__ __forceinline__ int above(int length) const {
     int sum = 0;
     for (int base = 0; base < batch; base += 64) {
       const int t = tiles_at(base);
-      const int n = t <= length ? 0 : causal ? upto(t, in_parts) - upto(length, in_parts) : t * (in_parts ? parts_of(t) : 1);
-      sum += lane_sum(n);
+      sum += lane_sum(t <= length ? 0 : causal ? upto(t) - upto(length) : t * parts_of(t));
     }
     return sum;
   }
-  // job (or tile) number `rank`; false if there is none
-  __device__ __forceinline__ bool find(int64_t rank, bool in_parts, Job* job) const {
+  // tiles longer than `length`, of one column
+  __device__ __forceinline__ int longer(int length) const {
+    int sum = 0;
+    for (int base = 0; base < batch; base += 64) {
+      const int t = tiles_at(base);
+      sum += lane_sum(t <= length ? 0 : causal ? t - length : t);
+    }
+    return sum;
+  }
+  // job number `rank`; false if there is none
+  __device__ __forceinline__ bool find(int64_t rank, Job* job) const {
     int lo = 0, hi = 0, passed = 0;  // above(lo) > row of jobs >= above(hi) = passed
     for (int base = 0; base < batch; base += 64) hi = max(hi, tiles_at(base));
     hi = lane_max(hi);
     const int row = (int)(rank / cols);
-    if (row >= above(0, in_parts)) return false;
+    if (row >= above(0)) return false;
     while (hi - lo > 1) {
-      const int mid = lo + ((hi - lo) >> 1), n = above(mid, in_parts);
+      const int mid = lo + ((hi - lo) >> 1), n = above(mid);
       if (n > row) {
         lo = mid;
       } else {
@@ -109,11 +122,10 @@ struct Jobs {
     }
     job->length = hi;
     job->parts = parts_of(hi);
-    const int per = in_parts ? job->parts : 1;
-    int k = (row - passed) / per;
-    job->part = row - passed - k * per;
+    int k = (row - passed) / job->parts;
+    job->part = row - passed - k * job->parts;
+    job->number = (longer(hi) + k) * cols + (int)(rank - (int64_t)row * cols);
     job->col = spread((int)(rank - (int64_t)row * cols), cols);
-    job->first = 0;
     // the k-th tile of this length
     int who = 0, tile = 0, t = 0;
     for (int base = 0; base < batch; base += 64) {
@@ -130,18 +142,31 @@ struct Jobs {
       k -= __builtin_amdgcn_readlane(sum, 63);
     }
     job->b = __builtin_amdgcn_readfirstlane(who);
-    job->tile = __builtin_amdgcn_readfirstlane(tile);  // causal: 0
+    job->tile = __builtin_amdgcn_readfirstlane(tile);
     t = __builtin_amdgcn_readfirstlane(t);
-    if (causal) job->tile = t - hi;  // counted from the sequence's longest
+    if (causal) job->tile = queries ? hi - 1 : t - hi;  // the last queries meet the most keys, the first keys the most queries
     return true;
   }
-  // number of the first part of tile number `rank` among all jobs
-  __device__ __forceinline__ int64_t first_part(int64_t rank, const Job& job) const {
-    const int row = (int)(rank / cols);
-    const int same = row - above(job.length, false);  // tiles of this length before it
-    return ((int64_t)above(job.length, true) + (int64_t)same * job.parts) * cols + (rank - (int64_t)row * cols);
-  }
 };
+
+// What packed_parts_kernel has to know of the jobs of a kind: how many tiles are in parts (each has two at least, of kMostParts), and of each its
+// sequence, its number there, the number of its first part among the jobs, and its parts.
+struct Cuts {
+  int32_t tiles, unused[3];
+  int4 tile[kMostParts / 2];
+};
+// The job of a workgroup; false if there is none.
+__device__ __forceinline__ bool take_job(const WaSeqLaunch& a, bool queries, int64_t rank, int cols, int share, Job* job) {
+  const Jobs jobs(threadIdx.x & 63, cols, share, queries);
+  Cuts* cuts = (Cuts*)a.cut_tiles + (queries ? 0 : 1);
+  if (rank == 0) {
+    const int n = jobs.longer(jobs.most) * cols;
+    if (threadIdx.x == 0) cuts->tiles = n;
+  }
+  if (!jobs.find(rank, job)) return false;
+  if (job->parts > 1 && job->part == 0 && threadIdx.x == 0) cuts->tile[job->number] = make_int4(job->b, job->tile, (int)rank, job->parts);
+  return true;
+}
 
 // Rows [row, row + ROWS) of g (`token` bytes apart) into a tile; rows past `last` are that row again.
 template <int RB, int ROWS>
@@ -158,7 +183,7 @@ __device__ __forceinline__ void copy_rows(const unsigned char* tile, const unsig
 }
 
 // dO . O of 8 columns, O with what its rounding left (dO . O of the rounded O alone gave dQ and dK an error of 0.0026 of their size where
-// this gives 0.0023 and rounding them alone 0.0017)
+// this gives 0.0024 and rounding them alone 0.0017)
 __device__ __forceinline__ float dot8(bf16x8 a, bf16x8 o, uint32_t rest0, uint32_t rest1, float sum) {
   typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
   const u16x8 bits = __builtin_bit_cast(u16x8, o);
@@ -167,18 +192,53 @@ __device__ __forceinline__ float dot8(bf16x8 a, bf16x8 o, uint32_t rest0, uint32
   return sum;
 }
 
+// rows[0]: scores from the log-sum-exp, so that P = exp2(c2 s); rows[1]: dP from -D. A wavefront 16 tokens of a head, D / 8 lanes a token.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLaunch a) {
+__global__ __launch_bounds__(256) void packed_rows_kernel(const WaSeqLaunch a) {
+  constexpr int L = D / 8, STEP = 64 / L;
+  const int lane = threadIdx.x & 63, c = (lane & (L - 1)) * 8;
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int h = (int)(id % a.heads), first = (int)(id / a.heads) * 16;
+  const int begin = min(max(a.starts[0], 0), a.tokens), end = min(max(a.starts[a.batch], 0), a.tokens);
+  const float c2 = a.scale * kLog2e;
+  bf16x8 dof[16 / STEP], of[16 / STEP];
+  float lse[16 / STEP];
+  uint32_t rest[16 / STEP][2];
+#pragma unroll
+  for (int i = 0; i < 16 / STEP; ++i) {
+    const int64_t tok = first + i * STEP + lane / L;
+    const bool valid = tok >= begin && tok < end;
+    dof[i] = load8((const uint16_t*)a.dout.at + tok * a.dout.token + h * a.dout.head + c, valid);
+    of[i] = load8((const uint16_t*)a.o.at + tok * a.o.token + h * a.o.head + c, valid);
+    const float* stat = a.lse_in + ((int64_t)h * a.tokens + tok) * a.lse_step;
+    lse[i] = valid ? stat[0] : 0.f;
+    rest[i][0] = valid ? *(const uint32_t*)(stat + 1 + c / 4) : 0;
+    rest[i][1] = valid ? *(const uint32_t*)(stat + 2 + c / 4) : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < 16 / STEP; ++i) {
+    const int64_t tok = first + i * STEP + lane / L;
+    float d = dot8(dof[i], of[i], rest[i][0], rest[i][1], 0.f);
+#pragma unroll
+    for (int x = L / 2; x > 0; x >>= 1) d += __shfl_xor(d, x);
+    if (c == 0 && tok >= begin && tok < end) {
+      float* to = a.rows + (int64_t)h * a.tokens + tok;
+      to[0] = -lse[i] * kLog2e / c2;
+      to[(int64_t)a.heads * a.tokens] = -d;
+    }
+  }
+}
+
+// Job `rank` of queries. lds: 2 tiles of KB keys and values.
+template <int D>
+__device__ __forceinline__ void query_job(const WaSeqLaunch& a, int64_t rank, unsigned char* lds) {
   using C = Bwd<D>;
   constexpr int KB = C::KB, BYTES = KB * C::RB, STAGE = 2 * BYTES;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
-
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   Job job;
-  if (!Jobs(lane, a.heads).find(blockIdx.x, true, &job)) return;
-  // causal: a tile's length is its number and one, and the longest is the last
-  const int b = job.b, tile = a.causal ? job.length - 1 : job.tile, h = job.col, hk = h / (a.heads / a.kv_heads);
+  if (!take_job(a, true, rank, a.heads, 3, &job)) return;
+  const int b = job.b, tile = job.tile, h = job.col, hk = h / (a.heads / a.kv_heads);
   const Seq s = one_seq(b);
   const int i0 = tile * kRows + w * 32, i = i0 + l32, i_last = s.n - 1;
   const bool valid = i <= i_last;
@@ -197,34 +257,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
   };
   copy(lo, 0);
 
-  // the wavefront's queries, their dO, and D
+  // the wavefront's queries and their dO
   bf16x8 qf[C::KS], dof[C::KS];
   const int64_t tok = s.first + i;
   const uint16_t* qg = (const uint16_t*)a.q.at + tok * a.q.token + h * a.q.head;
   const uint16_t* dog = (const uint16_t*)a.dout.at + tok * a.dout.token + h * a.dout.head;
-  const uint16_t* og = (const uint16_t*)a.o.at + tok * a.o.token + h * a.o.head;
-  const float* stat = a.lse_in + ((int64_t)h * a.tokens + tok) * a.lse_step;
-  float d = 0.f;
 #pragma unroll
   for (int x = 0; x < C::KS; ++x) {
     qf[x] = load8(qg + 16 * x + 8 * hf, valid);
     dof[x] = load8(dog + 16 * x + 8 * hf, valid);
-    uint32_t rest[2] = {0, 0};
-    if (valid) {
-      rest[0] = *(const uint32_t*)(stat + 1 + 4 * x + 2 * hf);
-      rest[1] = *(const uint32_t*)(stat + 2 + 4 * x + 2 * hf);
-    }
-    d = dot8(dof[x], load8(og + 16 * x + 8 * hf, valid), rest[0], rest[1], d);
   }
-  d = add_halves(d);
   const float c2 = a.scale * kLog2e;
-  float ref = 0.f;  // log-sum-exp in log2 units
-  if (valid) ref = *stat * kLog2e;
-  // For the side of the keys: what its products start from, scores from the log-sum-exp, so that P = exp2(c2 s), and dP from -D.
-  if (valid && hf == 0 && job.part == 0) {
-    float* to = a.rows + (int64_t)h * a.tokens + tok;
-    to[0] = -ref / c2;
-    to[(int64_t)a.heads * a.tokens] = -d;
+  float ref = 0.f, d = 0.f;  // log-sum-exp in log2 units, D
+  if (valid) {
+    const float* from = a.rows + (int64_t)h * a.tokens + tok;
+    ref = -from[0] * c2;
+    d = -from[(int64_t)a.heads * a.tokens];
   }
 
   const uint32_t k_row = row_operand<C::RB>(lane, 0), v_row = BYTES + row_operand<C::RB>(lane, 0);
@@ -298,24 +346,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dq_kernel(const WaSeqLa
     buf ^= 1;
   }
   if (job.parts > 1) {
-    store_part(a.part + ((int64_t)blockIdx.x * kRows + w * 32 + l32) * D, dq, a.scale, hf);
+    store_part(a.part + (rank * kRows + w * 32 + l32) * D, dq, a.scale, hf);
   } else if (valid) {
     store_row((uint16_t*)a.dq.at + tok * a.dq.token + h * a.dq.head, dq, a.scale, hf);
   }
 }
 
+// Job `rank` of keys. lds: 2 tiles of QB queries and dO, and the values; stat: their rows of a.rows.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqLaunch a) {
+__device__ __forceinline__ void key_job(const WaSeqLaunch& a, int64_t rank, unsigned char* lds, float (*stat)[2 * Bwd<D>::QB]) {
   using C = Bwd<D>;
-  constexpr int QB = C::QB, BYTES = QB * C::RB, STAGE = 2 * BYTES, VALUES = C::kValuesInLds ? kRows * C::RB : 0;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE + VALUES];
-  __shared__ __attribute__((aligned(1024))) float stat[2][2 * QB];  // the rows of a.rows
-
+  constexpr int QB = C::QB, BYTES = QB * C::RB, STAGE = 2 * BYTES;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   Job job;
-  if (!Jobs(lane, a.kv_heads).find(blockIdx.x, true, &job)) return;
-  // causal: the first tile of a sequence meets the queries of all of them
+  if (!take_job(a, false, rank, a.kv_heads, 4, &job)) return;
   const int b = job.b, tile = job.tile, hk = job.col, group = a.heads / a.kv_heads;
   const Seq s = one_seq(b);
   const int k0 = tile * kRows + w * 32, kj = k0 + l32;
@@ -458,7 +503,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
     buf ^= 1;
   }
   if (job.parts > 1) {
-    float* to = a.part + a.dq_part + ((int64_t)blockIdx.x * kRows + w * 32 + l32) * 2 * D;
+    float* to = a.part + a.dq_part + (rank * kRows + w * 32 + l32) * 2 * D;
     store_part(to, dk, a.scale, hf);
     store_part(to + D, dv, 1.f, hf);
   } else if (valid) {
@@ -467,56 +512,67 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_dkv_kernel(const WaSeqL
   }
 }
 
-// Adds the parts of cut tiles in order and rounds: four workgroups a tile, those of dQ first, then those of dK and dV.
 template <int D>
-__global__ __launch_bounds__(256) void packed_parts_kernel(const WaSeqLaunch a, int dq_tiles) {
-  const int64_t rank = blockIdx.x / 4;
-  const bool keys = rank >= dq_tiles;
-  const int cols = keys ? a.kv_heads : a.heads;
-  const Jobs jobs(threadIdx.x & 63, cols);
-  Job job;
-  const int64_t mine = keys ? rank - dq_tiles : rank;
-  if (!jobs.find(mine, false, &job) || job.parts == 1) return;
-  const Seq s = one_seq(job.b);
-  const int tile = !a.causal || keys ? job.tile : job.length - 1, width = keys ? 2 * D : D;
-  const int64_t first = jobs.first_part(mine, job), step = (int64_t)cols * kRows * width;
-  const float* from = a.part + (keys ? a.dq_part : 0) + first * kRows * width;
+__global__ __launch_bounds__(64 * kWaves, 2) void packed_grad_kernel(const WaSeqLaunch a, int key_jobs) {
+  using C = Bwd<D>;
+  constexpr int KEYS = 4 * C::QB * C::RB + (C::kValuesInLds ? kRows * C::RB : 0), QUERIES = 4 * C::KB * C::RB;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[KEYS > QUERIES ? KEYS : QUERIES];
+  __shared__ __attribute__((aligned(1024))) float stat[2][2 * C::QB];
+  if ((int)blockIdx.x < key_jobs)
+    key_job<D>(a, blockIdx.x, lds, stat);
+  else
+    query_job<D>(a, blockIdx.x - key_jobs, lds);
+}
+
+// Adds the parts of cut tiles in order and rounds: four workgroups a tile, first those of dQ, then those of dK and dV.
+template <int D>
+__global__ __launch_bounds__(256) void packed_parts_kernel(const WaSeqLaunch a) {
+  const bool keys = blockIdx.x >= 4 * kMostParts / 2;
+  const int number = blockIdx.x / 4 % (kMostParts / 2);
+  const Cuts* cuts = (const Cuts*)a.cut_tiles + (keys ? 1 : 0);
+  const int4 cut = cuts->tile[number];
+  if (number >= cuts->tiles) return;
+  const int cols = keys ? a.kv_heads : a.heads, col = spread(cut.z % cols, cols), width = keys ? 2 * D : D;
+  const Seq s = one_seq(__builtin_amdgcn_readfirstlane(cut.x));
+  const int64_t step = (int64_t)cols * kRows * width;
+  const float* from = a.part + (keys ? a.dq_part : 0) + (int64_t)cut.z * kRows * width;
   for (int x = threadIdx.x; x < kRows / 4 * width / 4; x += 256) {
     const int r = x / (width / 4) + blockIdx.x % 4 * (kRows / 4), c = x % (width / 4) * 4;
-    if (tile * kRows + r >= s.n) break;
+    if (cut.y * kRows + r >= s.n) break;
     const float* at = from + (int64_t)r * width + c;
-    float4 sum = *(const float4*)at;
-#pragma unroll 8
-    for (int y = 1; y < job.parts; ++y) {
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int y = 0; y < cut.w; ++y) {
       const float4 z = *(const float4*)(at + y * step);
       sum.x += z.x;
       sum.y += z.y;
       sum.z += z.z;
       sum.w += z.w;
     }
-    const int64_t tok = s.first + tile * kRows + r;
+    const int64_t tok = s.first + cut.y * kRows + r;
     const WaSeqRows& to = !keys ? a.dq : c < D ? a.dk : a.dv;
-    *(uint2*)((uint16_t*)to.at + tok * to.token + job.col * to.head + c % D) = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
+    *(uint2*)((uint16_t*)to.at + tok * to.token + col * to.head + c % D) = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
   }
 }
 
 // Tiles in parts are longer than a 512th of all, so that there are fewer than 1,024 parts (each of more than a half of that), of fewer
 // than 512 tiles; and no more than the sequences' tiles have.
 int64_t most_parts(const WaSeqLaunch& a, int cols) {
-  return std::min<int64_t>(2 * kSlots, wa_packed_backward_tiles(a) * cols * (((int64_t)a.tokens + kRows - 1) / kRows));
+  return std::min<int64_t>(kMostParts, wa_packed_backward_tiles(a) * cols * (((int64_t)a.tokens + kRows - 1) / kRows));
 }
 
 template <int D>
 hipError_t launch(const WaSeqLaunch& a, hipStream_t stream) {
   const int64_t tiles = wa_packed_backward_tiles(a);
-  // a job a tile, and for each part of a 512th of all one more at most
-  hipLaunchKernelGGL(packed_dq_kernel<D>, dim3((unsigned)(tiles * a.heads + kSlots)), dim3(64 * kWaves), 0, stream, a);
+  const int64_t row_waves = ((int64_t)a.tokens + 15) / 16 * a.heads;
+  hipLaunchKernelGGL(packed_rows_kernel<D>, dim3((unsigned)((row_waves + 3) / 4)), dim3(256), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(packed_dkv_kernel<D>, dim3((unsigned)(tiles * a.kv_heads + kSlots)), dim3(64 * kWaves), 0, stream, a);
+  // a job a tile, and for each part of a 512th of all one more at most; those of queries begin on the first XCD
+  const int64_t key_jobs = (tiles * a.kv_heads + kSlots + 7) / 8 * 8, query_jobs = tiles * a.heads + kSlots;
+  hipLaunchKernelGGL(packed_grad_kernel<D>, dim3((unsigned)(key_jobs + query_jobs)), dim3(64 * kWaves), 0, stream, a, (int)key_jobs);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  const int dq_tiles = (int)std::min<int64_t>(kSlots, tiles * a.heads), kv_tiles = (int)std::min<int64_t>(kSlots, tiles * a.kv_heads);
-  hipLaunchKernelGGL(packed_parts_kernel<D>, dim3(4 * (dq_tiles + kv_tiles)), dim3(256), 0, stream, a, dq_tiles);
+  hipLaunchKernelGGL(packed_parts_kernel<D>, dim3(4 * kMostParts), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -527,6 +583,7 @@ int64_t wa_packed_backward_tiles(const WaSeqLaunch& a) {
   return std::min<int64_t>(a.tokens, ((int64_t)a.tokens + (int64_t)(kRows - 1) * a.batch) / kRows);
 }
 
+size_t wa_packed_backward_cut_bytes() { return 2 * sizeof(Cuts); }
 int64_t wa_packed_backward_dq_floats(const WaSeqLaunch& a) { return most_parts(a, a.heads) * kRows * a.head_dim; }
 int64_t wa_packed_backward_part_floats(const WaSeqLaunch& a) {
   return wa_packed_backward_dq_floats(a) + most_parts(a, a.kv_heads) * kRows * 2 * a.head_dim;

@@ -45,6 +45,7 @@ struct WaSeqLaunch {
   WaSeqRows dout, dq, dk, dv;
   const float* lse_in;     // what the forward wrote, [heads][tokens] rows of lse_step
   float* rows;             // workspace: [2][heads][tokens]: what a query's products start from (packed_bwd.hip)
+  void* cut_tiles;         // workspace: which tiles have parts (packed_bwd.hip)
   int64_t dq_part;         // floats of `part` that the parts of dQ may take; those of dK and dV lie behind
 };
 
@@ -57,6 +58,7 @@ hipError_t wa_launch_paged_attn(const WaSeqLaunch& a, hipStream_t stream);
 
 // Gradient (packed_bwd.hip): tiles of 128 tokens of all sequences, at most; float32 results of tiles in parts, those of dQ and all.
 int64_t wa_packed_backward_tiles(const WaSeqLaunch& a);
+size_t wa_packed_backward_cut_bytes();
 int64_t wa_packed_backward_dq_floats(const WaSeqLaunch& a);
 int64_t wa_packed_backward_part_floats(const WaSeqLaunch& a);
 hipError_t wa_launch_packed_backward(const WaSeqLaunch& a, hipStream_t stream);
