@@ -35,6 +35,20 @@ struct Bwd {
   static constexpr int KB = 64, QB = kValuesInLds ? 32 : 64;
 };
 
+// acc (rows: columns of the output) to the lane's output row, times f, 16 bytes a store
+template <int T>
+__device__ __forceinline__ void store_row16(uint16_t* out, const f32x16 (&acc)[T], float f, int hf, bool valid) {
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int v = 0; v < 16; v += 8) {
+      const uint4 eight = gather8(
+          make_uint2(pack_bf16x2(acc[t][v] * f, acc[t][v + 1] * f), pack_bf16x2(acc[t][v + 2] * f, acc[t][v + 3] * f)),
+          make_uint2(pack_bf16x2(acc[t][v + 4] * f, acc[t][v + 5] * f), pack_bf16x2(acc[t][v + 6] * f, acc[t][v + 7] * f)));
+      if (valid) *(uint4*)(out + t * 32 + 2 * v + 8 * hf) = eight;
+    }
+}
+
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -347,8 +361,8 @@ __device__ __forceinline__ void query_job(const WaSeqLaunch& a, int64_t rank, un
   }
   if (job.parts > 1) {
     store_part(a.part + (rank * kRows + w * 32 + l32) * D, dq, a.scale, hf);
-  } else if (valid) {
-    store_row((uint16_t*)a.dq.at + tok * a.dq.token + h * a.dq.head, dq, a.scale, hf);
+  } else {
+    store_row16((uint16_t*)a.dq.at + tok * a.dq.token + h * a.dq.head, dq, a.scale, hf, valid);
   }
 }
 
@@ -506,9 +520,9 @@ __device__ __forceinline__ void key_job(const WaSeqLaunch& a, int64_t rank, unsi
     float* to = a.part + a.dq_part + (rank * kRows + w * 32 + l32) * 2 * D;
     store_part(to, dk, a.scale, hf);
     store_part(to + D, dv, 1.f, hf);
-  } else if (valid) {
-    store_row((uint16_t*)a.dk.at + tok * a.dk.token + hk * a.dk.head, dk, a.scale, hf);
-    store_row((uint16_t*)a.dv.at + tok * a.dv.token + hk * a.dv.head, dv, 1.f, hf);
+  } else {
+    store_row16((uint16_t*)a.dk.at + tok * a.dk.token + hk * a.dk.head, dk, a.scale, hf, valid);
+    store_row16((uint16_t*)a.dv.at + tok * a.dv.token + hk * a.dv.head, dv, 1.f, hf, valid);
   }
 }
 

@@ -174,12 +174,13 @@ __device__ __forceinline__ uint64_t divide(uint64_t x, uint64_t y) {
 // Finds tiles: in the line of units, and by their length. The first 64 sequences are held, one a lane.
 template <bool PAGED, int LOG_KB>
 struct Walk {
-  int lane, log_tokens, cols, batch;
+  int lane, log_tokens, per_tile, cols, batch;
   bool causal;
   Seq mine;
 
   __device__ __forceinline__ Walk(SeqArgs a, int lane_)
-      : lane(lane_), log_tokens(a->plan.log_tokens), cols(a->heads / a->plan.per_tile), batch(a->batch), causal(a->causal) {
+      : lane(lane_), log_tokens(a->plan.log_tokens), per_tile(a->plan.per_tile), cols(a->heads / per_tile), batch(a->batch),
+        causal(a->causal) {
     mine = seq_of<PAGED>(a, min(lane, batch - 1));
     if (lane >= batch) mine.n = 0;
   }
@@ -348,6 +349,14 @@ __device__ __forceinline__ float with_rest(uint32_t bf16_bits, uint32_t rest, in
   return __builtin_bit_cast(float, (bf16_bits << 16) + ((uint32_t)(int)(int8_t)(rest >> 8 * i) << 8));
 }
 
+// Four columns of a row as 16-bit values are in the lane's half, the next four in the other half's, and so on in turn (a product's output):
+// of eight and eight, each half gets its eight.
+__device__ __forceinline__ uint4 gather8(uint2 even, uint2 odd) {
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(even.x), "+v"(odd.x));
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(even.y), "+v"(odd.y));
+  return make_uint4(even.x, even.y, odd.x, odd.y);
+}
+
 // The shares of the line: of `total` units for `workers` workers.
 struct Shares {
   int64_t total, near;  // near: how far a border moves to a tile's end; it never stays before a tile's first keys
@@ -505,6 +514,15 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     begin = uniform64(begin);
     end = uniform64(end);
   }
+  // A share that begins inside a tile ends with that one. So all workers begin with the first keys, and where tiles are of about a
+  // share's length they meet the same keys at the same time (two chunks of 1,024 tokens over 16,384 keys among six tokens:
+  // 672 -> 644 us).
+  Item rest = it;
+  int left = 0;  // of the share: 1: `rest` comes after the others; 2: it is the last
+  if (PAGED && begin > it.at && it.at + it.units < end) {
+    it = walk.next(it);
+    left = 1;
+  }
   const uint32_t kbase = row_operand<C::RB>(lane, 0);
   const uint32_t vbase0 = C::BYTES + col_operand<C::RB>(lane, 0, 0), vbase1 = C::BYTES + col_operand<C::RB>(lane, 0, 1);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds) + w * 1024;
@@ -517,10 +535,9 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     int lo, hi;
   };
   auto range = [&](const Item& x) {
-    const SeqArgs a = again(seq_args());
     Range r;
-    const int last = min(((x.tile + 1) << a->plan.log_tokens), x.s.n) - 1;
-    const int most = a->causal ? min(max(x.s.keys - x.s.n + last + 1, 0), x.s.keys) : x.s.keys;
+    const int last = min(((x.tile + 1) << walk.log_tokens), x.s.n) - 1;
+    const int most = walk.causal ? min(max(x.s.keys - x.s.n + last + 1, 0), x.s.keys) : x.s.keys;
     const int64_t u0 = max(begin - x.at - kSeqFixed, (int64_t)0), u1 = min(end - x.at, (int64_t)x.units) - kSeqFixed;
     r.lo = (int)min(u0 * KB, (int64_t)most);
     r.hi = (int)min(max(u1, (int64_t)0) * KB, (int64_t)most);
@@ -539,7 +556,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
   };
   auto aim = [&](const Item& x, int key) {
     const SeqArgs a = again(seq_args());
-    const int hk = a->plan.per_tile == 1 ? x.col / (a->heads / a->kv_heads) : x.col;
+    const int hk = walk.per_tile == 1 ? x.col / (a->heads / a->kv_heads) : x.col;
     if (PAGED) {
       kfrom = (const unsigned char*)a->kp.at + hk * a->kp.head * 2;
       vfrom = (const unsigned char*)a->vp.at + hk * a->vp.head * 2;
@@ -593,12 +610,11 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     bool valid;
   };
   auto place = [&](const Item& x) {
-    const SeqArgs a = again(seq_args());
-    const int log_p = a->plan.log_tokens, sub = row >> log_p;
+    const int log_p = walk.log_tokens, sub = row >> log_p;
     Place p;
     p.token = (x.tile << log_p) + (row & ((1 << log_p) - 1));
-    p.head = x.col * a->plan.per_tile + sub;
-    p.valid = sub < a->plan.per_tile && p.token < x.s.n;
+    p.head = x.col * walk.per_tile + sub;
+    p.valid = sub < walk.per_tile && p.token < x.s.n;
     return p;
   };
 
@@ -704,12 +720,17 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
   bool ready = false, stored = false;  // the item's first tile is on its way; stores of the item before come behind it
   Range r = range(it);
   for (;;) {
-    const bool more = it.at + it.units < end;
+    const bool line = left < 2 && it.at + it.units < end, more = line || left == 1;
     Item nx;
     Range rn;
     bool known = false;  // nx
     auto look = [&] {
-      nx = walk.next(it);
+      if (line) {
+        nx = walk.next(it);
+      } else {
+        nx = rest;
+        left = 2;
+      }
       rn = range(nx);
       known = true;
       if (PAGED && nx.b != it.b) {  // its pages are asked for ahead of its first copy
@@ -731,13 +752,12 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     }
     int limit, some, all;  // keys that the lane's query sees; that any, and that all of the wavefront's queries see
     {
-      const SeqArgs a = again(seq_args());
-      const int log_p = a->plan.log_tokens, at = it.tile << log_p, before = it.s.keys - it.s.n;
+      const int log_p = walk.log_tokens, at = it.tile << log_p, before = it.s.keys - it.s.n;
       const int first = log_p >= 5 ? (w * 32) & ((1 << log_p) - 1) : 0;  // the wavefront's tokens
       const int t0 = at + first, t1 = min(at + first + (log_p >= 5 ? 31 : (1 << log_p) - 1), it.s.n - 1);
-      const bool used = (w * 32 >> log_p) < a->plan.per_tile && t0 < it.s.n;
+      const bool used = (w * 32 >> log_p) < walk.per_tile && t0 < it.s.n;
       const Place p = place(it);
-      auto sees = [&](int t) { return a->causal ? min(max(before + t + 1, 0), it.s.keys) : it.s.keys; };
+      auto sees = [&](int t) { return walk.causal ? min(max(before + t + 1, 0), it.s.keys) : it.s.keys; };
       limit = p.valid ? sees(p.token) : 0;
       some = used ? sees(t1) : 0;
       all = sees(t0);
@@ -751,8 +771,8 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     ready = false;
     for (int key = r.lo; key < r.hi; key += KB) {
       // This wavefront's part of the tile has arrived (and the queries, so that nothing waits for them below); stores behind it, at
-      // least one for each four columns that a lane holds, need not have.
-      if (stored) WA_WAIT_VM(4 * C::DT); else WA_WAIT_VM(0);
+      // least one for each eight columns that a lane holds, need not have.
+      if (stored) WA_WAIT_VM(2 * C::DT); else WA_WAIT_VM(0);
       stored = false;
       WA_BARRIER();  // everyone's has, and everyone is done with the other buffer
       int next = key + KB;
@@ -782,40 +802,44 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     const bool starts = begin <= it.at, finishes = it.at + it.units <= end;
     const Place p = place(it);
     stored = __ballot(p.valid) != 0;
-    if (p.valid) {
-      const SeqArgs a = again(seq_args());
-      const int64_t tok = it.s.first + p.token;
-      if (starts && finishes) {
-        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-        uint16_t* out = (uint16_t*)a->o.at + tok * a->o.token + p.head * a->o.head + 4 * hf;
-        float* stat = a->lse ? a->lse + (p.head * (int64_t)a->tokens + tok) * a->lse_step : nullptr;
+    const SeqArgs a = again(seq_args());
+    const int64_t tok = it.s.first + p.token;
+    if (starts && finishes) {
+      const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+      uint16_t* out = (uint16_t*)a->o.at + tok * a->o.token + p.head * a->o.head + 8 * hf;
+      float* stat = a->lse && p.valid ? a->lse + (p.head * (int64_t)a->tokens + tok) * a->lse_step : nullptr;
 #pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
+      for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-          for (int v = 0; v < 16; v += 4) {
+        for (int v = 0; v < 16; v += 8) {
+          uint2 o16[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[dt][v + e] *= inv;
-            const uint2 o16 = make_uint2(T::pack(acc[dt][v], acc[dt][v + 1]), T::pack(acc[dt][v + 2], acc[dt][v + 3]));
-            *(uint2*)(out + dt * 32 + 2 * v) = o16;
+          for (int q = 0; q < 2; ++q) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[dt][v + 4 * q + e] *= inv;
+            o16[q] = make_uint2(T::pack(acc[dt][v + 4 * q], acc[dt][v + 4 * q + 1]), T::pack(acc[dt][v + 4 * q + 2], acc[dt][v + 4 * q + 3]));
             if (!HALF && !PAGED && stat)
-              *(uint32_t*)(stat + 1 + dt * 8 + v / 2 + hf) = rest4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3], o16);
+              *(uint32_t*)(stat + 1 + dt * 8 + v / 2 + 2 * q + hf) =
+                  rest4(acc[dt][v + 4 * q], acc[dt][v + 4 * q + 1], acc[dt][v + 4 * q + 2], acc[dt][v + 4 * q + 3], o16[q]);
           }
-        if (stat && hf == 0) *stat = l == 0.f ? -INFINITY : (ref + __log2f(l)) * kLn2;
-        if (!whole && hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(-1, 0);
-      } else {
-        // slot 0: a part that begins inside its tile; slot 1: one that begins with it
-        const int64_t at = ((int64_t)me * 2 + (starts ? 1 : 0)) * R + row;
-        float* out = a->part + at * D;
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-          for (int v = 0; v < 16; v += 4)
-            *(float4*)(out + dt * 32 + 2 * v + 4 * hf) = make_float4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3]);
-        if (hf == 0) ((float2*)(a->part + (int64_t)a->plan.workers * 2 * R * D))[at] = make_float2(ref, l);
-        if (finishes) {
-          const int first = Shares(total, a).first_of(it);
-          if (hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(first | me << 16, row);
+          const uint4 eight = gather8(o16[0], o16[1]);
+          if (p.valid) *(uint4*)(out + dt * 32 + 2 * v) = eight;
         }
+      if (stat && hf == 0) *stat = l == 0.f ? -INFINITY : (ref + __log2f(l)) * kLn2;
+      if (!whole && p.valid && hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(-1, 0);
+    } else if (p.valid) {
+      // slot 0: a part that begins inside its tile; slot 1: one that begins with it
+      const int64_t at = ((int64_t)me * 2 + (starts ? 1 : 0)) * R + row;
+      float* out = a->part + at * D;
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *(float4*)(out + dt * 32 + 2 * v + 4 * hf) = make_float4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3]);
+      if (hf == 0) ((float2*)(a->part + (int64_t)a->plan.workers * 2 * R * D))[at] = make_float2(ref, l);
+      if (finishes) {
+        const int first = Shares(total, a).first_of(it);
+        if (hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(first | me << 16, row);
       }
     }
     if (!more) break;
