@@ -30,6 +30,7 @@ WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
   // Few keys a tile take less time than a join (one wavefront: 100 sequences of up to 300 keys 23.5 -> 19.7 us, but 16 of 500 19.6 ->
   // 24.6; four: 512 tokens of 32 heads 25.0 -> 18.0, 1,000 of 16 sequences 21.7 -> 14.4, of one 24.7 -> 27.4).
   const int64_t keys = a.paged ? (int64_t)a.table_width << a.page_shift : a.tokens;
+  // Packed sequences of one wavefront a tile (a mean of 32 tokens at most) are always whole.
   p.whole = p.waves == 4 || !a.paged ? keys <= 512 || (!a.paged && mean <= 128)
                                      : keys <= 256 || (keys <= 512 && wa_seq_most_tiles(a, p) >= 256);
   return p;

@@ -70,7 +70,7 @@ struct Job {
 
 // All tiles of all sequences and `cols` heads, longest first, those longer than `most` in parts of about equal length: `most` takes as
 // long as a 512th of all work, so that a call of few tiles fills the chip's workgroups (two a compute unit) once, and one of many is not cut.
-// A pair of a key and a query takes four products for dK and dV and three for dQ.
+// Sequences that overlap (starts that descend) could have more tiles and parts than there is room for: they have no jobs. A pair of a key and a query takes four products for dK and dV and three for dQ.
 // Causal tiles have the lengths 1 to T of a sequence of T tiles, others T. Each workgroup finds its job itself: the lengths are on the
 // device. The first 64 sequences are held, one a lane.
 struct Jobs {
@@ -81,19 +81,21 @@ struct Jobs {
   // share: of the kind of jobs in all work, in sevenths
   __device__ __forceinline__ Jobs(int lane_, int cols_, int share, bool queries_)
       : a(seq_args()), lane(lane_), cols(cols_), batch(a->batch), causal(a->causal), queries(queries_) {
-    mine = tiles_of(lane);
-    int64_t sum = 0;
+    int64_t sum = 0, tokens = 0;
     for (int base = 0; base < batch; base += 64) {
-      const int64_t t = tiles_at(base);
+      const int n = tokens_of(base + lane);
+      const int64_t t = tiles(n);
+      if (base == 0) mine = (int)t;
+      tokens += n;
       sum += causal ? t * (t + 1) / 2 : t * t;
     }
+    if (lane64(lane_prefix_sum64(tokens, lane), 63) > again(a)->tokens) batch = mine = 0;
     sum = lane64(lane_prefix_sum64(sum, lane), 63) * cols;
     most = (int)((uint64_t)(7 * sum + share * kSlots - 1) / (share * kSlots));
   }
-  __device__ __forceinline__ int tiles_of(int b) const {
-    return b < batch ? (int)(((int64_t)seq_of<false>(again(a), b).n + kRows - 1) / kRows) : 0;
-  }
-  __device__ __forceinline__ int tiles_at(int base) const { return base == 0 ? mine : tiles_of(base + lane); }
+  __device__ __forceinline__ int tokens_of(int b) const { return b < batch ? seq_of<false>(again(a), b).n : 0; }
+  static __device__ __forceinline__ int tiles(int n) { return (n + kRows - 1) / kRows; }
+  __device__ __forceinline__ int tiles_at(int base) const { return base == 0 ? mine : tiles(tokens_of(base + lane)); }
   __device__ __forceinline__ int parts_of(int length) const { return (length + most - 1) / most; }
   // jobs of the first x lengths of a sequence
   __device__ __forceinline__ int upto(int x) const {

@@ -23,7 +23,7 @@
 //   found by a closed form, so all workers have the same to do whatever the lengths are. A border within a sixteenth of a share of a tile's
 //   end is moved there. A tile that several workers compute is joined by a second kernel, in key order: nothing is added with
 //   atomics, and equal calls give equal bits.
-//   Calls of few keys: a workgroup a tile, without the second kernel.
+//   Calls of few keys, and packed sequences of few tokens: a workgroup a tile, without the second kernel.
 #pragma once
 
 #include "diff_tiles.h"
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
   int64_t total, begin, end;
   Item it;
   int me = blockIdx.x;
-  bool whole = seq_args()->plan.whole;
+  bool whole = (W == 1 && !PAGED) || seq_args()->plan.whole;
   if (whole || !PAGED) {
     total = (int64_t)walk.above(0) * walk.cols;
     whole |= total >= (int64_t)kSeqWhole * seq_args()->plan.workers;
@@ -1014,18 +1014,21 @@ hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
   const int64_t grid = a.plan.whole ? most : whole ? std::max<int64_t>(most, a.plan.workers) : a.plan.workers;
   hipLaunchKernelGGL((seq_attn_kernel<HALF, D, W, PAGED>), dim3((unsigned)grid), dim3(64 * W), 0, stream, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.plan.whole) return e;
-  const int64_t rows = (int64_t)a.tokens * a.heads;
-  // a tile's parts, if all workers share the tiles that there are at least
-  const int64_t tiles = std::max<int64_t>(std::min(a.batch, a.tokens), a.tokens >> a.plan.log_tokens) * (a.heads / a.plan.per_tile);
-  if (a.plan.workers / tiles >= kSeqManyParts && rows <= (1 << 16)) {
-    hipLaunchKernelGGL((seq_join_many_kernel<HALF, D, W, PAGED>), dim3((unsigned)rows), dim3(4 * D), 0, stream, a);
-  } else {
-    constexpr int PER = 256 / (D / 4);
-    const int64_t wgs = std::min<int64_t>((rows + PER - 1) / PER, 2048);
-    hipLaunchKernelGGL((seq_join_few_kernel<HALF, D, W, PAGED>), dim3((unsigned)wgs), dim3(256), 0, stream, a, wgs * PER);
+  if constexpr (W == 4 || PAGED) {  // packed sequences of so few tokens are never cut (wa_seq_plan)
+    if (e != hipSuccess || a.plan.whole) return e;
+    const int64_t rows = (int64_t)a.tokens * a.heads;
+    // a tile's parts, if all workers share the tiles that there are at least
+    const int64_t tiles = std::max<int64_t>(std::min(a.batch, a.tokens), a.tokens >> a.plan.log_tokens) * (a.heads / a.plan.per_tile);
+    if (a.plan.workers / tiles >= kSeqManyParts && rows <= (1 << 16)) {
+      hipLaunchKernelGGL((seq_join_many_kernel<HALF, D, W, PAGED>), dim3((unsigned)rows), dim3(4 * D), 0, stream, a);
+    } else {
+      constexpr int PER = 256 / (D / 4);
+      const int64_t wgs = std::min<int64_t>((rows + PER - 1) / PER, 2048);
+      hipLaunchKernelGGL((seq_join_few_kernel<HALF, D, W, PAGED>), dim3((unsigned)wgs), dim3(256), 0, stream, a, wgs * PER);
+    }
+    return hipGetLastError();
   }
-  return hipGetLastError();
+  return e;
 }
 
 template <bool PAGED>

@@ -344,3 +344,51 @@ def test_starts_outside_the_rows():
     assert torch.all(kept == 3.0)
     none = q[:0]
     assert W.packed_attn(none, k[:0], v[:0], torch.zeros(2, dtype=torch.int32, device="cuda")).shape == none.shape
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,h,hk,d,dtype", [
+    ([700, 0, 333, 1], 4, 2, 64, BF), ([700, 0, 333, 1], 4, 2, 128, BF), ([1, 900, 300], 3, 1, 128, FP), (([0] * 10 + [1500]) * 6, 1, 1, 64, BF),
+    ([1500, 700, 900, 1000], 32, 16, 64, BF)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_cut_and_dealt_out(lens, h, hk, d, dtype, causal):
+    """Batches whose tiles are cut between workgroups; the last: one of more tiles than twice the workgroups, which are dealt out."""
+    check(make(lens, h, hk, d, dtype, front=2, spare=70), causal)
+
+
+@pytest.mark.gpu
+def test_sequences_that_overlap():
+    """Starts that descend: the gradient leaves all rows, the forward those of no sequence."""
+    q, k, v, starts, dout = make([200, 56], 2, 2, 64, spare=10)
+    o, lse = W.packed_attn(q, k, v, starts, return_lse=True)
+    twice = torch.tensor([0, 256, 0, 256], dtype=torch.int32, device="cuda")
+    kept = [torch.full_like(x, 3.0) for x in (q, k, v, q)]
+    W.packed_attn_backward(dout, q, k, v, o, lse, twice, out=kept[:3])
+    W.packed_attn(q, k, v, twice, out=kept[3])
+    assert all(torch.all(x == 3.0) for x in kept[:3]) and torch.all(kept[3][256:] == 3.0)
+
+
+@pytest.mark.gpu
+def test_workspaces():
+    """What a workspace holds before does not matter; a smaller one is left alone; calls on two streams have their own."""
+    q, k, v, starts, dout = make([900, 340], 4, 2, 64)
+    o, lse = W.packed_attn(q, k, v, starts, return_lse=True)
+    grads = W.packed_attn_backward(dout, q, k, v, o, lse, starts)
+    need = W.packed_attn_workspace_size(1240, 2, 4, 2, 64), W.packed_attn_backward_workspace_size(1240, 2, 4, 2, 64)
+    dirty = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in need]
+    assert torch.equal(W.packed_attn(q, k, v, starts, workspace=dirty[0]), o)
+    assert all(torch.equal(x, y) for x, y in zip(W.packed_attn_backward(dout, q, k, v, o, lse, starts, workspace=dirty[1]), grads))
+    small = [x.fill_(9)[:-1] for x in dirty]
+    assert torch.equal(W.packed_attn(q, k, v, starts, workspace=small[0]), o)
+    assert all(torch.equal(x, y) for x, y in zip(W.packed_attn_backward(dout, q, k, v, o, lse, starts, workspace=small[1]), grads))
+    assert all(torch.all(x == 9) for x in small)
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for x in streams:
+        x.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for x in streams:
+            with torch.cuda.stream(x):
+                got.append((W.packed_attn(q, k, v, starts), W.packed_attn_backward(dout, q, k, v, o, lse, starts)))
+    torch.cuda.synchronize()
+    for o2, g2 in got:
+        assert torch.equal(o2, o) and all(torch.equal(x, y) for x, y in zip(g2, grads))

@@ -292,3 +292,54 @@ def test_prompt_chunks_tokens():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, W.paged_attn(q, kp, vp, tables, starts, lens))
+
+
+@pytest.mark.gpu
+def test_lengths_outside_the_table():
+    """kv_lens below 0 and past the table are taken into it; sequences that share one table (a stride of 0); a dirty workspace."""
+    (q, kp, vp, tables, starts, kv), k, v = make([96, 300], [1, 70], 4, 2, 64, 32)
+    one = tables[1:2, :9]                       # 288 tokens
+    wide = one.expand(2, -1)
+    lens = torch.tensor([-5, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    dirty = torch.full((W.packed_attn_workspace_size(71, 2, 4, 2, 64),), 255, dtype=torch.uint8, device="cuda")
+    o, lse = W.paged_attn(q, kp, vp, wide, starts, lens, return_lse=True, workspace=dirty)
+    ref = S.paged(f64(q), [f64(k[1][:0]), f64(k[1][:288])], [f64(v[1][:0]), f64(v[1][:288])], starts.tolist())
+    close(o, ref["o"], ref["tol"]["o"], "o")
+    check_lse(lse, ref["lse"])
+    assert not o[0].any() and torch.equal(W.paged_attn(q, kp, vp, one.repeat(2, 1), starts, lens), o)
+
+
+@pytest.mark.gpu
+def test_fork_and_compact_between_tokens():
+    """A prompt, two forks of it, another token for each, the prompt given back and the pool compacted, another token: every answer
+    against packed attention's oracle over that sequence's own tokens."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    h, hk, d, page, n = 4, 2, 64, 16, 41
+    refs, tables, lens, status = (torch.zeros(x, dtype=torch.int32, device="cuda") for x in (20, (4, 5), 4, 1))
+    pool = torch.full((2, 20, hk, page, d), float("nan"), dtype=BF, device="cuda")
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    keys = [[torch.zeros(0, hk, d, device="cuda", dtype=BF)] * 2 for _ in range(4)]
+
+    def tokens(counts):
+        starts = [sum(counts[:i]) for i in range(5)]
+        q, k, v = (torch.randn((starts[-1], m, d), generator=g, device="cuda").to(BF) for m in (h, hk, hk))
+        for s in range(4):
+            keys[s] = [torch.cat([x, y[starts[s]:starts[s + 1]]]) for x, y in zip(keys[s], (k, v))]
+        W.page_grow(refs, tables, lens, dev([len(x[0]) for x in keys]), page=page, status=status)
+        W.page_store(k, v, *pool, tables, dev(starts), lens, status=status)
+        o = W.paged_attn(q, *pool, tables, dev(starts), lens, status=status)
+        ref = S.paged(f64(q), [f64(x) for x, _ in keys], [f64(x) for _, x in keys], starts)
+        close(o, ref["o"], ref["tol"]["o"], str(counts))
+        assert not status.any() and lens.tolist() == [len(x[0]) for x in keys]
+    tokens([n, 0, 0, 20])
+    W.page_fork(pool, refs, tables, lens, dev([0, 0]), dev([1, 2]), page=page, status=status)
+    keys[1], keys[2] = list(keys[0]), list(keys[0])
+    assert refs[:5].tolist() == [3, 3, 1, 1, 1] and int(refs.sum()) == 11
+    tokens([1, 1, 8, 1])
+    W.page_free(refs, tables, lens, dev([0, 3]), page=page, status=status)
+    keys[0] = keys[3] = [x[:0] for x in keys[0]]
+    used = dev([0])
+    W.page_compact(pool, refs, tables, lens, page=page, used=used, status=status)
+    assert used.item() == 5 and refs.tolist() == [2, 2, 1, 1, 1] + [0] * 15
+    tokens([0, 9, 1, 0])
+    tokens([5, 1, 0, 1])

@@ -300,3 +300,13 @@ def test_captured():
     check.grow(n.tolist())
     check.compact(False)
     assert all(torch.equal(x, y) for x, y in zip([check.pool, *check.state()], want))
+
+
+@pytest.mark.gpu
+def test_growth_past_the_pool():
+    """Two hundred sequences that want more pages than there are: those that find enough go on taking them."""
+    rng = random.Random(5)
+    both = Both(300, 200, 12, 4)
+    for _ in range(3):
+        both.grow([rng.choice([0, n, n + rng.randint(1, 20), 48, 49]) for n in both.h[2]])
+    assert both.want == P.EXHAUSTED and min(both.h[0]) == 1
