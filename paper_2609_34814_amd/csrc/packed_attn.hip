@@ -27,12 +27,16 @@ WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
   // token of 32 sequences 162 us with 1,024, 197 with 1,280).
   p.workers = p.waves == 4 ? 512 : 1024;
   p.min_units = 4;
-  // Few keys a tile take less time than a join (one wavefront: 100 sequences of up to 300 keys 23.5 -> 19.7 us, but 16 of 500 19.6 ->
-  // 24.6; four: 512 tokens of 32 heads 25.0 -> 18.0, 1,000 of 16 sequences 21.7 -> 14.4, of one 24.7 -> 27.4).
-  const int64_t keys = a.paged ? (int64_t)a.table_width << a.page_shift : a.tokens;
-  // Packed sequences of one wavefront a tile (a mean of 32 tokens at most) are always whole.
-  p.whole = p.waves == 4 || !a.paged ? keys <= 512 || (!a.paged && mean <= 128)
-                                     : keys <= 256 || (keys <= 512 && wa_seq_most_tiles(a, p) >= 256);
+  // Calls whose tiles are never cut need no second kernel. Packed: tiles of fifteen tiles of keys at most (kSeqLongest), many short sequences
+  // (1,000 tokens of 16: 21.7 -> 14.4 us), and those of one wavefront a tile. Over a cache, whose lengths the host does not know, tables of
+  // few keys: few keys a tile take less time than a join (one wavefront: 100 sequences of up to 300 keys 23.5 -> 19.7 us, but 16 of 500
+  // 19.6 -> 24.6; four: 512 tokens of 32 heads 25.0 -> 18.0).
+  if (a.paged) {
+    const int64_t keys = (int64_t)a.table_width << a.page_shift;
+    p.whole = keys <= (p.waves == 4 ? 512 : 256) || (p.waves == 1 && keys <= 512 && wa_seq_most_tiles(a, p) >= 256);
+  } else {
+    p.whole = a.tokens <= 960 || mean <= 128;
+  }
   return p;
 }
 

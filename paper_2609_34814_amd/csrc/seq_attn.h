@@ -6,7 +6,10 @@
 // that would leave an eighth of the rows empty), so the heads of a group read a tile of keys once. A wavefront computes, a tile
 // of KB keys at a time (copied into LDS while the one before is worked on), S^T = K Q^T (v_mfma_f32_32x32x16: keys in registers, one
 // query a lane), the running maximum and sum of its queries, P^T rounded to 16 bits, and O^T += V^T P^T, whose operand P^T is in the
-// registers that S^T came out in. Scores, maxima, sums and O are float32; P is rounded to the inputs' type because the matrix cores
+// registers that S^T came out in. Of four wavefronts each computes the scores of a tile of keys beside the probabilities of the one
+// before, so that matrix products and exponentials of one wavefront run at the same time (32,768 tokens, 32 heads over 8, d 128: 8.2 ms where
+// they take turns, 7.8 so; 8,192 tokens of 7 documents, 16 over 4, d 64: 60 us and 51); one wavefront, which waits for the memory, has them take
+// turns. Scores, maxima, sums and O are float32; P is rounded to the inputs' type because the matrix cores
 // multiply that (half a step, 2^-9 or 2^-12 of each probability, which averages out over the keys of a row).
 //
 // Running maximum: O and l are rescaled only when a row's maximum grows by more than 2^8: probabilities up to 2^8 keep their
@@ -15,10 +18,10 @@
 //
 // Who computes what. The lengths are known on the device only; each workgroup finds its work itself from the lengths, a sequence a lane,
 // which costs no launch before this one.
-//   Many tiles of packed sequences: a workgroup a tile, those with the most keys first, so that the chip stays full to the end, and
+//   Many tiles of packed sequences, or ones of about equal length: a workgroup a tile, those with the most keys first, so that the chip stays full to the end, and
 //   those that run together read the same keys at about the same time (one prompt of 32,768 tokens, 32 heads over 8, d 128: 9.6 ms where
-//   equal shares of the work begin anywhere in a tile, 8.2 so).
-//   Few tiles, and those of a paged cache: the work is a line of units, one for each tile of keys of each query tile and two for its
+//   equal shares of the work begin anywhere in a tile, 8.2 so, when both were measured).
+//   Others, and those of a paged cache: the work is a line of units, one for each tile of keys of each query tile and two for its
 //   beginning and end, sequence after sequence and within one key head after key head. Worker w of G takes the units [w U / G, (w + 1) U / G),
 //   found by a closed form, so all workers have the same to do whatever the lengths are. A border within a sixteenth of a share of a tile's
 //   end is moved there. A tile that several workers compute is joined by a second kernel, in key order: nothing is added with
@@ -31,13 +34,17 @@
 #include "wavealign.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace wa {
 
 constexpr float kSeqGrow = 8.f;  // log2 units
 constexpr int kSeqAhead = 4;     // operands read ahead
-// Packed tiles are dealt out whole where there are so many times the workers of them.
-constexpr int kSeqWhole = 2;
+// Packed tiles are dealt out whole where there are so many times the workers of them, and where the longest takes no longer than the line
+// would: with parts to store and to join, a worker's share s takes about 22 + 2.2 s us, whole tiles 4 + 1.05 longest + 0.7 s, so where
+// longest <= 17 + 10/7 s (d 128, in tiles of 64 keys; d 64 about the same). 2,400 tokens of 3 prompts, 32 heads over 8: 59 us along the
+// line, 44 whole; 8,192 of one, 8 heads over 1: 168 and 185.
+constexpr int kSeqWhole = 4, kSeqLongest = 17;
 // What a tile costs beside its keys, in tiles of keys.
 constexpr int kSeqFixed = 2;
 
@@ -221,6 +228,22 @@ struct Walk {
     int64_t sum = lane64(head.upto, 63);
     for (int base = 64; base < batch; base += 64) sum += lane64(sums(base).upto, 63);
     return sum;
+  }
+  // whether the longest tile is hardly longer than a share (see kSeqLongest)
+  __device__ __forceinline__ bool even(int workers) const {
+    int64_t all = 0;
+    int longest = 0;
+    for (int base = 0; base < batch; base += 64) {
+      const Seq s = seq_at(base);
+      const Line l = line(s);
+      const int t = tiles(s);
+      if (t == 0) continue;
+      const int64_t units = l.upto(t);
+      all += cols * units;
+      longest = max(longest, (int)(units - l.upto(t - 1)));
+    }
+    all = lane64(lane_prefix_sum64(all, lane), 63);
+    return (int64_t)(lane_max(longest) - kSeqLongest) * workers * 7 <= all * 10;
   }
   // the item that holds unit x, which is below the total; head: sums(0)
   __device__ __forceinline__ Item find(int64_t x, const Sums& head) const {
@@ -473,7 +496,7 @@ struct Rows {
 };
 
 template <bool HALF, int D, int W, bool PAGED>
-__global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) {
+__global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void seq_attn_kernel(const WaSeqLaunch) {
   using C = SeqTile<D, W>;
   using T = SeqType<HALF>;
   constexpr int KB = C::KB, R = 32 * W;
@@ -488,7 +511,8 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
   bool whole = (W == 1 && !PAGED) || seq_args()->plan.whole;
   if (whole || !PAGED) {
     total = (int64_t)walk.above(0) * walk.cols;
-    whole |= total >= (int64_t)kSeqWhole * seq_args()->plan.workers;
+    const int workers = seq_args()->plan.workers;
+    if (!whole) whole = total >= (int64_t)kSeqWhole * workers || walk.even(workers);
   }
   if (me == 0 && tid == 0) *seq_args()->any_cut = !whole;
   if (whole) {
@@ -568,39 +592,59 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     from_b = x.b;
     from_keys = x.s.keys;
   };
-  // copies the tile of keys and of values at `key`; returns which 16 keys of it lie in no page
-  auto copy = [&](int key, int buf) -> uint32_t {
-    const uint32_t to = lds0 + buf * C::STAGE;
-    const int left = from_keys - key;
-    int lane_o = lane;
-    asm volatile("" : "+v"(lane_o));  // the last tiles' offsets are not held across the loop
-    if constexpr (!PAGED) {
-      krows.copy(kfrom, left, to, w, lane_o);
-      vrows.copy(vfrom, left, to + C::BYTES, w, lane_o);
-      kfrom += (uint64_t)KB * krows.token;
-      vfrom += (uint64_t)KB * vrows.token;
-      return 0;
-    } else {
-      const SeqArgs a = again(seq_args());
-      const int shift = a->page_shift, first = key >> shift;
+  // Paged: the pages of the tile at `key`; returns which 16 keys of it lie in none.
+  typedef int Ids[KB / 16];
+  auto pages_at = [&](int key, Ids& ids) -> uint32_t {
+    uint32_t none = 0;
+    if constexpr (PAGED) {
+      const int shift = again(seq_args())->page_shift, first = key >> shift;
       if (first >> 6 != window) {
         window = first >> 6;
         entry = from_b == ahead_b && window == ahead_window ? entry_ahead : load_entry(from_b, from_keys, key);
-        bad = __ballot((uint32_t)entry >= (uint32_t)a->n_pages);
+        bad = __ballot((uint32_t)entry >= (uint32_t)again(seq_args())->n_pages);
       }
-      uint32_t none = 0;
-      int ids[KB / 16];
 #pragma unroll
       for (int j = 0; j < KB / 16; ++j) {
         const int e = (key + 16 * j) >> shift & 63;
         ids[j] = __builtin_amdgcn_readlane(entry, e);
         if (bad >> e & 1) none |= 1u << j;
       }
-      const int at = key & ((1 << shift) - 1);
-      krows.copy_pages(kfrom, a->kp.page * 2, ids, none, at, shift, left, to, w, lane_o);
-      vrows.copy_pages(vfrom, a->vp.page * 2, ids, none, at, shift, left, to + C::BYTES, w, lane_o);
-      return none;
     }
+    return none;
+  };
+  // copies the tile of keys, and that of values, at `key`
+  auto copy_keys = [&](int key, int buf, const Ids& ids, uint32_t none) {
+    const uint32_t to = lds0 + buf * C::STAGE;
+    const int left = from_keys - key;
+    int lane_o = lane;
+    asm volatile("" : "+v"(lane_o));  // the last tiles' offsets are not held across the loop
+    if constexpr (PAGED) {
+      const SeqArgs a = again(seq_args());
+      krows.copy_pages(kfrom, a->kp.page * 2, ids, none, key & ((1 << a->page_shift) - 1), a->page_shift, left, to, w, lane_o);
+    } else {
+      krows.copy(kfrom, left, to, w, lane_o);
+      kfrom += (uint64_t)KB * krows.token;
+    }
+  };
+  auto copy_values = [&](int key, int buf, const Ids& ids, uint32_t none) {
+    const uint32_t to = lds0 + buf * C::STAGE + C::BYTES;
+    const int left = from_keys - key;
+    int lane_o = lane;
+    asm volatile("" : "+v"(lane_o));
+    if constexpr (PAGED) {
+      const SeqArgs a = again(seq_args());
+      vrows.copy_pages(vfrom, a->vp.page * 2, ids, none, key & ((1 << a->page_shift) - 1), a->page_shift, left, to, w, lane_o);
+    } else {
+      vrows.copy(vfrom, left, to, w, lane_o);
+      vfrom += (uint64_t)KB * vrows.token;
+    }
+  };
+  auto copy = [&](int key, int buf) -> uint32_t {
+    Ids ids;
+    const uint32_t none = pages_at(key, ids);
+    copy_keys(key, buf, ids, none);
+    copy_values(key, buf, ids, none);
+    return none;
   };
 
   // this lane's row of a tile: token i of head `sub`
@@ -629,7 +673,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
   f32x16 acc[C::DT];
   float m_run, l_run;
   const float c2 = seq_args()->scale * kLog2e;
-  // One tile of keys. limit: of the lane's query; none: 16 keys without a page.
+  // One wavefront: a tile of keys. limit: of the lane's query; none: 16 keys without a page.
   auto work = [&](int key, uint32_t t, int limit, bool masked, uint32_t none) {
     // The operands' offsets are taken from their first in every tile, whose place is added before, one exclusive or each (opaque, so
     // that all of them are not held all along).
@@ -715,6 +759,116 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     __builtin_amdgcn_s_setprio(0);
   };
 
+  // Four wavefronts: the scores of a tile of keys, at place t,
+  constexpr int ROWS = C::KS * C::KT, COLS = 2 * C::KT * C::DT;
+  auto scores = [&](f32x16 (&s)[C::KT], uint32_t t) {
+    uint32_t kb = kbase + t;
+    asm volatile("" : "+v"(kb));
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[kt][v] = 0.f;
+    bf16x8 ring[kSeqAhead];
+#pragma unroll
+    for (int x = 0; x < kSeqAhead; ++x) ring[x] = read_row(lds + row_step(kb, x / C::KT) + x % C::KT * 32 * C::RB);
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x) {
+      WA_SCHED_FENCE();
+      s[x % C::KT] = T::mfma(ring[x % kSeqAhead], qf[x / C::KT], s[x % C::KT]);
+      const int y = x + kSeqAhead;
+      if (y < ROWS) ring[x % kSeqAhead] = read_row(lds + row_step(kb, y / C::KT) + y % C::KT * 32 * C::RB);
+    }
+    WA_SCHED_FENCE();
+  };
+  // and what follows from them, `s`, for the tile at `key`, with the scores of the next tile, `sn`, if NEXT: the maxima and the first
+  // probabilities beside the products of those scores, the others beside those of O. For 128 columns the scores' part goes first on a
+  // SIMD (8,192 tokens, 14 heads over 2: 280 -> 258 us); for 64 columns, of which three wavefronts share a SIMD, it does not pay.
+  auto step = [&](auto with_next, f32x16 (&s)[C::KT], f32x16 (&sn)[C::KT], int key, uint32_t t, int limit, bool masked, uint32_t none) {
+    constexpr bool NEXT = decltype(with_next)::value;
+    constexpr int PAIRS = 8 * C::KT, BEFORE = D == 128 ? 10 : 4;  // pairs of probabilities; those beside the scores (6 to 12: no change)
+    uint32_t kb = kbase + (t ^ C::STAGE), vb0 = vbase0 + t, vb1 = vbase1 + t;
+    asm volatile("" : "+v"(kb), "+v"(vb0), "+v"(vb1));
+    auto key_row = [&](int x) { return read_row(lds + row_step(kb, x / C::KT) + x % C::KT * 32 * C::RB); };
+    auto col = [&](int x) {
+      const int at = x / C::DT * 16 * C::RB;
+      return read_cols(lds + col_step(vb0, x % C::DT) + at, lds + col_step(vb1, x % C::DT) + at);
+    };
+    if (masked) {
+      const int rest = limit - key - 4 * hf;
+#pragma unroll
+      for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (kt * 32 + 8 * (v >> 2) + (v & 3) >= rest || (PAGED && (none >> (2 * kt + (v >> 3)) & 1))) s[kt][v] = -INFINITY;
+    }
+    bf16x8 ring[kSeqAhead], cring[kSeqAhead];
+    if constexpr (NEXT) {
+#pragma unroll
+      for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sn[kt][v] = 0.f;
+#pragma unroll
+      for (int x = 0; x < kSeqAhead; ++x) ring[x] = key_row(x);
+    }
+    float top = -INFINITY, ref = 0.f;
+    auto rise = [&] {
+      top = max_halves(top) * c2;
+      const bool grow = top > m_run + kSeqGrow;  // also from -inf; a row that has seen no key keeps -inf
+      if (__ballot(grow)) {
+        const float m_new = grow ? top : m_run;
+        const float f = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+        m_run = m_new;
+        l_run *= f;
+#pragma unroll
+        for (int t2 = 0; t2 < C::DT; ++t2)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[t2][v] *= f;
+      }
+      ref = m_run == -INFINITY ? 0.f : m_run - T::kBias;
+    };
+    uint32_t pk[2 * C::KT][4];
+    auto pairs = [&](int from, int to) {  // of probabilities, four of 16 keys
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i)
+        if (i >= from && i < to) {
+          const int v = 2 * (i & 7);
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 3][v], c2, -ref));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 3][v + 1], c2, -ref));
+          l_run += p0 + p1;
+          pk[i >> 2][i & 3] = T::pack(p0, p1);
+          asm volatile("" : "+v"(l_run));  // added here
+        }
+    };
+    if (D == 128) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x) {
+      WA_SCHED_FENCE();
+      if constexpr (NEXT) {
+        sn[x % C::KT] = T::mfma(ring[x % kSeqAhead], qf[x / C::KT], sn[x % C::KT]);
+        if (x + kSeqAhead < ROWS) ring[x % kSeqAhead] = key_row(x + kSeqAhead);
+      }
+      if (x >= ROWS - kSeqAhead) cring[x - (ROWS - kSeqAhead)] = col(x - (ROWS - kSeqAhead));
+      if (x < 4) {
+#pragma unroll
+        for (int e = 0; e < 4 * C::KT; ++e) top = fmaxf(top, s[x / (4 / C::KT)][x % (4 / C::KT) * 4 * C::KT + e]);
+        if (x == 3) rise();
+      } else {
+        pairs((BEFORE * (x - 4) + ROWS - 5) / (ROWS - 4), (BEFORE * (x - 3) + ROWS - 5) / (ROWS - 4));
+      }
+    }
+    if (D == 128) __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+    for (int x = 0; x < COLS; ++x) {
+      WA_SCHED_FENCE();
+      const int k16 = x / C::DT, dt = x % C::DT;
+      acc[dt] = T::mfma(cring[x % kSeqAhead], as_bf16x8(make_uint4(pk[k16][0], pk[k16][1], pk[k16][2], pk[k16][3])), acc[dt]);
+      if (x + kSeqAhead < COLS) cring[x % kSeqAhead] = col(x + kSeqAhead);
+      constexpr int N = COLS - C::DT;
+      pairs(BEFORE + ((PAIRS - BEFORE) * x + N - 1) / N, BEFORE + ((PAIRS - BEFORE) * (x + 1) + N - 1) / N);
+    }
+    WA_SCHED_FENCE();
+  };
+
   int buf = 0;
   uint32_t none = 0, any_bad = 0;
   bool ready = false, stored = false;  // the item's first tile is on its way; stores of the item before come behind it
@@ -739,7 +893,20 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
         entry_ahead = load_entry(nx.b, nx.s.keys, rn.lo);
       }
     };
-    if (ready) {
+    Ids ids;  // of the next tile
+    uint32_t none_next = 0;
+    if constexpr (W == 4) {
+      if (r.lo < r.hi) {
+        WA_BARRIER();  // of the item before
+        aim(it, r.lo);
+        none = copy(r.lo, 0);
+        if (r.lo + KB < r.hi) {
+          none_next = pages_at(r.lo + KB, ids);
+          copy_keys(r.lo + KB, 1, ids, none_next);
+        }
+      }
+      load_queries(it, qf);
+    } else if (ready) {
 #pragma unroll
       for (int s = 0; s < C::KS; ++s) qf[s] = qn[s];
     } else {
@@ -769,7 +936,43 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
     m_run = -INFINITY;
     l_run = 0.f;
     ready = false;
-    for (int key = r.lo; key < r.hi; key += KB) {
+    if constexpr (W == 4) {
+      if (r.lo < r.hi) {
+        f32x16 sa[C::KT];
+        WA_WAIT_VM(0);
+        WA_BARRIER();
+        const int mine = min(some, r.hi);
+        if (r.lo < mine) scores(sa, 0);
+        int key = r.lo, at = 0;
+        uint32_t now = 0;
+        auto turn = [&] {
+          WA_WAIT_VM(0);
+          WA_BARRIER();  // everyone has the tile's values and the next one's keys, and is done with its keys and the values before
+          now = none;
+          if (PAGED) any_bad |= now;
+          none = none_next;
+          if (key + KB < r.hi) copy_values(key + KB, at ^ 1, ids, none_next);
+          if (key + 2 * KB < r.hi) {
+            none_next = pages_at(key + 2 * KB, ids);
+            copy_keys(key + 2 * KB, at, ids, none_next);
+          }
+        };
+        for (; key + KB < mine; key += KB, at ^= 1) {
+          turn();
+          f32x16 sn[C::KT];
+          step(std::true_type(), sa, sn, key, at * C::STAGE, limit, key + KB > all || (PAGED && now), now);
+#pragma unroll
+          for (int kt = 0; kt < C::KT; ++kt) sa[kt] = sn[kt];
+        }
+        if (key < mine) {
+          turn();
+          step(std::false_type(), sa, sa, key, at * C::STAGE, limit, key + KB > all || (PAGED && now), now);
+          key += KB;
+          at ^= 1;
+        }
+        for (; key < r.hi; key += KB, at ^= 1) turn();
+      }
+    } else for (int key = r.lo; key < r.hi; key += KB) {
       // This wavefront's part of the tile has arrived (and the queries, so that nothing waits for them below); stores behind it, at
       // least one for each eight columns that a lane holds, need not have.
       if (stored) WA_WAIT_VM(2 * C::DT); else WA_WAIT_VM(0);
@@ -786,8 +989,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
           load_queries(nx, qn);
         }
       }
-      uint32_t none_next = 0;
-      if (go) none_next = copy(next, buf ^ 1);
+      none_next = go ? copy(next, buf ^ 1) : 0;
       if (more && !known) look();  // early, so that the last tile's copies do not wait for it
       any_bad |= none;
       if (key < some) work(key, buf * C::STAGE, limit, key + KB > all || (PAGED && none), none);
@@ -798,7 +1000,7 @@ __global__ __launch_bounds__(64 * W, 2) void seq_attn_kernel(const WaSeqLaunch) 
 
     // the item's end: whole rows to O, others to the worker's partial tiles
     const float l = add_halves(l_run);
-    const float ref = m_run == -INFINITY ? -INFINITY : m_run - T::kBias;
+    const float ref = m_run != -INFINITY ? m_run - T::kBias : l == 0.f ? -INFINITY : 0.f;  // the last: NaN, which a join has to find
     const bool starts = begin <= it.at, finishes = it.at + it.units <= end;
     const Place p = place(it);
     stored = __ballot(p.valid) != 0;
@@ -1010,8 +1212,7 @@ constexpr int64_t kSeqManyParts = 12;
 template <bool HALF, int D, int W, bool PAGED>
 hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
   const int64_t most = wa_seq_most_tiles(a, a.plan);
-  const bool whole = a.plan.whole || (!PAGED && most >= (int64_t)kSeqWhole * a.plan.workers);
-  const int64_t grid = a.plan.whole ? most : whole ? std::max<int64_t>(most, a.plan.workers) : a.plan.workers;
+  const int64_t grid = a.plan.whole ? most : PAGED ? a.plan.workers : std::max<int64_t>(most, a.plan.workers);
   hipLaunchKernelGGL((seq_attn_kernel<HALF, D, W, PAGED>), dim3((unsigned)grid), dim3(64 * W), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if constexpr (W == 4 || PAGED) {  // packed sequences of so few tokens are never cut (wa_seq_plan)

@@ -349,10 +349,11 @@ def test_starts_outside_the_rows():
 @pytest.mark.gpu
 @pytest.mark.parametrize("lens,h,hk,d,dtype", [
     ([700, 0, 333, 1], 4, 2, 64, BF), ([700, 0, 333, 1], 4, 2, 128, BF), ([1, 900, 300], 3, 1, 128, FP), (([0] * 10 + [1500]) * 6, 1, 1, 64, BF),
-    ([1500, 700, 900, 1000], 32, 16, 64, BF)])
+    ([1500, 700, 900, 1000], 32, 16, 64, BF), ([2100, 0, 333, 1], 4, 2, 64, BF), ([1, 2100, 333], 4, 2, 128, BF), ([1300, 70], 7, 1, 128, FP),
+    ([1250, 1], 40, 1, 64, FP)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_cut_and_dealt_out(lens, h, hk, d, dtype, causal):
-    """Batches whose tiles are cut between workgroups; the last: one of more tiles than twice the workgroups, which are dealt out."""
+    """Tiles that are dealt out whole, some more than the chip's workgroups, and batches of few and long ones, which are cut."""
     check(make(lens, h, hk, d, dtype, front=2, spare=70), causal)
 
 
@@ -371,10 +372,10 @@ def test_sequences_that_overlap():
 @pytest.mark.gpu
 def test_workspaces():
     """What a workspace holds before does not matter; a smaller one is left alone; calls on two streams have their own."""
-    q, k, v, starts, dout = make([900, 340], 4, 2, 64)
+    q, k, v, starts, dout = make([1900, 340], 4, 2, 64)
     o, lse = W.packed_attn(q, k, v, starts, return_lse=True)
     grads = W.packed_attn_backward(dout, q, k, v, o, lse, starts)
-    need = W.packed_attn_workspace_size(1240, 2, 4, 2, 64), W.packed_attn_backward_workspace_size(1240, 2, 4, 2, 64)
+    need = W.packed_attn_workspace_size(2240, 2, 4, 2, 64), W.packed_attn_backward_workspace_size(2240, 2, 4, 2, 64)
     dirty = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in need]
     assert torch.equal(W.packed_attn(q, k, v, starts, workspace=dirty[0]), o)
     assert all(torch.equal(x, y) for x, y in zip(W.packed_attn_backward(dout, q, k, v, o, lse, starts, workspace=dirty[1]), grads))
@@ -392,3 +393,20 @@ def test_workspaces():
     torch.cuda.synchronize()
     for o2, g2 in got:
         assert torch.equal(o2, o) and all(torch.equal(x, y) for x, y in zip(g2, grads))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[2100, 340], [40, 60]])
+@pytest.mark.parametrize("d,dtype", [(64, FP), (128, BF)])
+def test_queries_that_are_not_finite(lens, d, dtype):
+    """A query of NaN or of infinities gives NaN in its row, and in no other, cut tiles or not."""
+    q, k, v, starts, _ = make(lens, 4, 2, d, dtype, fused=False)
+    o = W.packed_attn(q, k, v, starts)
+    rows, heads = [3, lens[0] - 1, sum(lens) - 2], [0, 3, 2]
+    for r, h, x in zip(rows, heads, (float("nan"), float("inf"), float("-inf"))):
+        q[r, h] = x
+    got = W.packed_attn(q, k, v, starts)
+    assert all(torch.isnan(got[r, h]).all() for r, h in zip(rows, heads))
+    for r, h in zip(rows, heads):
+        got[r, h], o[r, h] = 0, 0
+    assert torch.equal(got, o)
