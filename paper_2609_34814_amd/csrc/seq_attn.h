@@ -592,16 +592,29 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
     from_b = x.b;
     from_keys = x.s.keys;
   };
+  // What the copies of a tile need of the arguments, read at once.
+  struct Pool {
+    int shift, pages;
+    int64_t k, v;  // bytes of a page
+  };
+  auto pool = [&] {
+    Pool p{};
+    if constexpr (PAGED) {
+      const SeqArgs a = again(seq_args());
+      p = {a->page_shift, a->n_pages, a->kp.page * 2, a->vp.page * 2};
+    }
+    return p;
+  };
   // Paged: the pages of the tile at `key`; returns which 16 keys of it lie in none.
   typedef int Ids[KB / 16];
-  auto pages_at = [&](int key, Ids& ids) -> uint32_t {
+  auto pages_at = [&](const Pool& pl, int key, Ids& ids) -> uint32_t {
     uint32_t none = 0;
     if constexpr (PAGED) {
-      const int shift = again(seq_args())->page_shift, first = key >> shift;
+      const int shift = pl.shift, first = key >> shift;
       if (first >> 6 != window) {
         window = first >> 6;
         entry = from_b == ahead_b && window == ahead_window ? entry_ahead : load_entry(from_b, from_keys, key);
-        bad = __ballot((uint32_t)entry >= (uint32_t)again(seq_args())->n_pages);
+        bad = __ballot((uint32_t)entry >= (uint32_t)pl.pages);
       }
 #pragma unroll
       for (int j = 0; j < KB / 16; ++j) {
@@ -613,37 +626,36 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
     return none;
   };
   // copies the tile of keys, and that of values, at `key`
-  auto copy_keys = [&](int key, int buf, const Ids& ids, uint32_t none) {
+  auto copy_keys = [&](const Pool& pl, int key, int buf, const Ids& ids, uint32_t none) {
     const uint32_t to = lds0 + buf * C::STAGE;
     const int left = from_keys - key;
     int lane_o = lane;
     asm volatile("" : "+v"(lane_o));  // the last tiles' offsets are not held across the loop
     if constexpr (PAGED) {
-      const SeqArgs a = again(seq_args());
-      krows.copy_pages(kfrom, a->kp.page * 2, ids, none, key & ((1 << a->page_shift) - 1), a->page_shift, left, to, w, lane_o);
+      krows.copy_pages(kfrom, pl.k, ids, none, key & ((1 << pl.shift) - 1), pl.shift, left, to, w, lane_o);
     } else {
       krows.copy(kfrom, left, to, w, lane_o);
       kfrom += (uint64_t)KB * krows.token;
     }
   };
-  auto copy_values = [&](int key, int buf, const Ids& ids, uint32_t none) {
+  auto copy_values = [&](const Pool& pl, int key, int buf, const Ids& ids, uint32_t none) {
     const uint32_t to = lds0 + buf * C::STAGE + C::BYTES;
     const int left = from_keys - key;
     int lane_o = lane;
     asm volatile("" : "+v"(lane_o));
     if constexpr (PAGED) {
-      const SeqArgs a = again(seq_args());
-      vrows.copy_pages(vfrom, a->vp.page * 2, ids, none, key & ((1 << a->page_shift) - 1), a->page_shift, left, to, w, lane_o);
+      vrows.copy_pages(vfrom, pl.v, ids, none, key & ((1 << pl.shift) - 1), pl.shift, left, to, w, lane_o);
     } else {
       vrows.copy(vfrom, left, to, w, lane_o);
       vfrom += (uint64_t)KB * vrows.token;
     }
   };
   auto copy = [&](int key, int buf) -> uint32_t {
+    const Pool pl = pool();
     Ids ids;
-    const uint32_t none = pages_at(key, ids);
-    copy_keys(key, buf, ids, none);
-    copy_values(key, buf, ids, none);
+    const uint32_t none = pages_at(pl, key, ids);
+    copy_keys(pl, key, buf, ids, none);
+    copy_values(pl, key, buf, ids, none);
     return none;
   };
 
@@ -901,8 +913,9 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
         aim(it, r.lo);
         none = copy(r.lo, 0);
         if (r.lo + KB < r.hi) {
-          none_next = pages_at(r.lo + KB, ids);
-          copy_keys(r.lo + KB, 1, ids, none_next);
+          const Pool pl = pool();
+          none_next = pages_at(pl, r.lo + KB, ids);
+          copy_keys(pl, r.lo + KB, 1, ids, none_next);
         }
       }
       load_queries(it, qf);
@@ -946,15 +959,16 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
         int key = r.lo, at = 0;
         uint32_t now = 0;
         auto turn = [&] {
+          const Pool pl = pool();
           WA_WAIT_VM(0);
           WA_BARRIER();  // everyone has the tile's values and the next one's keys, and is done with its keys and the values before
           now = none;
           if (PAGED) any_bad |= now;
           none = none_next;
-          if (key + KB < r.hi) copy_values(key + KB, at ^ 1, ids, none_next);
+          if (key + KB < r.hi) copy_values(pl, key + KB, at ^ 1, ids, none_next);
           if (key + 2 * KB < r.hi) {
-            none_next = pages_at(key + 2 * KB, ids);
-            copy_keys(key + 2 * KB, at, ids, none_next);
+            none_next = pages_at(pl, key + 2 * KB, ids);
+            copy_keys(pl, key + 2 * KB, at, ids, none_next);
           }
         };
         for (; key + KB < mine; key += KB, at ^= 1) {
