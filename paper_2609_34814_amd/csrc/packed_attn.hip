@@ -27,7 +27,7 @@ WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
   // token of 32 sequences 162 us with 1,024, 197 with 1,280).
   p.workers = p.waves == 4 ? 512 : 1024;
   p.min_units = 4;
-  // Calls whose tiles are never cut need no second kernel. Packed: tiles of fifteen tiles of keys at most (kSeqLongest), many short sequences
+  // Calls whose tiles are never cut need no second kernel. Packed: tiles of fifteen tiles of keys at most, many short sequences
   // (1,000 tokens of 16: 21.7 -> 14.4 us), and those of one wavefront a tile. Over a cache, whose lengths the host does not know, tables of
   // few keys: few keys a tile take less time than a join (one wavefront: 100 sequences of up to 300 keys 23.5 -> 19.7 us, but 16 of 500
   // 19.6 -> 24.6; four: 512 tokens of 32 heads 25.0 -> 18.0).

@@ -40,11 +40,14 @@ namespace wa {
 
 constexpr float kSeqGrow = 8.f;  // log2 units
 constexpr int kSeqAhead = 4;     // operands read ahead
-// Packed tiles are dealt out whole where there are so many times the workers of them, and where the longest takes no longer than the line
-// would: with parts to store and to join, a worker's share s takes about 22 + 2.2 s us, whole tiles 4 + 1.05 longest + 0.7 s, so where
-// longest <= 17 + 10/7 s (d 128, in tiles of 64 keys; d 64 about the same). 2,400 tokens of 3 prompts, 32 heads over 8: 59 us along the
-// line, 44 whole; 8,192 of one, 8 heads over 1: 168 and 185.
+// Packed tiles are dealt out whole where there are so many times the workers of them, and where that takes no longer than the line, in
+// which a worker's share of s units takes about 22 + 2.2 s us, with parts to store and to join (d 128, units of 64 keys; d 64 about the same).
+// Causal: whole tiles, of all lengths, take 4 + 1.05 longest + 0.7 s, so where longest <= 17 + 10/7 s. 2,400 tokens of 3 prompts, 32 heads over
+// 8: 59 us along the line, 44 whole; 8,192 of one, 8 heads over 1: 168 and 185.
+// Else tiles are about equal, and a last round of few of them counts: it takes 0.58 of a full one if it is half full or less. 6,000 tokens of
+// 16 heads, 752 tiles: 323 us along the line, 298 whole; 4,800, 608 tiles: 207 and 251.
 constexpr int kSeqWhole = 4, kSeqLongest = 17;
+
 // What a tile costs beside its keys, in tiles of keys.
 constexpr int kSeqFixed = 2;
 
@@ -229,7 +232,7 @@ struct Walk {
     for (int base = 64; base < batch; base += 64) sum += lane64(sums(base).upto, 63);
     return sum;
   }
-  // whether the longest tile is hardly longer than a share (see kSeqLongest)
+  // whether tiles are dealt out whole (see kSeqWhole)
   __device__ __forceinline__ bool even(int workers) const {
     int64_t all = 0;
     int longest = 0;
@@ -243,7 +246,10 @@ struct Walk {
       longest = max(longest, (int)(units - l.upto(t - 1)));
     }
     all = lane64(lane_prefix_sum64(all, lane), 63);
-    return (int64_t)(lane_max(longest) - kSeqLongest) * workers * 7 <= all * 10;
+    longest = lane_max(longest);
+    if (causal) return (int64_t)(longest - kSeqLongest) * workers * 7 <= all * 10;
+    const int64_t round = (int64_t)max(longest, 1) * workers, last = all - (int64_t)divide(all, round) * round;
+    return last == 0 || 58 * round - 100 * last <= (int64_t)1000 * workers + 9 * all;
   }
   // the item that holds unit x, which is below the total; head: sums(0)
   __device__ __forceinline__ Item find(int64_t x, const Sums& head) const {
@@ -512,7 +518,7 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
   if (whole || !PAGED) {
     total = (int64_t)walk.above(0) * walk.cols;
     const int workers = seq_args()->plan.workers;
-    if (!whole) whole = total >= (int64_t)kSeqWhole * workers || walk.even(workers);
+    if (!whole) whole = total >= (int64_t)(walk.causal ? kSeqWhole : 2 * kSeqWhole) * workers || walk.even(workers);
   }
   if (me == 0 && tid == 0) *seq_args()->any_cut = !whole;
   if (whole) {
