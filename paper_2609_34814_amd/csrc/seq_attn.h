@@ -18,14 +18,13 @@
 //
 // Who computes what. The lengths are known on the device only; each workgroup finds its work itself from the lengths, a sequence a lane,
 // which costs no launch before this one.
-//   Many tiles of packed sequences, or ones of about equal length: a workgroup a tile, those with the most keys first, so that the chip stays full to the end, and
-//   those that run together read the same keys at about the same time (one prompt of 32,768 tokens, 32 heads over 8, d 128: 9.6 ms where
-//   equal shares of the work begin anywhere in a tile, 8.2 so, when both were measured).
-//   Others, and those of a paged cache: the work is a line of units, one for each tile of keys of each query tile and two for its
-//   beginning and end, sequence after sequence and within one key head after key head. Worker w of G takes the units [w U / G, (w + 1) U / G),
-//   found by a closed form, so all workers have the same to do whatever the lengths are. A border within a sixteenth of a share of a tile's
-//   end is moved there. A tile that several workers compute is joined by a second kernel, in key order: nothing is added with
-//   atomics, and equal calls give equal bits.
+//   Many tiles of four wavefronts, or ones of about equal length: a workgroup a tile, of packed sequences those with the most keys first, so
+//   that the chip stays full to the end, and those that run together read the same keys at about the same time (one prompt of 32,768 tokens,
+//   32 heads over 8, d 128: 9.6 ms where equal shares of the work begin anywhere in a tile, 8.2 so, when both were measured).
+//   Others: the work is a line of units, one for each tile of keys of each query tile and two for its beginning and end, sequence after
+//   sequence and within one key head after key head. Worker w of G takes the units [w U / G, (w + 1) U / G), found by a closed form, so all
+//   workers have the same to do whatever the lengths are. A border within a sixteenth of a share of a tile's end is moved there. A tile
+//   that several workers compute is joined by a second kernel, in key order: nothing is added with atomics, and equal calls give equal bits.
 //   Calls of few keys, and packed sequences of few tokens: a workgroup a tile, without the second kernel.
 #pragma once
 
@@ -40,12 +39,13 @@ namespace wa {
 
 constexpr float kSeqGrow = 8.f;  // log2 units
 constexpr int kSeqAhead = 4;     // operands read ahead
-// Packed tiles are dealt out whole where there are so many times the workers of them, and where that takes no longer than the line, in
+// Tiles of four wavefronts are dealt out whole where there are so many times the workers of them, and where that takes no longer than the line, in
 // which a worker's share of s units takes about 22 + 2.2 s us, with parts to store and to join (d 128, units of 64 keys; d 64 about the same).
 // Causal: whole tiles, of all lengths, take 4 + 1.05 longest + 0.7 s, so where longest <= 17 + 10/7 s. 2,400 tokens of 3 prompts, 32 heads over
 // 8: 59 us along the line, 44 whole; 8,192 of one, 8 heads over 1: 168 and 185.
-// Else tiles are about equal, and a last round of few of them counts: it takes 0.58 of a full one if it is half full or less. 6,000 tokens of
-// 16 heads, 752 tiles: 323 us along the line, 298 whole; 4,800, 608 tiles: 207 and 251.
+// Not causal, or behind many cached keys, tiles are about equal, and a last round of few of them counts: it takes 0.65 of a full one if it is
+// half full or less, else 0.9. 6,000 tokens of 16 heads, not causal, 752 tiles: 323 us along the line, 298 whole; 4,800, 608 tiles: 207 and 251;
+// over a cache 4,096 tokens behind 12,288, 32 heads over 8: 955 and 908; 1,024 behind 7,168: 152 and 175.
 constexpr int kSeqWhole = 4, kSeqLongest = 17;
 
 // What a tile costs beside its keys, in tiles of keys.
@@ -247,9 +247,9 @@ struct Walk {
     }
     all = lane64(lane_prefix_sum64(all, lane), 63);
     longest = lane_max(longest);
-    if (causal) return (int64_t)(longest - kSeqLongest) * workers * 7 <= all * 10;
+    if (!PAGED && causal) return (int64_t)(longest - kSeqLongest) * workers * 7 <= all * 10;
     const int64_t round = (int64_t)max(longest, 1) * workers, last = all - (int64_t)divide(all, round) * round;
-    return last == 0 || 58 * round - 100 * last <= (int64_t)1000 * workers + 9 * all;
+    return last == 0 || (2 * last > round ? 90 : 65) * round - 100 * last <= (int64_t)1000 * workers + 9 * all;
   }
   // the item that holds unit x, which is below the total; head: sums(0)
   __device__ __forceinline__ Item find(int64_t x, const Sums& head) const {
@@ -515,10 +515,10 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
   Item it;
   int me = blockIdx.x;
   bool whole = (W == 1 && !PAGED) || seq_args()->plan.whole;
-  if (whole || !PAGED) {
+  if (whole || !PAGED || W == 4) {
     total = (int64_t)walk.above(0) * walk.cols;
     const int workers = seq_args()->plan.workers;
-    if (!whole) whole = total >= (int64_t)(walk.causal ? kSeqWhole : 2 * kSeqWhole) * workers || walk.even(workers);
+    if (!whole) whole = total >= (int64_t)(!PAGED && walk.causal ? kSeqWhole : 2 * kSeqWhole) * workers || walk.even(workers);
   }
   if (me == 0 && tid == 0) *seq_args()->any_cut = !whole;
   if (whole) {
@@ -1232,7 +1232,7 @@ constexpr int64_t kSeqManyParts = 12;
 template <bool HALF, int D, int W, bool PAGED>
 hipError_t seq_launch(const WaSeqLaunch& a, hipStream_t stream) {
   const int64_t most = wa_seq_most_tiles(a, a.plan);
-  const int64_t grid = a.plan.whole ? most : PAGED ? a.plan.workers : std::max<int64_t>(most, a.plan.workers);
+  const int64_t grid = a.plan.whole ? most : PAGED && W == 1 ? a.plan.workers : std::max<int64_t>(most, a.plan.workers);
   hipLaunchKernelGGL((seq_attn_kernel<HALF, D, W, PAGED>), dim3((unsigned)grid), dim3(64 * W), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if constexpr (W == 4 || PAGED) {  // packed sequences of so few tokens are never cut (wa_seq_plan)

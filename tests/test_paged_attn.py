@@ -343,3 +343,13 @@ def test_fork_and_compact_between_tokens():
     assert used.item() == 5 and refs.tolist() == [2, 2, 1, 1, 1] + [0] * 15
     tokens([0, 9, 1, 0])
     tokens([5, 1, 0, 1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,new,h,hk,d,dtype", [
+    ([900, 500, 1300], [300, 500, 64], 32, 8, 64, BF), ([900, 500, 1300], [300, 500, 64], 32, 8, 128, FP),
+    ([400] * 70, [60, 0] * 35, 16, 2, 64, BF), ([3000, 200], [500, 1], 4, 1, 128, BF)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_chunks_whole_and_cut(lens, new, h, hk, d, dtype, causal):
+    """Chunks whose tiles are dealt out whole, and long ones that are cut between workgroups."""
+    check(lens, new, h, hk, d, 16, dtype, causal)
