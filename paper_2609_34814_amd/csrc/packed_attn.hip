@@ -23,7 +23,7 @@ WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
     p.per_tile = 1;
     p.log_tokens = log_tokens(1);
   }
-  // Workgroups that the chip holds: two a compute unit of four wavefronts, four of one (a fifth does not fit beside the LDS of four: one
+  // Workgroups that the chip holds: two a compute unit of four wavefronts (of d 64 three fit, which as workers are no faster), four of one (a fifth does not fit beside the LDS of four: one
   // token of 32 sequences 162 us with 1,024, 197 with 1,280).
   p.workers = p.waves == 4 ? 512 : 1024;
   p.min_units = 4;

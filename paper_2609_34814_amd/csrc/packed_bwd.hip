@@ -7,8 +7,8 @@
 //   queries  128 queries of a head, over their keys: dQ.
 // They run in one launch, those of keys first, which take longer, so that the others fill the chip while the last of them end (8,192 tokens of 7
 // documents, 16 heads over 4, d 128: 163 + 121 us one after another, 240 together: 0.93 PFLOP/s of the seven products, matrix cores 50% busy;
-// what bounds it is two wavefronts a SIMD that take turns at products and exponentials). Long tiles are computed in parts, which packed_parts_kernel adds
-// in order.
+// what bounds it is two wavefronts a SIMD that take turns at products and exponentials). Long tiles are computed in parts, which
+// packed_parts_kernel adds in order.
 // Both recompute the scores and dP. A wavefront holds 32 queries (keys) with their accumulators in registers, and the other side's
 // tiles pass through LDS, copied one ahead. Scores come out with the wavefront's own index in the lanes and the other in the
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are. Two wavefronts share a SIMD; the one that is
@@ -71,7 +71,8 @@ struct Job {
 
 // All tiles of all sequences and `cols` heads, longest first, those longer than `most` in parts of about equal length: `most` takes as
 // long as a 512th of all work, so that a call of few tiles fills the chip's workgroups (two a compute unit) once, and one of many is not cut.
-// Sequences that overlap (starts that descend) could have more tiles and parts than there is room for: they have no jobs. A pair of a key and a query takes four products for dK and dV and three for dQ.
+// Sequences that overlap (starts that descend) could have more tiles and parts than there is room for: they have no jobs. A pair of a
+// key and a query takes four products for dK and dV and three for dQ.
 // Causal tiles have the lengths 1 to T of a sequence of T tiles, others T. Each workgroup finds its job itself: the lengths are on the
 // device. The first 64 sequences are held, one a lane.
 struct Jobs {
