@@ -821,7 +821,7 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, ta
     to = _rows(o, "out", q.dtype, q.shape)
     _int32(status, "status", (1,))
     index = _index(q=q, k_pages=k_pages, v_pages=v_pages, tables=tables, starts=starts, kv_lens=kv_lens, out=out,
-                        status=status, workspace=workspace)
+                   status=status, workspace=workspace)
     workspace = _room(workspace, _seq_size("wa_seq_attn_workspace_size", shape), q.device)
     lse = q.new_empty((h, t), dtype=torch.float32) if return_lse else None
     _call_on(index, lib.wa_paged_attn, *args, starts.data_ptr(), kv_lens.data_ptr(), shape,
@@ -908,7 +908,7 @@ def page_fork(pool: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor, lens
     _int32(children, "children", (n,))
     _int32(status, "status", (1,))
     index = _index(pool=pool, refs=refs, tables=tables, lens=lens, parents=parents, children=children, status=status,
-                        workspace=workspace)
+                   workspace=workspace)
     workspace = _room(workspace, _seq_size("wa_page_workspace_size", _page_sizes(refs, tables, page), n), refs.device)
     _call_on(index, lib.wa_page_fork, state, at, parents.data_ptr(), children.data_ptr(), n, _ptr(status), workspace.data_ptr(),
              workspace.numel())
@@ -939,7 +939,7 @@ def page_compact(pool: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor, l
     _int32(used, "used", (1,))
     _int32(status, "status", (1,))
     index = _index(pool=pool, refs=refs, tables=tables, lens=lens, out_refs=out_refs, out_tables=out_tables, used=used,
-                        status=status, workspace=workspace)
+                   status=status, workspace=workspace)
     workspace = _room(workspace, _seq_size("wa_page_workspace_size", _page_sizes(refs, tables, page), 0), refs.device)
     _call_on(index, lib.wa_page_compact, state, at, _ptr(refs if out_refs is None else out_refs),
              _ptr(tables if out_tables is None else out_tables), _ptr(used), _ptr(status), workspace.data_ptr(), workspace.numel())
