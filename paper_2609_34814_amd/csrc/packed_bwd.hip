@@ -74,30 +74,46 @@ struct Job {
 // Sequences that overlap (starts that descend) could have more tiles and parts than there is room for: they have no jobs. A pair of a
 // key and a query takes four products for dK and dV and three for dQ.
 // Causal tiles have the lengths 1 to T of a sequence of T tiles, others T. Each workgroup finds its job itself: the lengths are on the
-// device. The first 64 sequences are held, one a lane.
+// device. The tiles of the first 64 kHeld sequences are held, one a lane.
+template <int kHeld>
 struct Jobs {
   SeqArgs a;
-  int lane, cols, batch, mine, most;
+  int lane, cols, batch, held[kHeld], most;
   bool causal, queries;
 
   // share: of the kind of jobs in all work, in sevenths
   __device__ __forceinline__ Jobs(int lane_, int cols_, int share, bool queries_)
       : a(seq_args()), lane(lane_), cols(cols_), batch(a->batch), causal(a->causal), queries(queries_) {
     int64_t sum = 0, tokens = 0;
-    for (int base = 0; base < batch; base += 64) {
-      const int n = tokens_of(base + lane);
-      const int64_t t = tiles(n);
-      if (base == 0) mine = (int)t;
-      tokens += n;
+    int n[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) n[i] = 64 * i < batch ? tokens_of(64 * i + lane) : 0;
+    auto add = [&](int x) {
+      const int64_t t = tiles(x);
+      tokens += x;
       sum += causal ? t * (t + 1) / 2 : t * t;
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      held[i] = tiles(n[i]);
+      if (64 * i < batch) add(n[i]);
     }
-    if (lane64(lane_prefix_sum64(tokens, lane), 63) > again(a)->tokens) batch = mine = 0;
+    for (int base = 64 * kHeld; base < batch; base += 64) add(tokens_of(base + lane));
+    if (lane64(lane_prefix_sum64(tokens, lane), 63) > again(a)->tokens) batch = 0;
     sum = lane64(lane_prefix_sum64(sum, lane), 63) * cols;
     most = (int)((uint64_t)(7 * sum + share * kSlots - 1) / (share * kSlots));
   }
   __device__ __forceinline__ int tokens_of(int b) const { return b < batch ? seq_of<false>(again(a), b).n : 0; }
   static __device__ __forceinline__ int tiles(int n) { return (n + kRows - 1) / kRows; }
-  __device__ __forceinline__ int tiles_at(int base) const { return base == 0 ? mine : tiles(tokens_of(base + lane)); }
+  // f(first sequence, tiles of sequence first + lane) for all, while it says so
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (64 * i >= batch || !f(64 * i, held[i])) return;
+    for (int base = 64 * kHeld; base < batch; base += 64)
+      if (!f(base, tiles(tokens_of(base + lane)))) return;
+  }
   __device__ __forceinline__ int parts_of(int length) const { return (length + most - 1) / most; }
   // jobs of the first x lengths of a sequence
   __device__ __forceinline__ int upto(int x) const {
@@ -107,25 +123,28 @@ struct Jobs {
   // those of tiles longer than `length`, of one column
   __device__ __forceinline__ int above(int length) const {
     int sum = 0;
-    for (int base = 0; base < batch; base += 64) {
-      const int t = tiles_at(base);
-      sum += lane_sum(t <= length ? 0 : causal ? upto(t) - upto(length) : t * parts_of(t));
-    }
-    return sum;
+    each([&](int, int t) {
+      sum += t <= length ? 0 : causal ? upto(t) - upto(length) : t * parts_of(t);
+      return true;
+    });
+    return lane_sum(sum);
   }
   // tiles longer than `length`, of one column
   __device__ __forceinline__ int longer(int length) const {
     int sum = 0;
-    for (int base = 0; base < batch; base += 64) {
-      const int t = tiles_at(base);
-      sum += lane_sum(t <= length ? 0 : causal ? t - length : t);
-    }
-    return sum;
+    each([&](int, int t) {
+      sum += t <= length ? 0 : causal ? t - length : t;
+      return true;
+    });
+    return lane_sum(sum);
   }
   // job number `rank`; false if there is none
   __device__ __forceinline__ bool find(int64_t rank, Job* job) const {
     int lo = 0, hi = 0, passed = 0;  // above(lo) > row of jobs >= above(hi) = passed
-    for (int base = 0; base < batch; base += 64) hi = max(hi, tiles_at(base));
+    each([&](int, int t) {
+      hi = max(hi, t);
+      return true;
+    });
     hi = lane_max(hi);
     const int row = (int)(rank / cols);
     if (row >= above(0)) return false;
@@ -146,19 +165,19 @@ struct Jobs {
     job->col = spread((int)(rank - (int64_t)row * cols), cols);
     // the k-th tile of this length
     int who = 0, tile = 0, t = 0;
-    for (int base = 0; base < batch; base += 64) {
-      t = tiles_at(base);
-      const int n = causal ? t >= hi : t == hi ? t : 0, sum = lane_prefix_sum(n);
+    each([&](int base, int x) {
+      const int n = causal ? x >= hi : x == hi ? x : 0, sum = lane_prefix_sum(n);
       const uint64_t past = __ballot(sum > k);
       if (past) {
         const int l = __builtin_ctzll(past);
         who = base + l;
         tile = k - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(n, l));
-        t = __builtin_amdgcn_readlane(t, l);
-        break;
+        t = __builtin_amdgcn_readlane(x, l);
+        return false;
       }
       k -= __builtin_amdgcn_readlane(sum, 63);
-    }
+      return true;
+    });
     job->b = __builtin_amdgcn_readfirstlane(who);
     job->tile = __builtin_amdgcn_readfirstlane(tile);
     t = __builtin_amdgcn_readfirstlane(t);
@@ -174,8 +193,9 @@ struct Cuts {
   int4 tile[kMostParts / 2];
 };
 // The job of a workgroup; false if there is none.
-__device__ __forceinline__ bool take_job(const WaSeqLaunch& a, bool queries, int64_t rank, int cols, int share, Job* job) {
-  const Jobs jobs(threadIdx.x & 63, cols, share, queries);
+template <int kHeld>
+__device__ __forceinline__ bool find_job(const WaSeqLaunch& a, bool queries, int64_t rank, int cols, int share, Job* job) {
+  const Jobs<kHeld> jobs(threadIdx.x & 63, cols, share, queries);
   Cuts* cuts = (Cuts*)a.cut_tiles + (queries ? 0 : 1);
   if (rank == 0) {
     const int n = jobs.longer(jobs.most) * cols;
@@ -184,6 +204,11 @@ __device__ __forceinline__ bool take_job(const WaSeqLaunch& a, bool queries, int
   if (!jobs.find(rank, job)) return false;
   if (job->parts > 1 && job->part == 0 && threadIdx.x == 0) cuts->tile[job->number] = make_int4(job->b, job->tile, (int)rank, job->parts);
   return true;
+}
+// Up to 64 sequences have a path of their own (a step of 2,311 tokens in 5 documents: 55 us, 57 along the other, which takes 160 where one
+// that holds 64 takes 219: the gradient of 600 documents of 30 tokens, 8 heads of 64).
+__device__ __forceinline__ bool take_job(const WaSeqLaunch& a, bool queries, int64_t rank, int cols, int share, Job* job) {
+  return a.batch <= 64 ? find_job<1>(a, queries, rank, cols, share, job) : find_job<8>(a, queries, rank, cols, share, job);
 }
 
 // Rows [row, row + ROWS) of g (`token` bytes apart) into a tile; rows past `last` are that row again.
@@ -531,7 +556,7 @@ __device__ __forceinline__ void key_job(const WaSeqLaunch& a, int64_t rank, unsi
 }
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void packed_grad_kernel(const WaSeqLaunch a, int key_jobs) {
+__global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void packed_grad_kernel(const WaSeqLaunch a, int key_jobs) {
   using C = Bwd<D>;
   constexpr int KEYS = 4 * C::QB * C::RB + (C::kValuesInLds ? kRows * C::RB : 0), QUERIES = 4 * C::KB * C::RB;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[KEYS > QUERIES ? KEYS : QUERIES];

@@ -309,22 +309,48 @@ struct Walk {
     scalar(it);
   }
 
-  // Tiles of one column that are number t and above in their sequences.
-  __device__ __forceinline__ int above(int t) const {
+  // Tiles of the sequences of one column, those of the first 512 held, one a lane, so that they are read once.
+  struct Counts {
+    static constexpr int kHeld = 8;
+    int c[kHeld];
+  };
+  __device__ __forceinline__ Counts counts() const {
+    Counts x;
+#pragma unroll
+    for (int i = 0; i < Counts::kHeld; ++i) x.c[i] = i == 0 ? tiles(mine) : 64 * i < batch ? tiles(seq_at(64 * i)) : 0;
+    return x;
+  }
+  // f(first sequence, tiles of sequence first + lane) for all, while it says so
+  template <typename F>
+  __device__ __forceinline__ void each(const Counts& x, F&& f) const {
+#pragma unroll
+    for (int i = 0; i < Counts::kHeld; ++i)
+      if (64 * i >= batch || !f(64 * i, x.c[i])) return;
+    for (int base = 64 * Counts::kHeld; base < batch; base += 64)
+      if (!f(base, tiles(seq_at(base)))) return;
+  }
+  // tiles that are number t and above in their sequences
+  __device__ __forceinline__ int above(const Counts& x, int t) const {
     int sum = 0;
-    for (int base = 0; base < batch; base += 64) sum += lane_sum(max(tiles(seq_at(base)) - t, 0));
-    return sum;
+    each(x, [&](int, int n) {
+      sum += max(n - t, 0);
+      return true;
+    });
+    return lane_sum(sum);
   }
   // Tile `rank` of all, by falling number: of packed sequences those that see the most keys first. rank is below above(0) cols.
-  __device__ __forceinline__ Item ranked(int64_t rank) const {
+  __device__ __forceinline__ Item ranked(const Counts& x, int64_t rank) const {
     const int row = (int)divide(rank, cols);
     Item it;
     it.col = (int)(rank - (int64_t)row * cols);
     int most = 0;
-    for (int base = 0; base < batch; base += 64) most = max(most, tiles(seq_at(base)));
+    each(x, [&](int, int n) {
+      most = max(most, n);
+      return true;
+    });
     int lo = 0, hi = lane_max(most), passed = 0;  // above(lo) > row >= above(hi) = passed
     while (hi - lo > 1) {
-      const int mid = lo + ((hi - lo) >> 1), m = above(mid);
+      const int mid = lo + ((hi - lo) >> 1), m = above(x, mid);
       if (m > row) {
         lo = mid;
       } else {
@@ -333,16 +359,17 @@ struct Walk {
       }
     }
     int k = row - passed, who = 0;
-    for (int base = 0; base < batch; base += 64) {
-      uint64_t there = __ballot(tiles(seq_at(base)) > lo);
+    each(x, [&](int base, int n) {
+      uint64_t there = __ballot(n > lo);
       const int m = __popcll(there);
       if (k < m) {
         for (; k > 0; --k) there &= there - 1;
         who = base + __builtin_ctzll(there);
-        break;
+        return false;
       }
       k -= m;
-    }
+      return true;
+    });
     it.b = __builtin_amdgcn_readfirstlane(who);
     it.tile = lo;
     it.s = seq(it.b);
@@ -515,15 +542,17 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
   Item it;
   int me = blockIdx.x;
   bool whole = (W == 1 && !PAGED) || seq_args()->plan.whole;
+  typename Walk<PAGED, C::LOG_KB>::Counts counts;
   if (whole || !PAGED || W == 4) {
-    total = (int64_t)walk.above(0) * walk.cols;
+    counts = walk.counts();
+    total = (int64_t)walk.above(counts, 0) * walk.cols;
     const int workers = seq_args()->plan.workers;
     if (!whole) whole = total >= (int64_t)(!PAGED && walk.causal ? kSeqWhole : 2 * kSeqWhole) * workers || walk.even(workers);
   }
   if (me == 0 && tid == 0) *seq_args()->any_cut = !whole;
   if (whole) {
     if (me >= total) return;
-    it = walk.ranked(me);
+    it = walk.ranked(counts, me);
     begin = 0;
     end = it.units;
   } else {

@@ -410,3 +410,13 @@ def test_queries_that_are_not_finite(lens, d, dtype):
     for r, h in zip(rows, heads):
         got[r, h], o[r, h] = 0, 0
     assert torch.equal(got, o)
+
+
+@pytest.mark.gpu
+def test_hundreds_of_sequences():
+    """More than the 512 whose lengths are held: 700 short ones with long ones between them."""
+    rng = np.random.default_rng(7)
+    lens = [int(x) for x in rng.integers(0, 7, 700)]
+    lens[3], lens[555], lens[690] = 300, 260, 140
+    check(make(lens, 2, 1, 64))
+    check(make(lens, 2, 2, 128), causal=False)
