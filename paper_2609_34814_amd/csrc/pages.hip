@@ -74,11 +74,13 @@ __global__ __launch_bounds__(kThreads) void page_grow_kernel(const WaPageLaunch 
     const int have = pages_of(a.lens[s], a.shift), want = pages_of(a.first[s], a.shift);
     return want <= have ? 0 : want > a.width ? kNone : want - have;
   };
-  int wanted = 0;  // no more than there are
+  // Pages wanted in all, where a need past the pool counts as one page more than it has, so that it always leaves `have` behind (1,024 needs
+  // of up to 2^20 pages fit an int).
+  int wanted = 0;
   for (int base = 0; base < a.sequences; base += kThreads) {
     const int s = base + threadIdx.x, n = s < a.sequences ? need(s) : 0;
     int total;
-    const int at = before_me<kThreads>(min(max(n, 0), a.n_pages), &total, lds);
+    const int at = before_me<kThreads>(min(max(n, 0), a.n_pages + 1), &total, lds);
     if (s < a.sequences) offset[s] = (int)min((int64_t)wanted + at, (int64_t)INT32_MAX);
     if (n == kNone) report(a.status, WA_PAGE_EXHAUSTED);
     wanted = (int)min((int64_t)wanted + total, (int64_t)a.n_pages + 1);
@@ -104,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void page_grow_kernel(const WaPageLaunch 
   __syncthreads();
   for (int s = threadIdx.x >> 6; s < a.sequences; s += kThreads / 64) {
     const int n = need(s), from = offset[s], have_pages = pages_of(a.lens[s], a.shift);
-    if (n == kNone || from == kNone) continue;
+    if (n == kNone || from == kNone || n > have - from) continue;
     for (int i = lane; i < n; i += 64) {
       const int p = list[from + i];
       a.tables[(int64_t)s * a.width + have_pages + i] = p;

@@ -310,3 +310,28 @@ def test_growth_past_the_pool():
     for _ in range(3):
         both.grow([rng.choice([0, n, n + rng.randint(1, 20), 48, 49]) for n in both.h[2]])
     assert both.want == P.EXHAUSTED and min(both.h[0]) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [[96, 0], [96, 33], [33, 96], [64, 0], [0, 65], [96, 96], [64, 1], [129, 96]])
+@pytest.mark.parametrize("lens", [[0, 0], [16, 0], [0, 40]])
+def test_growth_past_an_empty_pool(new, lens):
+    """A prompt of more pages than the pool has, in a table with room for it, alone and beside one that fits; the workspace holds page 0
+    everywhere, so that what is read past the free pages shows in the tables."""
+    both = Both(4, 2, 8, 16)
+    both.grow(lens)
+    work = torch.zeros(W.page_workspace_size(4, 2, 8, page=16), dtype=torch.uint8, device="cuda")
+    W.page_grow(*both.state(), both.dev(new), page=16, status=both.status, workspace=work)
+    both.want |= P.grow(*both.h, new, 16)
+    both.check()
+
+
+@pytest.mark.gpu
+def test_growth_of_one_past_a_large_pool():
+    """The same with more sequences than a workgroup has threads: each alone wants more than there is, then all want something."""
+    both = Both(1000, 1100, 1200, 1)
+    for s in (0, 1030, 1099):
+        both.grow([1001 if i == s else 0 for i in range(1100)])
+        assert both.h[2] == [0] * 1100 and both.want == P.EXHAUSTED
+    both.grow([1001 if i == 5 else 1 for i in range(1100)])
+    assert sum(both.h[2]) == 1000
