@@ -547,8 +547,8 @@ wa_status wa_packed_attn_backward_workspace_size(const wa_seq_shape* shape, size
 /* Gradient of wa_packed_attn, bf16 only (dS = P (dP - dO . O) lies below fp16's range): with dO of O it writes
  *   dV = P^T dO, dQ = scale dS K, dK = scale dS^T Q, dP = dO V^T, dV and dK summed over the heads of a key head,
  * probabilities recomputed in float32 from stats, sums in float32, P and dS rounded to bf16 for the matrix products. Rows of no
- * sequence are left as they were; where sequences overlap (starts that descend) all rows are. Nothing is added with atomics:
- * equal calls give equal bits.
+ * sequence are left as they were; where starts descend anywhere (once taken into 0..tokens), so that sequences could overlap, all rows
+ * are. Nothing is added with atomics: equal calls give equal bits.
  *   dout, o, stats   dO [tokens][H][d]; what wa_packed_attn wrote
  *   dq, dk, dv     out, shaped as q, k and v
  *   workspace      >= wa_packed_attn_backward_workspace_size(shape), 256-byte aligned

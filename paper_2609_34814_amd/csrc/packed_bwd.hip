@@ -71,8 +71,8 @@ struct Job {
 
 // All tiles of all sequences and `cols` heads, longest first, those longer than `most` in parts of about equal length: `most` takes as
 // long as a 512th of all work, so that a call of few tiles fills the chip's workgroups (two a compute unit) once, and one of many is not cut.
-// Sequences that overlap (starts that descend) could have more tiles and parts than there is room for: they have no jobs. A pair of a
-// key and a query takes four products for dK and dV and three for dQ.
+// Where starts descend there are no jobs: sequences could overlap, which would write rows twice, in no order, and have more tiles and parts
+// than there is room for. A pair of a key and a query takes four products for dK and dV and three for dQ.
 // Causal tiles have the lengths 1 to T of a sequence of T tiles, others T. Each workgroup finds its job itself: the lengths are on the
 // device. The tiles of the first 64 kHeld sequences are held, one a lane.
 template <int kHeld>
@@ -84,13 +84,13 @@ struct Jobs {
   // share: of the kind of jobs in all work, in sevenths
   __device__ __forceinline__ Jobs(int lane_, int cols_, int share, bool queries_)
       : a(seq_args()), lane(lane_), cols(cols_), batch(a->batch), causal(a->causal), queries(queries_) {
-    int64_t sum = 0, tokens = 0;
-    int n[kHeld];
+    int64_t sum = 0;
+    int n[kHeld], least = 0;  // below 0: starts descend
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) n[i] = 64 * i < batch ? tokens_of(64 * i + lane) : 0;
     auto add = [&](int x) {
       const int64_t t = tiles(x);
-      tokens += x;
+      least = min(least, x);
       sum += causal ? t * (t + 1) / 2 : t * t;
     };
 #pragma unroll
@@ -99,11 +99,16 @@ struct Jobs {
       if (64 * i < batch) add(n[i]);
     }
     for (int base = 64 * kHeld; base < batch; base += 64) add(tokens_of(base + lane));
-    if (lane64(lane_prefix_sum64(tokens, lane), 63) > again(a)->tokens) batch = 0;
+    if (__ballot(least < 0)) batch = 0;
     sum = lane64(lane_prefix_sum64(sum, lane), 63) * cols;
     most = (int)((uint64_t)(7 * sum + share * kSlots - 1) / (share * kSlots));
   }
-  __device__ __forceinline__ int tokens_of(int b) const { return b < batch ? seq_of<false>(again(a), b).n : 0; }
+  // below 0 where the next sequence begins before this one
+  __device__ __forceinline__ int tokens_of(int b) const {
+    if (b >= batch) return 0;
+    const SeqArgs x = again(a);
+    return min(max(x->starts[b + 1], 0), x->tokens) - min(max(x->starts[b], 0), x->tokens);
+  }
   static __device__ __forceinline__ int tiles(int n) { return (n + kRows - 1) / kRows; }
   // f(first sequence, tiles of sequence first + lane) for all, while it says so
   template <typename F>

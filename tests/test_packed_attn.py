@@ -420,3 +420,27 @@ def test_hundreds_of_sequences():
     lens[3], lens[555], lens[690] = 300, 260, 140
     check(make(lens, 2, 1, 64))
     check(make(lens, 2, 2, 128), causal=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("starts", [
+    [0, 100, 50, 100], [0, 100, 99, 100], [0, 100, 50, 50], [100, 0, 100], [0, 120, -7, 60], [0] * 70 + [100, 50, 100], [0] * 600 + [100, 50, 100]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradient_where_starts_descend(starts, d):
+    """Fewer tokens in all than there are rows, so that only the order of the starts says that sequences overlap: no row is written."""
+    q, k, v, good, dout = make([100, 50], 2, 1, d, spare=50)
+    o, lse = W.packed_attn(q, k, v, good, return_lse=True)
+    kept = [torch.full_like(x, 3.0) for x in (q, k, v)]
+    W.packed_attn_backward(dout, q, k, v, o, lse, torch.tensor(starts, dtype=torch.int32, device="cuda"), out=kept)
+    assert all(torch.all(x == 3.0) for x in kept)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("far", [[-9, 100, 2 ** 31 - 1], [0, 100, 2 ** 31 - 1, 300, 160], [-5, -7, 0, 100, 150]])
+def test_gradient_of_starts_outside_the_rows(far):
+    """Starts below 0 and past the last row are taken into it, also where they descend there alone."""
+    q, k, v, starts, dout = make([100, 50], 2, 1, 64)
+    o, lse = W.packed_attn(q, k, v, starts, return_lse=True)
+    want = W.packed_attn_backward(dout, q, k, v, o, lse, starts)
+    got = W.packed_attn_backward(dout, q, k, v, o, lse, torch.tensor(far, dtype=torch.int32, device="cuda"))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
