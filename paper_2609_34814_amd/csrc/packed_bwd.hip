@@ -14,6 +14,7 @@
 // registers, so P and dS, rounded to bf16, are operands of the following products as they are. Two wavefronts share a SIMD; the one that is
 // at scores and dP goes first (16,384 tokens, 32 heads over 8, d 128: 7.24 -> 6.65 ms).
 
+#include "packed_jobs.h"
 #include "seq_attn.h"
 
 #include <algorithm>
@@ -23,7 +24,6 @@ namespace {
 using namespace wa;
 
 constexpr int kRows = 128, kWaves = 4, kAhead = 2;
-constexpr uint32_t kSlots = 512, kMostParts = 2 * kSlots;
 
 // Neighbouring units, which may share keys, on one XCD where eight divides their number.
 __device__ __forceinline__ int spread(int u, int units) { return units % 8 ? u : u % 8 * (units / 8) + u / 8; }
@@ -78,19 +78,20 @@ struct Job {
 template <int kHeld>
 struct Jobs {
   SeqArgs a;
-  int lane, cols, batch, held[kHeld], most;
+  int lane, cols, batch, held[kHeld], longest, most;
   bool causal, queries;
 
   // share: of the kind of jobs in all work, in sevenths
   __device__ __forceinline__ Jobs(int lane_, int cols_, int share, bool queries_)
       : a(seq_args()), lane(lane_), cols(cols_), batch(a->batch), causal(a->causal), queries(queries_) {
     int64_t sum = 0;
-    int n[kHeld], least = 0;  // below 0: starts descend
+    int n[kHeld], least = 0, top = 0;  // least: below 0 where starts descend
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) n[i] = 64 * i < batch ? tokens_of(64 * i + lane) : 0;
     auto add = [&](int x) {
       const int64_t t = tiles(x);
       least = min(least, x);
+      top = max(top, (int)t);
       sum += causal ? t * (t + 1) / 2 : t * t;
     };
 #pragma unroll
@@ -101,7 +102,8 @@ struct Jobs {
     for (int base = 64 * kHeld; base < batch; base += 64) add(tokens_of(base + lane));
     if (__ballot(least < 0)) batch = 0;
     sum = lane64(lane_prefix_sum64(sum, lane), 63) * cols;
-    most = (int)((uint64_t)(7 * sum + share * kSlots - 1) / (share * kSlots));
+    longest = lane_max(top);
+    most = longest_whole(sum, share, longest);
   }
   // below 0 where the next sequence begins before this one
   __device__ __forceinline__ int tokens_of(int b) const {
@@ -119,17 +121,11 @@ struct Jobs {
     for (int base = 64 * kHeld; base < batch; base += 64)
       if (!f(base, tiles(tokens_of(base + lane)))) return;
   }
-  __device__ __forceinline__ int parts_of(int length) const { return (length + most - 1) / most; }
-  // jobs of the first x lengths of a sequence
-  __device__ __forceinline__ int upto(int x) const {
-    const int q = x / most, r = x - q * most;
-    return q * (q + 1) / 2 * most + r * (q + 1);
-  }
   // those of tiles longer than `length`, of one column
   __device__ __forceinline__ int above(int length) const {
     int sum = 0;
     each([&](int, int t) {
-      sum += t <= length ? 0 : causal ? upto(t) - upto(length) : t * parts_of(t);
+      sum += t <= length ? 0 : causal ? jobs_upto(t, most) - jobs_upto(length, most) : t * parts_of(t, most);
       return true;
     });
     return lane_sum(sum);
@@ -145,12 +141,7 @@ struct Jobs {
   }
   // job number `rank`; false if there is none
   __device__ __forceinline__ bool find(int64_t rank, Job* job) const {
-    int lo = 0, hi = 0, passed = 0;  // above(lo) > row of jobs >= above(hi) = passed
-    each([&](int, int t) {
-      hi = max(hi, t);
-      return true;
-    });
-    hi = lane_max(hi);
+    int lo = 0, hi = longest, passed = 0;  // above(lo) > row of jobs >= above(hi) = passed
     const int row = (int)(rank / cols);
     if (row >= above(0)) return false;
     while (hi - lo > 1) {
@@ -163,7 +154,7 @@ struct Jobs {
       }
     }
     job->length = hi;
-    job->parts = parts_of(hi);
+    job->parts = parts_of(hi, most);
     int k = (row - passed) / job->parts;
     job->part = row - passed - k * job->parts;
     job->number = (longer(hi) + k) * cols + (int)(rank - (int64_t)row * cols);
