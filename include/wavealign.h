@@ -533,7 +533,7 @@ wa_status wa_seq_attn_workspace_size(const wa_seq_shape* shape, size_t* bytes);
  *   stats      out float [H][tokens][1 + d/4] (fp16: [H][tokens][1]), nullable: the natural-log sum-exp of a query's scaled scores
  *              and then, for the gradient, what O's columns lost in rounding, a byte each
  *   workspace  >= wa_seq_attn_workspace_size(shape), 256-byte aligned
- * Outputs and workspace overlap neither inputs nor each other (refused; outputs may interleave in one tensor of equal token strides).
+ * Outputs and workspace overlap neither inputs nor each other (refused; tensors may interleave in one, by token or by head).
  * How the work is cut follows from the lengths, so equal calls give equal bits; the bits of a sequence may
  * depend on the lengths of the others. */
 wa_status wa_packed_attn(const wa_token_rows* q, const wa_token_rows* k, const wa_token_rows* v, const int32_t* starts,
@@ -607,8 +607,7 @@ wa_status wa_paged_attn(const wa_token_rows* q, const wa_pages* k, const wa_page
  * (n = starts[b + 1] - starts[b]; kv_lens counts the new tokens). Places before token 0 are left out. Two sequences must not
  * store into one page's row.
  *   k, v      [tokens][Hk][d] rows (shape->heads is not used)
- *   k_pages, v_pages   out; they overlap neither inputs nor each other (but may interleave, page by page or token by token,
- *             with equal strides)
+ *   k_pages, v_pages   out; they overlap neither inputs nor each other (but may interleave, by page, by head or by token)
  *   status    as for wa_paged_attn; rows without a page are left out */
 wa_status wa_page_store(const wa_token_rows* k, const wa_token_rows* v, const wa_pages* k_pages, const wa_pages* v_pages,
                         const wa_page_tables* tables, const int32_t* starts, const int32_t* kv_lens,

@@ -499,26 +499,55 @@ wa_status check_seq_options(const wa_seq_options* o, WaSeqLaunch* a) {
   return WA_OK;
 }
 
-// Memory of a tensor: `count` blocks of `inner` bytes, `step` bytes apart. Vectors are one block.
+// Memory of a tensor: blocks of `inner` bytes, `count` of them `step` bytes apart, so many of those the next step apart, and so on: the largest
+// step first, each at least what lies inside it. Vectors are one block.
 struct SeqSpan {
+  struct Level {
+    int64_t step, count;
+  };
   const char* name;
   const void* at;  // null: not given
-  size_t inner, step, count;
   bool written;
-  size_t fine = 0, fine_step = 0;  // the same memory as smaller blocks, 0: none
-  size_t bytes() const { return count ? (count - 1) * step + inner : 0; }
+  int64_t inner, bytes;  // bytes: from the first to the last
+  int levels;
+  Level level[3];
+
+  SeqSpan() : SeqSpan(nullptr, nullptr, 0, false) {}
+  SeqSpan(const char* name_, const void* at_, size_t inner_, bool written_)
+      : name(name_), at(at_), written(written_), inner((int64_t)inner_), bytes((int64_t)inner_), levels(0), level{} {}
+  // levels of one are none
+  SeqSpan with(int64_t step, int64_t count) const {
+    SeqSpan x = *this;
+    if (count > 1) {
+      x.level[x.levels++] = {step, count};
+      x.bytes += step * (count - 1);
+    }
+    return x;
+  }
+  // the same of the blocks inside `from` levels
+  int64_t extent(int from) const {
+    int64_t n = inner;
+    for (int i = from; i < levels; ++i) n += level[i].step * (level[i].count - 1);
+    return n;
+  }
 };
+// Whether blocks of x inside its first i levels and of y inside its first j meet, y's beginning `ahead` bytes behind x's. At the larger of the
+// two steps, two blocks of x at most can meet one of y: the one that y's begins in or behind, and the next.
+bool blocks_meet(const SeqSpan& x, int i, const SeqSpan& y, int j, int64_t ahead) {
+  if (ahead >= x.extent(i) || -ahead >= y.extent(j)) return false;
+  const int64_t sx = i < x.levels ? x.level[i].step : 0, sy = j < y.levels ? y.level[j].step : 0, step = std::max(sx, sy);
+  if (!step) return true;
+  const int64_t nx = sx == step ? x.level[i].count : 1, ny = sy == step ? y.level[j].count : 1;
+  const int in_x = sx == step ? i + 1 : i, in_y = sy == step ? j + 1 : j;
+  if (x.extent(in_x) > step || y.extent(in_y) > step) return true;
+  const int64_t first = ahead >= 0 ? ahead / step : -((-ahead + step - 1) / step);
+  for (int64_t k = first; k <= first + 1; ++k)  // x's block is the k-th after y's
+    if (k < nx && -k < ny && blocks_meet(x, in_x, y, in_y, ahead - k * step)) return true;
+  return false;
+}
 bool spans_meet(const SeqSpan& x, const SeqSpan& y) {
-  const uintptr_t p = (uintptr_t)x.at, q = (uintptr_t)y.at;
-  if (!x.at || !y.at || !x.bytes() || !y.bytes() || p >= q + y.bytes() || q >= p + x.bytes()) return false;
-  // blocks of equal steps: apart where each fits beside the other, in every round of the step
-  auto apart = [&](size_t step, size_t one, size_t other) {
-    if (!step) return false;
-    const size_t ahead = (size_t)(q > p ? q - p : p - q) % step, off = q >= p ? ahead : (step - ahead) % step;
-    return off >= one && off + other <= step;
-  };
-  if (x.count > 1 && y.count > 1 && x.step == y.step && apart(x.step, x.inner, y.inner)) return false;
-  return !(x.fine_step == y.fine_step && apart(x.fine_step, x.fine, y.fine));
+  const int64_t ahead = (int64_t)((uintptr_t)y.at - (uintptr_t)x.at);
+  return ahead < x.bytes && -ahead < y.bytes && x.at && y.at && x.inner && y.inner && blocks_meet(x, 0, y, 0, ahead);
 }
 wa_status check_seq_spans(std::initializer_list<SeqSpan> spans) {
   for (const SeqSpan& x : spans)
@@ -526,7 +555,7 @@ wa_status check_seq_spans(std::initializer_list<SeqSpan> spans) {
       if (x.written && &x != &y && spans_meet(x, y)) return fail(WA_ERR_INVALID_ARG, "%s overlaps %s", x.name, y.name);
   return WA_OK;
 }
-SeqSpan flat(const char* name, const void* at, size_t bytes, bool written) { return {name, at, bytes, bytes, 1, written}; }
+SeqSpan flat(const char* name, const void* at, size_t bytes, bool written) { return {name, at, bytes, written}; }
 
 constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxTokenStride = int64_t(1) << 24;
 
@@ -543,10 +572,11 @@ wa_status check_rows(const wa_token_rows* r, const char* name, int tokens, int h
   if (written && !((by_token && (heads < 2 || h >= d)) || (by_head && (tokens < 2 || t >= d))))
     return fail(WA_ERR_INVALID_ARG, "%s: elements of an output coincide (strides %lld and %lld)", name, (long long)t, (long long)h);
   *out = {r->at, t, h};
-  if (by_token && tokens > 1)
-    *span = {name, r->at, (size_t)row * 2, (size_t)t * 2, (size_t)tokens, written};
-  else if (by_head && heads > 1)
-    *span = {name, r->at, (size_t)head * 2, (size_t)h * 2, (size_t)heads, written};
+  const SeqSpan one = flat(name, r->at, (size_t)d * 2, written);
+  if (by_token)  // heads that coincide: a token's bytes are one block
+    *span = heads < 2 || h >= d ? one.with(t * 2, tokens).with(h * 2, heads) : flat(name, r->at, (size_t)row * 2, written).with(t * 2, tokens);
+  else if (by_head)
+    *span = tokens < 2 || t >= d ? one.with(h * 2, heads).with(t * 2, tokens) : flat(name, r->at, (size_t)head * 2, written).with(h * 2, heads);
   else
     *span = flat(name, r->at, (size_t)((tokens - 1) * t + row) * 2, written);
   return WA_OK;
@@ -586,13 +616,20 @@ wa_status check_pages(const wa_pages* p, const char* name, const WaSeqLaunch& a,
     return fail(WA_ERR_ALIGNMENT, "%s: strides %lld, %lld and %lld are not multiples of 8", name, (long long)s, (long long)h, (long long)t);
   const int64_t tokens = int64_t(1) << a.page_shift, head = (tokens - 1) * t + a.head_dim, row = (a.kv_heads - 1) * h + a.head_dim;
   const int64_t page = (tokens - 1) * t + row;
-  const bool nested = (t >= a.head_dim && (a.kv_heads < 2 || h >= head)) || (t >= row && (a.kv_heads < 2 || h >= a.head_dim));
-  if (written && !(nested && (a.n_pages < 2 || s >= page)))
+  const bool by_head = t >= a.head_dim && (a.kv_heads < 2 || h >= head), by_token = t >= row && (a.kv_heads < 2 || h >= a.head_dim);
+  if (written && !((by_head || by_token) && (a.n_pages < 2 || s >= page)))
     return fail(WA_ERR_INVALID_ARG, "%s: elements of an output coincide (strides %lld, %lld and %lld)", name, (long long)s, (long long)h,
                 (long long)t);
   *out = {p->at, s, h, t};
-  *span = {name, p->at, (size_t)page * 2, (size_t)s * 2, (size_t)a.n_pages, written};
-  if (t >= row && s % t == 0) span->fine = (size_t)row * 2, span->fine_step = (size_t)t * 2;
+  const SeqSpan rows = flat(name, p->at, (size_t)a.head_dim * 2, written), pages = rows.with(s * 2, a.n_pages);
+  if (a.n_pages > 1 && s < page)
+    *span = flat(name, p->at, (size_t)((a.n_pages - 1) * s + page) * 2, written);
+  else if (by_token)
+    *span = pages.with(t * 2, tokens).with(h * 2, a.kv_heads);
+  else if (by_head)
+    *span = pages.with(h * 2, a.kv_heads).with(t * 2, tokens);
+  else
+    *span = flat(name, p->at, (size_t)page * 2, written).with(s * 2, a.n_pages);
   return WA_OK;
 }
 

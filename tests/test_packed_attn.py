@@ -98,6 +98,63 @@ def test_interleaved_outputs():
     assert _backward(lib, t, lse=None) == INVALID
 
 
+def _meets(call, t, shape):
+    """Whether a call is refused for tensors of rows that overlap; those apart are for starts inside the workspace."""
+    assert call(_lib(), t, shape=shape, starts=BASE - (1 << 30) + 256) == INVALID
+    said = _lib().wa_last_error()
+    assert b"overlaps" in said
+    return said != b"workspace overlaps starts"
+
+
+@pytest.mark.parametrize("order,tokens", [("thcd", 100), ("htcd", 100), ("chtd", 100), ("thcd", 1), ("htcd", 1), ("tchd", 1)])
+def test_outputs_interleaved_in_any_order(order, tokens):
+    """Four heads of q, k, v, o and their gradients as parts (c) of one tensor, whatever the order of tokens, heads and parts: apart, and
+    not one of them eight elements further."""
+    size, steps, n = dict(t=tokens, h=4, c=8, d=64), {}, 1
+    for x in reversed(order):
+        steps[x], n = n, n * size[x]
+    at = BASE + (1 << 24)
+    names = "q k v o dout dq dk dv".split()
+    t = {x: (at + 2 * i * steps["c"], steps["t"], steps["h"]) for i, x in enumerate(names)}
+    shape = _shape(tokens=tokens, heads=4, kv_heads=4)
+    assert not _meets(_forward, t, shape) and not _meets(_backward, t, shape)
+    # the part before belongs to the call everywhere, the part behind where it is a gradient
+    for call, x, by in ((_forward, "o", -16), (_backward, "dq", -16), (_backward, "dq", 16), (_backward, "dk", 16), (_backward, "dv", -16)):
+        assert _meets(call, {**t, x: (t[x][0] + by, *t[x][1:])}, shape), (x, by)
+
+
+def test_overlaps_against_sets_of_addresses():
+    """The output and an input of random strides, by token or by head: refused where they share an address, and nowhere else."""
+    rng, seen = np.random.default_rng(11), [0, 0]
+    d = 64
+
+    def strides(tokens, heads):
+        if rng.random() < 0.5:
+            h = d + 8 * int(rng.integers(0, 30))
+            return (heads - 1) * h + d + 8 * int(rng.integers(0, 60)), h
+        t = d + 8 * int(rng.integers(0, 30))
+        return t, (tokens - 1) * t + d + 8 * int(rng.integers(0, 60))
+
+    def rows(at, t, h, tokens, heads):
+        return {at + 2 * (i * t + j * h + c) for i in range(tokens) for j in range(heads) for c in range(0, d, 8)}
+    for _ in range(3000):
+        tokens, kv = int(rng.integers(1, 5)), int(rng.integers(1, 4))
+        heads = kv * int(rng.integers(1, 3))
+        t = _tensors()
+        o = strides(tokens, heads)
+        k = o if heads == kv and rng.random() < 0.7 else strides(tokens, kv)
+        at, by = BASE + (1 << 24), 16 * int(rng.integers(-90, 90))
+        t["o"], t["k"] = (at, *o), (at + by, *k)
+        for x, n in (("q", heads), ("v", kv)):
+            t[x] = (t[x][0], n * d, d)
+        meets = bool(rows(at, *o, tokens, heads) & rows(at + by, *k, tokens, kv))
+        seen[meets] += 1
+        got = _meets(_forward, t, _shape(tokens=tokens, heads=heads, kv_heads=kv))
+        if o == k or meets:
+            assert got == meets, (tokens, heads, kv, o, k, by)
+    assert min(seen) > 500
+
+
 def _host(t=20, h=4, hk=2, d=64, dtype=torch.bfloat16):
     return dict(q=torch.zeros(t, h, d, dtype=dtype), k=torch.zeros(t, hk, d, dtype=dtype), v=torch.zeros(t, hk, d, dtype=dtype),
                 starts=torch.zeros(3, dtype=torch.int32))
@@ -444,3 +501,18 @@ def test_gradient_of_starts_outside_the_rows(far):
     want = W.packed_attn_backward(dout, q, k, v, o, lse, starts)
     got = W.packed_attn_backward(dout, q, k, v, o, lse, torch.tensor(far, dtype=torch.int32, device="cuda"))
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_parts_of_a_projection_by_head(d):
+    """q, k, v of [T][H][3][d], O and the three gradients in one [T][H][4][d]: the bits of contiguous tensors."""
+    q, k, v, starts, dout = make([70, 200], 2, 2, d, fused=False)
+    o, lse = W.packed_attn(q, k, v, starts, return_lse=True)
+    grads = W.packed_attn_backward(dout, q, k, v, o, lse, starts)
+    x = torch.stack([q, k, v], dim=2)
+    y = torch.full((270, 2, 4, d), 7.0, dtype=BF, device="cuda")
+    parts = [x[:, :, i] for i in range(3)]
+    o2, lse2 = W.packed_attn(*parts, starts, return_lse=True, out=y[:, :, 0])
+    got = W.packed_attn_backward(dout, *parts, o2, lse2, starts, out=[y[:, :, i] for i in (1, 2, 3)])
+    assert torch.equal(o2, o) and torch.equal(lse2[..., 0], lse[..., 0]) and all(torch.equal(a, b) for a, b in zip(got, grads))

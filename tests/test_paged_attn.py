@@ -86,6 +86,21 @@ def test_interleaved_pages(step, k, v, meets):
     assert (b"pages overlaps" in _lib().wa_last_error()) == meets
 
 
+@pytest.mark.parametrize("order", ["pcht", "phct", "phtc", "pcth", "ptch", "pthc", "cpht"])
+def test_pages_interleaved_in_any_order(order):
+    """Keys and values (c) of a pool of 20 pages of 16 tokens, 2 heads of 64, in any order: apart, and not eight elements further."""
+    size, steps, n = dict(p=20, c=2, h=2, t=16), {}, 64
+    for x in reversed(order):
+        steps[x], n = n, n * size[x]
+    at, step = BASE + (8 << 20), (steps["p"], steps["h"], steps["t"])
+    for by, meets in ((0, False), (-8, True), (8, True)):
+        pages = {"kp": (at, *step), "vp": (at + 2 * (steps["c"] + by), *step)}
+        if order == "cpht" and by > 0:
+            continue                        # behind all keys
+        assert _call(True, pages=pages, status=TABLES[0]) == INVALID
+        assert (b"pages overlaps" in _lib().wa_last_error()) == meets, by
+
+
 @pytest.mark.parametrize("kw", [
     dict(k_pages=torch.zeros(4, 2, 16, 64)), dict(k_pages=torch.zeros(4, 3, 16, 64, dtype=BF)), dict(k_pages=torch.zeros(4, 16, 64, dtype=BF)),
     dict(v_pages=torch.zeros(5, 2, 16, 64, dtype=BF)), dict(v_pages=torch.zeros(4, 2, 64, 16, dtype=BF).transpose(2, 3)),
@@ -353,3 +368,16 @@ def test_fork_and_compact_between_tokens():
 def test_chunks_whole_and_cut(lens, new, h, hk, d, dtype, causal):
     """Chunks whose tiles are dealt out whole, and long ones that are cut between workgroups."""
     check(lens, new, h, hk, d, 16, dtype, causal)
+
+
+@pytest.mark.gpu
+def test_pages_by_head():
+    """Keys and values beside each other in every head of a page: stored and read as from pools of their own."""
+    args, k, v = make([130, 40], [33, 1], 4, 2, 64, 16)
+    o = W.paged_attn(*args)
+    pages = args[1].shape[0]
+    pool = torch.full((pages, 2, 2, 16, 64), float("nan"), dtype=BF, device="cuda")
+    flat = torch.tensor([0, 130, 170], dtype=torch.int32, device="cuda")
+    W.page_store(torch.cat(k), torch.cat(v), pool[:, :, 0], pool[:, :, 1], args[3], flat, args[5])
+    assert all(torch.equal(pool[:, :, i].nan_to_num(5.0), args[1 + i].nan_to_num(5.0)) for i in range(2))
+    assert torch.equal(W.paged_attn(args[0], pool[:, :, 0], pool[:, :, 1], *args[3:]), o)
