@@ -496,8 +496,9 @@ wa_status wa_diff_attn_backward(const void* dout, const void* q, const void* k, 
 /* ---- packed sequences ---- */
 
 /* Rows [tokens][heads][head_dim] of 16-bit values; element (t, h, c) lies at t token_stride + h head_stride + c elements, so a
- * tensor may be a part of a fused projection's output, or head-major. `at` is 16-byte aligned, strides are multiples of 8, token
- * strides of keys and values below 2^24. An input's stride may be 0; elements of an output may not coincide. */
+ * tensor may be a part of a fused projection's output, or head-major. `at` is 16-byte aligned, strides are multiples of 8, of a token
+ * below 2^24 and of a head below 2^40, and the last element lies less than 2^46 behind the first. An input's stride may be 0; elements
+ * of an output may not coincide. */
 typedef struct wa_token_rows {
   void* at;               /* inputs are only read */
   int64_t token_stride;
@@ -570,7 +571,7 @@ enum {
 
 /* Keys or values in pages, [pages][Hk][page][head_dim]: element (p, h, i, c) lies at p page_stride + h head_stride +
  * i token_stride + c elements, so keys and values may share a pool in any order. `at` is 16-byte aligned, strides are
- * multiples of 8, token strides below 2^24. */
+ * multiples of 8, of a token below 2^24, of a head and a page below 2^40, and the last element lies less than 2^46 behind the first. */
 typedef struct wa_pages {
   void* at;
   int64_t page_stride;

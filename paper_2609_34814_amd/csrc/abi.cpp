@@ -558,6 +558,8 @@ wa_status check_seq_spans(std::initializer_list<SeqSpan> spans) {
 SeqSpan flat(const char* name, const void* at, size_t bytes, bool written) { return {name, at, bytes, written}; }
 
 constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxTokenStride = int64_t(1) << 24;
+// A tensor's first and last element are less than this apart, so that what is computed of its strides fits 64 bits, in bytes too.
+constexpr double kMaxExtent = 70368744177664.0;  // 2^46
 
 // Rows [tokens][heads][d], checked; *span: their memory.
 wa_status check_rows(const wa_token_rows* r, const char* name, int tokens, int heads, int d, bool written, WaSeqRows* out, SeqSpan* span) {
@@ -567,6 +569,9 @@ wa_status check_rows(const wa_token_rows* r, const char* name, int tokens, int h
   if (t < 0 || h < 0 || t >= kMaxTokenStride || h >= kMaxStride)
     return fail(WA_ERR_UNSUPPORTED, "%s: strides %lld and %lld are outside 0..2^24 and 0..2^40", name, (long long)t, (long long)h);
   if (t % 8 || h % 8) return fail(WA_ERR_ALIGNMENT, "%s: strides %lld and %lld are not multiples of 8", name, (long long)t, (long long)h);
+  if ((double)(tokens - 1) * t + (double)(heads - 1) * h >= kMaxExtent)
+    return fail(WA_ERR_UNSUPPORTED, "%s: strides %lld and %lld of %d tokens and %d heads span 2^46 elements", name, (long long)t,
+                (long long)h, tokens, heads);
   const int64_t row = (heads - 1) * h + d, head = (tokens - 1) * t + d;
   const bool by_token = tokens < 2 || t >= row, by_head = heads < 2 || h >= head;
   if (written && !((by_token && (heads < 2 || h >= d)) || (by_head && (tokens < 2 || t >= d))))
@@ -614,6 +619,9 @@ wa_status check_pages(const wa_pages* p, const char* name, const WaSeqLaunch& a,
                 (long long)h, (long long)t);
   if (s % 8 || h % 8 || t % 8)
     return fail(WA_ERR_ALIGNMENT, "%s: strides %lld, %lld and %lld are not multiples of 8", name, (long long)s, (long long)h, (long long)t);
+  if ((double)(a.n_pages - 1) * s + (double)(a.kv_heads - 1) * h + (double)(1 << a.page_shift) * t >= kMaxExtent)
+    return fail(WA_ERR_UNSUPPORTED, "%s: strides %lld, %lld and %lld of %d pages and %d heads span 2^46 elements", name, (long long)s,
+                (long long)h, (long long)t, a.n_pages, a.kv_heads);
   const int64_t tokens = int64_t(1) << a.page_shift, head = (tokens - 1) * t + a.head_dim, row = (a.kv_heads - 1) * h + a.head_dim;
   const int64_t page = (tokens - 1) * t + row;
   const bool by_head = t >= a.head_dim && (a.kv_heads < 2 || h >= head), by_token = t >= row && (a.kv_heads < 2 || h >= a.head_dim);

@@ -155,6 +155,17 @@ def test_overlaps_against_sets_of_addresses():
     assert min(seen) > 500
 
 
+def test_strides_past_64_bits():
+    """Head strides that times the heads pass 64 bits, as if heads lay inside a token: refused for every tensor."""
+    lib, heads, kv = _lib(), 1 << 25, 1 << 18
+    t = {x: (BASE << i, n * 64, 64) for i, (x, n) in enumerate((("q", heads), ("k", kv), ("v", kv), ("o", heads)))}
+    t = {x: (at, 0 if at == BASE else 64, hs) for x, (at, _, hs) in t.items()}
+    shape = _shape(tokens=1, batch=1, heads=heads, kv_heads=kv)
+    for x, n in (("q", heads), ("k", kv), ("v", kv), ("o", heads)):
+        assert _forward(lib, {**t, x: (t[x][0], 64, 1 << 39)}, shape=shape, size=16) == UNSUP, x
+    assert _forward(lib, t, shape=shape, size=16) == WORK
+
+
 def _host(t=20, h=4, hk=2, d=64, dtype=torch.bfloat16):
     return dict(q=torch.zeros(t, h, d, dtype=dtype), k=torch.zeros(t, hk, d, dtype=dtype), v=torch.zeros(t, hk, d, dtype=dtype),
                 starts=torch.zeros(3, dtype=torch.int32))

@@ -86,6 +86,15 @@ def test_interleaved_pages(step, k, v, meets):
     assert (b"pages overlaps" in _lib().wa_last_error()) == meets
 
 
+@pytest.mark.parametrize("store", [False, True])
+def test_strides_past_64_bits(store):
+    """Page strides that times the pages pass 64 bits are refused."""
+    for name, where in (("kp", 2 << 20), ("vp", 3 << 20)):
+        pages = {name: (BASE + where, 1 << 39, 1024, 64)}
+        assert _call(store, pages=pages, tables=(*TABLES[:3], (1 << 25) + 1, 16)) == UNSUP
+        assert b"span" in _lib().wa_last_error()
+
+
 @pytest.mark.parametrize("order", ["pcht", "phct", "phtc", "pcth", "ptch", "pthc", "cpht"])
 def test_pages_interleaved_in_any_order(order):
     """Keys and values (c) of a pool of 20 pages of 16 tokens, 2 heads of 64, in any order: apart, and not eight elements further."""
