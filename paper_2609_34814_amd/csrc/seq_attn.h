@@ -917,7 +917,7 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
   };
 
   int buf = 0;
-  uint32_t none = 0, any_bad = 0;
+  uint32_t none = 0, any_bad = 0, item_bad = 0;  // bad: of the keys that were passed, those without a page
   bool ready = false, stored = false;  // the item's first tile is on its way; stores of the item before come behind it
   Range r = range(it);
   for (;;) {
@@ -998,7 +998,7 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
           WA_WAIT_VM(0);
           WA_BARRIER();  // everyone has the tile's values and the next one's keys, and is done with its keys and the values before
           now = none;
-          if (PAGED) any_bad |= now;
+          if (PAGED) item_bad |= now;
           none = none_next;
           if (key + KB < r.hi) copy_values(pl, key + KB, at ^ 1, ids, none_next);
           if (key + 2 * KB < r.hi) {
@@ -1040,7 +1040,7 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
       }
       none_next = go ? copy(next, buf ^ 1) : 0;
       if (more && !known) look();  // early, so that the last tile's copies do not wait for it
-      any_bad |= none;
+      item_bad |= none;
       if (key < some) work(key, buf * C::STAGE, limit, key + KB > all || (PAGED && none), none);
       none = none_next;
       buf ^= 1;
@@ -1053,10 +1053,15 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
     const bool starts = begin <= it.at, finishes = it.at + it.units <= end;
     const Place p = place(it);
     stored = __ballot(p.valid) != 0;
+    // Where all scores are -inf (infinite queries, products past float32) a softmax is 0 / 0; where the row sees no key, O is 0. (Of packed
+    // sequences each sees one.)
+    const bool undefined = r.lo < r.hi && item_bad == 0 && (!PAGED || !walk.causal || it.s.keys - it.s.n + p.token >= r.lo);
+    any_bad |= item_bad;
+    item_bad = 0;
     const SeqArgs a = again(seq_args());
     const int64_t tok = it.s.first + p.token;
     if (starts && finishes) {
-      const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+      const float inv = l > 0.f ? 1.f / l : l == 0.f && !undefined ? 0.f : NAN;
       uint16_t* out = (uint16_t*)a->o.at + tok * a->o.token + p.head * a->o.head + 8 * hf;
       float* stat = a->lse && p.valid ? a->lse + (p.head * (int64_t)a->tokens + tok) * a->lse_step : nullptr;
 #pragma unroll
@@ -1087,7 +1092,7 @@ __global__ __launch_bounds__(64 * W, D == 64 && W == 4 && !PAGED ? 3 : 2) void s
 #pragma unroll
         for (int v = 0; v < 16; v += 4)
           *(float4*)(out + dt * 32 + 2 * v + 4 * hf) = make_float4(acc[dt][v], acc[dt][v + 1], acc[dt][v + 2], acc[dt][v + 3]);
-      if (hf == 0) ((float2*)(a->part + (int64_t)a->plan.workers * 2 * R * D))[at] = make_float2(ref, l);
+      if (hf == 0) ((float2*)(a->part + (int64_t)a->plan.workers * 2 * R * D))[at] = make_float2(ref, l == 0.f && undefined ? -1.f : l);
       if (finishes) {
         const int first = Shares(total, a).first_of(it);
         if (hf == 0) a->cuts[tok * a->heads + p.head] = make_int2(first | me << 16, row);
@@ -1118,9 +1123,10 @@ struct JoinRow {
   }
   // a part that begins with its tile lies in slot 1, others in slot 0
   __device__ __forceinline__ int64_t at(int c) const { return ((int64_t)c * 2 + (c == begin ? 1 : 0)) * R + row; }
-  // columns [c, c + 4) of the row; o, l: summed over the parts, taken against `top`
-  __device__ __forceinline__ void finish(const WaSeqLaunch& a, float4 o, float l, float top, int c) const {
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+  // columns [c, c + 4) of the row; o, l: summed over the parts, taken against `top`; undefined: a part has keys, whose scores are all -inf
+  // (its l is -1)
+  __device__ __forceinline__ void finish(const WaSeqLaunch& a, float4 o, float l, float top, bool undefined, int c) const {
+    const float inv = l > 0.f ? 1.f / l : l == 0.f && !undefined ? 0.f : NAN;
     o.x *= inv;
     o.y *= inv;
     o.z *= inv;
@@ -1157,6 +1163,7 @@ __global__ __launch_bounds__(256) void seq_join_few_kernel(const WaSeqLaunch a, 
       some &= some - 1;
       const JoinRow<HALF, D, W, PAGED> row(a, base + who * groups, make_int2(__shfl(cut.x, who, L), __shfl(cut.y, who, L)));
       float top = -INFINITY, l = 0.f;
+      bool undefined = false;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int w = row.begin; w <= row.end; w += 4) {
         float2 s[4];
@@ -1180,6 +1187,7 @@ __global__ __launch_bounds__(256) void seq_join_few_kernel(const WaSeqLaunch a, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float f = s[i].x == -INFINITY || w + i > row.end ? 0.f : __builtin_amdgcn_exp2f(s[i].x - high);
+          undefined |= s[i].y < 0.f;
           l += f * s[i].y;
           o.x += f * x[i].x;
           o.y += f * x[i].y;
@@ -1187,7 +1195,7 @@ __global__ __launch_bounds__(256) void seq_join_few_kernel(const WaSeqLaunch a, 
           o.w += f * x[i].w;
         }
       }
-      row.finish(a, o, l, top, c);
+      row.finish(a, o, l, top, undefined, c);
     }
   }
 }
@@ -1204,9 +1212,11 @@ __global__ __launch_bounds__(4 * D) void seq_join_many_kernel(const WaSeqLaunch 
   const JoinRow<HALF, D, W, PAGED> row(a, blockIdx.x, cut);
   const int team = threadIdx.x / L, lane = threadIdx.x & (L - 1), c = 4 * lane;
   float top = -INFINITY, l = 0.f;
+  bool undefined = false;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float high, const float2& s, const float4& x) {  // both taken against `high`
     const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - high);
+    undefined |= s.y < 0.f;
     l += f * s.y;
     o.x += f * x.x;
     o.y += f * x.y;
@@ -1242,7 +1252,7 @@ __global__ __launch_bounds__(4 * D) void seq_join_many_kernel(const WaSeqLaunch 
     for (int i = 0; i < AHEAD; ++i) add(high, s[i], x[i]);
   }
   sums[team][lane] = o;
-  if (lane == 0) stats[team] = make_float2(top, l);
+  if (lane == 0) stats[team] = make_float2(top, l == 0.f && undefined ? -1.f : l);
   __syncthreads();
   if (team) return;
   float high = top;
@@ -1251,7 +1261,7 @@ __global__ __launch_bounds__(4 * D) void seq_join_many_kernel(const WaSeqLaunch 
   raise(high);
 #pragma unroll
   for (int x = 1; x < TEAMS; ++x) add(high, stats[x], sums[x][lane]);  // in one order
-  row.finish(a, o, l, top, c);
+  row.finish(a, o, l, top, undefined, c);
 }
 
 // Parts from which on a workgroup joins a row alone (one token of 64 sequences, 5 parts: 61 us where a workgroup of 1,024 threads does

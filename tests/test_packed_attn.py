@@ -527,3 +527,29 @@ def test_parts_of_a_projection_by_head(d):
     o2, lse2 = W.packed_attn(*parts, starts, return_lse=True, out=y[:, :, 0])
     got = W.packed_attn_backward(dout, *parts, o2, lse2, starts, out=[y[:, :, i] for i in (1, 2, 3)])
     assert torch.equal(o2, o) and torch.equal(lse2[..., 0], lse[..., 0]) and all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[1, 5], [40, 60], [2100, 340], [300] * 20])
+@pytest.mark.parametrize("d,dtype", [(64, FP), (128, BF)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_scores_that_are_all_minus_infinity(lens, d, dtype, causal):
+    """A softmax of -inf alone is 0 / 0: NaN in the row, -inf as its sum-exp, and no other row changes, whether the query holds the
+    infinity or (bf16) its product with the keys passes float32."""
+    q, k, v, starts, _ = make(lens, 4, 2, d, dtype, fused=False)
+    k[..., 0] = k[..., 0].abs() + 1
+    if dtype == BF:
+        k[..., 1] = 2.0 ** 100
+        q[..., 1] = 0
+    want, lse = W.packed_attn(q, k, v, starts, causal=causal, return_lse=True)
+    t = sum(lens)
+    rows, heads = [0, lens[0] - 1, t - 1], [0, 3, 2]
+    for r, h in zip(rows, heads):
+        q[r, h, 0] = float("-inf")
+    if dtype == BF:
+        q[rows[0], heads[0], 0], q[rows[0], heads[0], 1] = 1, -2.0 ** 100
+    got, lse2 = W.packed_attn(q, k, v, starts, causal=causal, return_lse=True)
+    for r, h in zip(rows, heads):
+        assert torch.isnan(got[r, h]).all() and lse2[h, r, 0] == -float("inf"), (r, h)
+        got[r, h], want[r, h], lse2[h, r], lse[h, r] = 0, 0, 0, 0
+    assert torch.equal(got, want) and torch.equal(lse[..., 0], lse2[..., 0])

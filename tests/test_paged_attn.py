@@ -390,3 +390,23 @@ def test_pages_by_head():
     W.page_store(torch.cat(k), torch.cat(v), pool[:, :, 0], pool[:, :, 1], args[3], flat, args[5])
     assert all(torch.equal(pool[:, :, i].nan_to_num(5.0), args[1 + i].nan_to_num(5.0)) for i in range(2))
     assert torch.equal(W.paged_attn(args[0], pool[:, :, 0], pool[:, :, 1], *args[3:]), o)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,new", [([20000], [1]), ([900, 3000], [1, 1]), ([2000, 40], [300, 40]), ([1, 3], [1, 3]), ([9000] * 4, [600, 1, 1, 1])])
+@pytest.mark.parametrize("d,dtype", [(64, BF), (128, FP)])
+def test_scores_that_are_all_minus_infinity(lens, new, d, dtype):
+    """As of packed sequences: a row of keys whose scores are all -inf is NaN; one that sees no key, or only keys of pages that there are
+    not, stays 0."""
+    args, k, v = make(lens, new, 4, 2, d, 16, dtype)
+    args[1][..., 0] = args[1][..., 0].abs() + 1        # places of no token hold NaN
+    want = W.paged_attn(*args)
+    args[0][0, 1, 0] = args[0][-1, 2, 0] = float("-inf")
+    got, lse = W.paged_attn(*args, return_lse=True)
+    for r, h in ((0, 1), (-1, 2)):
+        assert torch.isnan(got[r, h]).all() and lse[h, r] == -float("inf")
+        got[r, h], want[r, h] = 0, 0
+    assert torch.equal(got, want)
+    none = torch.full_like(args[3], -1)
+    assert not W.paged_attn(*args[:3], none, *args[4:]).any()
+    assert not W.paged_attn(*args[:5], torch.zeros_like(args[5])).any()
