@@ -553,3 +553,43 @@ def test_scores_that_are_all_minus_infinity(lens, d, dtype, causal):
         assert torch.isnan(got[r, h]).all() and lse2[h, r, 0] == -float("inf"), (r, h)
         got[r, h], want[r, h], lse2[h, r], lse[h, r] = 0, 0, 0, 0
     assert torch.equal(got, want) and torch.equal(lse[..., 0], lse2[..., 0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,h,hk", [([90, 1, 200], 4, 2), ([2100, 333], 2, 1), ([40, 3], 8, 1)])
+@pytest.mark.parametrize("d,dtype,scale,gain", [(64, BF, 0.25, 1.0), (128, BF, 0.2, 1.0), (64, FP, 1.0, 0.25), (128, FP, 0.01, 1.0),
+                                                (64, BF, 1e-30, 1.0), (128, BF, 1.0, 0.125)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_scale(lens, h, hk, d, dtype, scale, gain, causal):
+    """A scale of the caller's, forward and gradient; scale sum |q k| stays below the 30 that the tolerances count with."""
+    args = make(lens, h, hk, d, dtype, gain=gain)
+    q, k = (x.abs().float().transpose(0, 1) for x in args[:2])
+    assert scale * float(torch.matmul(q, k.repeat_interleave(h // hk, 0).transpose(1, 2).contiguous()).max()) < 30
+    check(args, causal, scale=scale)
+
+
+FAR = [("tokens", 300, 2), ("heads", 90, 3)]
+
+
+def far(kind, t, h, count):
+    """``count`` tensors [t][h][64] in one of more than 8 GiB: tokens 32 MiB apart, or heads 8 GiB."""
+    step = (2 ** 24 - 8, 64) if kind == "tokens" else (64 * count, 2 ** 32 + 64 * count * t)
+    pool = torch.empty((t - 1) * step[0] + (h - 1) * step[1] + 64 * h * count, dtype=BF, device="cuda")
+    return [pool.as_strided((t, h, 64), (*step, 1), 64 * i * (h if kind == "tokens" else 1)) for i in range(count)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,t,h", FAR)
+def test_offsets_past_32_bits(kind, t, h):
+    """Rows, gradients included, more than 2^32 bytes apart: the bits of contiguous tensors."""
+    q, k, v, starts, dout = make([t - 40, 40], h, h, 64, fused=False)
+    o, lse = W.packed_attn(q, k, v, starts, return_lse=True)
+    grads = W.packed_attn_backward(dout, q, k, v, o, lse, starts)
+    q2, k2, v2, o2, dout2, *grads2 = far(kind, t, h, 8)
+    assert 2 * ((t - 1) * q2.stride(0) + (h - 1) * q2.stride(1)) > 2 ** 32
+    for x, y in ((q2, q), (k2, k), (v2, v), (dout2, dout)):
+        x.copy_(y)
+    got, lse2 = W.packed_attn(q2, k2, v2, starts, return_lse=True, out=o2)
+    assert torch.equal(o2, o) and torch.equal(lse2[..., 0], lse[..., 0])
+    W.packed_attn_backward(dout2, q2, k2, v2, o2, lse2, starts, out=grads2)
+    assert all(torch.equal(x, y) for x, y in zip(grads2, grads))

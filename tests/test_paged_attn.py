@@ -10,7 +10,7 @@ import paper_2609_34814_amd as W                     # noqa: E402
 from oracle import seq_attention as S                # noqa: E402
 from paper_2609_34814_amd import _lib as L           # noqa: E402
 from tests.test_abi import _lib                      # noqa: E402
-from tests.test_packed_attn import BASE, check_lse, close, f64   # noqa: E402
+from tests.test_packed_attn import BASE, FAR, check_lse, close, f64, far   # noqa: E402
 
 INVALID, ALIGN, UNSUP, WORK = L.WA_ERR_INVALID_ARG, L.WA_ERR_ALIGNMENT, L.WA_ERR_UNSUPPORTED, L.WA_ERR_WORKSPACE
 BF, FP = torch.bfloat16, torch.float16
@@ -410,3 +410,55 @@ def test_scores_that_are_all_minus_infinity(lens, new, d, dtype):
     none = torch.full_like(args[3], -1)
     assert not W.paged_attn(*args[:3], none, *args[4:]).any()
     assert not W.paged_attn(*args[:5], torch.zeros_like(args[5])).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,new", [([300, 5, 64], [33, 5, 0]), ([5000, 17], [1, 1]), ([900, 3000], [300, 500])])
+@pytest.mark.parametrize("d,dtype,scale", [(64, BF, 0.25), (128, BF, 0.01), (128, FP, 0.2)])
+def test_scale(lens, new, d, dtype, scale):
+    args, k, v = make(lens, new, 4, 2, d, 16, dtype)
+    o, lse = W.paged_attn(*args, scale=scale, return_lse=True)
+    ref = S.paged(f64(args[0]), [f64(x) for x in k], [f64(x) for x in v], args[4].tolist(), scale=scale, u=torch.finfo(dtype).eps / 2)
+    close(o, ref["o"], ref["tol"]["o"], "o")
+    check_lse(lse, ref["lse"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [[1, 0, 1], [70, 3, 0]])
+def test_strided_queries_and_outputs(new):
+    """Queries and O head-major, and as parts of wider tensors; rows of no sequence keep what they hold."""
+    (q, *rest), _, _ = make([300, 40, 9], new, 4, 2, 64, 16)
+    n = q.shape[0]
+    want = W.paged_attn(q, *rest)
+    turned = q.transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.empty(4, n, 64, dtype=BF, device="cuda").transpose(0, 1)
+    assert W.paged_attn(turned, *rest, out=out) is out and torch.equal(out, want)
+    fused = torch.full((n, 9, 64), 7.0, dtype=BF, device="cuda")
+    fused[:, :4] = q
+    W.paged_attn(fused[:, :4], *rest, out=fused[:, 5:])
+    assert torch.equal(fused[:, 5:], want) and torch.equal(fused[:, :4], q) and torch.all(fused[:, 4] == 7.0)
+    wide = torch.full((n + 5, 4, 64), float("nan"), dtype=BF, device="cuda")
+    wide[3:3 + n] = q
+    kept, (tables, starts, lens) = torch.full_like(wide, 3.0), rest[2:]
+    W.paged_attn(wide, *rest[:2], tables, starts + 3, lens, out=kept)
+    assert torch.equal(kept[3:3 + n], want) and torch.all(kept[:3] == 3.0) and torch.all(kept[3 + n:] == 3.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,t,h", FAR)
+def test_rows_past_32_bits(kind, t, h):
+    """New keys and values, queries and O more than 2^32 bytes apart."""
+    (q, kp, vp, tables, starts, lens), k, v = make([t, 500], [t - 3, 3], h, h, 64, 32)
+    want = W.paged_attn(q, kp, vp, tables, starts, lens)
+    far_k, far_v, far_q, far_o = far(kind, t, h, 4)
+    far_q.copy_(q)
+    W.paged_attn(far_q, kp, vp, tables, starts, lens, out=far_o)
+    assert torch.equal(far_o, want)
+    new = [torch.cat([x[0][3:], x[1][-3:]]) for x in (k, v)]
+    far_k.copy_(new[0])
+    far_v.copy_(new[1])
+    pools = [x.clone() for x in (kp, vp)]
+    for x in (kp, vp):
+        x[tables[0, 1].long()] = 0
+    W.page_store(far_k, far_v, kp, vp, tables, starts, lens)
+    assert all(torch.equal(x.nan_to_num(5.0), y.nan_to_num(5.0)) for x, y in zip((kp, vp), pools))
