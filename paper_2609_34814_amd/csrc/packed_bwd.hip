@@ -281,7 +281,8 @@ __device__ __forceinline__ void query_job(const WaSeqLaunch& a, int64_t rank, un
   const Seq s = one_seq(b);
   const int i0 = tile * kRows + w * 32, i = i0 + l32, i_last = s.n - 1;
   const bool valid = i <= i_last;
-  const int limit = !valid ? 0 : a.causal ? i + 1 : s.n;
+  // Keys that the lane's query sees; of one key alone dP = D, so dS is 0 and not what rounding leaves: none counts.
+  const int sees = !valid ? 0 : a.causal ? i + 1 : s.n, limit = sees == 1 ? 0 : sees;
   const int some = i0 > i_last ? 0 : a.causal ? min(i0 + 32, s.n) : s.n, all = a.causal ? min(i0 + 1, s.n) : s.n;
   // this part's keys
   const int lo = job.length * job.part / job.parts * kRows, most = min(job.length * (job.part + 1) / job.parts * kRows, s.n);
@@ -408,6 +409,7 @@ __device__ __forceinline__ void key_job(const WaSeqLaunch& a, int64_t rank, unsi
   const int some = k0 >= s.n ? s.n : a.causal ? k0 : 0;                   // the wavefront's first
   const int all = a.causal ? min(k0 + 31, s.n - 1) : 0;                   // and its last
   const bool whole = k0 + 31 < s.n;
+  const int lone = a.causal || s.n == 1 ? 0 : -1;                         // the query that sees one key, whose dS is 0; its tile is masked
   // this part's queries, in tiles of QB from the last on, of each tile all heads: so key tiles of different numbers, which begin with
   // different queries, meet the same ones at the same time, and the caches hold them
   const int lead = a.causal ? tile : 0, first = (lead + job.length * job.part / job.parts) * kRows;
@@ -506,6 +508,7 @@ __device__ __forceinline__ void key_job(const WaSeqLaunch& a, int64_t rank, unsi
         const int q = q0 + 8 * (v >> 2) + (v & 3);
         if (q < from || q >= s.n) p[v] = 0.f;
       }
+      dp[0] *= q0 == lone ? 0.f : 1.f;
     }
 #pragma unroll
     for (int v = 0; v < 16; ++v) ds[v] = p[v] * dp[v];

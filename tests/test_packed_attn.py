@@ -593,3 +593,21 @@ def test_offsets_past_32_bits(kind, t, h):
     assert torch.equal(o2, o) and torch.equal(lse2[..., 0], lse[..., 0])
     W.packed_attn_backward(dout2, q2, k2, v2, o2, lse2, starts, out=grads2)
     assert all(torch.equal(x, y) for x, y in zip(grads2, grads))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[1], [1] * 70, [1, 40, 0, 1, 300], [2100, 1, 333]])
+def test_gradient_of_one_key(lens, d):
+    """A softmax over one key is 1 whatever the score is: dQ of each sequence's first query is 0 under a causal mask, and dQ and dK of a
+    sequence of one token always; dV is the sum of dO over the heads."""
+    q, k, v, starts, dout = make(lens, 4, 2, d)
+    for causal in (True, False):
+        o, lse = W.packed_attn(q, k, v, starts, causal=causal, return_lse=True)
+        dq, dk, dv = W.packed_attn_backward(dout, q, k, v, o, lse, starts, causal=causal)
+        for a, n in zip(starts.tolist(), lens):
+            if n and (causal or n == 1):
+                assert not dq[a].any(), (causal, a)
+            if n == 1:
+                assert not dk[a].any(), (causal, a)
+                assert torch.equal(dv[a].float(), dout[a].float().view(2, 2, d).sum(1).to(BF).float())
