@@ -506,7 +506,7 @@ typedef struct wa_token_rows {
 } wa_token_rows;
 
 typedef struct wa_seq_shape {
-  int32_t batch;      /* sequences */
+  int32_t batch;      /* sequences. Tiles are sized for tokens / batch: hundreds of empty ones beside a long one cost time, not results */
   int32_t tokens;     /* rows of the tensors of queries (packed: of all tensors); 0: nothing to do */
   int32_t heads;      /* H, a multiple of kv_heads */
   int32_t kv_heads;   /* Hk: heads h with equal h / (H / Hk) share keys and values */
@@ -528,7 +528,8 @@ wa_status wa_seq_attn_workspace_size(const wa_seq_shape* shape, size_t* bytes);
  * float32 scores (so a probability is off by some 2^-24 of the row's largest scaled score), sums and O, probabilities
  * rounded to the tensors' type for the product with V (in fp16 down to 2^-21 of the row's largest with all bits). Keys and
  * values of a sequence's tokens have to be finite (a query that is not gives NaN in its own row of O alone, as do scores that are all
- * -inf because they pass float32); rows of no sequence are not read (but the last row of a sequence may be read again in their place), and their outputs are left as they were.
+ * -inf because they pass float32); rows of no sequence are not read (but the last row of a sequence may be read again in their
+ * place), and their outputs are left as they were.
  *   q, o       [tokens][H][d];  k, v  [tokens][Hk][d]
  *   starts     int32 [batch + 1], device, ascending; values are taken into 0..tokens. A sequence may be empty
  *   stats      out float [H][tokens][1 + d/4] (fp16: [H][tokens][1]), nullable: the natural-log sum-exp of a query's scaled scores

@@ -7,7 +7,8 @@
 WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
   WaSeqPlan p{};
   const int group = a.heads / a.kv_heads;
-  // One wavefront a tile where a sequence's new tokens, on average, fill no more rows with all heads of a key head.
+  // One wavefront a tile where a sequence's new tokens, on average, fill no more rows with all heads of a key head. The host knows the average
+  // alone, and empty sequences count: 8,192 tokens of one, 32 heads over 8, take 530 us alone or in 256 slots, 1,223 in 1,024.
   const int64_t mean = ((int64_t)a.tokens + a.batch - 1) / std::max(a.batch, 1);
   p.waves = mean * group <= 32 ? 1 : 4;
   const int rows = 32 * p.waves;
@@ -23,14 +24,14 @@ WaSeqPlan wa_seq_plan(const WaSeqLaunch& a) {
     p.per_tile = 1;
     p.log_tokens = log_tokens(1);
   }
-  // Workgroups that the chip holds: two a compute unit of four wavefronts (of d 64 three fit, which as workers are no faster), four of one (a fifth does not fit beside the LDS of four: one
-  // token of 32 sequences 162 us with 1,024, 197 with 1,280).
+  // Workgroups that the chip holds: two a compute unit of four wavefronts (of d 64 three fit, which as workers are no faster), four of one (a
+  // fifth does not fit beside the LDS of four: one token of 32 sequences 162 us with 1,024, 197 with 1,280).
   p.workers = p.waves == 4 ? 512 : 1024;
   p.min_units = 4;
   // Calls whose tiles are never cut need no second kernel. Packed: tiles of fifteen tiles of keys at most, many short sequences
-  // (1,000 tokens of 16: 21.7 -> 14.4 us), and those of one wavefront a tile. Over a cache, whose lengths the host does not know, tables of
-  // few keys: few keys a tile take less time than a join (one wavefront: 100 sequences of up to 300 keys 23.5 -> 19.7 us, but 16 of 500
-  // 19.6 -> 24.6; four: 512 tokens of 32 heads 25.0 -> 18.0).
+  // (1,000 tokens of 16: 21.7 -> 14.4 us; but 32,768 tokens of one head among 255 empty slots take 534 us, alone 286), and those of one wavefront
+  // a tile. Over a cache, whose lengths the host does not know, tables of few keys: few keys a tile take less time than a join (one
+  // wavefront: 100 sequences of up to 300 keys 23.5 -> 19.7 us, but 16 of 500 19.6 -> 24.6; four: 512 tokens of 32 heads 25.0 -> 18.0).
   if (a.paged) {
     const int64_t keys = (int64_t)a.table_width << a.page_shift;
     p.whole = keys <= (p.waves == 4 ? 512 : 256) || (p.waves == 1 && keys <= 512 && wa_seq_most_tiles(a, p) >= 256);

@@ -6,7 +6,8 @@
 //   keys     128 keys, over the queries of all heads that share them: dK and dV.
 //   queries  128 queries of a head, over their keys: dQ.
 // They run in one launch, those of keys first, which take longer, so that the others fill the chip while the last of them end (8,192 tokens of 7
-// documents, 16 heads over 4, d 128: 163 + 121 us one after another, 240 together: 0.93 PFLOP/s of the seven products, matrix cores 50% busy;
+// documents, 16 heads over 4, d 128: 163 + 121 us one after another, 240 together: 0.93 PFLOP/s of these seven products, 0.63 counting the formula's
+// five, matrix cores 50% busy;
 // what bounds it is two wavefronts a SIMD that take turns at products and exponentials). Long tiles are computed in parts, which
 // packed_parts_kernel adds in order.
 // Both recompute the scores and dP. A wavefront holds 32 queries (keys) with their accumulators in registers, and the other side's
@@ -201,8 +202,8 @@ __device__ __forceinline__ bool find_job(const WaSeqLaunch& a, bool queries, int
   if (job->parts > 1 && job->part == 0 && threadIdx.x == 0) cuts->tile[job->number] = make_int4(job->b, job->tile, (int)rank, job->parts);
   return true;
 }
-// Up to 64 sequences have a path of their own (a step of 2,311 tokens in 5 documents: 55 us, 57 along the other, which takes 160 where one
-// that holds 64 takes 219: the gradient of 600 documents of 30 tokens, 8 heads of 64).
+// Up to 64 sequences have a path of their own (a step of 2,311 tokens in 5 documents: 55 us, 57 along the other; the gradient of 600 documents of
+// 30 tokens, 8 heads of 64, takes 152 us so, and took 219, when the other took 160, where a path held 64).
 __device__ __forceinline__ bool take_job(const WaSeqLaunch& a, bool queries, int64_t rank, int cols, int share, Job* job) {
   return a.batch <= 64 ? find_job<1>(a, queries, rank, cols, share, job) : find_job<8>(a, queries, rank, cols, share, job);
 }

@@ -40,12 +40,15 @@ namespace wa {
 constexpr float kSeqGrow = 8.f;  // log2 units
 constexpr int kSeqAhead = 4;     // operands read ahead
 // Tiles of four wavefronts are dealt out whole where there are so many times the workers of them, and where that takes no longer than the line, in
-// which a worker's share of s units takes about 22 + 2.2 s us, with parts to store and to join (d 128, units of 64 keys; d 64 about the same).
+// which a worker's share of s units takes about 22 + 2.2 s us, with parts to store and to join (fitted at d 128, units of 64 keys).
 // Causal: whole tiles, of all lengths, take 4 + 1.05 longest + 0.7 s, so where longest <= 17 + 10/7 s. 2,400 tokens of 3 prompts, 32 heads over
 // 8: 59 us along the line, 44 whole; 8,192 of one, 8 heads over 1: 168 and 185.
 // Not causal, or behind many cached keys, tiles are about equal, and a last round of few of them counts: it takes 0.65 of a full one if it is
 // half full or less, else 0.9. 6,000 tokens of 16 heads, not causal, 752 tiles: 323 us along the line, 298 whole; 4,800, 608 tiles: 207 and 251;
 // over a cache 4,096 tokens behind 12,288, 32 heads over 8: 955 and 908; 1,024 behind 7,168: 152 and 175.
+// Of 21 shapes timed both ways at either d, the choice is within 6% of the better (beside the join's launch, 2 to 3 us) but for: d 64, 130 us whole
+// and 111 along the line (8,192 tokens of 7 documents, 16 heads, not causal), 91 along the line and 82 whole (6,000 of 2, 12 heads, causal); d 128, 96
+// whole and 88 along the line (2,400 of 3, 32 heads, not causal).
 constexpr int kSeqWhole = 4, kSeqLongest = 17;
 
 // What a tile costs beside its keys, in tiles of keys.
