@@ -583,7 +583,7 @@ typedef struct wa_pages {
 /* Which pages sequences hold: token i of sequence b lies in row i % page of page tables[b table_stride + i / page]. */
 typedef struct wa_page_tables {
   const int32_t* tables;   /* device; entries behind a sequence's last page are not used */
-  int64_t table_stride;    /* table_width at least, or 0 where all sequences share one */
+  int64_t table_stride;    /* table_width at least, or 0 where all sequences share one; all tables span less than 2^46 entries */
   int32_t table_width;     /* entries of a sequence */
   int32_t n_pages;         /* pages of the pool */
   int32_t page;            /* tokens a page: a power of two, 16..4096 */

@@ -599,6 +599,8 @@ wa_status check_tables(const wa_page_tables* t, const int32_t* kv_lens, WaSeqLau
     return fail(WA_ERR_UNSUPPORTED, "a table of %d pages of %d tokens exceeds 2^30 tokens", t->table_width, t->page);
   if (t->table_stride < 0 || t->table_stride >= kMaxStride || (t->table_stride && t->table_stride < t->table_width && a->batch > 1))
     return fail(WA_ERR_INVALID_ARG, "table_stride %lld is below table_width %d", (long long)t->table_stride, t->table_width);
+  if ((double)(a->batch - 1) * t->table_stride >= kMaxExtent)
+    return fail(WA_ERR_UNSUPPORTED, "tables: stride %lld of %d sequences spans 2^46 entries", (long long)t->table_stride, a->batch);
   a->tables = t->tables; a->table_stride = t->table_stride; a->table_width = t->table_width; a->n_pages = t->n_pages;
   a->page_shift = 0;
   while ((1 << a->page_shift) < t->page) ++a->page_shift;

@@ -93,6 +93,8 @@ def test_strides_past_64_bits(store):
         pages = {name: (BASE + where, 1 << 39, 1024, 64)}
         assert _call(store, pages=pages, tables=(*TABLES[:3], (1 << 25) + 1, 16)) == UNSUP
         assert b"span" in _lib().wa_last_error()
+    many = L.SEQ_SHAPE.pack(1 << 25, 10, 4, 2, 64, L.WA_BF16)
+    assert _call(store, shape=many, tables=(TABLES[0], 1 << 39, *TABLES[2:])) == UNSUP and b"tables" in _lib().wa_last_error()
 
 
 @pytest.mark.parametrize("order", ["pcht", "phct", "phtc", "pcth", "ptch", "pthc", "cpht"])
